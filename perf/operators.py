@@ -215,7 +215,7 @@ def _own(s, c):
         return {"logp": s["out_logp"], "entropy": s["out_entropy"], "d_logits": s["d_logits"]}
     if kind == "policy":
         R.policy_loss(s["logp"], s["old"], s["adv"], s["out_loss"], s["out_grad"], seq_offsets=s["offsets"],
-                      ref_logp=s["ref"], entropy=s["entropy"], mask=s["mask"], d_entropy=s["out_grad_entropy"],
+                      token_advantages=c["per_token"], ref_logp=s["ref"], entropy=s["entropy"], mask=s["mask"], d_entropy=s["out_grad_entropy"],
                       **{k: c[k] for k in KEYS})
         return dict(_said(s["out_loss"]), d_logp=s["out_grad"], d_entropy=s["out_grad_entropy"])
     if kind == "preference":
@@ -224,7 +224,7 @@ def _own(s, c):
                           label_smoothing=c["label_smoothing"], margin=c["margin"])
         return dict(_said(s["out_loss"]), d_logp=s["out_grad"], rewards=s["out_rewards"])
     R.policy_loss_logits(s["logits"], s["targets"], s["old"], s["adv"], s["out_loss"], s["out_logp"], s["d_logits"],
-                         seq_offsets=s["offsets"], ref_logp=s["ref"], mask=s["mask"], out_entropy=s["out_entropy"],
+                         seq_offsets=s["offsets"], token_advantages=c["per_token"], ref_logp=s["ref"], mask=s["mask"], out_entropy=s["out_entropy"],
                          temperature=c["temp"], **{k: c[k] for k in KEYS})
     return dict(_said(s["out_loss"]), logp=s["out_logp"], entropy=s["out_entropy"], d_logits=s["d_logits"])
 
