@@ -343,6 +343,173 @@ rl_status rl_sample_logits_noalloc(int32_t n, int32_t vocab, const float* logits
                                    const rl_sample_params* sp, int32_t* out_tok, float* out_logp, void* stream);
 
 /* ---------------------------------------------------------------------
+ * Training stage: from logits to the gradient of the RL loss (Sec. 2.1: the
+ * policy loss consumes the responses' per-token log-probabilities, which
+ * generation and the inference stage above have produced).
+ *
+ * These calls need no context: they run on `stream` of the current device,
+ * allocate nothing, keep nothing from one call for the next and can be
+ * captured into a HIP graph.  Tokens are packed sequence after sequence, as
+ * rl_score's response tokens are.  Scratch memory is the caller's workspace
+ * (device, 256-byte aligned, contents arbitrary, at least the bytes that the
+ * matching function returns; NULL is accepted where that is 0); calls that
+ * may overlap in time need workspaces of their own.  Outputs may not overlap
+ * inputs or each other, but for d_logits, which may be the logits themselves
+ * (same ld).  Results do not depend on timing: every sum has a fixed order.
+ *
+ * Logits: [n][ld] of `dtype` (rl_dtype), n <= 2^20 rows, vocab <= 2^24
+ * entries each (any value >= 1), ld >= vocab; entries vocab .. ld - 1 of a
+ * row are neither read nor written.  The pointer needs the element's
+ * alignment only; rows that start on 16 bytes are the fastest.
+ * Temperature: finite, >= 0; 0 is taken as 1.  x = z / T below.
+ * ------------------------------------------------------------------- */
+
+/* Bytes of workspace for rl_token_logprobs (0 when the rows alone fill the
+ * chip, or for invalid sizes). */
+size_t rl_logprob_workspace_bytes(int32_t n, int32_t vocab);
+
+/* Log-probability of a given token under each row of logits, and the row's
+ * entropy:
+ *   out_logp[i]    = x_y - LSE(x), y = targets[i]; NaN for y outside [0, vocab)
+ *   out_entropy[i] = -sum_v p_v ln p_v, p = softmax(x)   (or NULL)
+ *   out_stats[i]   = { max_v z_v, ln sum_v exp((z_v - max) / T) }, float
+ *                    [n][2], what the backward pass needs (or NULL)
+ *  targets device int32 [n]; out_* device float.
+ * A logit of -inf is an entry of probability 0.  A row with a NaN or +inf
+ * logit, or of nothing but -inf, leaves NaN.  out_logp is never above 0. */
+rl_status rl_token_logprobs(int32_t n, int32_t vocab, int32_t dtype, const void* logits, int64_t ld,
+                            const int32_t* targets, float temperature, float* out_logp, float* out_entropy,
+                            float* out_stats, void* workspace, size_t ws_bytes, void* stream);
+
+/* Its backward pass: with g = d_logp[i] and e = d_entropy[i] (0 when NULL),
+ *   d_logits[i][v] = (g (1[v = y] - p_v) - e p_v (ln p_v + H)) / T
+ * rounded once to `dtype`; [n][ldd].
+ *  stats    out_stats of the forward call on the same logits and temperature.
+ *  entropy  its out_entropy; needed with d_entropy, else NULL.
+ * A row with g = e = 0 is written as zeros, whatever its logits are.  Where
+ * the target is outside [0, vocab), g is taken as 0. */
+rl_status rl_token_logprobs_backward(int32_t n, int32_t vocab, int32_t dtype, const void* logits, int64_t ld,
+                                     const int32_t* targets, float temperature, const float* stats,
+                                     const float* entropy, const float* d_logp, const float* d_entropy,
+                                     void* d_logits, int64_t ldd, void* stream);
+
+typedef enum rl_kl_kind {        /* estimator of KL(policy, reference) from d = clamp(ref_logp - logp, -20, 20) */
+    RL_KL_K1 = 1,                /* -d                                            */
+    RL_KL_K2 = 2,                /* d^2 / 2                                       */
+    RL_KL_K3 = 3                 /* exp(d) - d - 1                                */
+} rl_kl_kind;
+
+typedef enum rl_aggregate {      /* weight w of a counted token                   */
+    RL_AGG_TOKEN_MEAN = 0,       /* 1 / counted tokens                            */
+    RL_AGG_SEQUENCE_MEAN = 1,    /* 1 / (counted tokens of its sequence x sequences
+                                    with a counted token)                         */
+    RL_AGG_SUM = 2               /* 1                                             */
+} rl_aggregate;
+
+typedef struct rl_policy_params {
+    double  clip_low;            /* in [0, 1): the ratio is clipped below 1 - clip_low   */
+    double  clip_high;           /* >= 0: and above 1 + clip_high                        */
+    double  dual_clip;           /* 0: off; else > 1: bound of the ratio where the
+                                    advantage is negative                                */
+    double  kl_coef;
+    double  entropy_coef;
+    double  scale;               /* multiplies the loss and every gradient               */
+    int32_t kl;                  /* rl_kl_kind                                           */
+    int32_t aggregate;           /* rl_aggregate                                         */
+    int32_t token_advantages;    /* 0: one advantage a sequence, 1: one a token          */
+    int32_t reserved;            /* must be 0                                            */
+} rl_policy_params;
+
+/* The packed tokens of a policy loss (device pointers).  n <= 2^24 tokens
+ * (2^20 from logits), n_seqs <= 2^20. */
+typedef struct rl_policy_batch {
+    int32_t n;
+    int32_t n_seqs;
+    const int32_t* seq_offsets;  /* [n_seqs + 1], not decreasing, in [0, n]; NULL: one sequence of
+                                    n tokens (n_seqs = 1)                                */
+    const float* old_logp;       /* [n] log-probabilities at generation                  */
+    const float* ref_logp;       /* [n] under the reference policy, or NULL (kl_coef = 0) */
+    const float* advantages;     /* [n_seqs], or [n] with token_advantages               */
+    const uint8_t* mask;         /* [n], 0 takes a token out; or NULL                    */
+} rl_policy_batch;
+
+/* Bytes of workspace for rl_policy_loss, and for rl_policy_loss_logits (0
+ * for invalid sizes, and where none is needed). */
+size_t rl_policy_workspace_bytes(int32_t n, int32_t n_seqs);
+size_t rl_policy_logits_workspace_bytes(int32_t n, int32_t n_seqs, int32_t vocab);
+
+/* Clipped policy loss with a KL term and its gradient.  A token counts when
+ * its mask byte is not 0 and a sequence holds it; what stands at the other
+ * tokens is not looked at.  Over the counted tokens, in fp64,
+ *   r    = exp(clamp(logp - old_logp, -20, 20))
+ *   pg   = max(-A r, -A clamp(r, 1 - clip_low, 1 + clip_high)), and
+ *          -A dual_clip where A < 0 and r > dual_clip (dual_clip > 0)
+ *   loss = scale * sum w (pg + kl_coef kl - entropy_coef entropy)
+ *  logp      [n] log-probabilities now.
+ *  entropy   [n], or NULL (entropy_coef = 0).
+ *  out_loss  float [8]: loss; sum w pg; sum w kl; sum w entropy (the last two
+ *            0 without ref_logp and entropy); over the counted tokens the
+ *            share whose ratio the clip stops, the share that dual_clip
+ *            stops, and the mean of old_logp - logp; counted tokens.
+ *            All 0 where no token counts.
+ *  d_logp    [n] d loss / d logp: no gradient passes a ratio that is stopped
+ *            or a clamp that holds; 0 at tokens that do not count.
+ *  d_entropy [n] d loss / d entropy, or NULL. */
+rl_status rl_policy_loss(const rl_policy_batch* batch, const rl_policy_params* params, const float* logp,
+                         const float* entropy, float* out_loss, float* d_logp, float* d_entropy, void* workspace,
+                         size_t ws_bytes, void* stream);
+
+/* The same loss from logits to their gradient in one call: log-probabilities
+ * of `targets`, entropies (with entropy_coef != 0, when out_entropy must be
+ * given, or for out_entropy), loss and d loss / d logits.
+ *  out_logp     [n]; 0 at tokens that do not count.
+ *  out_entropy  [n] or NULL; 0 at tokens that do not count.
+ *  d_logits     [n][ldd] of dtype; may be the logits (ldd = ld).  Rows of
+ *               tokens that do not count are zeros, whatever their logits are.
+ * A counted token whose target is outside [0, vocab) makes the loss NaN. */
+rl_status rl_policy_loss_logits(const rl_policy_batch* batch, const rl_policy_params* params, int32_t vocab,
+                                int32_t dtype, const void* logits, int64_t ld, const int32_t* targets,
+                                float temperature, float* out_loss, float* out_logp, float* out_entropy,
+                                void* d_logits, int64_t ldd, void* workspace, size_t ws_bytes, void* stream);
+
+typedef enum rl_preference_form {
+    RL_PREF_SIGMOID = 0,         /* -(1 - s) ln sigmoid(h) - s ln sigmoid(-h), s = label_smoothing */
+    RL_PREF_HINGE = 1,           /* max(0, 1 - h)                                 */
+    RL_PREF_SQUARED = 2          /* ((h - 1/2) / beta)^2                          */
+} rl_preference_form;
+
+typedef struct rl_preference_params {
+    double  beta;                /* > 0                                           */
+    double  label_smoothing;     /* in [0, 1/2]; 0 but for RL_PREF_SIGMOID        */
+    double  margin;
+    double  scale;               /* multiplies the loss and the gradient          */
+    int32_t form;                /* rl_preference_form                            */
+    int32_t average;             /* 1: log ratios are means over counted tokens, 0: sums */
+} rl_preference_params;
+
+/* Bytes of workspace for rl_preference_loss (0 for invalid sizes). */
+size_t rl_preference_workspace_bytes(int32_t n, int32_t n_pairs);
+
+/* Preference loss of n_pairs answer pairs and its gradient: sequence 2p is
+ * pair p's chosen answer, sequence 2p + 1 its rejected one.  With R_s the sum
+ * (or mean) of logp - ref_logp over the counted tokens of sequence s (0 where
+ * it has none), h = beta (R_2p - R_2p+1) - margin; the loss is the mean of
+ * the form's values over the pairs, in fp64.
+ *  n <= 2^24 tokens, 1 <= n_pairs <= 2^19.
+ *  seq_offsets  device int32 [2 n_pairs + 1], not decreasing, in [0, n].
+ *  logp, ref_logp (or NULL: 0), mask (or NULL): device [n], as above.
+ *  out_loss     float [8]: loss; means over the pairs of the chosen reward,
+ *               the rejected one and their difference; share of pairs whose
+ *               chosen reward is the higher; means of the chosen and of the
+ *               rejected answers' summed (or mean) logp; n_pairs.
+ *  out_rewards  float [2 n_pairs]: beta R_s, or NULL.
+ *  d_logp       [n] d loss / d logp; 0 at tokens that do not count. */
+rl_status rl_preference_loss(int32_t n, int32_t n_pairs, const int32_t* seq_offsets, const float* logp,
+                             const float* ref_logp, const uint8_t* mask, const rl_preference_params* params,
+                             float* out_loss, float* out_rewards, float* d_logp, void* workspace, size_t ws_bytes,
+                             void* stream);
+
+/* ---------------------------------------------------------------------
  * Slot bookkeeping (host only; nothing is enqueued).
  * ------------------------------------------------------------------- */
 

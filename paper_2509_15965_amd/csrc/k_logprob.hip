@@ -1,0 +1,272 @@
+// k_logprob.hip -- token log-probabilities and entropies from logits, and the
+// gradient of both to the logits.
+//
+// With t_v = (z_v - m) log2(e) / T, m the row's largest logit: s = sum 2^t_v,
+// u = sum 2^t_v t_v, and
+//   log p_y = (z_y - m) / T - ln s        H = ln s - ln 2 u / s
+//   d z_v   = (g (1[v = y] - p_v) - ge p_v (ln p_v + H)) / T
+// The difference is taken before the product, so that neither the type's
+// lowest value nor -inf in a row makes an inf - inf of its own.
+#include "rl_device.h"
+#include "rl_internal.h"
+#include "train.h"
+
+#include <cfloat>
+
+namespace rl {
+
+namespace {
+
+// 16 bytes of logits at any element boundary.
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+template <typename T> constexpr int kVec = 16 / sizeof(T);
+
+template <typename T> __device__ __forceinline__ void load_vec(const T* p, float* v);
+template <> __device__ __forceinline__ void load_vec<float>(const float* p, float* v) {
+    const u32x4 w = *reinterpret_cast<const u32x4_any*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
+}
+template <> __device__ __forceinline__ void load_vec<uint16_t>(const uint16_t* p, float* v) {
+    const u32x4 w = *reinterpret_cast<const u32x4_any*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+template <typename T> __device__ __forceinline__ void store_vec(T* p, const float* v);
+template <> __device__ __forceinline__ void store_vec<float>(float* p, const float* v) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[i]);
+    *reinterpret_cast<u32x4_any*>(p) = w;
+}
+template <> __device__ __forceinline__ void store_vec<uint16_t>(uint16_t* p, const float* v) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w[i] = static_cast<uint32_t>(f32_to_bf16(v[2 * i])) | static_cast<uint32_t>(f32_to_bf16(v[2 * i + 1])) << 16;
+    *reinterpret_cast<u32x4_any*>(p) = w;
+}
+
+// Smallest exponent that enters a product: 2^kFloor is 0 in fp32, so an entry
+// of probability 0 adds 0 instead of 0 x inf.
+constexpr float kFloor = -200.0f;
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The sums of a part of a row relative to another m.
+__device__ __forceinline__ void rebase(RowPart& a, float m, float c) {
+    const float d = fmaxf((a.m - m) * c, -1e4f), f = exp2_hw(d);
+    a.u = f * (a.u + d * a.s);
+    a.s *= f;
+    a.m = m;
+}
+__device__ __forceinline__ RowPart merge(RowPart a, RowPart b, float c) {
+    const float m = fmaxf(a.m, b.m);
+    rebase(a, m, c);
+    rebase(b, m, c);
+    return RowPart{m, a.s + b.s, a.u + b.u};
+}
+
+template <int N> __device__ __forceinline__ void add_entries(RowPart& a, const float* v, float c) {
+    float m = a.m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = fmaxf(m, v[i]);
+    if (m != a.m) rebase(a, m, c);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float t = (v[i] - m) * c, e = exp2_hw(t);
+        a.s += e;
+        a.u += e * fmaxf(t, kFloor);
+    }
+}
+
+__device__ __forceinline__ RowPart merge_wave(RowPart a, float c) {
+    for (int off = 32; off > 0; off >>= 1)
+        a = merge(a, RowPart{__shfl_xor(a.m, off, 64), __shfl_xor(a.s, off, 64), __shfl_xor(a.u, off, 64)}, c);
+    return a;
+}
+
+template <typename T>
+__device__ __forceinline__ void finish_row(RowPart a, const T* z, int V, int y, float T_, int row, float* logp, float* ent,
+                                           float* stats) {
+    const double ln_s = log(static_cast<double>(a.s));
+    float lp = __builtin_nanf("");
+    if (y >= 0 && y < V)
+        lp = static_cast<float>((static_cast<double>(Elem<T>::load(z, y)) - a.m) / T_ - ln_s);
+    logp[row] = lp;
+    if (ent) {
+        const double h = ln_s - 0.69314718055994530942 * (static_cast<double>(a.u) / a.s);
+        ent[row] = static_cast<float>(h < 0.0 ? 0.0 : h);
+    }
+    if (stats) {
+        stats[2 * static_cast<size_t>(row)] = a.m;
+        stats[2 * static_cast<size_t>(row) + 1] = static_cast<float>(ln_s);
+    }
+}
+
+__device__ __forceinline__ void finish_dead(int row, float* logp, float* ent, float* stats) {
+    logp[row] = 0.0f;
+    if (ent) ent[row] = 0.0f;
+    if (stats) stats[2 * static_cast<size_t>(row)] = stats[2 * static_cast<size_t>(row) + 1] = 0.0f;
+}
+
+constexpr int kRowThreads = 256;
+
+// One workgroup per (row, vocabulary chunk); chunks of a row are merged in
+// order by token_logprobs_join_kernel.
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads) token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int V,
+        const int32_t* __restrict__ targets, float T_, float c, int chunk, bool check, PolicyArgs live,
+        RowPart* __restrict__ parts, float* __restrict__ logp, float* __restrict__ ent, float* __restrict__ stats) {
+    __shared__ RowPart sp[kRowThreads / 64];
+    const int row = blockIdx.x, nchunks = gridDim.y;
+    if (check && !token_counts(live, row)) {
+        if (threadIdx.x == 0 && nchunks == 1) finish_dead(row, logp, ent, stats);
+        return;
+    }
+    const T* z = logits + row * ld;
+    const int beg = blockIdx.y * chunk, end = min(V, beg + chunk);
+    RowPart a{-FLT_MAX, 0.0f, 0.0f};
+    constexpr int E = kVec<T>;
+    const int whole = beg + (end - beg) / E * E;
+    for (int v = beg + E * static_cast<int>(threadIdx.x); v < whole; v += E * kRowThreads) {
+        float x[E];
+        load_vec(z + v, x);
+        add_entries<E>(a, x, c);
+    }
+    if (whole + static_cast<int>(threadIdx.x) < end) {
+        const float x = Elem<T>::load(z, whole + threadIdx.x);
+        add_entries<1>(a, &x, c);
+    }
+    a = merge_wave(a, c);
+    if ((threadIdx.x & 63) == 0) sp[threadIdx.x >> 6] = a;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < kRowThreads / 64; ++w) a = merge(a, sp[w], c);
+    if (nchunks > 1)
+        parts[static_cast<size_t>(row) * nchunks + blockIdx.y] = a;
+    else
+        finish_row(a, z, V, targets[row], T_, row, logp, ent, stats);
+}
+
+// One wave per row.
+template <typename T>
+__global__ void __launch_bounds__(64) token_logprobs_join_kernel(const RowPart* __restrict__ parts, int nchunks,
+        const T* __restrict__ logits, int64_t ld, int V, const int32_t* __restrict__ targets, float T_, float c,
+        bool check, PolicyArgs live, float* __restrict__ logp, float* __restrict__ ent, float* __restrict__ stats) {
+    const int row = blockIdx.x;
+    if (check && !token_counts(live, row)) {
+        if (threadIdx.x == 0) finish_dead(row, logp, ent, stats);
+        return;
+    }
+    RowPart a{-FLT_MAX, 0.0f, 0.0f};
+    for (int k = threadIdx.x; k < nchunks; k += 64) a = merge(a, parts[static_cast<size_t>(row) * nchunks + k], c);
+    a = merge_wave(a, c);
+    if (threadIdx.x == 0) finish_row(a, logits + row * ld, V, targets[row], T_, row, logp, ent, stats);
+}
+
+// The gradient of an entry from its log2 probability q: p (A + B q).
+struct RowGrad { float A, B, top; };
+__device__ __forceinline__ RowGrad row_grad(float g, float ge, float H, float T_) {
+    const float i = 1.0f / T_;
+    return RowGrad{-(g + ge * H) * i, -ge * 0.69314718f * i, g * i};
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads) token_logprobs_backward_kernel(const T* logits, int64_t ld, int V,
+        const int32_t* __restrict__ targets, float T_, float c, const float* __restrict__ stats,
+        const float* __restrict__ ent, const float* __restrict__ d_logp, const float* __restrict__ d_ent, int chunk, T* dz,
+        int64_t ldd) {
+    const int row = blockIdx.y;
+    const T* z = logits + row * ld;
+    T* d = dz + row * ldd;
+    const int y = targets[row];
+    const float g = y >= 0 && y < V ? d_logp[row] : 0.0f, ge = d_ent ? d_ent[row] : 0.0f;
+    const bool zero = g == 0.0f && ge == 0.0f;
+    const RowGrad k = row_grad(g, ge, d_ent ? ent[row] : 0.0f, T_);
+    const float m = stats[2 * static_cast<size_t>(row)], l2 = stats[2 * static_cast<size_t>(row) + 1] * 1.44269504f;
+    const int beg = blockIdx.x * chunk, end = min(V, beg + chunk);
+    constexpr int E = kVec<T>;
+    const int whole = beg + (end - beg) / E * E;
+    auto entry = [&](float x, int v) {
+        const float q = (x - m) * c - l2;
+        const float r = exp2_hw(q) * (k.A + k.B * fmaxf(q, kFloor));
+        return v == y ? r + k.top : r;
+    };
+    for (int v = beg + E * static_cast<int>(threadIdx.x); v < whole; v += E * kRowThreads) {
+        float x[E] = {};
+        if (!zero) {
+            load_vec(z + v, x);
+#pragma unroll
+            for (int i = 0; i < E; ++i) x[i] = entry(x[i], v + i);
+        }
+        store_vec(d + v, x);
+    }
+    const int v = whole + threadIdx.x;
+    if (v < end) Elem<T>::store(d, v, zero ? 0.0f : entry(Elem<T>::load(z, v), v));
+}
+
+// About 1024 workgroups in all, of whole 2048-entry blocks.
+int split_chunk(int n, int V) {
+    const int64_t want = (1024 + n - 1) / n;
+    const int64_t chunk = (V + want - 1) / want;
+    return static_cast<int>((chunk + 2047) / 2048 * 2048);
+}
+
+float log2_scale(float T) { return static_cast<float>(1.4426950408889634 / static_cast<double>(T)); }
+
+template <typename T>
+hipError_t forward(const LogprobArgs& a, RowPart* parts, hipStream_t s) {
+    const int chunk = split_chunk(a.n, a.V), nchunks = (a.V + chunk - 1) / chunk;
+    const T* z = static_cast<const T*>(a.logits);
+    const PolicyArgs live = a.live ? *a.live : PolicyArgs{};
+    hipLaunchKernelGGL(token_logprobs_kernel<T>, dim3(a.n, nchunks), dim3(kRowThreads), 0, s, z, a.ld, a.V, a.targets, a.T,
+                       log2_scale(a.T), chunk, a.live != nullptr, live, parts, a.logp, a.ent, a.stats);
+    if (nchunks > 1)
+        hipLaunchKernelGGL(token_logprobs_join_kernel<T>, dim3(a.n), dim3(64), 0, s, parts, nchunks, z, a.ld, a.V,
+                           a.targets, a.T, log2_scale(a.T), a.live != nullptr, live, a.logp, a.ent, a.stats);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t logprob_parts(int n, int V) {
+    if (n <= 0) return 0;
+    const int chunk = split_chunk(n, V), nchunks = (V + chunk - 1) / chunk;
+    return nchunks > 1 ? static_cast<size_t>(n) * nchunks : 0;
+}
+
+hipError_t launch_token_logprobs(int dt, const LogprobArgs& a, RowPart* parts, hipStream_t s) {
+    if (a.n <= 0) return hipSuccess;
+    return dt == DT_F32 ? forward<float>(a, parts, s) : forward<uint16_t>(a, parts, s);
+}
+
+hipError_t launch_token_logprobs_backward(int dt, const void* logits, int64_t ld, int n, int V, const int32_t* targets,
+                                          float T, const float* stats, const float* ent, const float* g,
+                                          const float* ge, void* dz, int64_t ldd, hipStream_t s) {
+    // rows in y, at most 65535 a launch
+    constexpr int kRows = 32768;
+    const int chunk = 8192, nchunks = (V + chunk - 1) / chunk;
+    const size_t es = dt == DT_F32 ? 4 : 2;
+    for (int r = 0; r < n; r += kRows) {
+        const int m = n - r < kRows ? n - r : kRows;
+        const char* z = static_cast<const char*>(logits) + es * ld * r;
+        char* d = static_cast<char*>(dz) + es * ldd * r;
+        const float* e = ent ? ent + r : nullptr;
+        const float* h = ge ? ge + r : nullptr;
+        if (dt == DT_F32)
+            hipLaunchKernelGGL(token_logprobs_backward_kernel<float>, dim3(nchunks, m), dim3(kRowThreads), 0, s,
+                               reinterpret_cast<const float*>(z), ld, V, targets + r, T, log2_scale(T), stats + 2 * r, e,
+                               g + r, h, chunk, reinterpret_cast<float*>(d), ldd);
+        else
+            hipLaunchKernelGGL(token_logprobs_backward_kernel<uint16_t>, dim3(nchunks, m), dim3(kRowThreads), 0, s,
+                               reinterpret_cast<const uint16_t*>(z), ld, V, targets + r, T, log2_scale(T), stats + 2 * r,
+                               e, g + r, h, chunk, reinterpret_cast<uint16_t*>(d), ldd);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace rl

@@ -321,6 +321,55 @@ hipError_t launch_sample(const float* logits, int ld, int n, int V, const int32_
                          uint64_t seed, float T, SamplePart* parts,
                          int32_t* out_tok, float* out_logp, hipStream_t s);
 
+// ---- training stage (k_logprob.hip, k_loss.hip; entry points in train.cpp) ----
+
+// What a policy loss reads of its tokens, besides the log-probabilities.
+struct PolicyArgs {
+    int n, n_seqs;
+    const int32_t* offs;          // [n_seqs + 1], or null: one sequence of all n tokens
+    const float *old_logp, *ref, *adv;
+    const uint8_t* mask;          // or null
+    double lo, hi, dual;          // ratio bounds 1 - clip_low, 1 + clip_high; dual clip (0: off)
+    double kl_coef, ent_coef, scale;
+    int kl, agg, token_adv;
+};
+
+// Rows of logits and what to compute of them.
+struct LogprobArgs {
+    const void* logits; int64_t ld;
+    int n, V;
+    const int32_t* targets;
+    float T;                      // > 0
+    float *logp, *ent, *stats;    // ent, stats may be null
+    const PolicyArgs* live;       // or null: rows of tokens that do not count are skipped and leave zeros
+};
+
+// Sum over a vocabulary chunk of a row: largest logit m, sum of e = 2^t and of e t, t = (z - m) log2(e) / T.
+struct RowPart { float m, s, u; };
+
+size_t logprob_parts(int n, int V);   // RowParts a forward launch writes (0: one workgroup a row)
+hipError_t launch_token_logprobs(int dt, const LogprobArgs& a, RowPart* parts, hipStream_t s);
+hipError_t launch_token_logprobs_backward(int dt, const void* logits, int64_t ld, int n, int V, const int32_t* targets,
+                                          float T, const float* stats, const float* ent, const float* g,
+                                          const float* ge, void* dz, int64_t ldd, hipStream_t s);
+
+size_t policy_ws_bytes(int n, int n_seqs);
+// ent, d_logp and d_ent may be null (d_logp: the loss alone)
+hipError_t launch_policy_loss(const PolicyArgs& p, const float* logp, const float* ent, float* out, float* d_logp,
+                              float* d_ent, void* ws, hipStream_t s);
+
+struct PrefArgs {
+    int n, n_pairs;
+    const int32_t* offs;
+    const float *logp, *ref;
+    const uint8_t* mask;
+    double beta, smooth, margin, scale;
+    int form, average;
+    float *rewards, *d_logp;      // rewards may be null
+};
+size_t preference_ws_bytes(int n, int n_pairs);
+hipError_t launch_preference_loss(const PrefArgs& p, float* out, void* ws, hipStream_t s);
+
 // Copy the live K/V of n slots between the pool and a packed staging buffer
 // (dir 0: pool -> stage, dir 1: stage -> pool).  Slot i (lens[i] positions)
 // starts at byte base[i] of the stage: for layer l, kv-head h (index

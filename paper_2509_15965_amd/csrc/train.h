@@ -1,0 +1,83 @@
+// train.h -- device-side pieces that the training-stage kernels share: which
+// tokens count and with what weight, and the clipped policy loss of one token.
+#pragma once
+
+#include "rl_device.h"
+#include "rl_internal.h"
+
+namespace rl {
+
+// First and one-past-last token of sequence s, inside [0, n] whatever the offsets hold.
+__device__ __forceinline__ void seq_range(const int32_t* offs, int n, int s, int* a, int* b) {
+    const int lo = offs ? offs[s] : 0, hi = offs ? offs[s + 1] : n;
+    *a = lo < 0 ? 0 : lo > n ? n : lo;
+    *b = hi < *a ? *a : hi > n ? n : hi;
+}
+
+// Sequence of token i, or -1.
+__device__ __forceinline__ int seq_of(const int32_t* offs, int n_seqs, int i) {
+    if (!offs) return 0;
+    int lo = 0, hi = n_seqs + 1;   // first entry above i
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (offs[mid] <= i) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo - 1 < n_seqs ? lo - 1 : -1;
+}
+
+__device__ __forceinline__ bool token_counts(const PolicyArgs& p, int i) {
+    if (p.mask && !p.mask[i]) return false;
+    return !p.offs || (i >= p.offs[0] && i < p.offs[p.n_seqs]);
+}
+
+// The policy and KL terms of one counted token and their derivatives by its
+// log-probability.  fp64 throughout: a ratio next to a clip border falls on
+// the side that its inputs say, and a few hundred fp64 operations a token
+// cost less than reading it.  NaN passes every comparison and clamp below.
+struct TokenLoss {
+    double pg, kl, g, lr;
+    bool clipped, dual;
+};
+__device__ __forceinline__ double clamp20(double x) { return x < -20.0 ? -20.0 : x > 20.0 ? 20.0 : x; }
+__device__ __forceinline__ TokenLoss policy_token(const PolicyArgs& p, double logp, double old_logp, double ref, double A) {
+    TokenLoss t;
+    t.lr = logp - old_logp;
+    const double lr = clamp20(t.lr);
+    const double r = exp(lr);
+    t.clipped = (A > 0.0 && r > p.hi) || (A < 0.0 && r < p.lo);
+    t.dual = p.dual > 0.0 && A < 0.0 && r > p.dual;
+    const double bound = A > 0.0 ? p.hi : p.lo;
+    t.pg = -A * (t.dual ? p.dual : t.clipped ? bound : r);
+    t.g = t.clipped || t.dual || lr != t.lr ? 0.0 : -A * r;
+    if (t.lr != t.lr) t.g = t.lr;
+    t.kl = 0.0;
+    if (p.ref) {
+        const double raw = ref - logp, d = clamp20(raw);
+        double dk;
+        if (p.kl == 1) {
+            t.kl = -d;
+            dk = 1.0;
+        } else if (p.kl == 2) {
+            t.kl = 0.5 * d * d;
+            dk = -d;
+        } else {
+            const double e = expm1(d);
+            t.kl = e - d;
+            dk = -e;
+        }
+        if (p.kl_coef != 0.0 && (d == raw || d != d)) t.g += p.kl_coef * dk;
+    }
+    return t;
+}
+
+__device__ __forceinline__ double wave_sum(double v) {
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+__device__ __forceinline__ int wave_sum(int v) {
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+}  // namespace rl

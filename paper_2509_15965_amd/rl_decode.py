@@ -37,7 +37,10 @@ EXPORTS = ("rl_decode_kv_bytes", "rl_decode_workspace_bytes", "rl_decode_create"
            "rl_decode_rebind", "rl_decode_set_option", "rl_decode_kernel_stats",
            "rl_decode_reset_stats", "rl_decode_attn_plan_stats", "rl_probe_copy", "rl_probe_read", "rl_probe_mfma",
            "rl_probe_gumbel_bound",
-           "rl_sample_logits_noalloc", "rl_decode_tune_gemms", "rl_decode_gemm_plan", "rl_status_string",
+           "rl_sample_logits_noalloc", "rl_logprob_workspace_bytes", "rl_token_logprobs",
+           "rl_token_logprobs_backward", "rl_policy_workspace_bytes", "rl_policy_logits_workspace_bytes",
+           "rl_policy_loss", "rl_policy_loss_logits", "rl_preference_workspace_bytes", "rl_preference_loss",
+           "rl_decode_tune_gemms", "rl_decode_gemm_plan", "rl_status_string",
            "rl_decode_last_error")
 
 
@@ -79,6 +82,26 @@ class AttnPlanStats(C.Structure):
     _fields_ = [("steps", C.c_int64), ("items", C.c_int64), ("shared_items", C.c_int64),
                 ("pair_items", C.c_int64), ("lds_workgroups", C.c_int64)]
 
+
+class PolicyParams(C.Structure):
+    _fields_ = [("clip_low", C.c_double), ("clip_high", C.c_double), ("dual_clip", C.c_double),
+                ("kl_coef", C.c_double), ("entropy_coef", C.c_double), ("scale", C.c_double), ("kl", C.c_int32),
+                ("aggregate", C.c_int32), ("token_advantages", C.c_int32), ("reserved", C.c_int32)]
+
+
+class PolicyBatch(C.Structure):
+    _fields_ = [("n", C.c_int32), ("n_seqs", C.c_int32), ("seq_offsets", C.c_void_p), ("old_logp", C.c_void_p),
+                ("ref_logp", C.c_void_p), ("advantages", C.c_void_p), ("mask", C.c_void_p)]
+
+
+class PreferenceParams(C.Structure):
+    _fields_ = [("beta", C.c_double), ("label_smoothing", C.c_double), ("margin", C.c_double), ("scale", C.c_double),
+                ("form", C.c_int32), ("average", C.c_int32)]
+
+
+KL_KINDS = {"k1": 1, "k2": 2, "k3": 3}
+AGGREGATES = {"token_mean": 0, "sequence_mean": 1, "sum": 2}
+PREFERENCE_FORMS = {"sigmoid": 0, "hinge": 1, "squared": 2}
 
 _lib = None
 
@@ -147,6 +170,26 @@ def lib():
     L.rl_sample_logits_noalloc.argtypes = [i32, i32, vp, i32, vp, vp, vp, C.POINTER(SampleParams), vp, vp, vp]
     L.rl_probe_gumbel_bound.restype = C.c_int
     L.rl_probe_gumbel_bound.argtypes = [C.c_uint32, C.c_uint64, i32, vp, vp, vp]
+    i64, f32 = C.c_int64, C.c_float
+    L.rl_logprob_workspace_bytes.restype = sz
+    L.rl_logprob_workspace_bytes.argtypes = [i32, i32]
+    L.rl_token_logprobs.restype = C.c_int
+    L.rl_token_logprobs.argtypes = [i32, i32, i32, vp, i64, vp, f32, vp, vp, vp, vp, sz, vp]
+    L.rl_token_logprobs_backward.restype = C.c_int
+    L.rl_token_logprobs_backward.argtypes = [i32, i32, i32, vp, i64, vp, f32, vp, vp, vp, vp, vp, i64, vp]
+    L.rl_policy_workspace_bytes.restype = sz
+    L.rl_policy_workspace_bytes.argtypes = [i32, i32]
+    L.rl_policy_logits_workspace_bytes.restype = sz
+    L.rl_policy_logits_workspace_bytes.argtypes = [i32, i32, i32]
+    L.rl_policy_loss.restype = C.c_int
+    L.rl_policy_loss.argtypes = [C.POINTER(PolicyBatch), C.POINTER(PolicyParams), vp, vp, vp, vp, vp, vp, sz, vp]
+    L.rl_policy_loss_logits.restype = C.c_int
+    L.rl_policy_loss_logits.argtypes = [C.POINTER(PolicyBatch), C.POINTER(PolicyParams), i32, i32, vp, i64, vp, f32,
+                                        vp, vp, vp, vp, i64, vp, sz, vp]
+    L.rl_preference_workspace_bytes.restype = sz
+    L.rl_preference_workspace_bytes.argtypes = [i32, i32]
+    L.rl_preference_loss.restype = C.c_int
+    L.rl_preference_loss.argtypes = [i32, i32, vp, vp, vp, vp, C.POINTER(PreferenceParams), vp, vp, vp, vp, sz, vp]
     L.rl_status_string.restype = C.c_char_p
     L.rl_status_string.argtypes = [C.c_int]
     L.rl_decode_last_error.restype = C.c_char_p
@@ -417,3 +460,214 @@ def sample_logits_noalloc(logits: torch.Tensor, uids: torch.Tensor, pos_new: tor
                                         out_logp.data_ptr(), stream.cuda_stream)
     if st != RL_OK:
         raise RLError(st, "rl_sample_logits_noalloc")
+
+
+# -- training stage: losses and gradients on a caller's tensors ---------------
+# Outputs are the caller's tensors.  Every tensor is contiguous but for logits
+# and d_logits, whose rows may be apart (stride(0)).  Arguments are checked
+# before anything is enqueued: ValueError for a tensor of the wrong type, size
+# or device, RLError for what the library refuses.  `workspace`: a uint8
+# tensor of at least the matching *_workspace_bytes; made here when None.
+
+def _on(device, name: str, t: Optional[torch.Tensor], dtype, numel: Optional[int], optional: bool = False):
+    """Device pointer of a contiguous tensor of this type and size."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError(f"{name} is missing")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, not {t.device}")
+    if not t.is_contiguous() or (numel is not None and t.numel() != numel):
+        raise ValueError(f"{name} must be contiguous and hold {numel} entries, not {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _mask_on(device, mask: Optional[torch.Tensor], n: int):
+    return _on(device, "mask", mask, torch.bool if mask is not None and mask.dtype == torch.bool else torch.uint8, n, True)
+
+
+def _rows_on(device, name: str, t: torch.Tensor, dtype=None, shape=None):
+    """(pointer, row stride) of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or (dtype is not None and t.dtype != dtype) or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} must be a matrix {tuple(shape) if shape else ''} of {dtype or 'logits'}")
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, not {t.device}")
+    n, V = t.shape
+    ld = t.stride(0) if n > 1 else V
+    if (V > 1 and t.stride(1) != 1) or ld < V:
+        raise ValueError(f"{name}: entries of a row must be contiguous and rows apart, strides {t.stride()}")
+    return t.data_ptr(), ld
+
+
+def _gpu_of(t: torch.Tensor, name: str):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a GPU")
+    return t.device
+
+
+def _run_on(device, stream, nbytes: int, workspace: Optional[torch.Tensor], call, what: str):
+    """call(workspace pointer, its bytes, stream) with `device` current."""
+    if torch.cuda.current_device() != device.index:
+        with torch.cuda.device(device):
+            return _run_on(device, stream, nbytes, workspace, call, what)
+    current = torch.cuda.current_stream(device)
+    if stream is None:
+        stream = current
+    elif stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+    if workspace is not None:
+        if workspace.device != device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous uint8 tensor on {device}")
+        ws, nbytes = workspace.data_ptr(), workspace.numel()
+    elif nbytes:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        if stream != current:
+            workspace.record_stream(stream)
+        ws = workspace.data_ptr()
+    else:
+        ws = None
+    st = call(ws, nbytes, stream.cuda_stream)
+    if st != RL_OK:
+        raise RLError(st, what)
+
+
+def _dtype_code(t: torch.Tensor) -> int:
+    return RL_DTYPE_FP32 if t.dtype == torch.float32 else RL_DTYPE_BF16
+
+
+def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, out_logp: torch.Tensor, *,
+                   out_entropy: Optional[torch.Tensor] = None, out_stats: Optional[torch.Tensor] = None,
+                   temperature: float = 1.0, workspace: Optional[torch.Tensor] = None, stream=None):
+    """rl_token_logprobs: log-probabilities of `targets` (int32 [n]) under
+    logits [n][vocab], with the entropies and the statistics ([n][2]) that the
+    backward pass takes."""
+    dev = _gpu_of(logits, "logits")
+    z, ld = _rows_on(dev, "logits", logits)
+    n, V = logits.shape
+    y = _on(dev, "targets", targets, torch.int32, n)
+    lp = _on(dev, "out_logp", out_logp, torch.float32, n)
+    ent = _on(dev, "out_entropy", out_entropy, torch.float32, n, True)
+    st = _on(dev, "out_stats", out_stats, torch.float32, 2 * n, True)
+    L = lib()
+    _run_on(dev, stream, L.rl_logprob_workspace_bytes(n, V) if workspace is None else 0, workspace,
+            lambda ws, nb, s: L.rl_token_logprobs(n, V, _dtype_code(logits), z, ld, y, temperature, lp, ent, st, ws, nb, s),
+            "rl_token_logprobs")
+
+
+def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, stats: torch.Tensor, d_logp: torch.Tensor,
+                            d_logits: torch.Tensor, *, entropy: Optional[torch.Tensor] = None,
+                            d_entropy: Optional[torch.Tensor] = None, temperature: float = 1.0, stream=None):
+    """rl_token_logprobs_backward: d_logits (may be the logits) from the
+    gradients of the log-probabilities and, with the forward's `entropy`, of
+    the entropies."""
+    dev = _gpu_of(logits, "logits")
+    z, ld = _rows_on(dev, "logits", logits)
+    dz, ldd = _rows_on(dev, "d_logits", d_logits, logits.dtype, logits.shape)
+    n, V = logits.shape
+    y = _on(dev, "targets", targets, torch.int32, n)
+    st = _on(dev, "stats", stats, torch.float32, 2 * n)
+    g = _on(dev, "d_logp", d_logp, torch.float32, n)
+    ent = _on(dev, "entropy", entropy, torch.float32, n, True)
+    ge = _on(dev, "d_entropy", d_entropy, torch.float32, n, True)
+    L = lib()
+    _run_on(dev, stream, 0, None,
+            lambda ws, nb, s: L.rl_token_logprobs_backward(n, V, _dtype_code(logits), z, ld, y, temperature, st, ent, g,
+                                                           ge, dz, ldd, s), "rl_token_logprobs_backward")
+
+
+def _policy(dev, n: int, old_logp, advantages, token_advantages, seq_offsets, ref_logp, mask, clip_low, clip_high,
+            dual_clip, kl, kl_coef, entropy_coef, aggregate, scale):
+    """The structs of a policy loss over n tokens."""
+    if kl not in KL_KINDS or aggregate not in AGGREGATES:
+        raise ValueError(f"kl is one of {tuple(KL_KINDS)}, aggregate one of {tuple(AGGREGATES)}")
+    k = 1 if seq_offsets is None else seq_offsets.numel() - 1
+    if k < 1:
+        raise ValueError("seq_offsets holds one entry more than there are sequences")
+    batch = PolicyBatch(n, k, _on(dev, "seq_offsets", seq_offsets, torch.int32, k + 1, True),
+                        _on(dev, "old_logp", old_logp, torch.float32, n),
+                        _on(dev, "ref_logp", ref_logp, torch.float32, n, True),
+                        _on(dev, "advantages", advantages, torch.float32, n if token_advantages else k),
+                        _mask_on(dev, mask, n))
+    params = PolicyParams(clip_low, clip_high, dual_clip, kl_coef, entropy_coef, scale, KL_KINDS[kl],
+                          AGGREGATES[aggregate], int(bool(token_advantages)), 0)
+    return batch, params
+
+
+def policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor, out_loss: torch.Tensor,
+                d_logp: torch.Tensor, *, token_advantages: bool = False, seq_offsets: Optional[torch.Tensor] = None,
+                ref_logp: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                mask: Optional[torch.Tensor] = None, d_entropy: Optional[torch.Tensor] = None, clip_low: float = 0.2,
+                clip_high: float = 0.2, dual_clip: float = 0.0, kl: str = "k3", kl_coef: float = 0.0,
+                entropy_coef: float = 0.0, aggregate: str = "token_mean", scale: float = 1.0,
+                workspace: Optional[torch.Tensor] = None, stream=None):
+    """rl_policy_loss on packed tokens: out_loss [8] and the gradients of
+    logp and entropy.  advantages: one a sequence, or with token_advantages
+    one a token."""
+    dev = _gpu_of(logp, "logp")
+    n = logp.numel()
+    lp = _on(dev, "logp", logp, torch.float32, n)
+    ent = _on(dev, "entropy", entropy, torch.float32, n, True)
+    out = _on(dev, "out_loss", out_loss, torch.float32, 8)
+    g = _on(dev, "d_logp", d_logp, torch.float32, n)
+    ge = _on(dev, "d_entropy", d_entropy, torch.float32, n, True)
+    b, q = _policy(dev, n, old_logp, advantages, token_advantages, seq_offsets, ref_logp, mask, clip_low, clip_high,
+                   dual_clip, kl, kl_coef, entropy_coef, aggregate, scale)
+    L = lib()
+    _run_on(dev, stream, L.rl_policy_workspace_bytes(n, b.n_seqs) if workspace is None else 0, workspace,
+            lambda ws, nb, s: L.rl_policy_loss(C.byref(b), C.byref(q), lp, ent, out, g, ge, ws, nb, s), "rl_policy_loss")
+
+
+def policy_loss_logits(logits: torch.Tensor, targets: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor,
+                       out_loss: torch.Tensor, out_logp: torch.Tensor, d_logits: torch.Tensor, *,
+                       token_advantages: bool = False, seq_offsets: Optional[torch.Tensor] = None, ref_logp: Optional[torch.Tensor] = None,
+                       mask: Optional[torch.Tensor] = None, out_entropy: Optional[torch.Tensor] = None,
+                       temperature: float = 1.0, clip_low: float = 0.2, clip_high: float = 0.2, dual_clip: float = 0.0,
+                       kl: str = "k3", kl_coef: float = 0.0, entropy_coef: float = 0.0, aggregate: str = "token_mean",
+                       scale: float = 1.0, workspace: Optional[torch.Tensor] = None, stream=None):
+    """rl_policy_loss_logits: the policy loss of logits [n][vocab] and its
+    gradient d_logits (may be the logits) in one call."""
+    dev = _gpu_of(logits, "logits")
+    z, ld = _rows_on(dev, "logits", logits)
+    dz, ldd = _rows_on(dev, "d_logits", d_logits, logits.dtype, logits.shape)
+    n, V = logits.shape
+    y = _on(dev, "targets", targets, torch.int32, n)
+    out = _on(dev, "out_loss", out_loss, torch.float32, 8)
+    lp = _on(dev, "out_logp", out_logp, torch.float32, n)
+    ent = _on(dev, "out_entropy", out_entropy, torch.float32, n, True)
+    b, q = _policy(dev, n, old_logp, advantages, token_advantages, seq_offsets, ref_logp, mask, clip_low, clip_high,
+                   dual_clip, kl, kl_coef, entropy_coef, aggregate, scale)
+    L = lib()
+    _run_on(dev, stream, L.rl_policy_logits_workspace_bytes(n, b.n_seqs, V) if workspace is None else 0, workspace,
+            lambda ws, nb, s: L.rl_policy_loss_logits(C.byref(b), C.byref(q), V, _dtype_code(logits), z, ld, y,
+                                                      temperature, out, lp, ent, dz, ldd, ws, nb, s),
+            "rl_policy_loss_logits")
+
+
+def preference_loss(logp: torch.Tensor, seq_offsets: torch.Tensor, out_loss: torch.Tensor, d_logp: torch.Tensor, *,
+                    ref_logp: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                    out_rewards: Optional[torch.Tensor] = None, form: str = "sigmoid", average: bool = False,
+                    beta: float = 0.1, label_smoothing: float = 0.0, margin: float = 0.0, scale: float = 1.0,
+                    workspace: Optional[torch.Tensor] = None, stream=None):
+    """rl_preference_loss on packed tokens: sequences 2p and 2p + 1 are pair
+    p's chosen and rejected answers; out_loss [8] and the gradient of logp."""
+    dev = _gpu_of(logp, "logp")
+    n = logp.numel()
+    lp = _on(dev, "logp", logp, torch.float32, n)
+    P = (seq_offsets.numel() - 1) // 2
+    if form not in PREFERENCE_FORMS:
+        raise ValueError(f"form is one of {tuple(PREFERENCE_FORMS)}")
+    offs = _on(dev, "seq_offsets", seq_offsets, torch.int32, 2 * P + 1)
+    ref = _on(dev, "ref_logp", ref_logp, torch.float32, n, True)
+    m = _mask_on(dev, mask, n)
+    out = _on(dev, "out_loss", out_loss, torch.float32, 8)
+    rew = _on(dev, "out_rewards", out_rewards, torch.float32, 2 * P, True)
+    g = _on(dev, "d_logp", d_logp, torch.float32, n)
+    q = PreferenceParams(beta, label_smoothing, margin, scale, PREFERENCE_FORMS[form], int(average))
+    L = lib()
+    _run_on(dev, stream, L.rl_preference_workspace_bytes(n, P) if workspace is None else 0, workspace,
+            lambda ws, nb, s: L.rl_preference_loss(n, P, offs, lp, ref, m, C.byref(q), out, rew, g, ws, nb, s),
+            "rl_preference_loss")
