@@ -21,19 +21,20 @@ namespace {
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 template <typename T> constexpr int kVec = 16 / sizeof(T);
 
-template <typename T> __device__ __forceinline__ void load_vec(const T* p, float* v);
-template <> __device__ __forceinline__ void load_vec<float>(const float* p, float* v) {
-    const u32x4 w = *reinterpret_cast<const u32x4_any*>(p);
+template <typename T> __device__ __forceinline__ void unpack(u32x4 w, float* v);
+template <> __device__ __forceinline__ void unpack<float>(u32x4 w, float* v) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
 }
-template <> __device__ __forceinline__ void load_vec<uint16_t>(const uint16_t* p, float* v) {
-    const u32x4 w = *reinterpret_cast<const u32x4_any*>(p);
+template <> __device__ __forceinline__ void unpack<uint16_t>(u32x4 w, float* v) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         v[2 * i] = __uint_as_float(w[i] << 16);
         v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
+}
+template <typename T> __device__ __forceinline__ void load_vec(const T* p, float* v) {
+    unpack<T>(*reinterpret_cast<const u32x4_any*>(p), v);
 }
 template <typename T> __device__ __forceinline__ void store_vec(T* p, const float* v);
 template <> __device__ __forceinline__ void store_vec<float>(float* p, const float* v) {
@@ -43,10 +44,12 @@ template <> __device__ __forceinline__ void store_vec<float>(float* p, const flo
     *reinterpret_cast<u32x4_any*>(p) = w;
 }
 template <> __device__ __forceinline__ void store_vec<uint16_t>(uint16_t* p, const float* v) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
     u32x4 w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        w[i] = static_cast<uint32_t>(f32_to_bf16(v[2 * i])) | static_cast<uint32_t>(f32_to_bf16(v[2 * i + 1])) << 16;
+    for (int i = 0; i < 4; ++i)   // one v_cvt_pk_bf16_f32 (round to nearest even)
+        w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){v[2 * i], v[2 * i + 1]}, bf16x2));
     *reinterpret_cast<u32x4_any*>(p) = w;
 }
 
@@ -70,24 +73,38 @@ __device__ __forceinline__ RowPart merge(RowPart a, RowPart b, float c) {
     return RowPart{m, a.s + b.s, a.u + b.u};
 }
 
-template <int N> __device__ __forceinline__ void add_entries(RowPart& a, const float* v, float c) {
-    float m = a.m;
+// A lane's running sums.  They stay relative to the m they have until an entry
+// lies more than 2^64 above it: rebasing at every new maximum would cost an
+// exponential in nearly every vector of a wave (some lane always has one).
+struct LaneSum : RowPart { float top; };   // top: the largest entry
+constexpr float kAhead = 64.0f;
+
+template <int N, bool ENT> __device__ __forceinline__ void add_entries(LaneSum& a, const float* v, float c) {
+    float x = v[0];
 #pragma unroll
-    for (int i = 0; i < N; ++i) m = fmaxf(m, v[i]);
-    if (m != a.m) rebase(a, m, c);
+    for (int i = 1; i < N; ++i) x = fmaxf(x, v[i]);
+    a.top = fmaxf(a.top, x);
+    if ((x - a.m) * c > kAhead) rebase(a, x, c);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float t = (v[i] - m) * c, e = exp2_hw(t);
+        const float t = (v[i] - a.m) * c, e = exp2_hw(t);
         a.s += e;
-        a.u += e * fmaxf(t, kFloor);
+        if (ENT) a.u += e * fmaxf(t, kFloor);
     }
 }
 
-__device__ __forceinline__ RowPart merge_wave(RowPart a, float c) {
-    for (int off = 32; off > 0; off >>= 1)
+// Over groups of N consecutive lanes.  Lanes may differ in the last bit (a
+// product and sum become one fma on one side only): take one lane's.
+template <int N> __device__ __forceinline__ RowPart merge_lanes(RowPart a, float c) {
+#pragma unroll
+    for (int off = N / 2; off > 0; off >>= 1)
         a = merge(a, RowPart{__shfl_xor(a.m, off, 64), __shfl_xor(a.s, off, 64), __shfl_xor(a.u, off, 64)}, c);
     return a;
 }
+__device__ __forceinline__ float first_lane(float x) {
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
+__device__ __forceinline__ RowPart merge_wave(RowPart a, float c) { return merge_lanes<64>(a, c); }
 
 template <typename T>
 __device__ __forceinline__ void finish_row(RowPart a, const T* z, int V, int y, float T_, int row, float* logp, float* ent,
@@ -96,7 +113,7 @@ __device__ __forceinline__ void finish_row(RowPart a, const T* z, int V, int y, 
     float lp = __builtin_nanf("");
     if (y >= 0 && y < V)
         lp = static_cast<float>((static_cast<double>(Elem<T>::load(z, y)) - a.m) / T_ - ln_s);
-    logp[row] = lp;
+    logp[row] = lp > 0.0f ? 0.0f : lp;
     if (ent) {
         const double h = ln_s - 0.69314718055994530942 * (static_cast<double>(a.u) / a.s);
         ent[row] = static_cast<float>(h < 0.0 ? 0.0 : h);
@@ -117,7 +134,7 @@ constexpr int kRowThreads = 256;
 
 // One workgroup per (row, vocabulary chunk); chunks of a row are merged in
 // order by token_logprobs_join_kernel.
-template <typename T>
+template <typename T, bool ENT>
 __global__ void __launch_bounds__(kRowThreads) token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int V,
         const int32_t* __restrict__ targets, float T_, float c, int chunk, bool check, PolicyArgs live,
         RowPart* __restrict__ parts, float* __restrict__ logp, float* __restrict__ ent, float* __restrict__ stats) {
@@ -129,19 +146,20 @@ __global__ void __launch_bounds__(kRowThreads) token_logprobs_kernel(const T* __
     }
     const T* z = logits + row * ld;
     const int beg = blockIdx.y * chunk, end = min(V, beg + chunk);
-    RowPart a{-FLT_MAX, 0.0f, 0.0f};
+    LaneSum acc{{-FLT_MAX, 0.0f, 0.0f}, -FLT_MAX};
     constexpr int E = kVec<T>;
     const int whole = beg + (end - beg) / E * E;
     for (int v = beg + E * static_cast<int>(threadIdx.x); v < whole; v += E * kRowThreads) {
         float x[E];
         load_vec(z + v, x);
-        add_entries<E>(a, x, c);
+        add_entries<E, ENT>(acc, x, c);
     }
     if (whole + static_cast<int>(threadIdx.x) < end) {
         const float x = Elem<T>::load(z, whole + threadIdx.x);
-        add_entries<1>(a, &x, c);
+        add_entries<1, ENT>(acc, &x, c);
     }
-    a = merge_wave(a, c);
+    rebase(acc, acc.top, c);
+    RowPart a = merge_wave(acc, c);
     if ((threadIdx.x & 63) == 0) sp[threadIdx.x >> 6] = a;
     __syncthreads();
     if (threadIdx.x != 0) return;
@@ -209,6 +227,121 @@ __global__ void __launch_bounds__(kRowThreads) token_logprobs_backward_kernel(co
     if (v < end) Elem<T>::store(d, v, zero ? 0.0f : entry(Elem<T>::load(z, v), v));
 }
 
+// ---- the policy loss of a row and the gradient of its logits, the row read once ----
+
+// The row's 16-byte vectors stay in registers (NV a lane, vector i * THREADS +
+// lane) from the load to the gradient: sums as the loads arrive, one barrier,
+// the token's loss, then each vector's gradient is stored.  HBM traffic is one
+// read and one write of the logits where the forward and backward kernels need
+// two reads.  A lane's entries behind the row's last vector are -inf.
+template <typename T> __device__ __forceinline__ u32x4 nothing();
+template <> __device__ __forceinline__ u32x4 nothing<float>() { return u32x4{0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u}; }
+template <> __device__ __forceinline__ u32x4 nothing<uint16_t>() { return u32x4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u}; }
+
+template <typename T, int THREADS, int NV, bool ENT>
+__global__ void __launch_bounds__(THREADS) policy_rows_kernel(PolicyArgs p, const int32_t* __restrict__ counts,
+        const CountPart* __restrict__ cparts, int n_cparts, const T* logits, int64_t ld, int V,
+        const int32_t* __restrict__ targets, float T_, float c, T* dz, int64_t ldd, float* __restrict__ logp,
+        float* __restrict__ ent, double* __restrict__ parts) {
+    constexpr int E = kVec<T>, WAVES = THREADS / 64;
+    __shared__ RowPart sp[WAVES];
+    const int row = blockIdx.x, tid = threadIdx.x;
+    T* d = dz + row * ldd;
+    const int nvec = V / E, tail = V - nvec * E;
+    if (!token_counts(p, row)) {
+        const float zero[E] = {};
+        for (int i = tid; i < nvec; i += THREADS) store_vec(d + i * E, zero);
+        if (tid < tail) Elem<T>::store(d, nvec * E + tid, 0.0f);
+        if (tid == 0) {
+            logp[row] = 0.0f;
+            if (ent) ent[row] = 0.0f;
+            for (int k = 0; k < kPolicySums; ++k) parts[static_cast<size_t>(row) * kPolicySums + k] = 0.0;
+        }
+        return;
+    }
+    const T* z = logits + row * ld;
+    u32x4 w[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        w[i] = nothing<T>();
+        if (i * THREADS + tid < nvec) w[i] = *reinterpret_cast<const u32x4_any*>(z + static_cast<size_t>(i * THREADS + tid) * E);
+    }
+    const float last = tid < tail ? Elem<T>::load(z, nvec * E + tid) : -INFINITY;
+    const int y = targets[row];
+    const bool held = y >= 0 && y < V;
+    const float zy = held ? Elem<T>::load(z, y) : __builtin_nanf("");
+    const int s = seq_of(p.offs, p.n_seqs, row);
+    const double weight = policy_weight(p, s, counts, cparts, n_cparts);
+    const float adv = p.adv[p.token_adv ? row : s], old_logp = p.old_logp[row], ref = p.ref ? p.ref[row] : 0.0f;
+
+    LaneSum acc{{-FLT_MAX, 0.0f, 0.0f}, -FLT_MAX};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i * THREADS < nvec) {
+            float x[E];
+            unpack<T>(w[i], x);
+            add_entries<E, ENT>(acc, x, c);
+        }
+        __builtin_amdgcn_sched_barrier(0);   // a vector at a time: unpacked ones would not fit beside the row
+    }
+    add_entries<1, ENT>(acc, &last, c);
+    rebase(acc, acc.top, c);
+    RowPart a = merge_wave(acc, c);
+    if ((tid & 63) == 0) sp[tid >> 6] = a;
+    __syncthreads();
+    // the first lane's, in every wave the same bits: one log-probability for the whole row's gradient
+    a = merge_lanes<WAVES>(sp[tid % WAVES], c);
+    a = RowPart{first_lane(a.m), first_lane(a.s), first_lane(a.u)};
+
+    const double ln_s = log(static_cast<double>(a.s));
+    float lp = static_cast<float>((static_cast<double>(zy) - a.m) / T_ - ln_s);
+    lp = lp > 0.0f ? 0.0f : lp;
+    float H = 0.0f;
+    if (ENT) {
+        const double h = ln_s - 0.69314718055994530942 * (static_cast<double>(a.u) / a.s);
+        H = static_cast<float>(h < 0.0 ? 0.0 : h);
+    }
+    const TokenLoss t = policy_token(p, lp, old_logp, ref, adv);
+    const float g = held ? static_cast<float>(p.scale * weight * t.g) : 0.0f;
+    const float ge = ENT ? static_cast<float>(-p.scale * weight * p.ent_coef) : 0.0f;
+    if (tid == 0) {
+        logp[row] = lp;
+        if (ent) ent[row] = H;
+        double* o = parts + static_cast<size_t>(row) * kPolicySums;
+        o[0] = weight * t.pg;
+        o[1] = weight * t.kl;
+        o[2] = weight * H;
+        o[3] = t.clipped;
+        o[4] = t.dual;
+        o[5] = -t.lr;
+        o[6] = 1.0;
+    }
+    const bool zero = g == 0.0f && ge == 0.0f;
+    const RowGrad k = row_grad(g, ge, H, T_);
+    const float l2 = static_cast<float>(ln_s) * 1.44269504f;
+    auto entry = [&](float x, int v) {
+        const float q = (x - a.m) * c - l2;
+        const float r = exp2_hw(q) * (ENT ? k.A + k.B * fmaxf(q, kFloor) : k.A);
+        return v == y ? r + k.top : r;
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int v = i * THREADS + tid;
+        asm volatile("" : "+v"(w[i]));   // unpacked again: the values of the first pass would not fit beside the row
+        if (v < nvec) {
+            float x[E] = {};
+            if (!zero) {
+                unpack<T>(w[i], x);
+#pragma unroll
+                for (int j = 0; j < E; ++j) x[j] = entry(x[j], v * E + j);
+            }
+            store_vec(d + static_cast<size_t>(v) * E, x);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (tid < tail) Elem<T>::store(d, nvec * E + tid, zero ? 0.0f : entry(last, nvec * E + tid));
+}
+
 // About 1024 workgroups in all, of whole 2048-entry blocks.
 int split_chunk(int n, int V) {
     const int64_t want = (1024 + n - 1) / n;
@@ -223,7 +356,8 @@ hipError_t forward(const LogprobArgs& a, RowPart* parts, hipStream_t s) {
     const int chunk = split_chunk(a.n, a.V), nchunks = (a.V + chunk - 1) / chunk;
     const T* z = static_cast<const T*>(a.logits);
     const PolicyArgs live = a.live ? *a.live : PolicyArgs{};
-    hipLaunchKernelGGL(token_logprobs_kernel<T>, dim3(a.n, nchunks), dim3(kRowThreads), 0, s, z, a.ld, a.V, a.targets, a.T,
+    const auto kernel = a.ent ? token_logprobs_kernel<T, true> : token_logprobs_kernel<T, false>;
+    hipLaunchKernelGGL(kernel, dim3(a.n, nchunks), dim3(kRowThreads), 0, s, z, a.ld, a.V, a.targets, a.T,
                        log2_scale(a.T), chunk, a.live != nullptr, live, parts, a.logp, a.ent, a.stats);
     if (nchunks > 1)
         hipLaunchKernelGGL(token_logprobs_join_kernel<T>, dim3(a.n), dim3(64), 0, s, parts, nchunks, z, a.ld, a.V,
@@ -231,7 +365,42 @@ hipError_t forward(const LogprobArgs& a, RowPart* parts, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Vectors a lane holds at most: 20 take 80 of the 128 registers that 16 waves
+// a CU leave each lane.
+constexpr int kRowVecs = 20;
+
+template <typename T, int THREADS, int NV>
+hipError_t rows(const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz, int64_t ldd, hipStream_t s) {
+    const auto kernel = a.ent ? policy_rows_kernel<T, THREADS, NV, true> : policy_rows_kernel<T, THREADS, NV, false>;
+    hipLaunchKernelGGL(kernel, dim3(a.n), dim3(THREADS), 0, s, p, w.counts, w.cparts, w.n_cparts,
+                       static_cast<const T*>(a.logits), a.ld, a.V, a.targets, a.T, log2_scale(a.T), static_cast<T*>(dz), ldd,
+                       a.logp, a.ent, w.parts);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t rows_of(const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz, int64_t ldd, hipStream_t s) {
+    const int nvec = a.V / kVec<T>;
+    if (nvec <= 4 * 256) return rows<T, 256, 4>(p, w, a, dz, ldd, s);
+    if (nvec <= 8 * 256) return rows<T, 256, 8>(p, w, a, dz, ldd, s);
+    if (nvec <= 16 * 256) return rows<T, 256, 16>(p, w, a, dz, ldd, s);
+    if (nvec <= 20 * 256) return rows<T, 256, 20>(p, w, a, dz, ldd, s);
+    if (nvec <= 16 * 512) return rows<T, 512, 16>(p, w, a, dz, ldd, s);
+    if (nvec <= 20 * 512) return rows<T, 512, 20>(p, w, a, dz, ldd, s);
+    if (nvec <= 16 * 1024) return rows<T, 1024, 16>(p, w, a, dz, ldd, s);
+    return rows<T, 1024, kRowVecs>(p, w, a, dz, ldd, s);
+}
+
 }  // namespace
+
+bool policy_rows_fit(int dt, int n, int V) {
+    return n >= 192 && V / (dt == DT_F32 ? 4 : 8) <= kRowVecs * 1024;
+}
+
+hipError_t launch_policy_rows(int dt, const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz, int64_t ldd,
+                              hipStream_t s) {
+    return dt == DT_F32 ? rows_of<float>(p, w, a, dz, ldd, s) : rows_of<uint16_t>(p, w, a, dz, ldd, s);
+}
 
 size_t logprob_parts(int n, int V) {
     if (n <= 0) return 0;

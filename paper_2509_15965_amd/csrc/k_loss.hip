@@ -16,7 +16,6 @@ constexpr int kWaves = kThreads / 64;
 
 // Counted tokens of each sequence (one wave a sequence), and per workgroup
 // the counted tokens and the sequences that have some.
-struct CountPart { int32_t tokens, seqs; };
 constexpr int kMaxCountBlocks = 256;
 
 __global__ void __launch_bounds__(kThreads) policy_count_kernel(int n, int n_seqs, const int32_t* __restrict__ offs,
@@ -46,9 +45,7 @@ __global__ void __launch_bounds__(kThreads) policy_count_kernel(int n, int n_seq
     }
 }
 
-// Sums of a workgroup's tokens: sum w pg, sum w kl, sum w entropy, clipped,
-// dual-clipped, sum of old - new, counted tokens.
-constexpr int kSums = 7;
+constexpr int kSums = kPolicySums;
 
 template <int N> __device__ void block_sums(double* v, double* out) {
     __shared__ double sh[kWaves][N];
@@ -219,27 +216,46 @@ __global__ void __launch_bounds__(kThreads) preference_final_kernel(const double
 }  // namespace
 
 // counts, count partials, loss partials
-size_t policy_ws_bytes(int n, int n_seqs) {
+PolicyWs policy_ws(const PolicyArgs& p, void* ws) {
+    char* w = static_cast<char*>(ws);
+    PolicyWs r;
+    r.counts = reinterpret_cast<int32_t*>(w);
+    w += align256(static_cast<size_t>(p.n_seqs) * sizeof(int32_t));
+    r.cparts = reinterpret_cast<CountPart*>(w);
+    w += align256(kMaxCountBlocks * sizeof(CountPart));
+    r.parts = reinterpret_cast<double*>(w);
+    const int nc = (p.n_seqs + kWaves - 1) / kWaves;
+    r.n_cparts = nc < kMaxCountBlocks ? nc : kMaxCountBlocks;
+    return r;
+}
+
+static size_t ws_bytes(int n_parts, int n_seqs) {
     return align256(static_cast<size_t>(n_seqs) * sizeof(int32_t)) + align256(kMaxCountBlocks * sizeof(CountPart)) +
-           align256(static_cast<size_t>(blocks_of(n)) * kSums * sizeof(double));
+           align256(static_cast<size_t>(n_parts) * kSums * sizeof(double));
+}
+size_t policy_ws_bytes(int n, int n_seqs) { return ws_bytes(blocks_of(n), n_seqs); }
+size_t policy_rows_ws_bytes(int n, int n_seqs) { return ws_bytes(n, n_seqs); }
+
+hipError_t launch_policy_counts(const PolicyArgs& p, const PolicyWs& w, hipStream_t s) {
+    hipLaunchKernelGGL(policy_count_kernel, dim3(w.n_cparts), dim3(kThreads), 0, s, p.n, p.n_seqs, p.offs, p.mask, w.counts, w.cparts);
+    return hipGetLastError();
+}
+
+hipError_t launch_policy_final(const PolicyArgs& p, const PolicyWs& w, int n_parts, float* out, hipStream_t s) {
+    hipLaunchKernelGGL(policy_final_kernel, dim3(1), dim3(kThreads), 0, s, w.parts, n_parts, p.kl_coef, p.ent_coef, p.scale, out);
+    return hipGetLastError();
 }
 
 hipError_t launch_policy_loss(const PolicyArgs& p, const float* logp, const float* ent, float* out, float* d_logp,
                               float* d_ent, void* ws, hipStream_t s) {
-    char* w = static_cast<char*>(ws);
-    int32_t* counts = reinterpret_cast<int32_t*>(w);
-    w += align256(static_cast<size_t>(p.n_seqs) * sizeof(int32_t));
-    CountPart* cparts = reinterpret_cast<CountPart*>(w);
-    w += align256(kMaxCountBlocks * sizeof(CountPart));
-    double* parts = reinterpret_cast<double*>(w);
-    const int nc = (p.n_seqs + kWaves - 1) / kWaves, cblocks = nc < kMaxCountBlocks ? nc : kMaxCountBlocks;
-    hipLaunchKernelGGL(policy_count_kernel, dim3(cblocks), dim3(kThreads), 0, s, p.n, p.n_seqs, p.offs, p.mask, counts, cparts);
+    const PolicyWs w = policy_ws(p, ws);
+    hipError_t e = launch_policy_counts(p, w, s);
     const int nb = blocks_of(p.n);
     if (nb)
-        hipLaunchKernelGGL(policy_loss_kernel, dim3(nb), dim3(kThreads), 0, s, p, logp, ent, counts, cparts, cblocks, d_logp,
-                           d_ent, parts);
-    hipLaunchKernelGGL(policy_final_kernel, dim3(1), dim3(kThreads), 0, s, parts, nb, p.kl_coef, p.ent_coef, p.scale, out);
-    return hipGetLastError();
+        hipLaunchKernelGGL(policy_loss_kernel, dim3(nb), dim3(kThreads), 0, s, p, logp, ent, w.counts, w.cparts, w.n_cparts,
+                           d_logp, d_ent, w.parts);
+    if (e == hipSuccess) e = launch_policy_final(p, w, nb, out, s);
+    return e;
 }
 
 size_t preference_ws_bytes(int, int n_pairs) {

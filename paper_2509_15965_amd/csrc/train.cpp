@@ -48,7 +48,7 @@ struct LogitsWs {
 };
 LogitsWs logits_ws(int n, int n_seqs, int V) {
     LogitsWs w;
-    size_t at = policy_ws_bytes(n, n_seqs);
+    size_t at = policy_rows_ws_bytes(n, n_seqs);
     w.off_g = at;
     at += align256(sizeof(float) * n);
     w.off_ge = at;
@@ -151,6 +151,13 @@ rl_status rl_policy_loss_logits(const rl_policy_batch* batch, const rl_policy_pa
     float* stats = reinterpret_cast<float*>(base + w.off_stats);
     const float T = temperature == 0.0f ? 1.0f : temperature;
     const LogprobArgs a{logits, ld, p.n, vocab, targets, T, out_logp, out_entropy, stats, &p};
+    if (policy_rows_fit(dtype, p.n, vocab)) {
+        const PolicyWs pw = policy_ws(p, base);
+        hipError_t e = launch_policy_counts(p, pw, s);
+        if (e == hipSuccess) e = launch_policy_rows(dtype, p, pw, a, d_logits, ldd, s);
+        if (e == hipSuccess) e = launch_policy_final(p, pw, p.n, out_loss, s);
+        return status_of(e);
+    }
     hipError_t e = launch_token_logprobs(dtype, a, reinterpret_cast<RowPart*>(base + w.off_parts), s);
     if (e == hipSuccess) e = launch_policy_loss(p, out_logp, out_entropy, out_loss, g, ge, base, s);
     if (e == hipSuccess)

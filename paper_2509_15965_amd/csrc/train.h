@@ -80,4 +80,14 @@ __device__ __forceinline__ int wave_sum(int v) {
     return v;
 }
 
+// Weight of a counted token of sequence s: 1 / counted tokens, 1 / (its
+// sequence's x sequences that have some), or 1.  Every lane of a wave calls it.
+__device__ __forceinline__ double policy_weight(const PolicyArgs& p, int s, const int32_t* counts, const CountPart* cparts,
+                                                int n_cparts) {
+    if (p.agg == 2) return 1.0;
+    int tokens = 0, seqs = 0;
+    for (int k = threadIdx.x & 63; k < n_cparts; k += 64) { tokens += cparts[k].tokens; seqs += cparts[k].seqs; }
+    return p.agg == 0 ? 1.0 / wave_sum(tokens) : 1.0 / (static_cast<double>(counts[s]) * wave_sum(seqs));
+}
+
 }  // namespace rl
