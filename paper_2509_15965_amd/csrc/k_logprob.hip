@@ -33,24 +33,40 @@ template <> __device__ __forceinline__ void unpack<uint16_t>(u32x4 w, float* v) 
         v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
 }
-template <typename T> __device__ __forceinline__ void load_vec(const T* p, float* v) {
-    unpack<T>(*reinterpret_cast<const u32x4_any*>(p), v);
-}
-template <typename T> __device__ __forceinline__ void store_vec(T* p, const float* v);
-template <> __device__ __forceinline__ void store_vec<float>(float* p, const float* v) {
+template <typename T> __device__ __forceinline__ u32x4 pack(const float* v);
+template <> __device__ __forceinline__ u32x4 pack<float>(const float* v) {
     u32x4 w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[i]);
-    *reinterpret_cast<u32x4_any*>(p) = w;
+    return w;
 }
-template <> __device__ __forceinline__ void store_vec<uint16_t>(uint16_t* p, const float* v) {
+template <> __device__ __forceinline__ u32x4 pack<uint16_t>(const float* v) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     u32x4 w;
 #pragma unroll
     for (int i = 0; i < 4; ++i)   // one v_cvt_pk_bf16_f32 (round to nearest even)
         w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){v[2 * i], v[2 * i + 1]}, bf16x2));
-    *reinterpret_cast<u32x4_any*>(p) = w;
+    return w;
+}
+// Vector `first` of a row plus a lane's byte offset: scalar base, 32-bit lane offset.
+template <typename T> __device__ __forceinline__ T* vec_at(T* row, int first, uint32_t at) {
+    return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(row) + static_cast<size_t>(first) * 16 + at);
+}
+
+// Logits are streamed: non-temporal loads where nothing reads them again soon
+// (8192 x 152064 bf16 log-probabilities in 364 us, 6.8 TB/s; plain loads 410),
+// plain ones where the backward pass will, which then finds part of them in
+// the memory-side cache (both passes over 437 MB in 218 us and 230, over 1.2
+// GB in 582 and 596; gradients stored plainly and read plainly 262 and 689).
+// The gradient is stored non-temporally: 1792 x 32000 rows to gradients in 63
+// us, plainly 70, and with a reader of the gradient behind it 84 and 85.
+template <bool KEEP, typename T> __device__ __forceinline__ u32x4 load_row(const T* p) {
+    const u32x4_any* q = reinterpret_cast<const u32x4_any*>(p);
+    return KEEP ? *q : __builtin_nontemporal_load(q);
+}
+template <typename T> __device__ __forceinline__ void store_row(T* p, u32x4 w) {
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x4_any*>(p));
 }
 
 // Smallest exponent that enters a product: 2^kFloor is 0 in fp32, so an entry
@@ -107,15 +123,15 @@ __device__ __forceinline__ float first_lane(float x) {
 __device__ __forceinline__ RowPart merge_wave(RowPart a, float c) { return merge_lanes<64>(a, c); }
 
 template <typename T>
-__device__ __forceinline__ void finish_row(RowPart a, const T* z, int V, int y, float T_, int row, float* logp, float* ent,
-                                           float* stats) {
-    const double ln_s = log(static_cast<double>(a.s));
+__device__ __forceinline__ void finish_row(RowPart a, const T* z, int V, int y, double inv_T, int row, float* logp,
+                                           float* ent, float* stats) {
+    const double ln_s = ln_sum(a.s);
     float lp = __builtin_nanf("");
     if (y >= 0 && y < V)
-        lp = static_cast<float>((static_cast<double>(Elem<T>::load(z, y)) - a.m) / T_ - ln_s);
+        lp = static_cast<float>((static_cast<double>(Elem<T>::load(z, y)) - a.m) * inv_T - ln_s);
     logp[row] = lp > 0.0f ? 0.0f : lp;
     if (ent) {
-        const double h = ln_s - 0.69314718055994530942 * (static_cast<double>(a.u) / a.s);
+        const double h = ln_s - 0.69314718055994530942 * static_cast<double>(a.u / a.s);
         ent[row] = static_cast<float>(h < 0.0 ? 0.0 : h);
     }
     if (stats) {
@@ -134,9 +150,9 @@ constexpr int kRowThreads = 256;
 
 // One workgroup per (row, vocabulary chunk); chunks of a row are merged in
 // order by token_logprobs_join_kernel.
-template <typename T, bool ENT>
+template <typename T, bool ENT, bool KEEP>
 __global__ void __launch_bounds__(kRowThreads) token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int V,
-        const int32_t* __restrict__ targets, float T_, float c, int chunk, bool check, PolicyArgs live,
+        const int32_t* __restrict__ targets, double inv_T, float c, int chunk, bool check, PolicyArgs live,
         RowPart* __restrict__ parts, float* __restrict__ logp, float* __restrict__ ent, float* __restrict__ stats) {
     __shared__ RowPart sp[kRowThreads / 64];
     const int row = blockIdx.x, nchunks = gridDim.y;
@@ -151,7 +167,7 @@ __global__ void __launch_bounds__(kRowThreads) token_logprobs_kernel(const T* __
     const int whole = beg + (end - beg) / E * E;
     for (int v = beg + E * static_cast<int>(threadIdx.x); v < whole; v += E * kRowThreads) {
         float x[E];
-        load_vec(z + v, x);
+        unpack<T>(load_row<KEEP>(z + v), x);
         add_entries<E, ENT>(acc, x, c);
     }
     if (whole + static_cast<int>(threadIdx.x) < end) {
@@ -167,13 +183,13 @@ __global__ void __launch_bounds__(kRowThreads) token_logprobs_kernel(const T* __
     if (nchunks > 1)
         parts[static_cast<size_t>(row) * nchunks + blockIdx.y] = a;
     else
-        finish_row(a, z, V, targets[row], T_, row, logp, ent, stats);
+        finish_row(a, z, V, targets[row], inv_T, row, logp, ent, stats);
 }
 
 // One wave per row.
 template <typename T>
 __global__ void __launch_bounds__(64) token_logprobs_join_kernel(const RowPart* __restrict__ parts, int nchunks,
-        const T* __restrict__ logits, int64_t ld, int V, const int32_t* __restrict__ targets, float T_, float c,
+        const T* __restrict__ logits, int64_t ld, int V, const int32_t* __restrict__ targets, double inv_T, float c,
         bool check, PolicyArgs live, float* __restrict__ logp, float* __restrict__ ent, float* __restrict__ stats) {
     const int row = blockIdx.x;
     if (check && !token_counts(live, row)) {
@@ -183,19 +199,18 @@ __global__ void __launch_bounds__(64) token_logprobs_join_kernel(const RowPart* 
     RowPart a{-FLT_MAX, 0.0f, 0.0f};
     for (int k = threadIdx.x; k < nchunks; k += 64) a = merge(a, parts[static_cast<size_t>(row) * nchunks + k], c);
     a = merge_wave(a, c);
-    if (threadIdx.x == 0) finish_row(a, logits + row * ld, V, targets[row], T_, row, logp, ent, stats);
+    if (threadIdx.x == 0) finish_row(a, logits + row * ld, V, targets[row], inv_T, row, logp, ent, stats);
 }
 
 // The gradient of an entry from its log2 probability q: p (A + B q).
 struct RowGrad { float A, B, top; };
-__device__ __forceinline__ RowGrad row_grad(float g, float ge, float H, float T_) {
-    const float i = 1.0f / T_;
+__device__ __forceinline__ RowGrad row_grad(float g, float ge, float H, float i) {   // i = 1 / T
     return RowGrad{-(g + ge * H) * i, -ge * 0.69314718f * i, g * i};
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) token_logprobs_backward_kernel(const T* logits, int64_t ld, int V,
-        const int32_t* __restrict__ targets, float T_, float c, const float* __restrict__ stats,
+        const int32_t* __restrict__ targets, float inv_T, float c, const float* __restrict__ stats,
         const float* __restrict__ ent, const float* __restrict__ d_logp, const float* __restrict__ d_ent, int chunk, T* dz,
         int64_t ldd) {
     const int row = blockIdx.y;
@@ -204,7 +219,7 @@ __global__ void __launch_bounds__(kRowThreads) token_logprobs_backward_kernel(co
     const int y = targets[row];
     const float g = y >= 0 && y < V ? d_logp[row] : 0.0f, ge = d_ent ? d_ent[row] : 0.0f;
     const bool zero = g == 0.0f && ge == 0.0f;
-    const RowGrad k = row_grad(g, ge, d_ent ? ent[row] : 0.0f, T_);
+    const RowGrad k = row_grad(g, ge, d_ent ? ent[row] : 0.0f, inv_T);
     const float m = stats[2 * static_cast<size_t>(row)], l2 = stats[2 * static_cast<size_t>(row) + 1] * 1.44269504f;
     const int beg = blockIdx.x * chunk, end = min(V, beg + chunk);
     constexpr int E = kVec<T>;
@@ -217,11 +232,11 @@ __global__ void __launch_bounds__(kRowThreads) token_logprobs_backward_kernel(co
     for (int v = beg + E * static_cast<int>(threadIdx.x); v < whole; v += E * kRowThreads) {
         float x[E] = {};
         if (!zero) {
-            load_vec(z + v, x);
+            unpack<T>(load_row<false>(z + v), x);
 #pragma unroll
             for (int i = 0; i < E; ++i) x[i] = entry(x[i], v + i);
         }
-        store_vec(d + v, x);
+        store_row(d + v, pack<T>(x));
     }
     const int v = whole + threadIdx.x;
     if (v < end) Elem<T>::store(d, v, zero ? 0.0f : entry(Elem<T>::load(z, v), v));
@@ -239,107 +254,125 @@ template <> __device__ __forceinline__ u32x4 nothing<float>() { return u32x4{0xF
 template <> __device__ __forceinline__ u32x4 nothing<uint16_t>() { return u32x4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u}; }
 
 template <typename T, int THREADS, int NV, bool ENT>
-__global__ void __launch_bounds__(THREADS) policy_rows_kernel(PolicyArgs p, const int32_t* __restrict__ counts,
+__global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, const int32_t* __restrict__ counts,
         const CountPart* __restrict__ cparts, int n_cparts, const T* logits, int64_t ld, int V,
-        const int32_t* __restrict__ targets, float T_, float c, T* dz, int64_t ldd, float* __restrict__ logp,
+        const int32_t* __restrict__ targets, double inv_T, float c, T* dz, int64_t ldd, float* __restrict__ logp,
         float* __restrict__ ent, double* __restrict__ parts) {
     constexpr int E = kVec<T>, WAVES = THREADS / 64;
-    __shared__ RowPart sp[WAVES];
-    const int row = blockIdx.x, tid = threadIdx.x;
-    T* d = dz + row * ldd;
+    __shared__ RowPart sp[2][WAVES];
+    const int tid = threadIdx.x;
     const int nvec = V / E, tail = V - nvec * E;
-    if (!token_counts(p, row)) {
-        const float zero[E] = {};
-        for (int i = tid; i < nvec; i += THREADS) store_vec(d + i * E, zero);
-        if (tid < tail) Elem<T>::store(d, nvec * E + tid, 0.0f);
-        if (tid == 0) {
-            logp[row] = 0.0f;
-            if (ent) ent[row] = 0.0f;
-            for (int k = 0; k < kPolicySums; ++k) parts[static_cast<size_t>(row) * kPolicySums + k] = 0.0;
-        }
-        return;
-    }
-    const T* z = logits + row * ld;
+    const uint32_t at = tid * 16;
     u32x4 w[NV];
+    float last = -INFINITY;
+    int row = blockIdx.x;
+    bool live = token_counts(p, row);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        w[i] = nothing<T>();
-        if (i * THREADS + tid < nvec) w[i] = *reinterpret_cast<const u32x4_any*>(z + static_cast<size_t>(i * THREADS + tid) * E);
-    }
-    const float last = tid < tail ? Elem<T>::load(z, nvec * E + tid) : -INFINITY;
-    const int y = targets[row];
-    const bool held = y >= 0 && y < V;
-    const float zy = held ? Elem<T>::load(z, y) : __builtin_nanf("");
-    const int s = seq_of(p.offs, p.n_seqs, row);
-    const double weight = policy_weight(p, s, counts, cparts, n_cparts);
-    const float adv = p.adv[p.token_adv ? row : s], old_logp = p.old_logp[row], ref = p.ref ? p.ref[row] : 0.0f;
-
-    LaneSum acc{{-FLT_MAX, 0.0f, 0.0f}, -FLT_MAX};
+    for (int i = 0; i < NV; ++i) w[i] = nothing<T>();
+    if (live) {
+        const T* z = logits + row * ld;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if (i * THREADS < nvec) {
-            float x[E];
-            unpack<T>(w[i], x);
-            add_entries<E, ENT>(acc, x, c);
-        }
-        __builtin_amdgcn_sched_barrier(0);   // a vector at a time: unpacked ones would not fit beside the row
+        for (int i = 0; i < NV; ++i)
+            if (tid < nvec - i * THREADS) w[i] = load_row<false>(vec_at(z, i * THREADS, at));
+        if (tid < tail) last = Elem<T>::load(z, nvec * E + tid);
     }
-    add_entries<1, ENT>(acc, &last, c);
-    rebase(acc, acc.top, c);
-    RowPart a = merge_wave(acc, c);
-    if ((tid & 63) == 0) sp[tid >> 6] = a;
-    __syncthreads();
-    // the first lane's, in every wave the same bits: one log-probability for the whole row's gradient
-    a = merge_lanes<WAVES>(sp[tid % WAVES], c);
-    a = RowPart{first_lane(a.m), first_lane(a.s), first_lane(a.u)};
-
-    const double ln_s = log(static_cast<double>(a.s));
-    float lp = static_cast<float>((static_cast<double>(zy) - a.m) / T_ - ln_s);
-    lp = lp > 0.0f ? 0.0f : lp;
-    float H = 0.0f;
-    if (ENT) {
-        const double h = ln_s - 0.69314718055994530942 * (static_cast<double>(a.u) / a.s);
-        H = static_cast<float>(h < 0.0 ? 0.0 : h);
-    }
-    const TokenLoss t = policy_token(p, lp, old_logp, ref, adv);
-    const float g = held ? static_cast<float>(p.scale * weight * t.g) : 0.0f;
-    const float ge = ENT ? static_cast<float>(-p.scale * weight * p.ent_coef) : 0.0f;
-    if (tid == 0) {
-        logp[row] = lp;
-        if (ent) ent[row] = H;
-        double* o = parts + static_cast<size_t>(row) * kPolicySums;
-        o[0] = weight * t.pg;
-        o[1] = weight * t.kl;
-        o[2] = weight * H;
-        o[3] = t.clipped;
-        o[4] = t.dual;
-        o[5] = -t.lr;
-        o[6] = 1.0;
-    }
-    const bool zero = g == 0.0f && ge == 0.0f;
-    const RowGrad k = row_grad(g, ge, H, T_);
-    const float l2 = static_cast<float>(ln_s) * 1.44269504f;
-    auto entry = [&](float x, int v) {
-        const float q = (x - a.m) * c - l2;
-        const float r = exp2_hw(q) * (ENT ? k.A + k.B * fmaxf(q, kFloor) : k.A);
-        return v == y ? r + k.top : r;
-    };
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int v = i * THREADS + tid;
-        asm volatile("" : "+v"(w[i]));   // unpacked again: the values of the first pass would not fit beside the row
-        if (v < nvec) {
-            float x[E] = {};
-            if (!zero) {
-                unpack<T>(w[i], x);
-#pragma unroll
-                for (int j = 0; j < E; ++j) x[j] = entry(x[j], v * E + j);
+    for (int turn = 0; row < p.n; turn ^= 1) {
+        const int next = row + gridDim.x;
+        const bool next_live = next < p.n && token_counts(p, next);
+        const T* zn = logits + next * ld;
+        T* d = dz + row * ldd;
+        float m = 0.0f, l2 = 0.0f;
+        RowGrad k{0.0f, 0.0f, 0.0f};
+        int y = -1;
+        bool zero = true;
+        if (!live) {
+            if (tid == 0) {
+                logp[row] = 0.0f;
+                if (ent) ent[row] = 0.0f;
+                for (int q = 0; q < kPolicySums; ++q) parts[static_cast<size_t>(row) * kPolicySums + q] = 0.0;
             }
-            store_vec(d + static_cast<size_t>(v) * E, x);
+        } else {
+            y = targets[row];
+            const bool held = y >= 0 && y < V;
+            const float zy = held ? Elem<T>::load(logits + row * ld, y) : __builtin_nanf("");
+            const int s = seq_of(p.offs, p.n_seqs, row);
+            const double weight = policy_weight(p, s, counts, cparts, n_cparts);
+            const float adv = p.adv[p.token_adv ? row : s], old_logp = p.old_logp[row], ref = p.ref ? p.ref[row] : 0.0f;
+            LaneSum acc{{-FLT_MAX, 0.0f, 0.0f}, -FLT_MAX};
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (i * THREADS < nvec) {
+                    float x[E];
+                    unpack<T>(w[i], x);
+                    add_entries<E, ENT>(acc, x, c);
+                }
+                __builtin_amdgcn_sched_barrier(0);   // a vector at a time: unpacked ones would not fit beside the row
+            }
+            add_entries<1, ENT>(acc, &last, c);
+            rebase(acc, acc.top, c);
+            RowPart a = merge_wave(acc, c);
+            if ((tid & 63) == 0) sp[turn][tid >> 6] = a;
+            __syncthreads();
+            a = merge_lanes<WAVES>(sp[turn][tid % WAVES], c);
+            a = RowPart{first_lane(a.m), first_lane(a.s), first_lane(a.u)};
+            const double ln_s = ln_sum(a.s);
+            float lp = static_cast<float>((static_cast<double>(zy) - a.m) * inv_T - ln_s);
+            lp = lp > 0.0f ? 0.0f : lp;
+            float H = 0.0f;
+            if (ENT) {
+                const double h = ln_s - 0.69314718055994530942 * static_cast<double>(a.u / a.s);
+                H = static_cast<float>(h < 0.0 ? 0.0 : h);
+            }
+            const TokenLoss t = policy_token(p, lp, old_logp, ref, adv);
+            const float g = held ? static_cast<float>(p.scale * weight * t.g) : 0.0f;
+            const float ge = ENT ? static_cast<float>(-p.scale * weight * p.ent_coef) : 0.0f;
+            if (tid == 0) {
+                logp[row] = lp;
+                if (ent) ent[row] = H;
+                double* o = parts + static_cast<size_t>(row) * kPolicySums;
+                o[0] = weight * t.pg;
+                o[1] = weight * t.kl;
+                o[2] = weight * H;
+                o[3] = t.clipped;
+                o[4] = t.dual;
+                o[5] = -t.lr;
+                o[6] = 1.0;
+            }
+            zero = g == 0.0f && ge == 0.0f;
+            k = row_grad(g, ge, H, static_cast<float>(inv_T));
+            m = a.m;
+            l2 = static_cast<float>(ln_s) * 1.44269504f;
         }
-        __builtin_amdgcn_sched_barrier(0);
+        const int y_lane = y - tid * E;
+        int nv = nvec;
+        asm volatile("" : "+s"(nv));
+        auto entry = [&](float x, int v) {
+            const float q = (x - m) * c - l2;
+            const float r = exp2_hw(q) * (ENT ? k.A + k.B * fmaxf(q, kFloor) : k.A);
+            return v == y_lane ? r + k.top : r;
+        };
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            asm volatile("" : "+v"(w[i]));   // unpacked again: the values of the first pass would not fit beside the row
+            if (tid < nv - i * THREADS) {
+                float x[E] = {};
+                if (!zero) {
+                    unpack<T>(w[i], x);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) x[j] = entry(x[j], i * THREADS * E + j);
+                }
+                if (next_live) w[i] = load_row<false>(vec_at(zn, i * THREADS, at));
+                store_row(vec_at(d, i * THREADS, at), pack<T>(x));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (tid < tail) {
+            Elem<T>::store(d, nvec * E + tid, zero ? 0.0f : entry(last, nvec * E + tid - tid * E));
+            if (next_live) last = Elem<T>::load(zn, nvec * E + tid);
+        }
+        row = next;
+        live = next_live;
     }
-    if (tid < tail) Elem<T>::store(d, nvec * E + tid, zero ? 0.0f : entry(last, nvec * E + tid));
 }
 
 // About 1024 workgroups in all, of whole 2048-entry blocks.
@@ -356,12 +389,14 @@ hipError_t forward(const LogprobArgs& a, RowPart* parts, hipStream_t s) {
     const int chunk = split_chunk(a.n, a.V), nchunks = (a.V + chunk - 1) / chunk;
     const T* z = static_cast<const T*>(a.logits);
     const PolicyArgs live = a.live ? *a.live : PolicyArgs{};
-    const auto kernel = a.ent ? token_logprobs_kernel<T, true> : token_logprobs_kernel<T, false>;
-    hipLaunchKernelGGL(kernel, dim3(a.n, nchunks), dim3(kRowThreads), 0, s, z, a.ld, a.V, a.targets, a.T,
+    const bool keep = a.stats != nullptr;   // the backward pass follows
+    const auto kernel = a.ent ? (keep ? token_logprobs_kernel<T, true, true> : token_logprobs_kernel<T, true, false>)
+                              : (keep ? token_logprobs_kernel<T, false, true> : token_logprobs_kernel<T, false, false>);
+    hipLaunchKernelGGL(kernel, dim3(a.n, nchunks), dim3(kRowThreads), 0, s, z, a.ld, a.V, a.targets, 1.0 / a.T,
                        log2_scale(a.T), chunk, a.live != nullptr, live, parts, a.logp, a.ent, a.stats);
     if (nchunks > 1)
         hipLaunchKernelGGL(token_logprobs_join_kernel<T>, dim3(a.n), dim3(64), 0, s, parts, nchunks, z, a.ld, a.V,
-                           a.targets, a.T, log2_scale(a.T), a.live != nullptr, live, a.logp, a.ent, a.stats);
+                           a.targets, 1.0 / a.T, log2_scale(a.T), a.live != nullptr, live, a.logp, a.ent, a.stats);
     return hipGetLastError();
 }
 
@@ -372,8 +407,9 @@ constexpr int kRowVecs = 20;
 template <typename T, int THREADS, int NV>
 hipError_t rows(const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz, int64_t ldd, hipStream_t s) {
     const auto kernel = a.ent ? policy_rows_kernel<T, THREADS, NV, true> : policy_rows_kernel<T, THREADS, NV, false>;
-    hipLaunchKernelGGL(kernel, dim3(a.n), dim3(THREADS), 0, s, p, w.counts, w.cparts, w.n_cparts,
-                       static_cast<const T*>(a.logits), a.ld, a.V, a.targets, a.T, log2_scale(a.T), static_cast<T*>(dz), ldd,
+    const int fit = 256 * (1024 / THREADS);
+    hipLaunchKernelGGL(kernel, dim3(a.n < fit ? a.n : fit), dim3(THREADS), 0, s, p, w.counts, w.cparts, w.n_cparts,
+                       static_cast<const T*>(a.logits), a.ld, a.V, a.targets, 1.0 / a.T, log2_scale(a.T), static_cast<T*>(dz), ldd,
                        a.logp, a.ent, w.parts);
     return hipGetLastError();
 }
@@ -428,11 +464,11 @@ hipError_t launch_token_logprobs_backward(int dt, const void* logits, int64_t ld
         const float* h = ge ? ge + r : nullptr;
         if (dt == DT_F32)
             hipLaunchKernelGGL(token_logprobs_backward_kernel<float>, dim3(nchunks, m), dim3(kRowThreads), 0, s,
-                               reinterpret_cast<const float*>(z), ld, V, targets + r, T, log2_scale(T), stats + 2 * r, e,
+                               reinterpret_cast<const float*>(z), ld, V, targets + r, 1.0f / T, log2_scale(T), stats + 2 * r, e,
                                g + r, h, chunk, reinterpret_cast<float*>(d), ldd);
         else
             hipLaunchKernelGGL(token_logprobs_backward_kernel<uint16_t>, dim3(nchunks, m), dim3(kRowThreads), 0, s,
-                               reinterpret_cast<const uint16_t*>(z), ld, V, targets + r, T, log2_scale(T), stats + 2 * r,
+                               reinterpret_cast<const uint16_t*>(z), ld, V, targets + r, 1.0f / T, log2_scale(T), stats + 2 * r,
                                e, g + r, h, chunk, reinterpret_cast<uint16_t*>(d), ldd);
     }
     return hipGetLastError();

@@ -39,12 +39,33 @@ struct TokenLoss {
     double pg, kl, g, lr;
     bool clipped, dual;
 };
+// exp(x) - 1 for |x| <= 20 in fp64: with e = exp(x / 2^14) - 1 from its series
+// (x / 2^14 is at most 1.3e-3: the term after the fifth is 4e-21), fourteen
+// times e <- e (2 + e), each of which doubles the argument.  Within 2e-14 of
+// the value, with five constants where the library's exp and expm1 have some
+// fifty: beside a row in registers those do not fit.
+__device__ __forceinline__ double expm1_20(double x) {
+    const double r = x * (1.0 / 16384.0);
+    double e = r * (1.0 + r * (0.5 + r * (1.0 / 6.0 + r * (1.0 / 24.0 + r * (1.0 / 120.0)))));
+#pragma unroll
+    for (int i = 0; i < 14; ++i) e = e * (2.0 + e);
+    return e;
+}
+
+// ln s in fp64 for a sum 1 <= s <= 2^24: the hardware's fp32 logarithm, and one
+// Newton step (within 5e-9).  NaN for 0 and NaN.
+__device__ __forceinline__ double ln_sum(float s) {
+    const double y = static_cast<double>(__builtin_amdgcn_logf(s)) * 0.69314718055994530942;
+    const double d = s * (1.0 + expm1_20(-y)) - 1.0;
+    return y + d * (1.0 - 0.5 * d);
+}
+
 __device__ __forceinline__ double clamp20(double x) { return x < -20.0 ? -20.0 : x > 20.0 ? 20.0 : x; }
 __device__ __forceinline__ TokenLoss policy_token(const PolicyArgs& p, double logp, double old_logp, double ref, double A) {
     TokenLoss t;
     t.lr = logp - old_logp;
     const double lr = clamp20(t.lr);
-    const double r = exp(lr);
+    const double r = 1.0 + expm1_20(lr);
     t.clipped = (A > 0.0 && r > p.hi) || (A < 0.0 && r < p.lo);
     t.dual = p.dual > 0.0 && A < 0.0 && r > p.dual;
     const double bound = A > 0.0 ? p.hi : p.lo;
@@ -62,7 +83,7 @@ __device__ __forceinline__ TokenLoss policy_token(const PolicyArgs& p, double lo
             t.kl = 0.5 * d * d;
             dk = -d;
         } else {
-            const double e = expm1(d);
+            const double e = expm1_20(d);
             t.kl = e - d;
             dk = -e;
         }
