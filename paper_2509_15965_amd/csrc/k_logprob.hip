@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(kRowThreads) token_logprobs_kernel(const T* __
         RowPart* __restrict__ parts, float* __restrict__ logp, float* __restrict__ ent, float* __restrict__ stats) {
     __shared__ RowPart sp[kRowThreads / 64];
     const int row = blockIdx.x, nchunks = gridDim.y;
-    if (check && !token_counts(live, row)) {
+    if (check && counted_seq(live, row) < 0) {
         if (threadIdx.x == 0 && nchunks == 1) finish_dead(row, logp, ent, stats);
         return;
     }
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(64) token_logprobs_join_kernel(const RowPart* 
         const T* __restrict__ logits, int64_t ld, int V, const int32_t* __restrict__ targets, double inv_T, float c,
         bool check, PolicyArgs live, float* __restrict__ logp, float* __restrict__ ent, float* __restrict__ stats) {
     const int row = blockIdx.x;
-    if (check && !token_counts(live, row)) {
+    if (check && counted_seq(live, row) < 0) {
         if (threadIdx.x == 0) finish_dead(row, logp, ent, stats);
         return;
     }
@@ -260,44 +260,47 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
         float* __restrict__ ent, double* __restrict__ parts) {
     constexpr int E = kVec<T>, WAVES = THREADS / 64;
     __shared__ RowPart sp[2][WAVES];
+    __shared__ double sums[kPolicySums];   // of this workgroup's rows, the first lane's
     const int tid = threadIdx.x;
     const int nvec = V / E, tail = V - nvec * E;
     const uint32_t at = tid * 16;
     u32x4 w[NV];
     float last = -INFINITY;
+    if (tid == 0)
+        for (int q = 0; q < kPolicySums; ++q) sums[q] = 0.0;
     int row = blockIdx.x;
-    bool live = token_counts(p, row);
+    int seq = counted_seq(p, row);
+    const PolicyTotals totals = policy_totals(p, cparts, n_cparts);
 #pragma unroll
     for (int i = 0; i < NV; ++i) w[i] = nothing<T>();
-    if (live) {
+    if (seq >= 0) {
         const T* z = logits + row * ld;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (tid < nvec - i * THREADS) w[i] = load_row<false>(vec_at(z, i * THREADS, at));
         if (tid < tail) last = Elem<T>::load(z, nvec * E + tid);
     }
-    for (int turn = 0; row < p.n; turn ^= 1) {
+    int turn = 0;   // half of sp: of two rows in a row that use it, the second has a barrier behind the first's reads
+    while (row < p.n) {
         const int next = row + gridDim.x;
-        const bool next_live = next < p.n && token_counts(p, next);
+        const int next_seq = next < p.n ? counted_seq(p, next) : -1;
         const T* zn = logits + next * ld;
         T* d = dz + row * ldd;
         float m = 0.0f, l2 = 0.0f;
         RowGrad k{0.0f, 0.0f, 0.0f};
         int y = -1;
         bool zero = true;
-        if (!live) {
+        if (seq < 0) {
             if (tid == 0) {
                 logp[row] = 0.0f;
                 if (ent) ent[row] = 0.0f;
-                for (int q = 0; q < kPolicySums; ++q) parts[static_cast<size_t>(row) * kPolicySums + q] = 0.0;
             }
         } else {
             y = targets[row];
             const bool held = y >= 0 && y < V;
             const float zy = held ? Elem<T>::load(logits + row * ld, y) : __builtin_nanf("");
-            const int s = seq_of(p.offs, p.n_seqs, row);
-            const double weight = policy_weight(p, s, counts, cparts, n_cparts);
-            const float adv = p.adv[p.token_adv ? row : s], old_logp = p.old_logp[row], ref = p.ref ? p.ref[row] : 0.0f;
+            const double weight = policy_weight(p, totals, seq, counts);
+            const float adv = p.adv[p.token_adv ? row : seq], old_logp = p.old_logp[row], ref = p.ref ? p.ref[row] : 0.0f;
             LaneSum acc{{-FLT_MAX, 0.0f, 0.0f}, -FLT_MAX};
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -315,6 +318,7 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
             __syncthreads();
             a = merge_lanes<WAVES>(sp[turn][tid % WAVES], c);
             a = RowPart{first_lane(a.m), first_lane(a.s), first_lane(a.u)};
+            turn ^= 1;
             const double ln_s = ln_sum(a.s);
             float lp = static_cast<float>((static_cast<double>(zy) - a.m) * inv_T - ln_s);
             lp = lp > 0.0f ? 0.0f : lp;
@@ -329,14 +333,13 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
             if (tid == 0) {
                 logp[row] = lp;
                 if (ent) ent[row] = H;
-                double* o = parts + static_cast<size_t>(row) * kPolicySums;
-                o[0] = weight * t.pg;
-                o[1] = weight * t.kl;
-                o[2] = weight * H;
-                o[3] = t.clipped;
-                o[4] = t.dual;
-                o[5] = -t.lr;
-                o[6] = 1.0;
+                sums[0] += weight * t.pg;
+                sums[1] += weight * t.kl;
+                sums[2] += weight * H;
+                sums[3] += t.clipped;
+                sums[4] += t.dual;
+                sums[5] -= t.lr;
+                sums[6] += 1.0;
             }
             zero = g == 0.0f && ge == 0.0f;
             k = row_grad(g, ge, H, static_cast<float>(inv_T));
@@ -361,18 +364,20 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
 #pragma unroll
                     for (int j = 0; j < E; ++j) x[j] = entry(x[j], i * THREADS * E + j);
                 }
-                if (next_live) w[i] = load_row<false>(vec_at(zn, i * THREADS, at));
+                if (next_seq >= 0) w[i] = load_row<false>(vec_at(zn, i * THREADS, at));
                 store_row(vec_at(d, i * THREADS, at), pack<T>(x));
             }
             __builtin_amdgcn_sched_barrier(0);
         }
         if (tid < tail) {
             Elem<T>::store(d, nvec * E + tid, zero ? 0.0f : entry(last, nvec * E + tid - tid * E));
-            if (next_live) last = Elem<T>::load(zn, nvec * E + tid);
+            if (next_seq >= 0) last = Elem<T>::load(zn, nvec * E + tid);
         }
         row = next;
-        live = next_live;
+        seq = next_seq;
     }
+    if (tid == 0)
+        for (int q = 0; q < kPolicySums; ++q) parts[static_cast<size_t>(blockIdx.x) * kPolicySums + q] = sums[q];
 }
 
 // About 1024 workgroups in all, of whole 2048-entry blocks.
@@ -405,17 +410,17 @@ hipError_t forward(const LogprobArgs& a, RowPart* parts, hipStream_t s) {
 constexpr int kRowVecs = 20;
 
 template <typename T, int THREADS, int NV>
-hipError_t rows(const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz, int64_t ldd, hipStream_t s) {
+int rows(const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz, int64_t ldd, hipStream_t s) {
     const auto kernel = a.ent ? policy_rows_kernel<T, THREADS, NV, true> : policy_rows_kernel<T, THREADS, NV, false>;
-    const int fit = 256 * (1024 / THREADS);
-    hipLaunchKernelGGL(kernel, dim3(a.n < fit ? a.n : fit), dim3(THREADS), 0, s, p, w.counts, w.cparts, w.n_cparts,
-                       static_cast<const T*>(a.logits), a.ld, a.V, a.targets, 1.0 / a.T, log2_scale(a.T), static_cast<T*>(dz), ldd,
-                       a.logp, a.ent, w.parts);
-    return hipGetLastError();
+    const int fit = kCUs * (1024 / THREADS), grid = a.n < fit ? a.n : fit;
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(THREADS), 0, s, p, w.counts, w.cparts, w.n_cparts,
+                       static_cast<const T*>(a.logits), a.ld, a.V, a.targets, 1.0 / a.T, log2_scale(a.T),
+                       static_cast<T*>(dz), ldd, a.logp, a.ent, w.parts);
+    return grid;
 }
 
 template <typename T>
-hipError_t rows_of(const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz, int64_t ldd, hipStream_t s) {
+int rows_of(const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz, int64_t ldd, hipStream_t s) {
     const int nvec = a.V / kVec<T>;
     if (nvec <= 4 * 256) return rows<T, 256, 4>(p, w, a, dz, ldd, s);
     if (nvec <= 8 * 256) return rows<T, 256, 8>(p, w, a, dz, ldd, s);
@@ -434,8 +439,9 @@ bool policy_rows_fit(int dt, int n, int V) {
 }
 
 hipError_t launch_policy_rows(int dt, const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz, int64_t ldd,
-                              hipStream_t s) {
-    return dt == DT_F32 ? rows_of<float>(p, w, a, dz, ldd, s) : rows_of<uint16_t>(p, w, a, dz, ldd, s);
+                              int* n_parts, hipStream_t s) {
+    *n_parts = dt == DT_F32 ? rows_of<float>(p, w, a, dz, ldd, s) : rows_of<uint16_t>(p, w, a, dz, ldd, s);
+    return hipGetLastError();
 }
 
 size_t logprob_parts(int n, int V) {

@@ -357,25 +357,26 @@ hipError_t launch_token_logprobs_backward(int dt, const void* logits, int64_t ld
 struct CountPart { int32_t tokens, seqs; };
 // Sums over counted tokens: w pg, w kl, w entropy, clipped, dual-clipped, old - new log-probability, tokens.
 constexpr int kPolicySums = 7;
-// A policy loss's scratch: counted tokens of each sequence, their totals in
-// parts, and one kPolicySums a workgroup (or row).
+// A policy loss's scratch: counted tokens of each sequence and their totals in
+// parts (both null where the offsets say it all), and one kPolicySums a workgroup.
 struct PolicyWs {
     int32_t* counts;
     CountPart* cparts;
     int n_cparts;
     double* parts;
 };
+constexpr int kPolicyMaxRowParts = 1024;   // workgroups of a policy_rows launch
 PolicyWs policy_ws(const PolicyArgs& p, void* ws);
 size_t policy_ws_bytes(int n, int n_seqs);
-size_t policy_rows_ws_bytes(int n, int n_seqs);   // with one kPolicySums a row
+size_t policy_loss_ws_bytes(int n, int n_seqs);   // what launch_policy_loss alone needs
 hipError_t launch_policy_counts(const PolicyArgs& p, const PolicyWs& w, hipStream_t s);
 hipError_t launch_policy_final(const PolicyArgs& p, const PolicyWs& w, int n_parts, float* out, hipStream_t s);
 
-// Loss and gradient of rows that fit a workgroup's registers, one workgroup a
-// row, where there are rows enough (policy_rows_fit); parts gets one kPolicySums a row.
+// Loss and gradient of rows that fit a workgroup's registers, where there are
+// rows enough (policy_rows_fit); w.parts gets *n_parts entries.
 bool policy_rows_fit(int dt, int n, int V);
 hipError_t launch_policy_rows(int dt, const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz, int64_t ldd,
-                              hipStream_t s);
+                              int* n_parts, hipStream_t s);
 // ent, d_logp and d_ent may be null (d_logp: the loss alone)
 hipError_t launch_policy_loss(const PolicyArgs& p, const float* logp, const float* ent, float* out, float* d_logp,
                               float* d_ent, void* ws, hipStream_t s);

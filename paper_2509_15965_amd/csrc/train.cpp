@@ -48,7 +48,7 @@ struct LogitsWs {
 };
 LogitsWs logits_ws(int n, int n_seqs, int V) {
     LogitsWs w;
-    size_t at = policy_rows_ws_bytes(n, n_seqs);
+    size_t at = policy_ws_bytes(n, n_seqs);
     w.off_g = at;
     at += align256(sizeof(float) * n);
     w.off_ge = at;
@@ -111,7 +111,7 @@ rl_status rl_token_logprobs_backward(int32_t n, int32_t vocab, int32_t dtype, co
 }
 
 size_t rl_policy_workspace_bytes(int32_t n, int32_t n_seqs) {
-    return n < 0 || n > kMaxTokens || n_seqs < 1 || n_seqs > kMaxSeqs ? 0 : policy_ws_bytes(n, n_seqs);
+    return n < 0 || n > kMaxTokens || n_seqs < 1 || n_seqs > kMaxSeqs ? 0 : policy_loss_ws_bytes(n, n_seqs);
 }
 
 rl_status rl_policy_loss(const rl_policy_batch* batch, const rl_policy_params* params, const float* logp, const float* entropy,
@@ -120,7 +120,7 @@ rl_status rl_policy_loss(const rl_policy_batch* batch, const rl_policy_params* p
     if (!policy_ok(batch, params, &p) || !out_loss) return RL_ERR_INVALID_ARG;
     if (p.n > 0 && (!logp || !d_logp)) return RL_ERR_INVALID_ARG;
     if (!entropy && p.ent_coef != 0.0) return RL_ERR_INVALID_ARG;
-    if (const rl_status st = workspace_ok(workspace, ws_bytes, policy_ws_bytes(p.n, p.n_seqs)); st != RL_OK) return st;
+    if (const rl_status st = workspace_ok(workspace, ws_bytes, policy_loss_ws_bytes(p.n, p.n_seqs)); st != RL_OK) return st;
     return status_of(launch_policy_loss(p, logp, entropy, out_loss, d_logp, d_entropy, workspace, static_cast<hipStream_t>(stream)));
 }
 
@@ -154,8 +154,9 @@ rl_status rl_policy_loss_logits(const rl_policy_batch* batch, const rl_policy_pa
     if (policy_rows_fit(dtype, p.n, vocab)) {
         const PolicyWs pw = policy_ws(p, base);
         hipError_t e = launch_policy_counts(p, pw, s);
-        if (e == hipSuccess) e = launch_policy_rows(dtype, p, pw, a, d_logits, ldd, s);
-        if (e == hipSuccess) e = launch_policy_final(p, pw, p.n, out_loss, s);
+        int n_parts = 0;
+        if (e == hipSuccess) e = launch_policy_rows(dtype, p, pw, a, d_logits, ldd, &n_parts, s);
+        if (e == hipSuccess) e = launch_policy_final(p, pw, n_parts, out_loss, s);
         return status_of(e);
     }
     hipError_t e = launch_token_logprobs(dtype, a, reinterpret_cast<RowPart*>(base + w.off_parts), s);

@@ -14,21 +14,36 @@ __device__ __forceinline__ void seq_range(const int32_t* offs, int n, int s, int
     *b = hi < *a ? *a : hi > n ? n : hi;
 }
 
-// Sequence of token i, or -1.
-__device__ __forceinline__ int seq_of(const int32_t* offs, int n_seqs, int i) {
-    if (!offs) return 0;
-    int lo = 0, hi = n_seqs + 1;   // first entry above i
+// Entries of offs[lo .. hi) that are at most i (the entries do not decrease).
+__device__ __forceinline__ int count_upto(const int32_t* offs, int lo, int hi, int i) {
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         if (offs[mid] <= i) lo = mid + 1;
         else hi = mid;
     }
+    return lo;
+}
+
+// Sequence of token i, or -1, by a whole wave (i the same in every lane): 64
+// probes a round, two rounds up to 4095 sequences.
+__device__ __forceinline__ int seq_of_wave(const int32_t* offs, int n_seqs, int i) {
+    if (!offs) return 0;
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = n_seqs + 1;   // the first entry above i is in [lo, hi]
+    while (lo < hi) {
+        const int step = (hi - lo + 63) >> 6;
+        const int at = lo + (lane + 1) * step - 1;
+        const int c = __popcll(__ballot(at < hi && offs[at < hi ? at : hi - 1] <= i));
+        lo += c * step;
+        hi = lo + step - 1 < hi ? lo + step - 1 : hi;
+        lo = lo < hi ? lo : hi;
+    }
     return lo - 1 < n_seqs ? lo - 1 : -1;
 }
 
-__device__ __forceinline__ bool token_counts(const PolicyArgs& p, int i) {
-    if (p.mask && !p.mask[i]) return false;
-    return !p.offs || (i >= p.offs[0] && i < p.offs[p.n_seqs]);
+// Sequence of row i when its token counts, else -1 (the whole wave asks for one row).
+__device__ __forceinline__ int counted_seq(const PolicyArgs& p, int i) {
+    return p.mask && !p.mask[i] ? -1 : seq_of_wave(p.offs, p.n_seqs, i);
 }
 
 // The policy and KL terms of one counted token and their derivatives by its
@@ -101,14 +116,46 @@ __device__ __forceinline__ int wave_sum(int v) {
     return v;
 }
 
-// Weight of a counted token of sequence s: 1 / counted tokens, 1 / (its
-// sequence's x sequences that have some), or 1.  Every lane of a wave calls it.
-__device__ __forceinline__ double policy_weight(const PolicyArgs& p, int s, const int32_t* counts, const CountPart* cparts,
-                                                int n_cparts) {
+// What the weights divide by: counted tokens, sequences that have some.
+struct PolicyTotals { int tokens, seqs; };
+
+// Called by every lane of every wave; each wave sums for itself.  Without
+// counts (cparts null) no mask takes a token out, and they come from the offsets.
+__device__ __forceinline__ PolicyTotals policy_totals(const PolicyArgs& p, const CountPart* cparts, int n_cparts) {
+    const int lane = threadIdx.x & 63;
+    PolicyTotals t{0, 0};
+    if (p.agg == 2) return t;
+    if (cparts) {
+        for (int k = lane; k < n_cparts; k += 64) { t.tokens += cparts[k].tokens; t.seqs += cparts[k].seqs; }
+    } else if (p.agg == 1) {
+        for (int s = lane; s < p.n_seqs; s += 64) {
+            int a, b;
+            seq_range(p.offs, p.n, s, &a, &b);
+            t.tokens += b - a;
+            t.seqs += b > a;
+        }
+    } else {
+        int a, b, e;
+        seq_range(p.offs, p.n, 0, &a, &b);
+        seq_range(p.offs, p.n, p.n_seqs - 1, &e, &b);
+        return PolicyTotals{b - a, 0};
+    }
+    return PolicyTotals{wave_sum(t.tokens), wave_sum(t.seqs)};
+}
+
+// Weight of a counted token of sequence s.
+__device__ __forceinline__ double policy_weight(const PolicyArgs& p, const PolicyTotals& t, int s, const int32_t* counts) {
     if (p.agg == 2) return 1.0;
-    int tokens = 0, seqs = 0;
-    for (int k = threadIdx.x & 63; k < n_cparts; k += 64) { tokens += cparts[k].tokens; seqs += cparts[k].seqs; }
-    return p.agg == 0 ? 1.0 / wave_sum(tokens) : 1.0 / (static_cast<double>(counts[s]) * wave_sum(seqs));
+    if (p.agg == 0) return 1.0 / t.tokens;
+    int len;
+    if (counts) {
+        len = counts[s];
+    } else {
+        int a, b;
+        seq_range(p.offs, p.n, s, &a, &b);
+        len = b - a;
+    }
+    return 1.0 / (static_cast<double>(len) * t.seqs);
 }
 
 }  // namespace rl

@@ -90,7 +90,7 @@ def test_backward_no_rows():
 
 
 def policy(batch=(), params=(), logp=P, ent=P, out=P, g=P, ge=P, ws=P, nb=WS, logits=None):
-    b = R.PolicyBatch(10, 2, P, P, P, P, P)
+    b = R.PolicyBatch(10000, 2, P, P, P, P, P)
     q = R.PolicyParams(0.2, 0.2, 0.0, 0.1, 0.01, 1.0, 3, 0, 0, 0)
     for k, v in dict(batch).items():
         setattr(b, k, v)
