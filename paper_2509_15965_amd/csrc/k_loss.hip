@@ -76,16 +76,38 @@ __global__ void __launch_bounds__(kThreads) policy_count_kernel(int n, int n_seq
 
 constexpr int kSums = kPolicySums;
 
-// Sums over a workgroup of N values a lane; lane k < N of the first wave writes out[k].
-template <int N, int THREADS> __device__ void block_sums(double* v, double* out) {
-    __shared__ double sh[THREADS / 64][N];
+// Adds the lane that a DPP control names (nothing where it names none or the row is masked).
+template <int CTRL, int ROWS> __device__ __forceinline__ double add_dpp(double v) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<uint32_t>(b), CTRL, ROWS, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<uint32_t>(b >> 32), CTRL, ROWS, 0xF, false);
+    return v + __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
+}
+// Sums over a wave; lane 63 has them.  Within rows of 16 lanes, then row to
+// row: register moves, where shuffles would go through LDS twelve times a value.
+template <int N> __device__ __forceinline__ void wave_sums(double* v) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = wave_sum(v[k]);
-    if ((threadIdx.x & 63) == 0)
+    for (int k = 0; k < N; ++k) {
+        v[k] = add_dpp<0x111, 0xF>(v[k]);   // row_shr 1, 2, 4, 8
+        v[k] = add_dpp<0x112, 0xF>(v[k]);
+        v[k] = add_dpp<0x114, 0xF>(v[k]);
+        v[k] = add_dpp<0x118, 0xF>(v[k]);
+        v[k] = add_dpp<0x142, 0xA>(v[k]);   // lane 15 of rows 0 and 2 to rows 1 and 3
+        v[k] = add_dpp<0x143, 0xC>(v[k]);   // lane 31 to rows 2 and 3
+    }
+}
+
+// Sums over a workgroup of N values a lane; lane k < N of the first wave writes out[k].
+template <int N, int THREADS> __device__ __forceinline__ void block_sums(double* v, double* out) {
+    __shared__ double sh[THREADS / 64][N];
+    wave_sums<N>(v);
+    if ((threadIdx.x & 63) == 63)
+#pragma unroll
         for (int k = 0; k < N; ++k) sh[threadIdx.x >> 6][k] = v[k];
     __syncthreads();
     if (threadIdx.x < N) {
         double t = 0.0;
+#pragma unroll 1
         for (int w = 0; w < THREADS / 64; ++w) t += sh[w][threadIdx.x];
         out[threadIdx.x] = t;
     }
@@ -99,10 +121,13 @@ __device__ __forceinline__ void policy_outputs(const double* t, double kl_coef, 
     out[7] = static_cast<float>(t[6]);
 }
 
-// One token: its terms into v, its gradients out.  s: its sequence, or -1.
+// One token: its terms into v, its gradients out.
 struct TokenIn { float logp, old_logp, ref, ent; };
 __device__ __forceinline__ TokenIn load_token(const PolicyArgs& p, const float* logp, const float* ent, int i) {
-    return TokenIn{logp[i], p.old_logp[i], p.ref ? p.ref[i] : 0.0f, ent ? ent[i] : 0.0f};
+    TokenIn t{*nth(logp, i), *nth(p.old_logp, i), 0.0f, 0.0f};
+    if (p.ref) t.ref = *nth(p.ref, i);
+    if (ent) t.ent = *nth(ent, i);
+    return t;
 }
 __device__ __forceinline__ void one_token(const PolicyArgs& p, const TokenIn& in, bool live, float adv, double w, double* v,
                                           float* d_logp, float* d_ent, int i) {
@@ -119,59 +144,71 @@ __device__ __forceinline__ void one_token(const PolicyArgs& p, const TokenIn& in
         g = p.scale * w * t.g;
         ge = -p.scale * w * p.ent_coef;
     }
-    if (d_logp) d_logp[i] = static_cast<float>(g);
-    if (d_ent) d_ent[i] = static_cast<float>(ge);
+    if (d_logp) *nth(d_logp, i) = static_cast<float>(g);
+    if (d_ent) *nth(d_ent, i) = static_cast<float>(ge);
 }
 
-// Tokens of a workgroup, four a lane.  The sequences they lie in are found
-// once for the workgroup, then by each lane among those in LDS.
+// Tokens of a workgroup, four a lane, the next one's loads under the present
+// one's arithmetic.  The sequences they lie in are found once for the
+// workgroup, then by each lane among those in LDS.
 constexpr int kTokensPerLane = 4, kTokensPerBlock = kThreads * kTokensPerLane, kSpan = 512;
 
 __global__ void __launch_bounds__(kThreads) policy_loss_kernel(PolicyArgs p, const float* __restrict__ logp,
         const float* __restrict__ ent, const int32_t* __restrict__ counts, const CountPart* __restrict__ cparts,
         int n_cparts, float* __restrict__ d_logp, float* __restrict__ d_ent, double* __restrict__ parts) {
     __shared__ int32_t span[kSpan];
+    __shared__ double weight[kSpan + 1];
+    __shared__ float adv[kSpan + 1];
     __shared__ int32_t ends[2];
+    __shared__ PolicyTotals total;
     const int tid = threadIdx.x, first = blockIdx.x * kTokensPerBlock;
     const int last = min(p.n, first + kTokensPerBlock) - 1;
-    TokenIn in[kTokensPerLane];
-    bool live[kTokensPerLane];
-#pragma unroll
-    for (int k = 0; k < kTokensPerLane; ++k) {
-        const int i = min(first + k * kThreads + tid, last);
-        in[k] = load_token(p, logp, ent, i);
-        live[k] = !p.mask || p.mask[i];
+    int i = first + tid, at = min(i, last);
+    TokenIn next = load_token(p, logp, ent, at);
+    uint8_t next_m = p.mask ? *nth(p.mask, at) : 1;
+    float next_adv = p.token_adv ? *nth(p.adv, at) : 0.0f;
+    // two waves: offsets at most the first token, and at most the last; another: the totals
+    if (tid < 128) {
+        const int t = tid < 64 ? first : last;
+        const int s = seq_of_wave(p.offs, p.n_seqs, t);
+        if ((tid & 63) == 0) ends[tid >> 6] = !p.offs ? 1 : s >= 0 ? s + 1 : t < p.offs[0] ? 0 : p.n_seqs + 1;
+    } else if (tid < 192) {
+        const PolicyTotals t = policy_totals(p, cparts, n_cparts);
+        if (tid == 128) total = t;
     }
-    const PolicyTotals totals = policy_totals(p, cparts, n_cparts);
-    int s_lo = 0, s_hi = 0;
-    if (p.offs) {
-        // entries at most the first token, and at most the last
-        if (tid < 128) {
-            const int s = seq_of_wave(p.offs, p.n_seqs, tid < 64 ? first : last);
-            const int i = tid < 64 ? first : last;
-            if ((tid & 63) == 0) ends[tid >> 6] = s >= 0 ? s + 1 : i < p.offs[0] ? 0 : p.n_seqs + 1;
+    __syncthreads();
+    const int s_lo = min(ends[0], ends[1]), s_hi = max(ends[0], ends[1]);
+    const PolicyTotals totals = total;
+    const bool held = s_hi - s_lo <= kSpan;
+    if (held) {   // entry k: offset s_lo + k, sequence s_lo - 1 + k
+        for (int k = tid; k <= s_hi - s_lo; k += kThreads) {
+            if (k < s_hi - s_lo) span[k] = p.offs[s_lo + k];
+            const int s = s_lo - 1 + k;
+            if (s < 0 || s >= p.n_seqs) continue;
+            weight[k] = policy_weight(p, totals, s, counts);
+            if (!p.token_adv) adv[k] = p.adv[s];
         }
         __syncthreads();
-        s_lo = min(ends[0], ends[1]);
-        s_hi = max(ends[0], ends[1]);
-        if (s_hi - s_lo <= kSpan) {
-            for (int k = tid; k < s_hi - s_lo; k += kThreads) span[k] = p.offs[s_lo + k];
-            __syncthreads();
-        }
     }
     double v[kSums] = {};
-#pragma unroll
-    for (int k = 0; k < kTokensPerLane; ++k) {
-        const int i = first + k * kThreads + tid;
-        if (i > last) break;
-        int s = 0;
-        if (p.offs) {
-            const int c = s_hi - s_lo <= kSpan ? s_lo + count_upto(span, 0, s_hi - s_lo, i) : count_upto(p.offs, s_lo, s_hi, i);
-            s = c - 1 < p.n_seqs ? c - 1 : -1;
+#pragma unroll 1
+    for (; i <= last; i += kThreads) {
+        const TokenIn in = next;
+        const uint8_t m = next_m;
+        at = min(i + kThreads, last);
+        next = load_token(p, logp, ent, at);
+        if (p.mask) next_m = *nth(p.mask, at);
+        const int c = held ? s_lo + count_upto(span, 0, s_hi - s_lo, i) : count_upto(p.offs, s_lo, s_hi, i);
+        const int s = c - 1 < p.n_seqs ? c - 1 : -1;
+        const bool on = m && s >= 0;
+        float A = 0.0f;
+        double w = 0.0;
+        if (on) {
+            A = p.token_adv ? next_adv : held ? adv[c - s_lo] : p.adv[s];
+            w = held ? weight[c - s_lo] : policy_weight(p, totals, s, counts);
         }
-        const bool on = live[k] && s >= 0;
-        one_token(p, in[k], on, on ? p.adv[p.token_adv ? i : s] : 0.0f, on ? policy_weight(p, totals, s, counts) : 0.0, v,
-                  d_logp, d_ent, i);
+        if (p.token_adv) next_adv = *nth(p.adv, at);
+        one_token(p, in, on, A, w, v, d_logp, d_ent, i);
     }
     block_sums<kSums, kThreads>(v, parts + static_cast<size_t>(blockIdx.x) * kSums);
 }
@@ -196,51 +233,42 @@ constexpr int kSmallThreads = 1024, kSmallTokens = 4096, kSmallSeqs = 1024;
 
 __global__ void __launch_bounds__(kSmallThreads) policy_small_kernel(PolicyArgs p, const float* __restrict__ logp,
         const float* __restrict__ ent, float* __restrict__ d_logp, float* __restrict__ d_ent, float* __restrict__ out) {
-    constexpr int PER = kSmallTokens / kSmallThreads;
     __shared__ int32_t offs[kSmallSeqs + 1], counts[kSmallSeqs];
+    __shared__ int16_t seq[kSmallTokens];
     __shared__ int32_t total[2];
     __shared__ double t[kSums];
     const int tid = threadIdx.x;
-    TokenIn in[PER];
-    bool live[PER];
-    int seq[PER];
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        const int i = k * kSmallThreads + tid;
-        live[k] = i < p.n && (!p.mask || p.mask[i]);
-        if (live[k]) in[k] = load_token(p, logp, ent, i);
+    TokenIn next{};
+    if (tid < p.n) next = load_token(p, logp, ent, tid);
+    for (int s = tid; s <= p.n_seqs; s += kSmallThreads) {
+        offs[s] = p.offs ? p.offs[s] : s * p.n;
+        if (s < kSmallSeqs) counts[s] = 0;
     }
-    for (int s = tid; s <= p.n_seqs; s += kSmallThreads) offs[s] = p.offs ? p.offs[s] : s * p.n;
-    for (int s = tid; s < p.n_seqs; s += kSmallThreads) counts[s] = 0;
     if (tid < 2) total[tid] = 0;
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        const int c = count_upto(offs, 0, p.n_seqs + 1, k * kSmallThreads + tid);
-        seq[k] = live[k] && c - 1 < p.n_seqs ? c - 1 : -1;
-        if (seq[k] >= 0) atomicAdd(&counts[seq[k]], 1);
+#pragma unroll 1
+    for (int i = tid; i < p.n; i += kSmallThreads) {
+        const uint8_t m = p.mask ? *nth(p.mask, i) : 1;
+        const int c = count_upto(offs, 0, p.n_seqs + 1, i);
+        const int s = m && c - 1 < p.n_seqs ? c - 1 : -1;
+        seq[i] = static_cast<int16_t>(s);
+        if (s >= 0) atomicAdd(&counts[s], 1);
     }
     __syncthreads();
-    int tokens = 0, seqs = 0;
-    for (int s = tid; s < p.n_seqs; s += kSmallThreads) {
-        tokens += counts[s];
-        seqs += counts[s] > 0;
-    }
-    tokens = wave_sum(tokens);
-    seqs = wave_sum(seqs);
-    if ((tid & 63) == 0 && tokens) {
-        atomicAdd(&total[0], tokens);
-        atomicAdd(&total[1], seqs);
+    if (tid < p.n_seqs && counts[tid]) {   // kSmallSeqs lanes
+        atomicAdd(&total[0], counts[tid]);
+        atomicAdd(&total[1], 1);
     }
     __syncthreads();
     const PolicyTotals totals{total[0], total[1]};
     double v[kSums] = {};
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        const int i = k * kSmallThreads + tid, s = seq[k];
-        if (i < p.n)
-            one_token(p, in[k], s >= 0, s >= 0 ? p.adv[p.token_adv ? i : s] : 0.0f,
-                      s >= 0 ? policy_weight(p, totals, s, counts) : 0.0, v, d_logp, d_ent, i);
+#pragma unroll 1
+    for (int i = tid; i < p.n; i += kSmallThreads) {
+        const TokenIn in = next;
+        if (i + kSmallThreads < p.n) next = load_token(p, logp, ent, i + kSmallThreads);
+        const int s = seq[i];
+        one_token(p, in, s >= 0, s >= 0 ? *nth(p.adv, p.token_adv ? i : s) : 0.0f,
+                  s >= 0 ? policy_weight(p, totals, s, counts) : 0.0, v, d_logp, d_ent, i);
     }
     block_sums<kSums, kSmallThreads>(v, t);
     __syncthreads();
@@ -261,84 +289,75 @@ int blocks_of(int n) { return (n + kTokensPerBlock - 1) / kTokensPerBlock; }
 // logp chosen and rejected.
 constexpr int kPairSums = 6;
 
-__global__ void __launch_bounds__(kThreads) preference_kernel(PrefArgs p, double* __restrict__ parts) {
-    __shared__ double sums[6];   // log ratio, logp, counted tokens: chosen, rejected
-    const int pair = blockIdx.x;
-    if (pair == p.n_pairs) {     // tokens that no sequence holds
-        int a, b;
-        seq_range(p.offs, p.n, 0, &a, &b);
-        for (int i = threadIdx.x; i < a; i += kThreads) p.d_logp[i] = 0.0f;
-        seq_range(p.offs, p.n, 2 * p.n_pairs - 1, &a, &b);
-        for (int i = b + threadIdx.x; i < p.n; i += kThreads) p.d_logp[i] = 0.0f;
-        return;
-    }
-    int a[2], b[2];
-    double v[6] = {};
+// A sequence's sums: log ratio, logp, counted tokens.
+struct SeqSums { double ratio, logp, count; };
+
+// Lane `at` of `lanes` adds its share of tokens [a, b), the same lane the same token of every sequence:
+// equal sequences have equal sums wherever they lie.
+template <int U> __device__ __forceinline__ SeqSums seq_sums(const PrefArgs& p, int a, int b, int at, int lanes) {
+    SeqSums t{0.0, 0.0, 0.0};
+#pragma unroll 1
+    for (int i = a + at; i < b; i += U * lanes) {
+        float lp[U], ref[U] = {};
+        uint8_t m[U];
+        int q[U];
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        seq_range(p.offs, p.n, 2 * pair + side, &a[side], &b[side]);
-        for (int i = a[side] + threadIdx.x; i < b[side]; i += kThreads) {
-            if (p.mask && !p.mask[i]) continue;
-            const double lp = p.logp[i];
-            v[3 * side] += p.ref ? lp - p.ref[i] : lp;
-            v[3 * side + 1] += lp;
-            v[3 * side + 2] += 1.0;
+        for (int u = 0; u < U; ++u) {   // every load before any sum, none of them behind a lane's branch
+            q[u] = i + u * lanes < b ? i + u * lanes : i;
+            lp[u] = *nth(p.logp, q[u]);
+            m[u] = 1;
+        }
+        if (p.ref)
+#pragma unroll
+            for (int u = 0; u < U; ++u) ref[u] = *nth(p.ref, q[u]);
+        if (p.mask)
+#pragma unroll
+            for (int u = 0; u < U; ++u) m[u] = *nth(p.mask, q[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!m[u] || i + u * lanes >= b) continue;
+            t.ratio += static_cast<double>(lp[u]) - ref[u];
+            t.logp += lp[u];
+            t.count += 1.0;
         }
     }
-    block_sums<6, kThreads>(v, sums);
-    __syncthreads();
-    double per[2], R[2];
-    for (int side = 0; side < 2; ++side) {
-        const double cnt = sums[3 * side + 2];
-        per[side] = p.average && cnt > 0.0 ? 1.0 / cnt : 1.0;
-        R[side] = p.beta * (sums[3 * side] * per[side]);
-    }
-    const double h = R[0] - R[1] - p.margin;
-    double loss, dh;
-    if (p.form == 0) {
-        // ln sigmoid(x) = min(x, 0) - ln(1 + exp(-|x|))
-        const double tail = log1p(exp(-fabs(h)));
-        const double lp = (h < 0.0 ? h : 0.0) - tail, ln = (h > 0.0 ? -h : 0.0) - tail;
-        loss = -(1.0 - p.smooth) * lp - p.smooth * ln;
-        dh = h != h ? h : p.smooth - exp(ln);   // s sigmoid(h) - (1 - s) sigmoid(-h)
-    } else if (p.form == 1) {
-        loss = h >= 1.0 ? 0.0 : 1.0 - h;
-        dh = h >= 1.0 ? 0.0 : -1.0;
-    } else {
-        const double x = (h - 0.5) / p.beta;
-        loss = x * x;
-        dh = 2.0 * x / p.beta;
-    }
-    if (threadIdx.x == 0) {
-        double* o = parts + static_cast<size_t>(pair) * kPairSums;
-        o[0] = loss;
-        o[1] = R[0];
-        o[2] = R[1];
-        o[3] = R[0] > R[1];
-        o[4] = sums[1] * per[0];
-        o[5] = sums[4] * per[1];
-        if (p.rewards) {
-            p.rewards[2 * pair] = static_cast<float>(R[0]);
-            p.rewards[2 * pair + 1] = static_cast<float>(R[1]);
-        }
-    }
-    const double coef = p.scale * p.beta * dh / p.n_pairs;
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        const float g = static_cast<float>((side ? -coef : coef) * per[side]);
-        for (int i = a[side] + threadIdx.x; i < b[side]; i += kThreads) p.d_logp[i] = p.mask && !p.mask[i] ? 0.0f : g;
-    }
+    return t;
 }
 
-__global__ void __launch_bounds__(kThreads) preference_final_kernel(const double* __restrict__ parts, int n_pairs,
-                                                                    double scale, float* __restrict__ out) {
-    __shared__ double t[kPairSums];
-    double v[kPairSums] = {};
-    for (int b = threadIdx.x; b < n_pairs; b += kThreads)
-        for (int k = 0; k < kPairSums; ++k) v[k] += parts[static_cast<size_t>(b) * kPairSums + k];
-    block_sums<kPairSums, kThreads>(v, t);
-    __syncthreads();
-    if (threadIdx.x != 0) return;
+// Loss of a pair and the factors of its tokens' gradients, chosen and rejected.
+struct PairLoss { double loss, reward[2], logp[2], grad[2]; };
+__device__ __forceinline__ PairLoss pair_loss(const PrefArgs& p, const SeqSums* s) {
+    PairLoss r;
+    double per[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        per[k] = p.average && s[k].count > 0.0 ? 1.0 / s[k].count : 1.0;
+        r.reward[k] = p.beta * (s[k].ratio * per[k]);
+        r.logp[k] = s[k].logp * per[k];
+    }
+    const double h = r.reward[0] - r.reward[1] - p.margin;
+    double dh;
+    if (p.form == 0) {
+        // e = exp(-|h|): ln sigmoid(x) = min(x, 0) - ln(1 + e), and sigmoid(-|h|) = e / (1 + e)
+        const double e = exp_below(h < 0.0 ? h : -h), tail = log1p_unit(e), q = 1.0 / (1.0 + e);
+        const double lp = (h < 0.0 ? h : 0.0) - tail, ln = (h > 0.0 ? -h : 0.0) - tail;
+        r.loss = -(1.0 - p.smooth) * lp - p.smooth * ln;
+        dh = p.smooth - (h < 0.0 ? q : e * q);   // s sigmoid(h) - (1 - s) sigmoid(-h)
+    } else if (p.form == 1) {
+        r.loss = h >= 1.0 ? 0.0 : 1.0 - h;
+        dh = h >= 1.0 ? 0.0 : h < 1.0 ? -1.0 : h;
+    } else {
+        const double x = (h - 0.5) / p.beta;
+        r.loss = x * x;
+        dh = 2.0 * x / p.beta;
+    }
+    const double coef = p.scale * p.beta * dh / p.n_pairs;
+    r.grad[0] = coef * per[0];
+    r.grad[1] = -coef * per[1];
+    return r;
+}
+
+__device__ __forceinline__ void pair_outputs(const double* t, int n_pairs, double scale, float* out) {
     const double i = 1.0 / n_pairs;
     out[0] = static_cast<float>(scale * t[0] * i);
     out[1] = static_cast<float>(t[1] * i);
@@ -350,6 +369,190 @@ __global__ void __launch_bounds__(kThreads) preference_final_kernel(const double
     out[7] = static_cast<float>(n_pairs);
 }
 
+template <int U>
+__device__ __forceinline__ void write_grads(const PrefArgs& p, int a, int b, int at, int lanes, double grad) {
+    const float g = static_cast<float>(grad);
+#pragma unroll 1
+    for (int i = a + at; i < b; i += U * lanes) {
+        uint8_t m[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) m[u] = 1;
+        if (p.mask)
+#pragma unroll
+            for (int u = 0; u < U; ++u) m[u] = *nth(p.mask, i + u * lanes < b ? i + u * lanes : i);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + u * lanes < b) *nth(p.d_logp, i + u * lanes) = m[u] ? g : 0.0f;
+    }
+}
+
+__device__ __forceinline__ void write_pair(const PrefArgs& p, int pair, const PairLoss& r, double* o) {
+    o[0] = r.loss;
+    o[1] = r.reward[0];
+    o[2] = r.reward[1];
+    o[3] = r.reward[0] > r.reward[1];
+    o[4] = r.logp[0];
+    o[5] = r.logp[1];
+    if (p.rewards) {
+        p.rewards[2 * pair] = static_cast<float>(r.reward[0]);
+        p.rewards[2 * pair + 1] = static_cast<float>(r.reward[1]);
+    }
+}
+
+// Tokens before the first sequence and behind the last.
+template <int LANES> __device__ __forceinline__ void write_outside(const PrefArgs& p, int at) {
+    int a, b;
+    seq_range(p.offs, p.n, 0, &a, &b);
+#pragma unroll 1
+    for (int i = at; i < a; i += LANES) p.d_logp[i] = 0.0f;
+    seq_range(p.offs, p.n, 2 * p.n_pairs - 1, &a, &b);
+#pragma unroll 1
+    for (int i = b + at; i < p.n; i += LANES) p.d_logp[i] = 0.0f;
+}
+
+// One workgroup a pair, half of it a sequence; one more for the tokens that no sequence holds.
+constexpr int kPairThreads = 1024, kSide = kPairThreads / 2;
+
+__global__ void __launch_bounds__(kPairThreads) preference_kernel(PrefArgs p, double* __restrict__ parts) {
+    __shared__ SeqSums sums[2];
+    const int pair = blockIdx.x, tid = threadIdx.x, side = tid / kSide, at = tid % kSide;
+    if (pair == p.n_pairs) return write_outside<kPairThreads>(p, tid);
+    int a, b;
+    seq_range(p.offs, p.n, 2 * pair + side, &a, &b);
+    const SeqSums t = seq_sums<4>(p, a, b, at, kSide);
+    double v[6];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        v[3 * k] = side == k ? t.ratio : 0.0;
+        v[3 * k + 1] = side == k ? t.logp : 0.0;
+        v[3 * k + 2] = side == k ? t.count : 0.0;
+    }
+    block_sums<6, kPairThreads>(v, &sums[0].ratio);
+    __syncthreads();
+    const PairLoss r = pair_loss(p, sums);
+    write_grads<4>(p, a, b, at, kSide, side ? r.grad[1] : r.grad[0]);   // an index would put r into LDS
+    if (tid == 0) write_pair(p, pair, r, parts + static_cast<size_t>(pair) * kPairSums);
+}
+
+// Few pairs of many tokens: `cuts` workgroups a sequence.  Each adds up its
+// share; after that each adds up its pair's shares and writes its tokens.
+constexpr int kCutThreads = 256, kMaxCuts = kCutThreads;
+
+__device__ __forceinline__ void cut_range(const PrefArgs& p, int seq, int cut, int cuts, int* a, int* b) {
+    int lo, hi;
+    seq_range(p.offs, p.n, seq, &lo, &hi);
+    const int each = (hi - lo + cuts - 1) / cuts;
+    *a = min(hi, lo + cut * each);
+    *b = min(hi, *a + each);
+}
+
+__global__ void __launch_bounds__(kCutThreads) preference_sums_kernel(PrefArgs p, SeqSums* __restrict__ shares) {
+    if (static_cast<int>(blockIdx.y) == 2 * p.n_pairs) {
+        if (blockIdx.x == 0) write_outside<kCutThreads>(p, threadIdx.x);
+        return;
+    }
+    int a, b;
+    cut_range(p, blockIdx.y, blockIdx.x, gridDim.x, &a, &b);
+    const SeqSums t = seq_sums<4>(p, a, b, threadIdx.x, kCutThreads);
+    double v[3] = {t.ratio, t.logp, t.count};
+    block_sums<3, kCutThreads>(v, &shares[blockIdx.y * gridDim.x + blockIdx.x].ratio);
+}
+
+__global__ void __launch_bounds__(kCutThreads) preference_cut_kernel(PrefArgs p, const SeqSums* __restrict__ shares,
+                                                                     double* __restrict__ parts) {
+    __shared__ SeqSums sums[2];
+    const int tid = threadIdx.x, seq = blockIdx.y, pair = seq / 2, cuts = gridDim.x;
+    int a, b;
+    cut_range(p, seq, blockIdx.x, cuts, &a, &b);
+    double v[6] = {};
+    if (tid < cuts) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const SeqSums t = shares[(2 * pair + k) * cuts + tid];
+            v[3 * k] = t.ratio;
+            v[3 * k + 1] = t.logp;
+            v[3 * k + 2] = t.count;
+        }
+    }
+    block_sums<6, kCutThreads>(v, &sums[0].ratio);
+    __syncthreads();
+    const PairLoss r = pair_loss(p, sums);
+    write_grads<4>(p, a, b, tid, kCutThreads, seq & 1 ? r.grad[1] : r.grad[0]);
+    if (tid == 0 && blockIdx.x == 0 && !(seq & 1)) write_pair(p, pair, r, parts + static_cast<size_t>(pair) * kPairSums);
+}
+
+__global__ void __launch_bounds__(kFinalThreads) preference_final_kernel(const double* __restrict__ parts, int n_pairs,
+                                                                         double scale, float* __restrict__ out) {
+    __shared__ double t[kPairSums];
+    double v[kPairSums] = {};
+    for (int b = threadIdx.x; b < n_pairs; b += kFinalThreads)
+#pragma unroll
+        for (int k = 0; k < kPairSums; ++k) v[k] += parts[static_cast<size_t>(b) * kPairSums + k];
+    block_sums<kPairSums, kFinalThreads>(v, t);
+    __syncthreads();
+    if (threadIdx.x == 0) pair_outputs(t, n_pairs, scale, out);
+}
+
+// Few pairs of few tokens: one workgroup and one launch, its 16 waves shared out over the sequences.
+constexpr int kSmallPairs = 64, kSmallPairTokens = 16384, kSmallWaves = kSmallThreads / 64;
+bool preference_small(int n, int n_pairs) { return n_pairs <= kSmallPairs && n <= kSmallPairTokens; }
+
+__global__ void __launch_bounds__(kSmallThreads) preference_small_kernel(PrefArgs p, float* __restrict__ out) {
+    __shared__ SeqSums share[2 * kSmallPairs > kSmallWaves ? 2 * kSmallPairs : kSmallWaves];
+    __shared__ double grad[2 * kSmallPairs];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, seqs = 2 * p.n_pairs;
+    const int each = seqs < kSmallWaves ? kSmallWaves / seqs : 1;   // waves a sequence
+    const int lanes = 64 * each, at = (wave % each) * 64 + lane, turn = kSmallWaves / each;
+    write_outside<kSmallThreads>(p, tid);
+#pragma unroll 1
+    for (int s = wave / each; s < seqs; s += turn) {
+        int a, b;
+        seq_range(p.offs, p.n, s, &a, &b);
+        const SeqSums t = seq_sums<4>(p, a, b, at, lanes);
+        double w[3] = {t.ratio, t.logp, t.count};
+        wave_sums<3>(w);
+        if (lane == 63) share[s * each + wave % each] = SeqSums{w[0], w[1], w[2]};
+    }
+    __syncthreads();
+    if (wave == 0) {   // kSmallPairs lanes
+        double v[kPairSums] = {};
+        if (lane < p.n_pairs) {
+            SeqSums sums[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                sums[k] = SeqSums{0.0, 0.0, 0.0};
+#pragma unroll 1
+                for (int e = 0; e < each; ++e) {
+                    const SeqSums t = share[(2 * lane + k) * each + e];
+                    sums[k].ratio += t.ratio;
+                    sums[k].logp += t.logp;
+                    sums[k].count += t.count;
+                }
+            }
+            const PairLoss r = pair_loss(p, sums);
+            grad[2 * lane] = r.grad[0];
+            grad[2 * lane + 1] = r.grad[1];
+            write_pair(p, lane, r, v);
+        }
+        wave_sums<kPairSums>(v);
+        if (lane == 63) pair_outputs(v, p.n_pairs, p.scale, out);
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int s = wave / each; s < seqs; s += turn) {
+        int a, b;
+        seq_range(p.offs, p.n, s, &a, &b);
+        write_grads<4>(p, a, b, at, lanes, grad[s]);
+    }
+}
+
+// Workgroups a sequence where pairs alone do not fill the chip and are long
+// enough to cut (0: a workgroup a pair).
+int preference_cuts(int n, int n_pairs) {
+    if (n_pairs > 128 || n / n_pairs < 16384) return 0;
+    const int want = 1024 / (2 * n_pairs);
+    return want < kMaxCuts ? want : kMaxCuts;
+}
 
 // Sequences of more than 1024 tokens on average take a workgroup each, shorter ones a wave.
 bool count_by_workgroup(const PolicyArgs& p) { return p.n / p.n_seqs > 1024; }
@@ -408,14 +611,27 @@ hipError_t launch_policy_loss(const PolicyArgs& p, const float* logp, const floa
     return e;
 }
 
-size_t preference_ws_bytes(int, int n_pairs) {
-    return align256(static_cast<size_t>(n_pairs) * kPairSums * sizeof(double));
+size_t preference_ws_bytes(int n, int n_pairs) {
+    if (preference_small(n, n_pairs)) return 0;
+    return align256(static_cast<size_t>(n_pairs) * kPairSums * sizeof(double)) +
+           align256(static_cast<size_t>(preference_cuts(n, n_pairs)) * 2 * n_pairs * sizeof(SeqSums));
 }
 
 hipError_t launch_preference_loss(const PrefArgs& p, float* out, void* ws, hipStream_t s) {
+    if (preference_small(p.n, p.n_pairs)) {
+        hipLaunchKernelGGL(preference_small_kernel, dim3(1), dim3(kSmallThreads), 0, s, p, out);
+        return hipGetLastError();
+    }
     double* parts = static_cast<double*>(ws);
-    hipLaunchKernelGGL(preference_kernel, dim3(p.n_pairs + 1), dim3(kThreads), 0, s, p, parts);
-    hipLaunchKernelGGL(preference_final_kernel, dim3(1), dim3(kThreads), 0, s, parts, p.n_pairs, p.scale, out);
+    if (const int cuts = preference_cuts(p.n, p.n_pairs); cuts > 0) {
+        SeqSums* shares = reinterpret_cast<SeqSums*>(static_cast<char*>(ws) +
+                                                     align256(static_cast<size_t>(p.n_pairs) * kPairSums * sizeof(double)));
+        hipLaunchKernelGGL(preference_sums_kernel, dim3(cuts, 2 * p.n_pairs + 1), dim3(kCutThreads), 0, s, p, shares);
+        hipLaunchKernelGGL(preference_cut_kernel, dim3(cuts, 2 * p.n_pairs), dim3(kCutThreads), 0, s, p, shares, parts);
+    } else {
+        hipLaunchKernelGGL(preference_kernel, dim3(p.n_pairs + 1), dim3(kPairThreads), 0, s, p, parts);
+    }
+    hipLaunchKernelGGL(preference_final_kernel, dim3(1), dim3(kFinalThreads), 0, s, parts, p.n_pairs, p.scale, out);
     return hipGetLastError();
 }
 

@@ -62,9 +62,24 @@ struct TokenLoss {
 __device__ __forceinline__ double expm1_20(double x) {
     const double r = x * (1.0 / 16384.0);
     double e = r * (1.0 + r * (0.5 + r * (1.0 / 6.0 + r * (1.0 / 24.0 + r * (1.0 / 120.0)))));
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < 14; ++i) e = e * (2.0 + e);
     return e;
+}
+
+// exp(x) for any x <= 0: x = k ln 2 + r.
+__device__ __forceinline__ double exp_below(double x) {
+    const double lim = x < -1100.0 ? -1100.0 : x;
+    const double k = rint(lim * 1.4426950408889634);
+    const double r = (lim - k * 0.693147180369123816490) - k * 1.90821492927058770002e-10;   // ln 2 in two parts
+    return ldexp(1.0 + expm1_20(r), static_cast<int>(k));
+}
+
+// ln(1 + e) for 0 <= e <= 1 in fp64: with y near it, ln(1 + e) = y + ln(1 + d), d = (e - E) / (1 + E), E = exp(y) - 1.
+__device__ __forceinline__ double log1p_unit(double e) {
+    const double y = e < 1e-3 ? e : static_cast<double>(__builtin_amdgcn_logf(static_cast<float>(1.0 + e))) * 0.69314718055994530942;
+    const double E = expm1_20(y), d = (e - E) / (1.0 + E);
+    return y + d * (1.0 - 0.5 * d);
 }
 
 // ln s in fp64 for a sum 1 <= s <= 2^24: the hardware's fp32 logarithm, and one
@@ -107,10 +122,11 @@ __device__ __forceinline__ TokenLoss policy_token(const PolicyArgs& p, double lo
     return t;
 }
 
-__device__ __forceinline__ double wave_sum(double v) {
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+// Entry i of an array of fewer than 2^30 entries: scalar base, 32-bit offset.
+template <typename T> __device__ __forceinline__ T* nth(T* p, int i) {
+    return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(p) + static_cast<uint32_t>(i) * static_cast<uint32_t>(sizeof(T)));
 }
+
 __device__ __forceinline__ int wave_sum(int v) {
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     return v;
@@ -145,17 +161,18 @@ __device__ __forceinline__ PolicyTotals policy_totals(const PolicyArgs& p, const
 
 // Weight of a counted token of sequence s.
 __device__ __forceinline__ double policy_weight(const PolicyArgs& p, const PolicyTotals& t, int s, const int32_t* counts) {
-    if (p.agg == 2) return 1.0;
-    if (p.agg == 0) return 1.0 / t.tokens;
-    int len;
-    if (counts) {
-        len = counts[s];
-    } else {
+    double by = p.agg == 0 ? t.tokens : 1.0;
+    if (p.agg == 1) {
         int a, b;
-        seq_range(p.offs, p.n, s, &a, &b);
-        len = b - a;
+        if (counts) {
+            b = counts[s];
+        } else {
+            seq_range(p.offs, p.n, s, &a, &b);
+            b -= a;
+        }
+        by = static_cast<double>(b) * t.seqs;
     }
-    return 1.0 / (static_cast<double>(len) * t.seqs);
+    return 1.0 / by;
 }
 
 }  // namespace rl

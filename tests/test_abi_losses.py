@@ -140,7 +140,7 @@ def test_policy_loss_logits_refuses(bad):
     assert policy(**(dict(logits={}) | bad)) == R.RL_ERR_INVALID_ARG
 
 
-def preference(n=10, pairs=2, offs=P, logp=P, params=(), out=P, g=P, ws=P, nb=WS):
+def preference(n=100000, pairs=2, offs=P, logp=P, params=(), out=P, g=P, ws=P, nb=WS):
     q = R.PreferenceParams(0.1, 0.0, 0.0, 1.0, 0, 0)
     for k, v in dict(params).items():
         setattr(q, k, v)

@@ -528,7 +528,7 @@ def run_preference(b, use_ref=True, use_mask=True, **opts):
 
 
 PAIRS = [[1, 1], [3, 0], [0, 0], [1, 2, 0, 7], [255, 257], [1500, 900], [5000, 4], [64] * 40, [33000, 30001], [1, 2] * 700,
-         [20000, 17000, 3, 90]]
+         [20000, 17000, 3, 90], [700, 2500, 1, 0] * 20]
 
 
 @pytest.mark.parametrize("lens", PAIRS, ids=lambda l: f"{len(l)}x{sum(l)}")
