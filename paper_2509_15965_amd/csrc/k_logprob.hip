@@ -49,6 +49,11 @@ template <> __device__ __forceinline__ u32x4 pack<uint16_t>(const float* v) {
         w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){v[2 * i], v[2 * i + 1]}, bf16x2));
     return w;
 }
+// A vector of -inf.
+template <typename T> __device__ __forceinline__ u32x4 nothing();
+template <> __device__ __forceinline__ u32x4 nothing<float>() { return u32x4{0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u}; }
+template <> __device__ __forceinline__ u32x4 nothing<uint16_t>() { return u32x4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u}; }
+
 // Vector `first` of a row plus a lane's byte offset: scalar base, 32-bit lane offset.
 template <typename T> __device__ __forceinline__ T* vec_at(T* row, int first, uint32_t at) {
     return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(row) + static_cast<size_t>(first) * 16 + at);
@@ -148,38 +153,59 @@ __device__ __forceinline__ void finish_dead(int row, float* logp, float* ent, fl
 
 constexpr int kRowThreads = 256;
 
-// One workgroup per (row, vocabulary chunk); chunks of a row are merged in
-// order by token_logprobs_join_kernel.
-template <typename T, bool ENT, bool KEEP>
-__global__ void __launch_bounds__(kRowThreads) token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int V,
+// One workgroup per (row, vocabulary chunk), four vectors a lane in flight;
+// chunks of a row are merged in order by token_logprobs_join_kernel.
+template <typename T, int THREADS, bool ENT, bool KEEP>
+__global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int V,
         const int32_t* __restrict__ targets, double inv_T, float c, int chunk, bool check, PolicyArgs live,
         RowPart* __restrict__ parts, float* __restrict__ logp, float* __restrict__ ent, float* __restrict__ stats) {
-    __shared__ RowPart sp[kRowThreads / 64];
-    const int row = blockIdx.x, nchunks = gridDim.y;
+    constexpr int E = kVec<T>, U = 4, WAVES = THREADS / 64;
+    __shared__ RowPart sp[WAVES];
+    const int row = blockIdx.x, nchunks = gridDim.y, tid = threadIdx.x;
     if (check && counted_seq(live, row) < 0) {
-        if (threadIdx.x == 0 && nchunks == 1) finish_dead(row, logp, ent, stats);
+        if (tid == 0 && nchunks == 1) finish_dead(row, logp, ent, stats);
         return;
     }
-    const T* z = logits + row * ld;
     const int beg = blockIdx.y * chunk, end = min(V, beg + chunk);
+    const T* z = logits + row * ld + beg;
     LaneSum acc{{-FLT_MAX, 0.0f, 0.0f}, -FLT_MAX};
-    constexpr int E = kVec<T>;
-    const int whole = beg + (end - beg) / E * E;
-    for (int v = beg + E * static_cast<int>(threadIdx.x); v < whole; v += E * kRowThreads) {
-        float x[E];
-        unpack<T>(load_row<KEEP>(z + v), x);
-        add_entries<E, ENT>(acc, x, c);
+    const int nvec = (end - beg) / E, tail = end - beg - nvec * E;
+    const float last = tid < tail ? Elem<T>::load(z, nvec * E + tid) : -INFINITY;
+    int v = tid;
+#pragma unroll 1
+    for (; v + (U - 1) * THREADS < nvec; v += U * THREADS) {
+        u32x4 w[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] = load_row<KEEP>(z + static_cast<size_t>(v + u * THREADS) * E);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float x[E];
+            unpack<T>(w[u], x);
+            add_entries<E, ENT>(acc, x, c);
+        }
     }
-    if (whole + static_cast<int>(threadIdx.x) < end) {
-        const float x = Elem<T>::load(z, whole + threadIdx.x);
-        add_entries<1, ENT>(acc, &x, c);
+    if (v < nvec) {   // up to U - 1 vectors more; what is not there is -inf
+        u32x4 w[U - 1];
+#pragma unroll
+        for (int u = 0; u < U - 1; ++u) {
+            w[u] = nothing<T>();
+            if (v + u * THREADS < nvec) w[u] = load_row<KEEP>(z + static_cast<size_t>(v + u * THREADS) * E);
+        }
+#pragma unroll
+        for (int u = 0; u < U - 1; ++u) {
+            float x[E];
+            unpack<T>(w[u], x);
+            add_entries<E, ENT>(acc, x, c);
+        }
     }
+    add_entries<1, ENT>(acc, &last, c);
     rebase(acc, acc.top, c);
     RowPart a = merge_wave(acc, c);
-    if ((threadIdx.x & 63) == 0) sp[threadIdx.x >> 6] = a;
+    if ((tid & 63) == 0) sp[tid >> 6] = a;
     __syncthreads();
-    if (threadIdx.x != 0) return;
-    for (int w = 1; w < kRowThreads / 64; ++w) a = merge(a, sp[w], c);
+    if (tid >= 64) return;
+    a = merge_lanes<WAVES>(sp[tid % WAVES], c);
+    if (tid != 0) return;
     if (nchunks > 1)
         parts[static_cast<size_t>(row) * nchunks + blockIdx.y] = a;
     else
@@ -249,10 +275,6 @@ __global__ void __launch_bounds__(kRowThreads) token_logprobs_backward_kernel(co
 // the token's loss, then each vector's gradient is stored.  HBM traffic is one
 // read and one write of the logits where the forward and backward kernels need
 // two reads.  A lane's entries behind the row's last vector are -inf.
-template <typename T> __device__ __forceinline__ u32x4 nothing();
-template <> __device__ __forceinline__ u32x4 nothing<float>() { return u32x4{0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u}; }
-template <> __device__ __forceinline__ u32x4 nothing<uint16_t>() { return u32x4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u}; }
-
 template <typename T, int THREADS, int NV, bool ENT>
 __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, const int32_t* __restrict__ counts,
         const CountPart* __restrict__ cparts, int n_cparts, const T* logits, int64_t ld, int V,
@@ -380,28 +402,43 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
         for (int q = 0; q < kPolicySums; ++q) parts[static_cast<size_t>(blockIdx.x) * kPolicySums + q] = sums[q];
 }
 
-// About 1024 workgroups in all, of whole 2048-entry blocks.
-int split_chunk(int n, int V) {
-    const int64_t want = (1024 + n - 1) / n;
-    const int64_t chunk = (V + want - 1) / want;
-    return static_cast<int>((chunk + 2047) / 2048 * 2048);
+// How a row is cut.  A workgroup of 1024 lanes takes 7 us for 32000 bf16
+// logits, 13 for 152064; cut into chunks of 256 lanes and joined by a second
+// kernel 24 rows of 152064 take 8.3 (uncut 13.6), 128 rows 15.3 (16.3), 200
+// rows 20 (17).  At 50000 entries the cut would save 1 us of the GPU's time and
+// cost a launch.  Past 512 rows workgroups of 256 lanes fill the chip (600 rows
+// of 32000: 13 us, with 1024 lanes 15; 400 rows 11.6 and 11.4; 256 rows of
+// 152064: 30 and 18).
+struct RowCut { int chunk, nchunks, threads; };
+RowCut cut_rows(int n, int V) {
+    if (n < 160 && V > 65536) {
+        const int want = (512 + n - 1) / n, each = ((V + want - 1) / want + 2047) / 2048 * 2048;
+        const int chunk = each < 4096 ? 4096 : each;
+        return RowCut{chunk, (V + chunk - 1) / chunk, kRowThreads};
+    }
+    return RowCut{V, 1, n <= 512 && V > 8192 ? 1024 : kRowThreads};
 }
 
 float log2_scale(float T) { return static_cast<float>(1.4426950408889634 / static_cast<double>(T)); }
 
-template <typename T>
-hipError_t forward(const LogprobArgs& a, RowPart* parts, hipStream_t s) {
-    const int chunk = split_chunk(a.n, a.V), nchunks = (a.V + chunk - 1) / chunk;
-    const T* z = static_cast<const T*>(a.logits);
+template <typename T, int THREADS>
+void launch_forward(const LogprobArgs& a, const RowCut& r, RowPart* parts, hipStream_t s) {
     const PolicyArgs live = a.live ? *a.live : PolicyArgs{};
     const bool keep = a.stats != nullptr;   // the backward pass follows
-    const auto kernel = a.ent ? (keep ? token_logprobs_kernel<T, true, true> : token_logprobs_kernel<T, true, false>)
-                              : (keep ? token_logprobs_kernel<T, false, true> : token_logprobs_kernel<T, false, false>);
-    hipLaunchKernelGGL(kernel, dim3(a.n, nchunks), dim3(kRowThreads), 0, s, z, a.ld, a.V, a.targets, 1.0 / a.T,
-                       log2_scale(a.T), chunk, a.live != nullptr, live, parts, a.logp, a.ent, a.stats);
-    if (nchunks > 1)
-        hipLaunchKernelGGL(token_logprobs_join_kernel<T>, dim3(a.n), dim3(64), 0, s, parts, nchunks, z, a.ld, a.V,
-                           a.targets, 1.0 / a.T, log2_scale(a.T), a.live != nullptr, live, a.logp, a.ent, a.stats);
+    const auto kernel = a.ent ? (keep ? token_logprobs_kernel<T, THREADS, true, true> : token_logprobs_kernel<T, THREADS, true, false>)
+                              : (keep ? token_logprobs_kernel<T, THREADS, false, true> : token_logprobs_kernel<T, THREADS, false, false>);
+    hipLaunchKernelGGL(kernel, dim3(a.n, r.nchunks), dim3(THREADS), 0, s, static_cast<const T*>(a.logits), a.ld, a.V, a.targets,
+                       1.0 / a.T, log2_scale(a.T), r.chunk, a.live != nullptr, live, parts, a.logp, a.ent, a.stats);
+    if (r.nchunks > 1)
+        hipLaunchKernelGGL(token_logprobs_join_kernel<T>, dim3(a.n), dim3(64), 0, s, parts, r.nchunks,
+                           static_cast<const T*>(a.logits), a.ld, a.V, a.targets, 1.0 / a.T, log2_scale(a.T),
+                           a.live != nullptr, live, a.logp, a.ent, a.stats);
+}
+
+template <typename T> hipError_t forward(const LogprobArgs& a, RowPart* parts, hipStream_t s) {
+    const RowCut r = cut_rows(a.n, a.V);
+    if (r.threads == 1024) launch_forward<T, 1024>(a, r, parts, s);
+    else launch_forward<T, kRowThreads>(a, r, parts, s);
     return hipGetLastError();
 }
 
@@ -446,8 +483,8 @@ hipError_t launch_policy_rows(int dt, const PolicyArgs& p, const PolicyWs& w, co
 
 size_t logprob_parts(int n, int V) {
     if (n <= 0) return 0;
-    const int chunk = split_chunk(n, V), nchunks = (V + chunk - 1) / chunk;
-    return nchunks > 1 ? static_cast<size_t>(n) * nchunks : 0;
+    const RowCut r = cut_rows(n, V);
+    return r.nchunks > 1 ? static_cast<size_t>(n) * r.nchunks : 0;
 }
 
 hipError_t launch_token_logprobs(int dt, const LogprobArgs& a, RowPart* parts, hipStream_t s) {

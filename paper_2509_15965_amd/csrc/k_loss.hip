@@ -148,10 +148,9 @@ __device__ __forceinline__ void one_token(const PolicyArgs& p, const TokenIn& in
     if (d_ent) *nth(d_ent, i) = static_cast<float>(ge);
 }
 
-// Tokens of a workgroup, four a lane, the next one's loads under the present
-// one's arithmetic.  The sequences they lie in are found once for the
+// Tokens of a workgroup, loaded before anything else.  The sequences they lie in are found once for the
 // workgroup, then by each lane among those in LDS.
-constexpr int kTokensPerLane = 4, kTokensPerBlock = kThreads * kTokensPerLane, kSpan = 512;
+constexpr int kTokensPerLane = 2, kTokensPerBlock = kThreads * kTokensPerLane, kSpan = 512;
 
 __global__ void __launch_bounds__(kThreads) policy_loss_kernel(PolicyArgs p, const float* __restrict__ logp,
         const float* __restrict__ ent, const int32_t* __restrict__ counts, const CountPart* __restrict__ cparts,
@@ -163,10 +162,18 @@ __global__ void __launch_bounds__(kThreads) policy_loss_kernel(PolicyArgs p, con
     __shared__ PolicyTotals total;
     const int tid = threadIdx.x, first = blockIdx.x * kTokensPerBlock;
     const int last = min(p.n, first + kTokensPerBlock) - 1;
-    int i = first + tid, at = min(i, last);
-    TokenIn next = load_token(p, logp, ent, at);
-    uint8_t next_m = p.mask ? *nth(p.mask, at) : 1;
-    float next_adv = p.token_adv ? *nth(p.adv, at) : 0.0f;
+    TokenIn in[kTokensPerLane];
+    uint8_t m[kTokensPerLane];
+    float own_adv[kTokensPerLane];
+#pragma unroll
+    for (int k = 0; k < kTokensPerLane; ++k) {
+        const int at = min(first + k * kThreads + tid, last);
+        in[k] = load_token(p, logp, ent, at);
+        m[k] = 1;
+        own_adv[k] = 0.0f;
+        if (p.mask) m[k] = *nth(p.mask, at);
+        if (p.token_adv) own_adv[k] = *nth(p.adv, at);
+    }
     // two waves: offsets at most the first token, and at most the last; another: the totals
     if (tid < 128) {
         const int t = tid < 64 ? first : last;
@@ -191,24 +198,20 @@ __global__ void __launch_bounds__(kThreads) policy_loss_kernel(PolicyArgs p, con
         __syncthreads();
     }
     double v[kSums] = {};
-#pragma unroll 1
-    for (; i <= last; i += kThreads) {
-        const TokenIn in = next;
-        const uint8_t m = next_m;
-        at = min(i + kThreads, last);
-        next = load_token(p, logp, ent, at);
-        if (p.mask) next_m = *nth(p.mask, at);
+#pragma unroll
+    for (int k = 0; k < kTokensPerLane; ++k) {
+        const int i = first + k * kThreads + tid;
+        if (i > last) break;
         const int c = held ? s_lo + count_upto(span, 0, s_hi - s_lo, i) : count_upto(p.offs, s_lo, s_hi, i);
         const int s = c - 1 < p.n_seqs ? c - 1 : -1;
-        const bool on = m && s >= 0;
-        float A = 0.0f;
+        const bool on = m[k] && s >= 0;
+        float A = own_adv[k];
         double w = 0.0;
         if (on) {
-            A = p.token_adv ? next_adv : held ? adv[c - s_lo] : p.adv[s];
+            if (!p.token_adv) A = held ? adv[c - s_lo] : p.adv[s];
             w = held ? weight[c - s_lo] : policy_weight(p, totals, s, counts);
         }
-        if (p.token_adv) next_adv = *nth(p.adv, at);
-        one_token(p, in, on, A, w, v, d_logp, d_ent, i);
+        one_token(p, in[k], on, A, w, v, d_logp, d_ent, i);
     }
     block_sums<kSums, kThreads>(v, parts + static_cast<size_t>(blockIdx.x) * kSums);
 }

@@ -469,33 +469,29 @@ def sample_logits_noalloc(logits: torch.Tensor, uids: torch.Tensor, pos_new: tor
 # or device, RLError for what the library refuses.  `workspace`: a uint8
 # tensor of at least the matching *_workspace_bytes; made here when None.
 
-def _on(device, name: str, t: Optional[torch.Tensor], dtype, numel: Optional[int], optional: bool = False):
-    """Device pointer of a contiguous tensor of this type and size."""
+def _on(dev: int, name: str, t: Optional[torch.Tensor], dtype, numel: int, optional: bool = False):
+    """Device pointer of a contiguous tensor of this type and size on GPU `dev`."""
     if t is None:
         if optional:
             return None
         raise ValueError(f"{name} is missing")
-    if t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}, not {t.device}")
-    if not t.is_contiguous() or (numel is not None and t.numel() != numel):
-        raise ValueError(f"{name} must be contiguous and hold {numel} entries, not {tuple(t.shape)}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.get_device() == dev and t.numel() == numel and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be {dtype}, contiguous, of {numel} entries on cuda:{dev}, not {t.dtype} "
+                     f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
-def _mask_on(device, mask: Optional[torch.Tensor], n: int):
-    return _on(device, "mask", mask, torch.bool if mask is not None and mask.dtype == torch.bool else torch.uint8, n, True)
+def _mask_on(dev: int, mask: Optional[torch.Tensor], n: int):
+    return _on(dev, "mask", mask, torch.bool if mask is not None and mask.dtype == torch.bool else torch.uint8, n, True)
 
 
-def _rows_on(device, name: str, t: torch.Tensor, dtype=None, shape=None):
-    """(pointer, row stride) of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or (dtype is not None and t.dtype != dtype) or (shape is not None and t.shape != shape):
-        raise ValueError(f"{name} must be a matrix {tuple(shape) if shape else ''} of {dtype or 'logits'}")
-    if t.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}, not {t.device}")
+def _rows_on(dev: int, name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None):
+    """(pointer, row stride) of a float32 or bfloat16 matrix whose rows are contiguous."""
+    if t.dim() != 2 or t.dtype not in (torch.float32, torch.bfloat16) or t.get_device() != dev or (
+            like is not None and (t.dtype is not like.dtype or t.shape != like.shape)):
+        raise ValueError(f"{name} must be a matrix of float32 or bfloat16 on cuda:{dev}"
+                         + (f" like the logits ({tuple(like.shape)} {like.dtype})" if like is not None else "")
+                         + f", not {t.dtype} {tuple(t.shape)} on {t.device}")
     n, V = t.shape
     ld = t.stride(0) if n > 1 else V
     if (V > 1 and t.stride(1) != 1) or ld < V:
@@ -503,34 +499,35 @@ def _rows_on(device, name: str, t: torch.Tensor, dtype=None, shape=None):
     return t.data_ptr(), ld
 
 
-def _gpu_of(t: torch.Tensor, name: str):
+def _gpu_of(t: torch.Tensor, name: str) -> int:
     if not t.is_cuda:
         raise ValueError(f"{name} must be on a GPU")
-    return t.device
+    return t.get_device()
 
 
-def _run_on(device, stream, nbytes: int, workspace: Optional[torch.Tensor], call, what: str):
-    """call(workspace pointer, its bytes, stream) with `device` current."""
-    if torch.cuda.current_device() != device.index:
-        with torch.cuda.device(device):
-            return _run_on(device, stream, nbytes, workspace, call, what)
-    current = torch.cuda.current_stream(device)
-    if stream is None:
-        stream = current
-    elif stream.device != device:
-        raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+# the stream's handle without a Stream object around it (a sixth of a short call's time), where torch has it
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
+def _run_on(dev: int, stream, nbytes: int, workspace: Optional[torch.Tensor], call, what: str):
+    """call(workspace pointer, its bytes, stream) with GPU `dev` current."""
+    if torch.cuda.current_device() != dev:
+        with torch.cuda.device(dev):
+            return _run_on(dev, stream, nbytes, workspace, call, what)
+    if stream is not None and stream.device.index != dev:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{dev}")
+    ws = None
     if workspace is not None:
-        if workspace.device != device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
-            raise ValueError(f"workspace must be a contiguous uint8 tensor on {device}")
+        if workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous uint8 tensor on cuda:{dev}")
         ws, nbytes = workspace.data_ptr(), workspace.numel()
     elif nbytes:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        if stream != current:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        if stream is not None:
             workspace.record_stream(stream)
         ws = workspace.data_ptr()
-    else:
-        ws = None
-    st = call(ws, nbytes, stream.cuda_stream)
+    st = call(ws, nbytes, _current_stream(dev) if stream is None else stream.cuda_stream)
     if st != RL_OK:
         raise RLError(st, what)
 
@@ -566,7 +563,7 @@ def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, stats: 
     the entropies."""
     dev = _gpu_of(logits, "logits")
     z, ld = _rows_on(dev, "logits", logits)
-    dz, ldd = _rows_on(dev, "d_logits", d_logits, logits.dtype, logits.shape)
+    dz, ldd = _rows_on(dev, "d_logits", d_logits, logits)
     n, V = logits.shape
     y = _on(dev, "targets", targets, torch.int32, n)
     st = _on(dev, "stats", stats, torch.float32, 2 * n)
@@ -632,7 +629,7 @@ def policy_loss_logits(logits: torch.Tensor, targets: torch.Tensor, old_logp: to
     gradient d_logits (may be the logits) in one call."""
     dev = _gpu_of(logits, "logits")
     z, ld = _rows_on(dev, "logits", logits)
-    dz, ldd = _rows_on(dev, "d_logits", d_logits, logits.dtype, logits.shape)
+    dz, ldd = _rows_on(dev, "d_logits", d_logits, logits)
     n, V = logits.shape
     y = _on(dev, "targets", targets, torch.int32, n)
     out = _on(dev, "out_loss", out_loss, torch.float32, 8)
