@@ -1,12 +1,15 @@
 // k_logprob.hip -- token log-probabilities and entropies from logits, and the
 // gradient of both to the logits.
 //
-// With t_v = (z_v - m) log2(e) / T, m the row's largest logit: s = sum 2^t_v,
-// u = sum 2^t_v t_v, and
+// With c = log2(e) / T, t_v = (z_v - m) c, m the row's largest logit,
+// s = sum 2^t_v and u = sum 2^t_v t_v:
 //   log p_y = (z_y - m) / T - ln s        H = ln s - ln 2 u / s
 //   d z_v   = (g (1[v = y] - p_v) - ge p_v (ln p_v + H)) / T
-// The difference is taken before the product, so that neither the type's
-// lowest value nor -inf in a row makes an inf - inf of its own.
+// Exponents are one fma, z c - R: R stands for m c, and what rounding it costs
+// cancels (sums carry the R they are relative to; a gradient's factor takes
+// 2^(R rounded - R)).  Rows whose entries lie beyond 1e30 leave no such sum
+// (logits of the type's lowest value and nothing else, or of its largest);
+// those are taken again with the difference before the product.
 #include "rl_device.h"
 #include "rl_internal.h"
 #include "train.h"
@@ -94,24 +97,35 @@ __device__ __forceinline__ RowPart merge(RowPart a, RowPart b, float c) {
     return RowPart{m, a.s + b.s, a.u + b.u};
 }
 
-// A lane's running sums.  They stay relative to the m they have until an entry
-// lies more than 2^64 above it: rebasing at every new maximum would cost an
-// exponential in nearly every vector of a wave (some lane always has one).
-struct LaneSum : RowPart { float top; };   // top: the largest entry
-constexpr float kAhead = 64.0f;
+// A lane's running sums, relative to 2^R.  R stays until an entry lies more
+// than 2^64 above it: moving it to every new maximum would cost an exponential
+// in nearly every vector of a wave (some lane always has one).
+struct LaneSum { float R, s, u, top; };   // top: the largest entry
+constexpr float kAhead = 64.0f, kNowhere = -1e30f;
+__device__ __forceinline__ LaneSum empty_sum() { return LaneSum{kNowhere, 0.0f, 0.0f, -FLT_MAX}; }
 
 template <int N, bool ENT> __device__ __forceinline__ void add_entries(LaneSum& a, const float* v, float c) {
     float x = v[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) x = fmaxf(x, v[i]);
     a.top = fmaxf(a.top, x);
-    if ((x - a.m) * c > kAhead) rebase(a, x, c);
+    if (__builtin_fmaf(x, c, -a.R) > kAhead) {
+        const float R = x * c, d = fmaxf(a.R - R, -1e4f), f = exp2_hw(d);
+        a.u = f * (a.u + d * a.s);
+        a.s *= f;
+        a.R = R;
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float t = (v[i] - a.m) * c, e = exp2_hw(t);
+        const float t = __builtin_fmaf(v[i], c, -a.R), e = exp2_hw(t);
         a.s += e;
         if (ENT) a.u += e * fmaxf(t, kFloor);
     }
+}
+// The same relative to the lane's largest entry.
+__device__ __forceinline__ RowPart close_sum(const LaneSum& a, float c) {
+    const float d = a.s == 0.0f ? 0.0f : fmaxf(__builtin_fmaf(-a.top, c, a.R), -1e4f), f = exp2_hw(d);
+    return RowPart{a.top, f * a.s, f * (a.u + d * a.s)};
 }
 
 // Over groups of N consecutive lanes.  Lanes may differ in the last bit (a
@@ -126,6 +140,30 @@ __device__ __forceinline__ float first_lane(float x) {
     return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
 }
 __device__ __forceinline__ RowPart merge_wave(RowPart a, float c) { return merge_lanes<64>(a, c); }
+
+// Over a workgroup; every lane gets the first lane's bits.
+template <int WAVES> __device__ __forceinline__ RowPart merge_workgroup(RowPart a, RowPart* sp, float c) {
+    a = merge_wave(a, c);
+    if ((threadIdx.x & 63) == 0) sp[threadIdx.x >> 6] = a;
+    __syncthreads();
+    a = merge_lanes<WAVES>(sp[threadIdx.x % WAVES], c);
+    return RowPart{first_lane(a.m), first_lane(a.s), first_lane(a.u)};
+}
+
+// Whether the sums stand: at least the largest entry's 1, and no NaN.
+__device__ __forceinline__ bool stands(const RowPart& a) { return a.s > 0.5f && a.s < FLT_MAX; }
+
+// Entries [0, n) again, with the difference to m before the product.
+template <typename T, int WAVES> __device__ __forceinline__ RowPart sums_again(const T* z, int n, float m, float c, RowPart* sp) {
+    RowPart a{m, 0.0f, 0.0f};
+    for (int v = threadIdx.x; v < n; v += 64 * WAVES) {
+        const float t = (Elem<T>::load(z, v) - m) * c, e = exp2_hw(t);
+        a.s += e;
+        a.u += e * fmaxf(t, kFloor);
+    }
+    __syncthreads();   // sp is free
+    return merge_workgroup<WAVES>(a, sp, c);
+}
 
 template <typename T>
 __device__ __forceinline__ void finish_row(RowPart a, const T* z, int V, int y, double inv_T, int row, float* logp,
@@ -168,7 +206,7 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const T* __rest
     }
     const int beg = blockIdx.y * chunk, end = min(V, beg + chunk);
     const T* z = logits + row * ld + beg;
-    LaneSum acc{{-FLT_MAX, 0.0f, 0.0f}, -FLT_MAX};
+    LaneSum acc = empty_sum();
     const int nvec = (end - beg) / E, tail = end - beg - nvec * E;
     const float last = tid < tail ? Elem<T>::load(z, nvec * E + tid) : -INFINITY;
     int v = tid;
@@ -199,12 +237,8 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const T* __rest
         }
     }
     add_entries<1, ENT>(acc, &last, c);
-    rebase(acc, acc.top, c);
-    RowPart a = merge_wave(acc, c);
-    if ((tid & 63) == 0) sp[tid >> 6] = a;
-    __syncthreads();
-    if (tid >= 64) return;
-    a = merge_lanes<WAVES>(sp[tid % WAVES], c);
+    RowPart a = merge_workgroup<WAVES>(close_sum(acc, c), sp, c);
+    if (!stands(a)) a = sums_again<T, WAVES>(z, end - beg, a.m, c, sp);
     if (tid != 0) return;
     if (nchunks > 1)
         parts[static_cast<size_t>(row) * nchunks + blockIdx.y] = a;
@@ -228,44 +262,88 @@ __global__ void __launch_bounds__(64) token_logprobs_join_kernel(const RowPart* 
     if (threadIdx.x == 0) finish_row(a, logits + row * ld, V, targets[row], inv_T, row, logp, ent, stats);
 }
 
-// The gradient of an entry from its log2 probability q: p (A + B q).
-struct RowGrad { float A, B, top; };
-__device__ __forceinline__ RowGrad row_grad(float g, float ge, float H, float i) {   // i = 1 / T
-    return RowGrad{-(g + ge * H) * i, -ge * 0.69314718f * i, g * i};
+// Gradients of a row's entries (the same row in every lane): with q = z c - K, 2^q (A + B q); K = m c + log2 s
+// rounded to fp32, and A and B make up for that.  `top` is the target's own, with 1 - p_y as -(exp(log p_y) - 1):
+// a token that is certain has none.
+struct RowGrad {
+    float K, A, B, top;
+    float m, l2;
+    bool zero, far;   // far: K is beyond fp32, q = (z - m) c - l2
+};
+// ln_s: ln s; lp: log p_y; i: 1 / T
+__device__ __forceinline__ RowGrad row_grad(float g, float ge, float H, float i, float m, double ln_s, double lp, float c) {
+    RowGrad k;
+    const double l2 = ln_s * 1.4426950408889634, K = static_cast<double>(m) * c + l2;
+    k.K = static_cast<float>(K);
+    k.m = m;
+    k.l2 = static_cast<float>(l2);
+    k.far = __builtin_amdgcn_readfirstlane(!(fabs(K) < 1e37));
+    const float off = k.far ? 0.0f : static_cast<float>(static_cast<double>(k.K) - K), f = exp2_hw(off);
+    k.B = -ge * 0.69314718f * i;
+    k.A = f * (-(g + ge * H) * i + k.B * off);
+    k.B *= f;
+    const double q = lp < -140.0 ? -140.0 : lp;
+    const float p = exp2_hw(static_cast<float>(q * 1.4426950408889634));
+    k.top = i * (static_cast<float>(-g * expm1_20(clamp20(lp))) - ge * p * (static_cast<float>(q) + H));
+    k.zero = __builtin_amdgcn_readfirstlane(g == 0.0f && ge == 0.0f);
+    return k;
+}
+template <bool ENT> __device__ __forceinline__ float grad_of(const RowGrad& k, float q) {
+    return exp2_hw(q) * (ENT ? k.A + k.B * fmaxf(q, kFloor) : k.A);
+}
+// Of N entries; y: the target's place among them.
+template <int N, bool ENT> __device__ __forceinline__ void grad_entries(const RowGrad& k, float* x, float c, int y) {
+    if (k.far) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = (x[j] - k.m) * c - k.l2;
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = __builtin_fmaf(x[j], c, -k.K);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = grad_of<ENT>(k, x[j]);
+    if (static_cast<uint32_t>(y) < static_cast<uint32_t>(N)) {   // one lane of a row
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = j == y ? k.top : x[j];
+    }
 }
 
-template <typename T>
+template <typename T, bool ENT>
 __global__ void __launch_bounds__(kRowThreads) token_logprobs_backward_kernel(const T* logits, int64_t ld, int V,
-        const int32_t* __restrict__ targets, float inv_T, float c, const float* __restrict__ stats,
+        const int32_t* __restrict__ targets, double inv_T, float c, const float* __restrict__ stats,
         const float* __restrict__ ent, const float* __restrict__ d_logp, const float* __restrict__ d_ent, int chunk, T* dz,
         int64_t ldd) {
     const int row = blockIdx.y;
-    const T* z = logits + row * ld;
-    T* d = dz + row * ldd;
-    const int y = targets[row];
-    const float g = y >= 0 && y < V ? d_logp[row] : 0.0f, ge = d_ent ? d_ent[row] : 0.0f;
-    const bool zero = g == 0.0f && ge == 0.0f;
-    const RowGrad k = row_grad(g, ge, d_ent ? ent[row] : 0.0f, inv_T);
-    const float m = stats[2 * static_cast<size_t>(row)], l2 = stats[2 * static_cast<size_t>(row) + 1] * 1.44269504f;
-    const int beg = blockIdx.x * chunk, end = min(V, beg + chunk);
+    const int beg = blockIdx.x * chunk, n = min(V, beg + chunk) - beg, tid = threadIdx.x;
+    const T* z = logits + row * ld + beg;
+    T* d = dz + row * ldd + beg;
+    int y = targets[row];
+    const float g = y >= 0 && y < V ? d_logp[row] : 0.0f, ge = ENT ? d_ent[row] : 0.0f;
+    y -= beg;
+    const float m = stats[2 * static_cast<size_t>(row)];
+    const double ln_s = stats[2 * static_cast<size_t>(row) + 1];
+    double lp = y >= 0 && y < n ? (static_cast<double>(Elem<T>::load(z, y)) - m) * inv_T - ln_s : 0.0;
+    lp = lp > 0.0 ? 0.0 : lp;
+    const RowGrad k = row_grad(g, ge, ENT ? ent[row] : 0.0f, static_cast<float>(inv_T), m, ln_s, lp, c);
     constexpr int E = kVec<T>;
-    const int whole = beg + (end - beg) / E * E;
-    auto entry = [&](float x, int v) {
-        const float q = (x - m) * c - l2;
-        const float r = exp2_hw(q) * (k.A + k.B * fmaxf(q, kFloor));
-        return v == y ? r + k.top : r;
-    };
-    for (int v = beg + E * static_cast<int>(threadIdx.x); v < whole; v += E * kRowThreads) {
+    const int whole = n / E * E;
+    for (int v = E * tid; v < whole; v += E * kRowThreads) {
         float x[E] = {};
-        if (!zero) {
+        if (!k.zero) {
             unpack<T>(load_row<false>(z + v), x);
-#pragma unroll
-            for (int i = 0; i < E; ++i) x[i] = entry(x[i], v + i);
+            grad_entries<E, ENT>(k, x, c, y - v);
         }
         store_row(d + v, pack<T>(x));
     }
-    const int v = whole + threadIdx.x;
-    if (v < end) Elem<T>::store(d, v, zero ? 0.0f : entry(Elem<T>::load(z, v), v));
+    const int v = whole + tid;
+    if (v < n) {
+        float x = 0.0f;
+        if (!k.zero) {
+            x = Elem<T>::load(z, v);
+            grad_entries<1, ENT>(k, &x, c, y - v);
+        }
+        Elem<T>::store(d, v, x);
+    }
 }
 
 // ---- the policy loss of a row and the gradient of its logits, the row read once ----
@@ -308,10 +386,9 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
         const int next_seq = next < p.n ? counted_seq(p, next) : -1;
         const T* zn = logits + next * ld;
         T* d = dz + row * ldd;
-        float m = 0.0f, l2 = 0.0f;
-        RowGrad k{0.0f, 0.0f, 0.0f};
+        RowGrad k{};
+        k.zero = true;
         int y = -1;
-        bool zero = true;
         if (seq < 0) {
             if (tid == 0) {
                 logp[row] = 0.0f;
@@ -323,7 +400,7 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
             const float zy = held ? Elem<T>::load(logits + row * ld, y) : __builtin_nanf("");
             const double weight = policy_weight(p, totals, seq, counts);
             const float adv = p.adv[p.token_adv ? row : seq], old_logp = p.old_logp[row], ref = p.ref ? p.ref[row] : 0.0f;
-            LaneSum acc{{-FLT_MAX, 0.0f, 0.0f}, -FLT_MAX};
+            LaneSum acc = empty_sum();
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 if (i * THREADS < nvec) {
@@ -334,26 +411,23 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
                 __builtin_amdgcn_sched_barrier(0);   // a vector at a time: unpacked ones would not fit beside the row
             }
             add_entries<1, ENT>(acc, &last, c);
-            rebase(acc, acc.top, c);
-            RowPart a = merge_wave(acc, c);
-            if ((tid & 63) == 0) sp[turn][tid >> 6] = a;
-            __syncthreads();
-            a = merge_lanes<WAVES>(sp[turn][tid % WAVES], c);
-            a = RowPart{first_lane(a.m), first_lane(a.s), first_lane(a.u)};
+            RowPart a = merge_workgroup<WAVES>(close_sum(acc, c), sp[turn], c);
+            if (!stands(a)) a = sums_again<T, WAVES>(logits + row * ld, V, a.m, c, sp[turn]);
             turn ^= 1;
             const double ln_s = ln_sum(a.s);
-            float lp = static_cast<float>((static_cast<double>(zy) - a.m) * inv_T - ln_s);
-            lp = lp > 0.0f ? 0.0f : lp;
+            double lp = (static_cast<double>(zy) - a.m) * inv_T - ln_s;
+            lp = lp > 0.0 ? 0.0 : lp;
+            const float lp32 = static_cast<float>(lp);
             float H = 0.0f;
             if (ENT) {
                 const double h = ln_s - 0.69314718055994530942 * static_cast<double>(a.u / a.s);
                 H = static_cast<float>(h < 0.0 ? 0.0 : h);
             }
-            const TokenLoss t = policy_token(p, lp, old_logp, ref, adv);
+            const TokenLoss t = policy_token(p, lp32, old_logp, ref, adv);
             const float g = held ? static_cast<float>(p.scale * weight * t.g) : 0.0f;
             const float ge = ENT ? static_cast<float>(-p.scale * weight * p.ent_coef) : 0.0f;
             if (tid == 0) {
-                logp[row] = lp;
+                logp[row] = lp32;
                 if (ent) ent[row] = H;
                 sums[0] += weight * t.pg;
                 sums[1] += weight * t.kl;
@@ -363,28 +437,20 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
                 sums[5] -= t.lr;
                 sums[6] += 1.0;
             }
-            zero = g == 0.0f && ge == 0.0f;
-            k = row_grad(g, ge, H, static_cast<float>(inv_T));
-            m = a.m;
-            l2 = static_cast<float>(ln_s) * 1.44269504f;
+            k = row_grad(g, ge, H, static_cast<float>(inv_T), a.m, ln_s, lp, c);
+            if (!held) y = -1;
         }
-        const int y_lane = y - tid * E;
         int nv = nvec;
         asm volatile("" : "+s"(nv));
-        auto entry = [&](float x, int v) {
-            const float q = (x - m) * c - l2;
-            const float r = exp2_hw(q) * (ENT ? k.A + k.B * fmaxf(q, kFloor) : k.A);
-            return v == y_lane ? r + k.top : r;
-        };
+        const int y_lane = y - tid * E;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             asm volatile("" : "+v"(w[i]));   // unpacked again: the values of the first pass would not fit beside the row
             if (tid < nv - i * THREADS) {
                 float x[E] = {};
-                if (!zero) {
+                if (!k.zero) {
                     unpack<T>(w[i], x);
-#pragma unroll
-                    for (int j = 0; j < E; ++j) x[j] = entry(x[j], i * THREADS * E + j);
+                    grad_entries<E, ENT>(k, x, c, y_lane - i * THREADS * E);
                 }
                 if (next_seq >= 0) w[i] = load_row<false>(vec_at(zn, i * THREADS, at));
                 store_row(vec_at(d, i * THREADS, at), pack<T>(x));
@@ -392,7 +458,12 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
             __builtin_amdgcn_sched_barrier(0);
         }
         if (tid < tail) {
-            Elem<T>::store(d, nvec * E + tid, zero ? 0.0f : entry(last, nvec * E + tid - tid * E));
+            float x = 0.0f;
+            if (!k.zero) {
+                x = last;
+                grad_entries<1, ENT>(k, &x, c, y - nvec * E - tid);
+            }
+            Elem<T>::store(d, nvec * E + tid, x);
             if (next_seq >= 0) last = Elem<T>::load(zn, nvec * E + tid);
         }
         row = next;
@@ -506,13 +577,14 @@ hipError_t launch_token_logprobs_backward(int dt, const void* logits, int64_t ld
         const float* e = ent ? ent + r : nullptr;
         const float* h = ge ? ge + r : nullptr;
         if (dt == DT_F32)
-            hipLaunchKernelGGL(token_logprobs_backward_kernel<float>, dim3(nchunks, m), dim3(kRowThreads), 0, s,
-                               reinterpret_cast<const float*>(z), ld, V, targets + r, 1.0f / T, log2_scale(T), stats + 2 * r, e,
-                               g + r, h, chunk, reinterpret_cast<float*>(d), ldd);
+            hipLaunchKernelGGL((h ? token_logprobs_backward_kernel<float, true> : token_logprobs_backward_kernel<float, false>),
+                               dim3(nchunks, m), dim3(kRowThreads), 0, s, reinterpret_cast<const float*>(z), ld, V, targets + r,
+                               1.0 / T, log2_scale(T), stats + 2 * r, e, g + r, h, chunk, reinterpret_cast<float*>(d), ldd);
         else
-            hipLaunchKernelGGL(token_logprobs_backward_kernel<uint16_t>, dim3(nchunks, m), dim3(kRowThreads), 0, s,
-                               reinterpret_cast<const uint16_t*>(z), ld, V, targets + r, 1.0f / T, log2_scale(T), stats + 2 * r,
-                               e, g + r, h, chunk, reinterpret_cast<uint16_t*>(d), ldd);
+            hipLaunchKernelGGL((h ? token_logprobs_backward_kernel<uint16_t, true> : token_logprobs_backward_kernel<uint16_t, false>),
+                               dim3(nchunks, m), dim3(kRowThreads), 0, s, reinterpret_cast<const uint16_t*>(z), ld, V,
+                               targets + r, 1.0 / T, log2_scale(T), stats + 2 * r, e, g + r, h, chunk,
+                               reinterpret_cast<uint16_t*>(d), ldd);
     }
     return hipGetLastError();
 }

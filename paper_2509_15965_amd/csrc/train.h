@@ -82,12 +82,13 @@ __device__ __forceinline__ double log1p_unit(double e) {
     return y + d * (1.0 - 0.5 * d);
 }
 
-// ln s in fp64 for a sum 1 <= s <= 2^24: the hardware's fp32 logarithm, and one
-// Newton step (within 5e-9).  NaN for 0 and NaN.
+// ln s in fp64 for a positive fp32 sum: the exponent, the hardware's logarithm
+// of the mantissa in [1, 2) and one Newton step; 0 for 1, NaN for 0 and NaN.
 __device__ __forceinline__ double ln_sum(float s) {
-    const double y = static_cast<double>(__builtin_amdgcn_logf(s)) * 0.69314718055994530942;
-    const double d = s * (1.0 + expm1_20(-y)) - 1.0;
-    return y + d * (1.0 - 0.5 * d);
+    const float m = 2.0f * __builtin_amdgcn_frexp_mantf(s);
+    const double y = static_cast<double>(__builtin_amdgcn_logf(m)) * 0.69314718055994530942;
+    const double d = m * (1.0 + expm1_20(-y)) - 1.0;
+    return (__builtin_amdgcn_frexp_expf(s) - 1) * 0.69314718055994530942 + (y + d * (1.0 - 0.5 * d));
 }
 
 __device__ __forceinline__ double clamp20(double x) { return x < -20.0 ? -20.0 : x > 20.0 ? 20.0 : x; }
