@@ -59,7 +59,10 @@ template <> __device__ __forceinline__ u32x4 nothing<uint16_t>() { return u32x4{
 
 // Vector `first` of a row plus a lane's byte offset: scalar base, 32-bit lane offset.
 template <typename T> __device__ __forceinline__ T* vec_at(T* row, int first, uint32_t at) {
-    return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(row) + static_cast<size_t>(first) * 16 + at);
+    return reinterpret_cast<T*>(reinterpret_cast<char*>(row) + static_cast<size_t>(first) * 16 + at);
+}
+template <typename T> __device__ __forceinline__ const T* vec_at(const T* row, int first, uint32_t at) {
+    return reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + static_cast<size_t>(first) * 16 + at);
 }
 
 // Logits are streamed: non-temporal loads where nothing reads them again soon
@@ -401,9 +404,11 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
             const double weight = policy_weight(p, totals, seq, counts);
             const float adv = p.adv[p.token_adv ? row : seq], old_logp = p.old_logp[row], ref = p.ref ? p.ref[row] : 0.0f;
             LaneSum acc = empty_sum();
+            int nv = nvec;
+            asm volatile("" : "+s"(nv));   // or the comparisons of every turn are kept in registers
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (i * THREADS < nvec) {
+                if (i * THREADS < nv) {
                     float x[E];
                     unpack<T>(w[i], x);
                     add_entries<E, ENT>(acc, x, c);

@@ -125,7 +125,11 @@ __device__ __forceinline__ TokenLoss policy_token(const PolicyArgs& p, double lo
 
 // Entry i of an array of fewer than 2^30 entries: scalar base, 32-bit offset.
 template <typename T> __device__ __forceinline__ T* nth(T* p, int i) {
-    return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(p) + static_cast<uint32_t>(i) * static_cast<uint32_t>(sizeof(T)));
+    return reinterpret_cast<T*>(reinterpret_cast<char*>(p) + static_cast<uint32_t>(i) * static_cast<uint32_t>(sizeof(T)));
+}
+template <typename T> __device__ __forceinline__ const T* nth(const T* p, int i) {
+    return reinterpret_cast<const T*>(reinterpret_cast<const char*>(p) +
+                                      static_cast<uint32_t>(i) * static_cast<uint32_t>(sizeof(T)));
 }
 
 __device__ __forceinline__ int wave_sum(int v) {
