@@ -457,8 +457,15 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
                     unpack<T>(w[i], x);
                     grad_entries<E, ENT>(k, x, c, y_lane - i * THREADS * E);
                 }
-                if (next_seq >= 0) w[i] = load_row<false>(vec_at(zn, i * THREADS, at));
                 store_row(vec_at(d, i * THREADS, at), pack<T>(x));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            // Four stores, then four loads: 8192 rows of 152064 bf16 logits in 1006 us, one by one 1019, in twos 1023, in
+            // eights 1013; a whole row of stores first 992, and then 59 us for 1792 rows of 32000 where fours take 56.
+            if (next_seq >= 0 && (i % 4 == 3 || i == NV - 1)) {
+#pragma unroll
+                for (int j = i / 4 * 4; j <= i; ++j)
+                    if (tid < nv - j * THREADS) w[j] = load_row<false>(vec_at(zn, j * THREADS, at));
             }
             __builtin_amdgcn_sched_barrier(0);
         }
