@@ -355,17 +355,19 @@ rl_status rl_sample_logits_noalloc(int32_t n, int32_t vocab, const float* logits
  * matching function returns; NULL is accepted where that is 0); calls that
  * may overlap in time need workspaces of their own.  Outputs may not overlap
  * inputs or each other, but for d_logits, which may be the logits themselves
- * (same ld).  Results do not depend on timing: every sum has a fixed order.
+ * (same ld); else the two lie wholly apart, from the first row to the last.
+ * Results do not depend on timing: every sum has a fixed order.
  *
  * Logits: [n][ld] of `dtype` (rl_dtype), n <= 2^20 rows, vocab <= 2^24
  * entries each (any value >= 1), ld >= vocab; entries vocab .. ld - 1 of a
  * row are neither read nor written.  The pointer needs the element's
  * alignment only; rows that start on 16 bytes are the fastest.
- * Temperature: finite, >= 0; 0 is taken as 1.  x = z / T below.
+ * Temperature: 0, which is taken as 1, or finite and at least 1e-30.
+ * x = z / T below.
  * ------------------------------------------------------------------- */
 
-/* Bytes of workspace for rl_token_logprobs (0 when the rows alone fill the
- * chip, or for invalid sizes). */
+/* Bytes of workspace for rl_token_logprobs (0 for invalid sizes, and where
+ * no row is cut: most sizes). */
 size_t rl_logprob_workspace_bytes(int32_t n, int32_t vocab);
 
 /* Log-probability of a given token under each row of logits, and the row's
@@ -487,7 +489,8 @@ typedef struct rl_preference_params {
     int32_t average;             /* 1: log ratios are means over counted tokens, 0: sums */
 } rl_preference_params;
 
-/* Bytes of workspace for rl_preference_loss (0 for invalid sizes). */
+/* Bytes of workspace for rl_preference_loss (0 for invalid sizes, and where
+ * none is needed). */
 size_t rl_preference_workspace_bytes(int32_t n, int32_t n_pairs);
 
 /* Preference loss of n_pairs answer pairs and its gradient: sequence 2p is

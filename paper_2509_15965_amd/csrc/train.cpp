@@ -13,6 +13,8 @@ namespace {
 
 constexpr int kMaxRows = 1 << 20, kMaxVocab = 1 << 24, kMaxTokens = 1 << 24, kMaxSeqs = 1 << 20, kMaxPairs = 1 << 19;
 
+constexpr float kMinTemperature = 1e-30f;   // 1 / T and log2(e) / T are finite in fp32
+
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 size_t elem_bytes(int dtype) { return dtype == RL_DTYPE_FP32 ? 4 : 2; }
@@ -20,7 +22,7 @@ rl_status status_of(hipError_t e) { return e == hipSuccess ? RL_OK : RL_ERR_HIP;
 
 bool rows_ok(int32_t n, int32_t vocab, int32_t dtype, int64_t ld, float T) {
     return n >= 0 && n <= kMaxRows && vocab >= 1 && vocab <= kMaxVocab && (dtype == RL_DTYPE_FP32 || dtype == RL_DTYPE_BF16) &&
-           ld >= vocab && ld <= (int64_t(1) << 40) / (n > 0 ? n : 1) && T >= 0.0f && std::isfinite(T);
+           ld >= vocab && ld <= (int64_t(1) << 40) / (n > 0 ? n : 1) && (T == 0.0f || T >= kMinTemperature) && std::isfinite(T);
 }
 
 // bytes from the first to past the last entry of a matrix of rows

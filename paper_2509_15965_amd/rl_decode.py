@@ -475,7 +475,7 @@ def _on(dev: int, name: str, t: Optional[torch.Tensor], dtype, numel: int, optio
         if optional:
             return None
         raise ValueError(f"{name} is missing")
-    if t.dtype is dtype and t.get_device() == dev and t.numel() == numel and t.is_contiguous():
+    if t.dtype is dtype and t.get_device() == dev and t.numel() == numel < 1 << 31 and t.is_contiguous():
         return t.data_ptr()
     raise ValueError(f"{name} must be {dtype}, contiguous, of {numel} entries on cuda:{dev}, not {t.dtype} "
                      f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
@@ -494,8 +494,9 @@ def _rows_on(dev: int, name: str, t: torch.Tensor, like: Optional[torch.Tensor] 
                          + f", not {t.dtype} {tuple(t.shape)} on {t.device}")
     n, V = t.shape
     ld = t.stride(0) if n > 1 else V
-    if (V > 1 and t.stride(1) != 1) or ld < V:
-        raise ValueError(f"{name}: entries of a row must be contiguous and rows apart, strides {t.stride()}")
+    if (V > 1 and t.stride(1) != 1) or ld < V or V >= 1 << 31:
+        raise ValueError(f"{name}: entries of a row must be contiguous, fewer than 2^31, and rows apart: {tuple(t.shape)} "
+                         f"with strides {t.stride()}")
     return t.data_ptr(), ld
 
 

@@ -174,3 +174,18 @@ def test_binding_refuses_host_tensors():
         R.policy_loss_logits(z, y, f, f, torch.zeros(8), f, z)
     with pytest.raises(ValueError, match="GPU"):
         R.preference_loss(f, torch.zeros(3, dtype=torch.int32), torch.zeros(8), f)
+
+
+@pytest.mark.parametrize("T", [1e-31, 1e-45, -0.0])
+def test_temperatures_whose_reciprocal_is_no_float(T):
+    # -0.0 is 0: taken as 1 (no rows, so nothing runs)
+    want = R.RL_OK if T == 0 else R.RL_ERR_INVALID_ARG
+    assert logprobs(n=0, T=T) == want and backward(n=0, T=T) == want
+    if T:
+        assert policy(logits=dict(T=T)) == want
+
+
+def test_interleaved_gradient_rows_are_refused():
+    # d_logits' rows between the logits' rows: neither in place nor apart
+    assert backward(ld=200, ldd=200, dz=P + 200) == R.RL_ERR_INVALID_ARG
+    assert policy(logits=dict(ld=200, ldd=200, dz=P + 200)) == R.RL_ERR_INVALID_ARG

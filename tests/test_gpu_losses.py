@@ -473,6 +473,112 @@ def test_policy_loss_logits_entropy_output_changes_nothing_else():
     near(res[0][0], res[1][0], 40 * rel(V), 2 * U)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("V", [5, 1000, 9001])
+@pytest.mark.parametrize("T", [1.0, 0.7])
+def test_policy_loss_logits_rows_that_are_not_ordinary(V, dtype, T):
+    """The same twelve rows among many and alone: what is no number, of one value or out of range gives the same either way,
+    and other rows do not notice."""
+    low = torch.finfo(dtype).min
+    n, k, at = 1100, 12, 40
+    z, y = make(n, V, dtype, V, spread=1.0)
+    odd = z[at:at + k]
+    odd[0] = -INF
+    odd[1] = -INF
+    odd[1, V // 2] = 3.0
+    odd[2] = low
+    odd[3, 1:] = low
+    odd[4, V - 1] = INF
+    odd[5, 0] = NAN
+    odd[6] = 0.0
+    odd[9] = -INF
+    odd[9, :2] = 1.0
+    odd[10, 0], odd[10, 1] = -low, low
+    odd[11] = -low
+    y[at:at + k] = torch.tensor([0, V // 2, 1, 0, 0, 0, 2, -1, V, V - 1, 0, 3], dtype=torch.int32)
+    q, lp, H = formula(z, y, T)
+    old = torch.where(lp.isfinite(), lp, -1.0).clamp(min=-30).float()
+    adv = torch.linspace(-1.0, 2.0, n, device=DEV)
+    o = dict(clip_low=0.5, clip_high=8.0, token_advantages=True, aggregate="sum", entropy_coef=0.02)
+    res = []
+    for a, b in ((0, n), (at, at + k)):
+        out, olp, ent = torch.empty(8, device=DEV), torch.empty(b - a, device=DEV), torch.empty(b - a, device=DEV)
+        dz = torch.full((b - a, V), 9.0, device=DEV, dtype=dtype)
+        R.policy_loss_logits(z[a:b], y[a:b], old[a:b], adv[a:b], out, olp, dz, out_entropy=ent, temperature=T, **o)
+        assert out[0].isnan()
+        res.append((olp, ent, dz))
+    (olp, ent, dz), (olp2, ent2, dz2) = res
+    rows = [i for i in range(k) if i not in (0, 4, 5)]
+    i = torch.tensor(rows, device=DEV)
+    assert ent[at + i].isfinite().all() and olp[at + torch.tensor([0, 4, 5, 7, 8], device=DEV)].isnan().all()
+    assert dz[at + torch.tensor([0, 4, 5], device=DEV)].isnan().any(1).all()
+    assert dz[at + i].isfinite().all() and not dz[at + 1].any() and not dz[at + 10].any()
+    # both ways are within the bounds of the formula, so twice those apart
+    near(ent[at + i], ent2[i], 12 * rel(V) * (1 + math.log(V)), 4 * U)
+    j = torch.tensor([1, 2, 3, 6, 10, 11], device=DEV)
+    near(olp[at + j], olp2[j], 8 * rel(V), 4 * U)
+    assert olp[at + 9] == -INF and olp2[9] == -INF
+    for r in rows:
+        g = adv[at + r].abs().double() + 0.02 * (2 + math.log(V))
+        near(dz[at + r], dz2[r], g / T * 40 * rel(V), 2.0 ** -7 if dtype == BF else 40 * rel(V))
+    # ordinary rows against the formula; ratios are 1, inside the clip
+    plain = torch.ones(n, dtype=torch.bool, device=DEV)
+    plain[at:at + k] = False
+    near(olp[plain], lp[plain], 4 * rel(V), 2 * U)
+    g = (-adv.double() * (olp.double() - old.double()).exp())[plain]
+    ge = torch.full_like(g, -0.02)
+    err, step = gradient_tol(q[plain], H[plain], g, ge, T, dtype, V)
+    err += q[plain].exp() * 0.02 / T * 6 * rel(V) * (1 + math.log(V))      # of the entropy in the formula
+    near(dz[plain], gradient(q[plain], H[plain], y[plain], g, ge, T), err + (g.abs() / T * 4 * U)[:, None], step + 4 * U)
+
+
+@pytest.mark.parametrize("n", [191, 192, 1023, 1025, 2500])
+@pytest.mark.parametrize("offs", [None, "none", "ends"])
+def test_policy_loss_logits_rows_without_a_token(n, offs):
+    """Runs of rows that do not count, at every place of a workgroup's rows, without offsets, with none that count, and
+    with rows before the first and behind the last sequence."""
+    V = 300
+    z, y = make(n, V, BF, n)
+    mask = (torch.arange(n, device=DEV) // 7 % 3 != 0) if offs is None else torch.ones(n, device=DEV, dtype=torch.bool)
+    dead = ~mask
+    so = None
+    if offs == "none":
+        mask[:] = False
+        dead[:] = True
+    elif offs == "ends":
+        so = torch.tensor([60, 60, n - 90], device=DEV, dtype=torch.int32)
+        dead[:60] = dead[n - 90:] = True
+        mask = None
+    z[dead] = NAN
+    y[dead] = -7
+    q, lp, H = formula(z, y, 1.0)
+    old = torch.where(dead, NAN, lp).float()
+    adv = torch.full((n,), 1.5, device=DEV)
+    adv[dead] = NAN
+    out, olp = torch.full((8,), 3.0, device=DEV), torch.full((n,), 3.0, device=DEV)
+    dz = torch.full_like(z, 9.0)
+    R.policy_loss_logits(z, y, old, adv, out, olp, dz, mask=mask, seq_offsets=so, token_advantages=True, clip_high=4.0)
+    live = int((~dead).sum())
+    assert not dz[dead].any() and not olp[dead].any() and float(out[7]) == live
+    if not live:
+        assert not out.any()
+        return
+    near(olp[~dead], lp[~dead], 4 * rel(V), 2 * U)
+    near(out[0], torch.tensor(-1.5, device=DEV), 1.5 * 8 * rel(V), 2 * U)
+    g = (-1.5 / live) * (olp.double() - old.double()).exp()[~dead]
+    qd, yd = q[~dead], y[~dead]
+    err, step = gradient_tol(qd, H[~dead], g, None, 1.0, BF, V)
+    near(dz[~dead], gradient(qd, H[~dead], yd, g, None, 1.0), err + (g.abs() * 4 * U)[:, None], step + 4 * U)
+
+
+def test_policy_loss_counts_in_long_sequences():
+    """Masks counted by a wave, a workgroup and a wide one: sequences of every length among others of it, odd starts."""
+    for lens in ([40] * 300 + [1, 0, 17], [1500, 3000, 1, 0, 2047], [50001, 1, 16385, 30000], [70001]):
+        b = batch(lens, len(lens), masked=0.3, before=3, behind=2)
+        for aggregate in ("token_mean", "sequence_mean"):
+            check_policy(*run_policy(b, dict(aggregate=aggregate)))
+
+
 # -------------------------------------------------------------------------------------------- preference loss
 
 def preference_formula(lp, ref, offs, live, *, form, average, beta, label_smoothing, margin, scale):
@@ -689,6 +795,33 @@ def test_binding_refusals():
         with pytest.raises(R.RLError) as e:
             call()
         assert e.value.status == R.RL_ERR_INVALID_ARG, k
+
+
+def test_sizes_past_32_bits_are_refused():
+    f = lambda k: torch.zeros(k, device=DEV)
+    y = torch.zeros(1, device=DEV, dtype=torch.int32)
+    big = torch.empty(1, (1 << 32) + 5, device=DEV, dtype=BF)     # 5 to a 32-bit argument
+    with pytest.raises(ValueError):
+        R.token_logprobs(big, y, f(1))
+    many = big.view(-1)[:(1 << 32)].view(torch.float32)           # 2^31 entries
+    with pytest.raises(ValueError):
+        R.policy_loss(many, many, f(1), f(8), many)
+    with pytest.raises(ValueError):
+        R.preference_loss(many, torch.zeros(3, device=DEV, dtype=torch.int32), f(8), many)
+
+
+def test_lying_offsets_through_rows_stay_in_bounds():
+    n, V = 400, 24
+    z, y = make(n, V, F32, 2)
+    old, adv = torch.zeros(n, device=DEV), torch.ones(2, device=DEV)
+    for offs in ([-5, 30, 400], [0, 900, 400], [50, 10, 400], [0, 0, 1 << 30], [400, 400, 400], [-9, -3, -1]):
+        o = torch.tensor(offs, dtype=torch.int32, device=DEV)
+        big, lps = torch.full((n + 64, V), 4.0, device=DEV), torch.full((n + 64,), 4.0, device=DEV)
+        for aggregate in ("token_mean", "sequence_mean"):
+            R.policy_loss_logits(z, y, old, adv, torch.empty(8, device=DEV), lps[32:32 + n], big[32:32 + n], seq_offsets=o,
+                                 aggregate=aggregate)
+        for t in (big, lps):
+            assert (t[:32] == 4.0).all() and (t[32 + n:] == 4.0).all()
 
 
 def test_offsets_that_lie_stay_in_bounds():
