@@ -21,17 +21,19 @@ __device__ __forceinline__ int nonzero_bytes(uint32_t x) {
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
 
 // Counted tokens of each sequence, and per workgroup the counted tokens and
-// the sequences that have some.  LANES lanes a sequence: a wave reads 1024
-// mask bytes at once, a workgroup 4096.
+// the sequences that have some.  LANES lanes a sequence, 16 mask bytes a lane
+// at once.
 constexpr int kMaxCountBlocks = 1024;
 
+template <int LANES> constexpr int kCountThreads = LANES > kThreads ? LANES : kThreads;
+
 template <int LANES>
-__global__ void __launch_bounds__(kThreads) policy_count_kernel(int n, int n_seqs, const int32_t* __restrict__ offs,
+__global__ void __launch_bounds__(kCountThreads<LANES>) policy_count_kernel(int n, int n_seqs, const int32_t* __restrict__ offs,
                                                                 const uint8_t* __restrict__ mask,
                                                                 int32_t* __restrict__ counts, CountPart* __restrict__ parts) {
-    constexpr int GROUPS = kThreads / LANES, W = LANES / 64;
-    __shared__ int32_t part[kWaves];
-    __shared__ CountPart sp[kWaves];
+    constexpr int THREADS = kCountThreads<LANES>, WAVES = THREADS / 64, GROUPS = THREADS / LANES, W = LANES / 64;
+    __shared__ int32_t part[WAVES];
+    __shared__ CountPart sp[WAVES];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int group = threadIdx.x / LANES, at = threadIdx.x % LANES;
     CountPart mine{0, 0};
@@ -69,7 +71,7 @@ __global__ void __launch_bounds__(kThreads) policy_count_kernel(int n, int n_seq
     if (lane == 0) sp[wave] = mine;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kWaves; ++w) { mine.tokens += sp[w].tokens; mine.seqs += sp[w].seqs; }
+        for (int w = 1; w < WAVES; ++w) { mine.tokens += sp[w].tokens; mine.seqs += sp[w].seqs; }
         parts[blockIdx.x] = mine;
     }
 }
@@ -557,8 +559,13 @@ int preference_cuts(int n, int n_pairs) {
     return want < kMaxCuts ? want : kMaxCuts;
 }
 
-// Sequences of more than 1024 tokens on average take a workgroup each, shorter ones a wave.
-bool count_by_workgroup(const PolicyArgs& p) { return p.n / p.n_seqs > 1024; }
+// Lanes that count a sequence: a mask of one sequence of 2^20 tokens takes 17
+// us more than none with 1024, 53 with 256; of 8 x 131072 4.5 and 9; of 512 x
+// 1500 with 256 lanes 5.
+int count_lanes(const PolicyArgs& p) {
+    const int mean = p.n / p.n_seqs;
+    return mean > 16384 ? 1024 : mean > 1024 ? 256 : 64;
+}
 
 }  // namespace
 
@@ -569,7 +576,7 @@ PolicyWs policy_ws(const PolicyArgs& p, void* ws) {
     if (policy_needs_counts(p)) {
         r.counts = reinterpret_cast<int32_t*>(w);
         r.cparts = reinterpret_cast<CountPart*>(w + align256(static_cast<size_t>(p.n_seqs) * sizeof(int32_t)));
-        const int nc = count_by_workgroup(p) ? p.n_seqs : (p.n_seqs + kWaves - 1) / kWaves;
+        const int nc = count_lanes(p) > 64 ? p.n_seqs : (p.n_seqs + kWaves - 1) / kWaves;
         r.n_cparts = nc < kMaxCountBlocks ? nc : kMaxCountBlocks;
     }
     w += align256(static_cast<size_t>(p.n_seqs) * sizeof(int32_t)) + align256(kMaxCountBlocks * sizeof(CountPart));
@@ -587,8 +594,10 @@ size_t policy_ws_bytes(int n, int n_seqs) {
 
 hipError_t launch_policy_counts(const PolicyArgs& p, const PolicyWs& w, hipStream_t s) {
     if (!w.counts) return hipSuccess;
-    const auto kernel = count_by_workgroup(p) ? policy_count_kernel<kThreads> : policy_count_kernel<64>;
-    hipLaunchKernelGGL(kernel, dim3(w.n_cparts), dim3(kThreads), 0, s, p.n, p.n_seqs, p.offs, p.mask, w.counts, w.cparts);
+    const int lanes = count_lanes(p);
+    const auto kernel = lanes == 1024 ? policy_count_kernel<1024> : lanes == 256 ? policy_count_kernel<256> : policy_count_kernel<64>;
+    hipLaunchKernelGGL(kernel, dim3(w.n_cparts), dim3(lanes > kThreads ? lanes : kThreads), 0, s, p.n, p.n_seqs, p.offs, p.mask,
+                       w.counts, w.cparts);
     return hipGetLastError();
 }
 
