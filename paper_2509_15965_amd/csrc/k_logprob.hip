@@ -311,6 +311,11 @@ template <int N, bool ENT> __device__ __forceinline__ void grad_entries(const Ro
     }
 }
 
+// A workgroup a chunk of a row, two 16-byte vectors a lane: the row's logarithm, the target's gradient and the factors are
+// worked out once a lane, in fp64, and then each vector is a load, an exponential an entry and a store.  Bound by memory:
+// 4096 x 151936 bf16, 2.5 GB in and out, 406 us (6.1 TB/s, part of the logits from the cache that the forward pass has
+// filled), with one vector a lane 428, with four 412, eight 457; 24 rows 5.5 us (5.7, 5.7 and 6.8); 2048 x 20000 fp32 53
+// (four 56, eight 61).
 template <typename T, bool ENT>
 __global__ void __launch_bounds__(kRowThreads) token_logprobs_backward_kernel(const T* logits, int64_t ld, int V,
         const int32_t* __restrict__ targets, double inv_T, float c, const float* __restrict__ stats,
@@ -539,13 +544,18 @@ int rows(const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz,
     return grid;
 }
 
+// The narrowest workgroup that holds a row, so that a CU has up to four rows in different phases (1792 x 32000 bf16: 256
+// lanes 49 us, 512 50, 1024 63; 8192 x 8000: 68, 98, 170); up to two rows a CU twice that (192 rows of 32000: 13.6 us, with
+// 256 lanes 15.6; 500 of 40000: 20.2 and 22.1; 600 of 32000: 24.2 and 22.2).
 template <typename T>
 int rows_of(const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz, int64_t ldd, hipStream_t s) {
     const int nvec = a.V / kVec<T>;
     if (nvec <= 4 * 256) return rows<T, 256, 4>(p, w, a, dz, ldd, s);
     if (nvec <= 8 * 256) return rows<T, 256, 8>(p, w, a, dz, ldd, s);
-    if (nvec <= 16 * 256) return rows<T, 256, 16>(p, w, a, dz, ldd, s);
-    if (nvec <= 20 * 256) return rows<T, 256, 20>(p, w, a, dz, ldd, s);
+    const bool few = a.n <= 2 * kCUs;
+    if (nvec <= 16 * 256 && !few) return rows<T, 256, 16>(p, w, a, dz, ldd, s);
+    if (nvec <= 20 * 256 && !few) return rows<T, 256, 20>(p, w, a, dz, ldd, s);
+    if (nvec <= 10 * 512) return rows<T, 512, 10>(p, w, a, dz, ldd, s);
     if (nvec <= 16 * 512) return rows<T, 512, 16>(p, w, a, dz, ldd, s);
     if (nvec <= 20 * 512) return rows<T, 512, 20>(p, w, a, dz, ldd, s);
     if (nvec <= 16 * 1024) return rows<T, 1024, 16>(p, w, a, dz, ldd, s);
@@ -554,8 +564,13 @@ int rows_of(const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* 
 
 }  // namespace
 
+// One kernel beside the forward, loss and backward kernels, whose times stand in brackets: one row of 4096 fp32 logits 9.5
+// us (11.3), 32 of 32000 bf16 12.8 (14.4), one of 50000 14.6 (14.8).  Fewer than 96 wider rows are cut over the chip by
+// those: one of 65536 15.9 (14.9), 32 of 152064 25.1 (19.1), 64 of 80000 18.9 (19.2), 96 of 152064 26.9 (29.1), 1024 of
+// 152064 133 (162).
 bool policy_rows_fit(int dt, int n, int V) {
-    return n >= 192 && V / (dt == DT_F32 ? 4 : 8) <= kRowVecs * 1024;
+    const int nvec = V / (dt == DT_F32 ? 4 : 8);
+    return n >= (nvec <= 6 * 1024 ? 1 : 96) && nvec <= kRowVecs * 1024;
 }
 
 hipError_t launch_policy_rows(int dt, const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz, int64_t ldd,
@@ -580,8 +595,8 @@ hipError_t launch_token_logprobs_backward(int dt, const void* logits, int64_t ld
                                           const float* ge, void* dz, int64_t ldd, hipStream_t s) {
     // rows in y, at most 65535 a launch
     constexpr int kRows = 32768;
-    const int chunk = 8192, nchunks = (V + chunk - 1) / chunk;
     const size_t es = dt == DT_F32 ? 4 : 2;
+    const int chunk = 2 * kRowThreads * static_cast<int>(16 / es), nchunks = (V + chunk - 1) / chunk;
     for (int r = 0; r < n; r += kRows) {
         const int m = n - r < kRows ? n - r : kRows;
         const char* z = static_cast<const char*>(logits) + es * ld * r;

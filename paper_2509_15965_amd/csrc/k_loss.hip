@@ -150,10 +150,11 @@ __device__ __forceinline__ void one_token(const PolicyArgs& p, const TokenIn& in
     if (d_ent) *nth(d_ent, i) = static_cast<float>(ge);
 }
 
-// Tokens of a workgroup, loaded before anything else.  The sequences they lie in are found once for the
-// workgroup, then by each lane among those in LDS.
-constexpr int kTokensPerLane = 2, kTokensPerBlock = kThreads * kTokensPerLane, kSpan = 512;
+// K tokens a lane, loaded before anything else.  The sequences they lie in are found once for the workgroup, then by each
+// lane among those in LDS.
+constexpr int kSpan = 512;
 
+template <int K>
 __global__ void __launch_bounds__(kThreads) policy_loss_kernel(PolicyArgs p, const float* __restrict__ logp,
         const float* __restrict__ ent, const int32_t* __restrict__ counts, const CountPart* __restrict__ cparts,
         int n_cparts, float* __restrict__ d_logp, float* __restrict__ d_ent, double* __restrict__ parts) {
@@ -162,13 +163,13 @@ __global__ void __launch_bounds__(kThreads) policy_loss_kernel(PolicyArgs p, con
     __shared__ float adv[kSpan + 1];
     __shared__ int32_t ends[2];
     __shared__ PolicyTotals total;
-    const int tid = threadIdx.x, first = blockIdx.x * kTokensPerBlock;
-    const int last = min(p.n, first + kTokensPerBlock) - 1;
-    TokenIn in[kTokensPerLane];
-    uint8_t m[kTokensPerLane];
-    float own_adv[kTokensPerLane];
+    const int tid = threadIdx.x, first = blockIdx.x * (K * kThreads);
+    const int last = min(p.n, first + K * kThreads) - 1;
+    TokenIn in[K];
+    uint8_t m[K];
+    float own_adv[K];
 #pragma unroll
-    for (int k = 0; k < kTokensPerLane; ++k) {
+    for (int k = 0; k < K; ++k) {
         const int at = min(first + k * kThreads + tid, last);
         in[k] = load_token(p, logp, ent, at);
         m[k] = 1;
@@ -201,7 +202,7 @@ __global__ void __launch_bounds__(kThreads) policy_loss_kernel(PolicyArgs p, con
     }
     double v[kSums] = {};
 #pragma unroll
-    for (int k = 0; k < kTokensPerLane; ++k) {
+    for (int k = 0; k < K; ++k) {
         const int i = first + k * kThreads + tid;
         if (i > last) break;
         const int c = held ? s_lo + count_upto(span, 0, s_hi - s_lo, i) : count_upto(p.offs, s_lo, s_hi, i);
@@ -233,8 +234,10 @@ __global__ void __launch_bounds__(kFinalThreads) policy_final_kernel(const doubl
 }
 
 // The whole loss of few tokens in one workgroup and one launch: counts by
-// integer atomics in LDS, tokens, sums.
-constexpr int kSmallThreads = 1024, kSmallTokens = 4096, kSmallSeqs = 1024;
+// integer atomics in LDS, tokens, sums.  Bound by one CU's fp64: 256 tokens
+// 5.6 us where two or three launches take 9 and 11, 2048 9.6 (8.5 and 11.2),
+// 4096 14.7 (8.5 and 11.2).
+constexpr int kSmallThreads = 1024, kSmallTokens = 2048, kSmallSeqs = 1024;
 
 __global__ void __launch_bounds__(kSmallThreads) policy_small_kernel(PolicyArgs p, const float* __restrict__ logp,
         const float* __restrict__ ent, float* __restrict__ d_logp, float* __restrict__ d_ent, float* __restrict__ out) {
@@ -286,7 +289,13 @@ bool policy_small(int n, int n_seqs) { return n <= kSmallTokens && n_seqs <= kSm
 bool policy_needs_counts(const PolicyArgs& p) { return p.agg != 2 && (p.mask || (p.agg == 1 && p.n_seqs > 1024)); }
 
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
-int blocks_of(int n) { return (n + kTokensPerBlock - 1) / kTokensPerBlock; }
+// Two tokens a lane (768000 tokens: 14.8 us, with one 17.1, with four 15.0), and one where two workgroups a CU hold all
+// that way (51200 tokens: 9.4 us, with two 10.7; 120000: 9.3 and 10.1).
+int tokens_per_lane(int n) { return n <= 2 * kCUs * kThreads ? 1 : 2; }
+int blocks_of(int n) {
+    const int each = kThreads * tokens_per_lane(n);
+    return (n + each - 1) / each;
+}
 
 // ---- preference loss -------------------------------------------------------
 
@@ -415,7 +424,8 @@ template <int LANES> __device__ __forceinline__ void write_outside(const PrefArg
     for (int i = b + at; i < p.n; i += LANES) p.d_logp[i] = 0.0f;
 }
 
-// One workgroup a pair, half of it a sequence; one more for the tokens that no sequence holds.
+// One workgroup a pair, half of it a sequence (256 pairs of 2 x 1500 tokens 9.9 us with the last kernel; bound by latency:
+// loads, sums, the pair's loss, stores, 9 MB in and out); one more for the tokens that no sequence holds.
 constexpr int kPairThreads = 1024, kSide = kPairThreads / 2;
 
 __global__ void __launch_bounds__(kPairThreads) preference_kernel(PrefArgs p, double* __restrict__ parts) {
@@ -498,8 +508,10 @@ __global__ void __launch_bounds__(kFinalThreads) preference_final_kernel(const d
     if (threadIdx.x == 0) pair_outputs(t, n_pairs, scale, out);
 }
 
-// Few pairs of few tokens: one workgroup and one launch, its 16 waves shared out over the sequences.
-constexpr int kSmallPairs = 64, kSmallPairTokens = 16384, kSmallWaves = kSmallThreads / 64;
+// Few pairs of few tokens: one workgroup and one launch, its 16 waves shared out over the sequences.  4 pairs of 2 x 200
+// tokens 5.4 us (8.7 by a workgroup a pair and a last one), 16 of 2 x 512 8.8 (9.0), 32 of 2 x 200 10.7 (8.7); one of 2 x
+// 8192 8.5 (10.4), of 2 x 20000 14.1 (10.7 cut).
+constexpr int kSmallPairs = 16, kSmallPairTokens = 16384, kSmallWaves = kSmallThreads / 64;
 bool preference_small(int n, int n_pairs) { return n_pairs <= kSmallPairs && n <= kSmallPairTokens; }
 
 __global__ void __launch_bounds__(kSmallThreads) preference_small_kernel(PrefArgs p, float* __restrict__ out) {
@@ -519,7 +531,7 @@ __global__ void __launch_bounds__(kSmallThreads) preference_small_kernel(PrefArg
         if (lane == 63) share[s * each + wave % each] = SeqSums{w[0], w[1], w[2]};
     }
     __syncthreads();
-    if (wave == 0) {   // kSmallPairs lanes
+    if (wave == 0) {   // a lane a pair
         double v[kPairSums] = {};
         if (lane < p.n_pairs) {
             SeqSums sums[2];
@@ -552,7 +564,9 @@ __global__ void __launch_bounds__(kSmallThreads) preference_small_kernel(PrefArg
 }
 
 // Workgroups a sequence where pairs alone do not fill the chip and are long
-// enough to cut (0: a workgroup a pair).
+// enough to cut (0: a workgroup a pair): one pair of 2 x 20000 10.7 us (uncut
+// 17.2), 8 of them 12.1 (17.6), 128 20.2 (21.0), 200 25.5 (23.0); 8 of 2 x 8192
+// 11.9 (12.4).
 int preference_cuts(int n, int n_pairs) {
     if (n_pairs > 128 || n / n_pairs < 16384) return 0;
     const int want = 1024 / (2 * n_pairs);
@@ -617,7 +631,7 @@ hipError_t launch_policy_loss(const PolicyArgs& p, const float* logp, const floa
     hipError_t e = launch_policy_counts(p, w, s);
     const int nb = blocks_of(p.n);
     if (nb)
-        hipLaunchKernelGGL(policy_loss_kernel, dim3(nb), dim3(kThreads), 0, s, p, logp, ent, w.counts, w.cparts, w.n_cparts,
+        hipLaunchKernelGGL((tokens_per_lane(p.n) == 1 ? policy_loss_kernel<1> : policy_loss_kernel<2>), dim3(nb), dim3(kThreads), 0, s, p, logp, ent, w.counts, w.cparts, w.n_cparts,
                            d_logp, d_ent, w.parts);
     if (e == hipSuccess) e = launch_policy_final(p, w, nb, out, s);
     return e;

@@ -474,7 +474,7 @@ def test_policy_loss_logits_entropy_output_changes_nothing_else():
 
 
 @pytest.mark.parametrize("dtype", [F32, BF])
-@pytest.mark.parametrize("V", [5, 1000, 9001])
+@pytest.mark.parametrize("V", [5, 1000, 9001, 70001])
 @pytest.mark.parametrize("T", [1.0, 0.7])
 def test_policy_loss_logits_rows_that_are_not_ordinary(V, dtype, T):
     """The same twelve rows among many and alone: what is no number, of one value or out of range gives the same either way,
