@@ -151,7 +151,8 @@ __device__ __forceinline__ void one_token(const PolicyArgs& p, const TokenIn& in
 }
 
 // K tokens a lane, loaded before anything else.  The sequences they lie in are found once for the workgroup, then by each
-// lane among those in LDS.
+// lane among those in LDS.  512 sequences of 1500 tokens: 14.8 us with the last kernel, 19.2 with a mask's count before
+// it, where 21 MB are 4 us of the memory: bound by one workgroup's chain of loads, search, fp64 exponentials and sums.
 constexpr int kSpan = 512;
 
 template <int K>

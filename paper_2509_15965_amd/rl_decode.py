@@ -523,14 +523,21 @@ def _run_on(dev: int, stream, nbytes: int, workspace: Optional[torch.Tensor], ca
         if workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace must be a contiguous uint8 tensor on cuda:{dev}")
         ws, nbytes = workspace.data_ptr(), workspace.numel()
-    elif nbytes:
+    elif nbytes and stream is None:
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        if stream is not None:
-            workspace.record_stream(stream)
+        ws = workspace.data_ptr()
+    elif nbytes:
+        with torch.cuda.stream(stream):   # memory of that stream: the current one may still be using what it has freed
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
         ws = workspace.data_ptr()
     st = call(ws, nbytes, _current_stream(dev) if stream is None else stream.cuda_stream)
     if st != RL_OK:
         raise RLError(st, what)
+
+
+def _temperature(T: float) -> float:
+    """T for a float argument; what fp32 would round to 0 (which stands for 1) is refused like its neighbours."""
+    return T if T == 0.0 or abs(T) > 1e-31 else -1.0
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -552,7 +559,8 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, out_logp: torch.
     st = _on(dev, "out_stats", out_stats, torch.float32, 2 * n, True)
     L = lib()
     _run_on(dev, stream, L.rl_logprob_workspace_bytes(n, V) if workspace is None else 0, workspace,
-            lambda ws, nb, s: L.rl_token_logprobs(n, V, _dtype_code(logits), z, ld, y, temperature, lp, ent, st, ws, nb, s),
+            lambda ws, nb, s: L.rl_token_logprobs(n, V, _dtype_code(logits), z, ld, y, _temperature(temperature), lp, ent,
+                                              st, ws, nb, s),
             "rl_token_logprobs")
 
 
@@ -573,8 +581,8 @@ def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, stats: 
     ge = _on(dev, "d_entropy", d_entropy, torch.float32, n, True)
     L = lib()
     _run_on(dev, stream, 0, None,
-            lambda ws, nb, s: L.rl_token_logprobs_backward(n, V, _dtype_code(logits), z, ld, y, temperature, st, ent, g,
-                                                           ge, dz, ldd, s), "rl_token_logprobs_backward")
+            lambda ws, nb, s: L.rl_token_logprobs_backward(n, V, _dtype_code(logits), z, ld, y, _temperature(temperature),
+                                                           st, ent, g, ge, dz, ldd, s), "rl_token_logprobs_backward")
 
 
 def _policy(dev, n: int, old_logp, advantages, token_advantages, seq_offsets, ref_logp, mask, clip_low, clip_high,
@@ -641,7 +649,7 @@ def policy_loss_logits(logits: torch.Tensor, targets: torch.Tensor, old_logp: to
     L = lib()
     _run_on(dev, stream, L.rl_policy_logits_workspace_bytes(n, b.n_seqs, V) if workspace is None else 0, workspace,
             lambda ws, nb, s: L.rl_policy_loss_logits(C.byref(b), C.byref(q), V, _dtype_code(logits), z, ld, y,
-                                                      temperature, out, lp, ent, dz, ldd, ws, nb, s),
+                                                      _temperature(temperature), out, lp, ent, dz, ldd, ws, nb, s),
             "rl_policy_loss_logits")
 
 

@@ -758,6 +758,43 @@ def test_streams_and_graph_replays(lens, V, dtype):
             assert torch.equal(other[k], eager[(i + 1) % 3][k]), (i, k)
 
 
+def test_workspace_of_a_call_on_another_stream():
+    """What the current stream has freed and still uses is no workspace of a call on another stream."""
+    n, V = 400, 3001
+    z, y = make(n, V, F32, 3)
+    b = batch([n], 3)
+    f = lambda *s: torch.empty(*s, device=DEV)
+    want, got = (f(8), f(n), f(n, V)), (f(8), f(n), f(n, V))
+    R.policy_loss_logits(z, y, b["old"], b["adv"], *want, aggregate="sequence_mean", mask=b["mask"])
+    x = torch.randn(4096, 4096, device=DEV)
+    nbytes = R.lib().rl_policy_logits_workspace_bytes(n, 1, V)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(8):
+        x = x @ x * 1e-3
+    held = [torch.empty(nbytes, dtype=torch.uint8, device=DEV) for _ in range(4)]
+    for h in held:
+        h.fill_(255)                  # when the products are done
+    del held, h
+    R.policy_loss_logits(z, y, b["old"], b["adv"], *got, aggregate="sequence_mean", mask=b["mask"], stream=side)
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert torch.equal(g, w)
+
+
+def test_temperatures_that_fp32_takes_for_0():
+    z, y = make(2, 9, F32, 1)
+    for T in (1e-50, -1e-50, 1e-31, NAN):
+        with pytest.raises(R.RLError):
+            R.token_logprobs(z, y, torch.empty(2, device=DEV), temperature=T)
+    lp = torch.empty(2, device=DEV)
+    R.token_logprobs(z, y, lp, temperature=0)
+    near(lp, formula(z, y, 1.0)[1], 4 * rel(9), 2 * U)
+    # the smallest that is taken, a float: |z| < 16, so log-probabilities are within 32e30, which fp32 holds
+    R.token_logprobs(z, y, lp, temperature=1e-30)
+    near(lp, formula(z, y, float(torch.tensor(1e-30)))[1], 4 * rel(9), 2 * U)
+
+
 def test_binding_refusals():
     n, V = 4, 16
     z, y = make(n, V, BF, 1)
