@@ -118,12 +118,18 @@ template <int N, bool ENT> __device__ __forceinline__ void add_entries(LaneSum& 
         a.s *= f;
         a.R = R;
     }
+    // The vector's own sums first: a small entry leaves no trace in a sum of hundreds (log-probabilities under 152064
+    // logits at T = 0.6 were 6.4e-7 too high on average, 7.4e-7 off in the mean square; now 8e-8 and 3.1e-7, of which
+    // rounding them to fp32 is 2.8e-7).
+    float s = 0.0f, u = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const float t = __builtin_fmaf(v[i], c, -a.R), e = exp2_hw(t);
-        a.s += e;
-        if (ENT) a.u += e * fmaxf(t, kFloor);
+        s += e;
+        if (ENT) u += e * fmaxf(t, kFloor);
     }
+    a.s += s;
+    if (ENT) a.u += u;
 }
 // The same relative to the lane's largest entry.
 __device__ __forceinline__ RowPart close_sum(const LaneSum& a, float c) {
