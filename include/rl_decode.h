@@ -464,7 +464,8 @@ rl_status rl_policy_loss(const rl_policy_batch* batch, const rl_policy_params* p
 /* The same loss from logits to their gradient in one call: log-probabilities
  * of `targets`, entropies (with entropy_coef != 0, when out_entropy must be
  * given, or for out_entropy), loss and d loss / d logits.
- *  out_logp     [n]; 0 at tokens that do not count.
+ *  out_logp     [n]; 0 at tokens that do not count.  The loss is of the
+ *               log-probabilities before they are rounded to float.
  *  out_entropy  [n] or NULL; 0 at tokens that do not count.
  *  d_logits     [n][ldd] of dtype; may be the logits (ldd = ld).  Rows of
  *               tokens that do not count are zeros, whatever their logits are.

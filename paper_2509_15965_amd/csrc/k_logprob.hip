@@ -176,12 +176,14 @@ template <typename T, int WAVES> __device__ __forceinline__ RowPart sums_again(c
 
 template <typename T>
 __device__ __forceinline__ void finish_row(RowPart a, const T* z, int V, int y, double inv_T, int row, float* logp,
-                                           float* ent, float* stats) {
+                                           float* ent, float* stats, float* rest) {
     const double ln_s = ln_sum(a.s);
-    float lp = __builtin_nanf("");
-    if (y >= 0 && y < V)
-        lp = static_cast<float>((static_cast<double>(Elem<T>::load(z, y)) - a.m) * inv_T - ln_s);
-    logp[row] = lp > 0.0f ? 0.0f : lp;
+    double lp = __builtin_nan("");
+    if (y >= 0 && y < V) lp = (static_cast<double>(Elem<T>::load(z, y)) - a.m) * inv_T - ln_s;
+    lp = lp > 0.0 ? 0.0 : lp;
+    const float lp32 = static_cast<float>(lp);
+    logp[row] = lp32;
+    if (rest) rest[row] = lp32 < -FLT_MAX ? 0.0f : static_cast<float>(lp - lp32);
     if (ent) {
         const double h = ln_s - 0.69314718055994530942 * static_cast<double>(a.u / a.s);
         ent[row] = static_cast<float>(h < 0.0 ? 0.0 : h);
@@ -255,7 +257,7 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const T* __rest
     if (nchunks > 1)
         parts[static_cast<size_t>(row) * nchunks + blockIdx.y] = a;
     else
-        finish_row(a, z, V, targets[row], inv_T, row, logp, ent, stats);
+        finish_row(a, z, V, targets[row], inv_T, row, logp, ent, stats, live.rest);
 }
 
 // One wave per row.
@@ -271,7 +273,7 @@ __global__ void __launch_bounds__(64) token_logprobs_join_kernel(const RowPart* 
     RowPart a{-FLT_MAX, 0.0f, 0.0f};
     for (int k = threadIdx.x; k < nchunks; k += 64) a = merge(a, parts[static_cast<size_t>(row) * nchunks + k], c);
     a = merge_wave(a, c);
-    if (threadIdx.x == 0) finish_row(a, logits + row * ld, V, targets[row], inv_T, row, logp, ent, stats);
+    if (threadIdx.x == 0) finish_row(a, logits + row * ld, V, targets[row], inv_T, row, logp, ent, stats, live.rest);
 }
 
 // Gradients of a row's entries (the same row in every lane): with q = z c - K, 2^q (A + B q); K = m c + log2 s
@@ -447,7 +449,7 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
                 const double h = ln_s - 0.69314718055994530942 * static_cast<double>(a.u / a.s);
                 H = static_cast<float>(h < 0.0 ? 0.0 : h);
             }
-            const TokenLoss t = policy_token(p, lp32, old_logp, ref, adv);
+            const TokenLoss t = policy_token(p, lp, old_logp, ref, adv);
             const float g = held ? static_cast<float>(p.scale * weight * t.g) : 0.0f;
             const float ge = ENT ? static_cast<float>(-p.scale * weight * p.ent_coef) : 0.0f;
             if (tid == 0) {

@@ -124,9 +124,10 @@ __device__ __forceinline__ void policy_outputs(const double* t, double kl_coef, 
 }
 
 // One token: its terms into v, its gradients out.
-struct TokenIn { float logp, old_logp, ref, ent; };
+struct TokenIn { float logp, old_logp, ref, ent, rest; };
 __device__ __forceinline__ TokenIn load_token(const PolicyArgs& p, const float* logp, const float* ent, int i) {
-    TokenIn t{*nth(logp, i), *nth(p.old_logp, i), 0.0f, 0.0f};
+    TokenIn t{*nth(logp, i), *nth(p.old_logp, i), 0.0f, 0.0f, 0.0f};
+    if (p.rest) t.rest = *nth(p.rest, i);
     if (p.ref) t.ref = *nth(p.ref, i);
     if (ent) t.ent = *nth(ent, i);
     return t;
@@ -135,7 +136,7 @@ __device__ __forceinline__ void one_token(const PolicyArgs& p, const TokenIn& in
                                           float* d_logp, float* d_ent, int i) {
     double g = 0.0, ge = 0.0;
     if (live) {
-        const TokenLoss t = policy_token(p, in.logp, in.old_logp, in.ref, adv);
+        const TokenLoss t = policy_token(p, static_cast<double>(in.logp) + in.rest, in.old_logp, in.ref, adv);
         v[0] += w * t.pg;
         v[1] += w * t.kl;
         v[2] += w * in.ent;

@@ -332,6 +332,7 @@ struct PolicyArgs {
     double lo, hi, dual;          // ratio bounds 1 - clip_low, 1 + clip_high; dual clip (0: off)
     double kl_coef, ent_coef, scale;
     int kl, agg, token_adv;
+    float* rest;                  // [n] what rounding logp to fp32 took away, or null: nothing
 };
 
 // Rows of logits and what to compute of them.

@@ -44,9 +44,9 @@ rl_status workspace_ok(const void* ws, size_t have, size_t need) {
 size_t logprob_ws(int n, int V) { return align256(logprob_parts(n, V) * sizeof(RowPart)); }
 
 // What rl_policy_loss_logits keeps between its kernels: the loss's own, d_logp
-// and d_entropy, the rows' statistics, the vocabulary chunks' sums.
+// and d_entropy, what logp lost by rounding, the rows' statistics, the vocabulary chunks' sums.
 struct LogitsWs {
-    size_t off_g, off_ge, off_stats, off_parts, bytes;
+    size_t off_g, off_ge, off_rest, off_stats, off_parts, bytes;
 };
 LogitsWs logits_ws(int n, int n_seqs, int V) {
     LogitsWs w;
@@ -54,6 +54,8 @@ LogitsWs logits_ws(int n, int n_seqs, int V) {
     w.off_g = at;
     at += align256(sizeof(float) * n);
     w.off_ge = at;
+    at += align256(sizeof(float) * n);
+    w.off_rest = at;
     at += align256(sizeof(float) * n);
     w.off_stats = at;
     at += align256(2 * sizeof(float) * n);
@@ -74,7 +76,7 @@ bool policy_ok(const rl_policy_batch* b, const rl_policy_params* q, PolicyArgs* 
     if (b->n > 0 && (!b->old_logp || !b->advantages)) return false;
     *p = PolicyArgs{b->n, b->n_seqs, b->seq_offsets, b->old_logp, b->ref_logp, b->advantages, b->mask, 1.0 - q->clip_low,
                     1.0 + q->clip_high, q->dual_clip, q->kl_coef, q->entropy_coef, q->scale, q->kl, q->aggregate,
-                    q->token_advantages};
+                    q->token_advantages, nullptr};
     return true;
 }
 
@@ -161,6 +163,7 @@ rl_status rl_policy_loss_logits(const rl_policy_batch* batch, const rl_policy_pa
         if (e == hipSuccess) e = launch_policy_final(p, pw, n_parts, out_loss, s);
         return status_of(e);
     }
+    p.rest = reinterpret_cast<float*>(base + w.off_rest);
     hipError_t e = launch_token_logprobs(dtype, a, reinterpret_cast<RowPart*>(base + w.off_parts), s);
     if (e == hipSuccess) e = launch_policy_loss(p, out_logp, out_entropy, out_loss, g, ge, base, s);
     if (e == hipSuccess)

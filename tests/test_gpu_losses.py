@@ -446,15 +446,19 @@ def test_policy_loss_logits(n, V, dtype, lens, inplace, T, ent):
     if out_ent is not None:
         near(out_ent, torch.where(dead, 0.0, H), 6 * rel(V) * (1 + math.log(V)), 2 * U)
     # the loss and the tokens' gradients of the log-probabilities that came out
+    # (theirs before rounding, at most x = U |lp| away.  A token's pg moves by |pg| x, its KL by |exp(d) - 1| x < x, since
+    # |d| < 0.7 here; weights sum to 1.  A gradient moves by |g| x, and kl_coef exp(d) w x < 0.11 w x for its KL)
     want = policy_formula(out_lp, old, ref, b["adv"], out_ent, b["offs"], ~dead, **o)
     w, wg, wge, size = want
     dev = lambda a: torch.tensor(a, device=DEV, dtype=torch.double)
-    near(out, dev(w), 1e-12 * (1 + size), 2 * U)
+    x = U * torch.where(dead, 0.0, lp).abs()
+    near(out, dev(w), 1e-12 * (1 + size) + o["scale"] * (size + 1) * float(x.max()), 2 * U)
     g, ge = dev(wg), dev(wge) if ent else None
     err, step = gradient_tol(q, H, g, ge, T, dtype, V)
     full = gradient(q, H, y, g, ge, T)
     full[dead], err[dead] = 0.0, 0.0
-    near(dz, full, err + (g.abs() / T * 4 * U)[:, None], step + 4 * U)
+    moved = (g.abs() + 0.11 * o["scale"]) * x / T
+    near(dz, full, err + (g.abs() / T * 4 * U + moved)[:, None], step + 4 * U)
     if not inplace:
         assert (store[:, V:] == 9.0).all()
 
@@ -529,7 +533,9 @@ def test_policy_loss_logits_rows_that_are_not_ordinary(V, dtype, T):
     ge = torch.full_like(g, -0.02)
     err, step = gradient_tol(q[plain], H[plain], g, ge, T, dtype, V)
     err += q[plain].exp() * 0.02 / T * 6 * rel(V) * (1 + math.log(V))      # of the entropy in the formula
-    near(dz[plain], gradient(q[plain], H[plain], y[plain], g, ge, T), err + (g.abs() / T * 4 * U)[:, None], step + 4 * U)
+    # g is of log-probabilities before rounding: U |lp| of it
+    near(dz[plain], gradient(q[plain], H[plain], y[plain], g, ge, T),
+         err + (g.abs() / T * (4 + lp[plain].abs()) * U)[:, None], step + 4 * U)
 
 
 @pytest.mark.parametrize("n", [191, 192, 1023, 1025, 2500])
@@ -568,7 +574,8 @@ def test_policy_loss_logits_rows_without_a_token(n, offs):
     g = (-1.5 / live) * (olp.double() - old.double()).exp()[~dead]
     qd, yd = q[~dead], y[~dead]
     err, step = gradient_tol(qd, H[~dead], g, None, 1.0, BF, V)
-    near(dz[~dead], gradient(qd, H[~dead], yd, g, None, 1.0), err + (g.abs() * 4 * U)[:, None], step + 4 * U)
+    # g is of log-probabilities before rounding: U |lp| of it
+    near(dz[~dead], gradient(qd, H[~dead], yd, g, None, 1.0), err + (g.abs() * (4 + lp[~dead].abs()) * U)[:, None], step + 4 * U)
 
 
 def test_policy_loss_counts_in_long_sequences():
