@@ -114,7 +114,7 @@ template <int N, bool ENT> __device__ __forceinline__ void add_entries(LaneSum& 
     a.top = fmaxf(a.top, x);
     if (__builtin_fmaf(x, c, -a.R) > kAhead) {
         const float R = x * c, d = fmaxf(a.R - R, -1e4f), f = exp2_hw(d);
-        a.u = f * (a.u + d * a.s);
+        if (ENT) a.u = f * (a.u + d * a.s);
         a.s *= f;
         a.R = R;
     }
@@ -131,32 +131,59 @@ template <int N, bool ENT> __device__ __forceinline__ void add_entries(LaneSum& 
     a.s += s;
     if (ENT) a.u += u;
 }
-// The same relative to the lane's largest entry.
-__device__ __forceinline__ RowPart close_sum(const LaneSum& a, float c) {
+// The same relative to the lane's largest entry.  Without ENT, u is for straight() alone: every entry counts as the
+// lane's largest.
+template <bool ENT> __device__ __forceinline__ RowPart close_sum(const LaneSum& a, float c) {
     const float d = a.s == 0.0f ? 0.0f : fmaxf(__builtin_fmaf(-a.top, c, a.R), -1e4f), f = exp2_hw(d);
-    return RowPart{a.top, f * a.s, f * (a.u + d * a.s)};
+    return RowPart{a.top, f * a.s, ENT ? f * (a.u + d * a.s) : 0.0f};
 }
 
-// Over groups of N consecutive lanes.  Lanes may differ in the last bit (a
-// product and sum become one fma on one side only): take one lane's.
-template <int N> __device__ __forceinline__ RowPart merge_lanes(RowPart a, float c) {
-#pragma unroll
-    for (int off = N / 2; off > 0; off >>= 1)
-        a = merge(a, RowPart{__shfl_xor(a.m, off, 64), __shfl_xor(a.s, off, 64), __shfl_xor(a.u, off, 64)}, c);
-    return a;
+// A lane's value moved by register (`old` where the control names no lane or the row of 16 is masked).
+template <int CTRL, int ROWS> __device__ __forceinline__ float moved(float old, float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(old), __float_as_uint(v), CTRL, ROWS, 0xF, false));
 }
-__device__ __forceinline__ float first_lane(float x) {
-    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+template <int LANE> __device__ __forceinline__ float of_lane(float v) {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), LANE));
 }
-__device__ __forceinline__ RowPart merge_wave(RowPart a, float c) { return merge_lanes<64>(a, c); }
+// Over the first N lanes, 16 or 64: to the right within rows of 16, then row to row.
+template <int N> __device__ __forceinline__ float max_of(float v) {
+    v = fmaxf(v, moved<0x111, 0xF>(v, v));
+    v = fmaxf(v, moved<0x112, 0xF>(v, v));
+    v = fmaxf(v, moved<0x114, 0xF>(v, v));
+    v = fmaxf(v, moved<0x118, 0xF>(v, v));
+    if (N == 64) {
+        v = fmaxf(v, moved<0x142, 0xA>(v, v));
+        v = fmaxf(v, moved<0x143, 0xC>(v, v));
+    }
+    return of_lane<N - 1>(v);
+}
+template <int N> __device__ __forceinline__ float sum_of(float v) {
+    v += moved<0x111, 0xF>(0.0f, v);
+    v += moved<0x112, 0xF>(0.0f, v);
+    v += moved<0x114, 0xF>(0.0f, v);
+    v += moved<0x118, 0xF>(0.0f, v);
+    if (N == 64) {
+        v += moved<0x142, 0xA>(0.0f, v);
+        v += moved<0x143, 0xC>(0.0f, v);
+    }
+    return of_lane<N - 1>(v);
+}
+// The sums of the first N lanes' parts, the same bits in every lane.
+template <int N> __device__ __forceinline__ RowPart merge_of(RowPart a, float c) {
+    const float m = max_of<N>(a.m);
+    rebase(a, m, c);
+    return RowPart{m, sum_of<N>(a.s), sum_of<N>(a.u)};
+}
 
-// Over a workgroup; every lane gets the first lane's bits.
+// Over a workgroup, the same bits in every lane.
 template <int WAVES> __device__ __forceinline__ RowPart merge_workgroup(RowPart a, RowPart* sp, float c) {
-    a = merge_wave(a, c);
-    if ((threadIdx.x & 63) == 0) sp[threadIdx.x >> 6] = a;
+    static_assert(WAVES <= 16);
+    a = merge_of<64>(a, c);
+    const int lane = threadIdx.x & 63;
+    if (lane == 0) sp[threadIdx.x >> 6] = a;
     __syncthreads();
-    a = merge_lanes<WAVES>(sp[threadIdx.x % WAVES], c);
-    return RowPart{first_lane(a.m), first_lane(a.s), first_lane(a.u)};
+    a = lane < WAVES ? sp[lane] : RowPart{-FLT_MAX, 0.0f, 0.0f};
+    return merge_of<16>(a, c);
 }
 
 // Whether the sums stand: at least the largest entry's 1, and no NaN.
@@ -174,10 +201,16 @@ template <typename T, int WAVES> __device__ __forceinline__ RowPart sums_again(c
     return merge_workgroup<WAVES>(a, sp, c);
 }
 
+// ln sum exp((z - m) / T): of the sum with c in fp32, ln s, plus what c's rounding did to it, (log2(e) / T - c) / c =
+// bend / ln 2 times the mean of ln 2 t.  Near 1e-8 times 5 to 20, but the same way for every row.
+__device__ __forceinline__ double straight(double ln_c, const RowPart& a, float bend) {
+    return a.s > 1.0f ? ln_c + bend * (a.u / a.s) : ln_c;
+}
+
 template <typename T>
-__device__ __forceinline__ void finish_row(RowPart a, const T* z, int V, int y, double inv_T, int row, float* logp,
+__device__ __forceinline__ void finish_row(RowPart a, const T* z, int V, int y, double inv_T, float bend, int row, float* logp,
                                            float* ent, float* stats, float* rest) {
-    const double ln_s = ln_sum(a.s);
+    const double ln_c = ln_sum(a.s), ln_s = straight(ln_c, a, bend);
     double lp = __builtin_nan("");
     if (y >= 0 && y < V) lp = (static_cast<double>(Elem<T>::load(z, y)) - a.m) * inv_T - ln_s;
     lp = lp > 0.0 ? 0.0 : lp;
@@ -185,7 +218,7 @@ __device__ __forceinline__ void finish_row(RowPart a, const T* z, int V, int y, 
     logp[row] = lp32;
     if (rest) rest[row] = lp32 < -FLT_MAX ? 0.0f : static_cast<float>(lp - lp32);
     if (ent) {
-        const double h = ln_s - 0.69314718055994530942 * static_cast<double>(a.u / a.s);
+        const double h = ln_c - 0.69314718055994530942 * static_cast<double>(a.u / a.s);
         ent[row] = static_cast<float>(h < 0.0 ? 0.0 : h);
     }
     if (stats) {
@@ -209,7 +242,7 @@ constexpr int kRowThreads = 256;
 // rows by a row's own latency.
 template <typename T, int THREADS, bool ENT, bool KEEP>
 __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int V,
-        const int32_t* __restrict__ targets, double inv_T, float c, int chunk, bool check, PolicyArgs live,
+        const int32_t* __restrict__ targets, double inv_T, float c, float bend, int chunk, bool check, PolicyArgs live,
         RowPart* __restrict__ parts, float* __restrict__ logp, float* __restrict__ ent, float* __restrict__ stats) {
     constexpr int E = kVec<T>, U = 4, WAVES = THREADS / 64;
     __shared__ RowPart sp[WAVES];
@@ -251,19 +284,19 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const T* __rest
         }
     }
     add_entries<1, ENT>(acc, &last, c);
-    RowPart a = merge_workgroup<WAVES>(close_sum(acc, c), sp, c);
+    RowPart a = merge_workgroup<WAVES>(close_sum<ENT>(acc, c), sp, c);
     if (!stands(a)) a = sums_again<T, WAVES>(z, end - beg, a.m, c, sp);
     if (tid != 0) return;
     if (nchunks > 1)
         parts[static_cast<size_t>(row) * nchunks + blockIdx.y] = a;
     else
-        finish_row(a, z, V, targets[row], inv_T, row, logp, ent, stats, live.rest);
+        finish_row(a, z, V, targets[row], inv_T, bend, row, logp, ent, stats, live.rest);
 }
 
 // One wave per row.
 template <typename T>
 __global__ void __launch_bounds__(64) token_logprobs_join_kernel(const RowPart* __restrict__ parts, int nchunks,
-        const T* __restrict__ logits, int64_t ld, int V, const int32_t* __restrict__ targets, double inv_T, float c,
+        const T* __restrict__ logits, int64_t ld, int V, const int32_t* __restrict__ targets, double inv_T, float c, float bend,
         bool check, PolicyArgs live, float* __restrict__ logp, float* __restrict__ ent, float* __restrict__ stats) {
     const int row = blockIdx.x;
     if (check && counted_seq(live, row) < 0) {
@@ -272,8 +305,8 @@ __global__ void __launch_bounds__(64) token_logprobs_join_kernel(const RowPart* 
     }
     RowPart a{-FLT_MAX, 0.0f, 0.0f};
     for (int k = threadIdx.x; k < nchunks; k += 64) a = merge(a, parts[static_cast<size_t>(row) * nchunks + k], c);
-    a = merge_wave(a, c);
-    if (threadIdx.x == 0) finish_row(a, logits + row * ld, V, targets[row], inv_T, row, logp, ent, stats, live.rest);
+    a = merge_of<64>(a, c);
+    if (threadIdx.x == 0) finish_row(a, logits + row * ld, V, targets[row], inv_T, bend, row, logp, ent, stats, live.rest);
 }
 
 // Gradients of a row's entries (the same row in every lane): with q = z c - K, 2^q (A + B q); K = m c + log2 s
@@ -380,7 +413,7 @@ __global__ void __launch_bounds__(kRowThreads) token_logprobs_backward_kernel(co
 template <typename T, int THREADS, int NV, bool ENT>
 __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, const int32_t* __restrict__ counts,
         const CountPart* __restrict__ cparts, int n_cparts, const T* logits, int64_t ld, int V,
-        const int32_t* __restrict__ targets, double inv_T, float c, T* dz, int64_t ldd, float* __restrict__ logp,
+        const int32_t* __restrict__ targets, double inv_T, float c, float bend, T* dz, int64_t ldd, float* __restrict__ logp,
         float* __restrict__ ent, double* __restrict__ parts) {
     constexpr int E = kVec<T>, WAVES = THREADS / 64;
     __shared__ RowPart sp[2][WAVES];
@@ -437,16 +470,16 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
                 __builtin_amdgcn_sched_barrier(0);   // a vector at a time: unpacked ones would not fit beside the row
             }
             add_entries<1, ENT>(acc, &last, c);
-            RowPart a = merge_workgroup<WAVES>(close_sum(acc, c), sp[turn], c);
+            RowPart a = merge_workgroup<WAVES>(close_sum<ENT>(acc, c), sp[turn], c);
             if (!stands(a)) a = sums_again<T, WAVES>(logits + row * ld, V, a.m, c, sp[turn]);
             turn ^= 1;
-            const double ln_s = ln_sum(a.s);
+            const double ln_c = ln_sum(a.s), ln_s = straight(ln_c, a, bend);
             double lp = (static_cast<double>(zy) - a.m) * inv_T - ln_s;
             lp = lp > 0.0 ? 0.0 : lp;
             const float lp32 = static_cast<float>(lp);
             float H = 0.0f;
             if (ENT) {
-                const double h = ln_s - 0.69314718055994530942 * static_cast<double>(a.u / a.s);
+                const double h = ln_c - 0.69314718055994530942 * static_cast<double>(a.u / a.s);
                 H = static_cast<float>(h < 0.0 ? 0.0 : h);
             }
             const TokenLoss t = policy_token(p, lp, old_logp, ref, adv);
@@ -524,6 +557,9 @@ RowCut cut_rows(int n, int V) {
 }
 
 float log2_scale(float T) { return static_cast<float>(1.4426950408889634 / static_cast<double>(T)); }
+float bend_of(float T) {
+    return static_cast<float>((1.4426950408889634 / static_cast<double>(T) / log2_scale(T) - 1.0) * 0.69314718055994530942);
+}
 
 template <typename T, int THREADS>
 void launch_forward(const LogprobArgs& a, const RowCut& r, RowPart* parts, hipStream_t s) {
@@ -532,10 +568,10 @@ void launch_forward(const LogprobArgs& a, const RowCut& r, RowPart* parts, hipSt
     const auto kernel = a.ent ? (keep ? token_logprobs_kernel<T, THREADS, true, true> : token_logprobs_kernel<T, THREADS, true, false>)
                               : (keep ? token_logprobs_kernel<T, THREADS, false, true> : token_logprobs_kernel<T, THREADS, false, false>);
     hipLaunchKernelGGL(kernel, dim3(a.n, r.nchunks), dim3(THREADS), 0, s, static_cast<const T*>(a.logits), a.ld, a.V, a.targets,
-                       1.0 / a.T, log2_scale(a.T), r.chunk, a.live != nullptr, live, parts, a.logp, a.ent, a.stats);
+                       1.0 / a.T, log2_scale(a.T), bend_of(a.T), r.chunk, a.live != nullptr, live, parts, a.logp, a.ent, a.stats);
     if (r.nchunks > 1)
         hipLaunchKernelGGL(token_logprobs_join_kernel<T>, dim3(a.n), dim3(64), 0, s, parts, r.nchunks,
-                           static_cast<const T*>(a.logits), a.ld, a.V, a.targets, 1.0 / a.T, log2_scale(a.T),
+                           static_cast<const T*>(a.logits), a.ld, a.V, a.targets, 1.0 / a.T, log2_scale(a.T), bend_of(a.T),
                            a.live != nullptr, live, a.logp, a.ent, a.stats);
 }
 
@@ -555,7 +591,7 @@ int rows(const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz,
     const auto kernel = a.ent ? policy_rows_kernel<T, THREADS, NV, true> : policy_rows_kernel<T, THREADS, NV, false>;
     const int fit = kCUs * (1024 / THREADS), grid = a.n < fit ? a.n : fit;
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(THREADS), 0, s, p, w.counts, w.cparts, w.n_cparts,
-                       static_cast<const T*>(a.logits), a.ld, a.V, a.targets, 1.0 / a.T, log2_scale(a.T),
+                       static_cast<const T*>(a.logits), a.ld, a.V, a.targets, 1.0 / a.T, log2_scale(a.T), bend_of(a.T),
                        static_cast<T*>(dz), ldd, a.logp, a.ent, w.parts);
     return grid;
 }
