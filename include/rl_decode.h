@@ -362,8 +362,9 @@ rl_status rl_sample_logits_noalloc(int32_t n, int32_t vocab, const float* logits
  * entries each (any value >= 1), ld >= vocab; entries vocab .. ld - 1 of a
  * row are neither read nor written.  The pointer needs the element's
  * alignment only; rows that start on 16 bytes are the fastest.
- * Temperature: 0, which is taken as 1, or finite and at least 1e-30.
- * x = z / T below.
+ * Temperature: 0, which is taken as 1, or from 1e-30 to 1e30.  x = z / T
+ * below.  A double: rounded to float it would move every log-probability of
+ * a batch the same way.
  * ------------------------------------------------------------------- */
 
 /* Bytes of workspace for rl_token_logprobs (0 for invalid sizes, and where
@@ -380,7 +381,7 @@ size_t rl_logprob_workspace_bytes(int32_t n, int32_t vocab);
  * A logit of -inf is an entry of probability 0.  A row with a NaN or +inf
  * logit, or of nothing but -inf, leaves NaN.  out_logp is never above 0. */
 rl_status rl_token_logprobs(int32_t n, int32_t vocab, int32_t dtype, const void* logits, int64_t ld,
-                            const int32_t* targets, float temperature, float* out_logp, float* out_entropy,
+                            const int32_t* targets, double temperature, float* out_logp, float* out_entropy,
                             float* out_stats, void* workspace, size_t ws_bytes, void* stream);
 
 /* Its backward pass: with g = d_logp[i] and e = d_entropy[i] (0 when NULL),
@@ -391,7 +392,7 @@ rl_status rl_token_logprobs(int32_t n, int32_t vocab, int32_t dtype, const void*
  * A row with g = e = 0 is written as zeros, whatever its logits are.  Where
  * the target is outside [0, vocab), g is taken as 0. */
 rl_status rl_token_logprobs_backward(int32_t n, int32_t vocab, int32_t dtype, const void* logits, int64_t ld,
-                                     const int32_t* targets, float temperature, const float* stats,
+                                     const int32_t* targets, double temperature, const float* stats,
                                      const float* entropy, const float* d_logp, const float* d_entropy,
                                      void* d_logits, int64_t ldd, void* stream);
 
@@ -472,7 +473,7 @@ rl_status rl_policy_loss(const rl_policy_batch* batch, const rl_policy_params* p
  * A counted token whose target is outside [0, vocab) makes the loss NaN. */
 rl_status rl_policy_loss_logits(const rl_policy_batch* batch, const rl_policy_params* params, int32_t vocab,
                                 int32_t dtype, const void* logits, int64_t ld, const int32_t* targets,
-                                float temperature, float* out_loss, float* out_logp, float* out_entropy,
+                                double temperature, float* out_loss, float* out_logp, float* out_entropy,
                                 void* d_logits, int64_t ldd, void* workspace, size_t ws_bytes, void* stream);
 
 typedef enum rl_preference_form {

@@ -556,9 +556,9 @@ RowCut cut_rows(int n, int V) {
     return RowCut{V, 1, n <= 512 && V > 8192 ? 1024 : kRowThreads};
 }
 
-float log2_scale(float T) { return static_cast<float>(1.4426950408889634 / static_cast<double>(T)); }
-float bend_of(float T) {
-    return static_cast<float>((1.4426950408889634 / static_cast<double>(T) / log2_scale(T) - 1.0) * 0.69314718055994530942);
+float log2_scale(double T) { return static_cast<float>(1.4426950408889634 / T); }
+float bend_of(double T) {
+    return static_cast<float>((1.4426950408889634 / T / log2_scale(T) - 1.0) * 0.69314718055994530942);
 }
 
 template <typename T, int THREADS>
@@ -643,7 +643,7 @@ hipError_t launch_token_logprobs(int dt, const LogprobArgs& a, RowPart* parts, h
 }
 
 hipError_t launch_token_logprobs_backward(int dt, const void* logits, int64_t ld, int n, int V, const int32_t* targets,
-                                          float T, const float* stats, const float* ent, const float* g,
+                                          double T, const float* stats, const float* ent, const float* g,
                                           const float* ge, void* dz, int64_t ldd, hipStream_t s) {
     // rows in y, at most 65535 a launch
     constexpr int kRows = 32768;

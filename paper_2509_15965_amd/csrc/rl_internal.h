@@ -340,7 +340,7 @@ struct LogprobArgs {
     const void* logits; int64_t ld;
     int n, V;
     const int32_t* targets;
-    float T;                      // > 0
+    double T;                     // > 0
     float *logp, *ent, *stats;    // ent, stats may be null
     const PolicyArgs* live;       // or null: rows of tokens that do not count are skipped and leave zeros
 };
@@ -351,7 +351,7 @@ struct RowPart { float m, s, u; };
 size_t logprob_parts(int n, int V);   // RowParts a forward launch writes (0: one workgroup a row)
 hipError_t launch_token_logprobs(int dt, const LogprobArgs& a, RowPart* parts, hipStream_t s);
 hipError_t launch_token_logprobs_backward(int dt, const void* logits, int64_t ld, int n, int V, const int32_t* targets,
-                                          float T, const float* stats, const float* ent, const float* g,
+                                          double T, const float* stats, const float* ent, const float* g,
                                           const float* ge, void* dz, int64_t ldd, hipStream_t s);
 
 // Counted tokens, and sequences that have some, of a group of sequences.

@@ -13,16 +13,16 @@ namespace {
 
 constexpr int kMaxRows = 1 << 20, kMaxVocab = 1 << 24, kMaxTokens = 1 << 24, kMaxSeqs = 1 << 20, kMaxPairs = 1 << 19;
 
-constexpr float kMinTemperature = 1e-30f;   // 1 / T and log2(e) / T are finite in fp32
+constexpr double kMinTemperature = 1e-30, kMaxTemperature = 1e30;   // 1 / T and log2(e) / T are normal fp32 numbers
 
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 size_t elem_bytes(int dtype) { return dtype == RL_DTYPE_FP32 ? 4 : 2; }
 rl_status status_of(hipError_t e) { return e == hipSuccess ? RL_OK : RL_ERR_HIP; }
 
-bool rows_ok(int32_t n, int32_t vocab, int32_t dtype, int64_t ld, float T) {
+bool rows_ok(int32_t n, int32_t vocab, int32_t dtype, int64_t ld, double T) {
     return n >= 0 && n <= kMaxRows && vocab >= 1 && vocab <= kMaxVocab && (dtype == RL_DTYPE_FP32 || dtype == RL_DTYPE_BF16) &&
-           ld >= vocab && ld <= (int64_t(1) << 40) / (n > 0 ? n : 1) && (T == 0.0f || T >= kMinTemperature) && std::isfinite(T);
+           ld >= vocab && ld <= (int64_t(1) << 40) / (n > 0 ? n : 1) && (T == 0.0 || (T >= kMinTemperature && T <= kMaxTemperature));
 }
 
 // bytes from the first to past the last entry of a matrix of rows
@@ -89,19 +89,19 @@ size_t rl_logprob_workspace_bytes(int32_t n, int32_t vocab) {
 }
 
 rl_status rl_token_logprobs(int32_t n, int32_t vocab, int32_t dtype, const void* logits, int64_t ld, const int32_t* targets,
-                            float temperature, float* out_logp, float* out_entropy, float* out_stats, void* workspace,
+                            double temperature, float* out_logp, float* out_entropy, float* out_stats, void* workspace,
                             size_t ws_bytes, void* stream) {
     if (!rows_ok(n, vocab, dtype, ld, temperature)) return RL_ERR_INVALID_ARG;
     if (n == 0) return RL_OK;
     if (!logits || !targets || !out_logp || !aligned(logits, elem_bytes(dtype))) return RL_ERR_INVALID_ARG;
     if (const rl_status st = workspace_ok(workspace, ws_bytes, logprob_ws(n, vocab)); st != RL_OK) return st;
-    const LogprobArgs a{logits, ld, n, vocab, targets, temperature == 0.0f ? 1.0f : temperature, out_logp, out_entropy,
+    const LogprobArgs a{logits, ld, n, vocab, targets, temperature == 0.0 ? 1.0 : temperature, out_logp, out_entropy,
                         out_stats, nullptr};
     return status_of(launch_token_logprobs(dtype, a, static_cast<RowPart*>(workspace), static_cast<hipStream_t>(stream)));
 }
 
 rl_status rl_token_logprobs_backward(int32_t n, int32_t vocab, int32_t dtype, const void* logits, int64_t ld,
-                                     const int32_t* targets, float temperature, const float* stats, const float* entropy,
+                                     const int32_t* targets, double temperature, const float* stats, const float* entropy,
                                      const float* d_logp, const float* d_entropy, void* d_logits, int64_t ldd, void* stream) {
     if (!rows_ok(n, vocab, dtype, ld, temperature) || !rows_ok(n, vocab, dtype, ldd, temperature)) return RL_ERR_INVALID_ARG;
     if (n == 0) return RL_OK;
@@ -109,7 +109,7 @@ rl_status rl_token_logprobs_backward(int32_t n, int32_t vocab, int32_t dtype, co
     if (!logits || !targets || !stats || !d_logp || !d_logits || (d_entropy && !entropy)) return RL_ERR_INVALID_ARG;
     if (!aligned(logits, es) || !aligned(d_logits, es) || !place_ok(logits, ld, d_logits, ldd, n, vocab, es))
         return RL_ERR_INVALID_ARG;
-    return status_of(launch_token_logprobs_backward(dtype, logits, ld, n, vocab, targets, temperature == 0.0f ? 1.0f : temperature,
+    return status_of(launch_token_logprobs_backward(dtype, logits, ld, n, vocab, targets, temperature == 0.0 ? 1.0 : temperature,
                                                     stats, entropy, d_logp, d_entropy, d_logits, ldd,
                                                     static_cast<hipStream_t>(stream)));
 }
@@ -134,7 +134,7 @@ size_t rl_policy_logits_workspace_bytes(int32_t n, int32_t n_seqs, int32_t vocab
 }
 
 rl_status rl_policy_loss_logits(const rl_policy_batch* batch, const rl_policy_params* params, int32_t vocab, int32_t dtype,
-                                const void* logits, int64_t ld, const int32_t* targets, float temperature, float* out_loss,
+                                const void* logits, int64_t ld, const int32_t* targets, double temperature, float* out_loss,
                                 float* out_logp, float* out_entropy, void* d_logits, int64_t ldd, void* workspace,
                                 size_t ws_bytes, void* stream) {
     PolicyArgs p;
@@ -153,7 +153,7 @@ rl_status rl_policy_loss_logits(const rl_policy_batch* batch, const rl_policy_pa
     float* g = reinterpret_cast<float*>(base + w.off_g);
     float* ge = p.ent_coef != 0.0 ? reinterpret_cast<float*>(base + w.off_ge) : nullptr;
     float* stats = reinterpret_cast<float*>(base + w.off_stats);
-    const float T = temperature == 0.0f ? 1.0f : temperature;
+    const double T = temperature == 0.0 ? 1.0 : temperature;
     const LogprobArgs a{logits, ld, p.n, vocab, targets, T, out_logp, out_entropy, stats, &p};
     if (policy_rows_fit(dtype, p.n, vocab)) {
         const PolicyWs pw = policy_ws(p, base);

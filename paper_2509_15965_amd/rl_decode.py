@@ -174,9 +174,9 @@ def lib():
     L.rl_logprob_workspace_bytes.restype = sz
     L.rl_logprob_workspace_bytes.argtypes = [i32, i32]
     L.rl_token_logprobs.restype = C.c_int
-    L.rl_token_logprobs.argtypes = [i32, i32, i32, vp, i64, vp, f32, vp, vp, vp, vp, sz, vp]
+    L.rl_token_logprobs.argtypes = [i32, i32, i32, vp, i64, vp, C.c_double, vp, vp, vp, vp, sz, vp]
     L.rl_token_logprobs_backward.restype = C.c_int
-    L.rl_token_logprobs_backward.argtypes = [i32, i32, i32, vp, i64, vp, f32, vp, vp, vp, vp, vp, i64, vp]
+    L.rl_token_logprobs_backward.argtypes = [i32, i32, i32, vp, i64, vp, C.c_double, vp, vp, vp, vp, vp, i64, vp]
     L.rl_policy_workspace_bytes.restype = sz
     L.rl_policy_workspace_bytes.argtypes = [i32, i32]
     L.rl_policy_logits_workspace_bytes.restype = sz
@@ -184,7 +184,7 @@ def lib():
     L.rl_policy_loss.restype = C.c_int
     L.rl_policy_loss.argtypes = [C.POINTER(PolicyBatch), C.POINTER(PolicyParams), vp, vp, vp, vp, vp, vp, sz, vp]
     L.rl_policy_loss_logits.restype = C.c_int
-    L.rl_policy_loss_logits.argtypes = [C.POINTER(PolicyBatch), C.POINTER(PolicyParams), i32, i32, vp, i64, vp, f32,
+    L.rl_policy_loss_logits.argtypes = [C.POINTER(PolicyBatch), C.POINTER(PolicyParams), i32, i32, vp, i64, vp, C.c_double,
                                         vp, vp, vp, vp, i64, vp, sz, vp]
     L.rl_preference_workspace_bytes.restype = sz
     L.rl_preference_workspace_bytes.argtypes = [i32, i32]
@@ -535,11 +535,6 @@ def _run_on(dev: int, stream, nbytes: int, workspace: Optional[torch.Tensor], ca
         raise RLError(st, what)
 
 
-def _temperature(T: float) -> float:
-    """T for a float argument; what fp32 would round to 0 (which stands for 1) is refused like its neighbours."""
-    return T if T == 0.0 or abs(T) > 1e-31 else -1.0
-
-
 def _dtype_code(t: torch.Tensor) -> int:
     return RL_DTYPE_FP32 if t.dtype == torch.float32 else RL_DTYPE_BF16
 
@@ -559,8 +554,7 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, out_logp: torch.
     st = _on(dev, "out_stats", out_stats, torch.float32, 2 * n, True)
     L = lib()
     _run_on(dev, stream, L.rl_logprob_workspace_bytes(n, V) if workspace is None else 0, workspace,
-            lambda ws, nb, s: L.rl_token_logprobs(n, V, _dtype_code(logits), z, ld, y, _temperature(temperature), lp, ent,
-                                              st, ws, nb, s),
+            lambda ws, nb, s: L.rl_token_logprobs(n, V, _dtype_code(logits), z, ld, y, temperature, lp, ent, st, ws, nb, s),
             "rl_token_logprobs")
 
 
@@ -581,8 +575,8 @@ def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, stats: 
     ge = _on(dev, "d_entropy", d_entropy, torch.float32, n, True)
     L = lib()
     _run_on(dev, stream, 0, None,
-            lambda ws, nb, s: L.rl_token_logprobs_backward(n, V, _dtype_code(logits), z, ld, y, _temperature(temperature),
-                                                           st, ent, g, ge, dz, ldd, s), "rl_token_logprobs_backward")
+            lambda ws, nb, s: L.rl_token_logprobs_backward(n, V, _dtype_code(logits), z, ld, y, temperature, st, ent, g,
+                                                           ge, dz, ldd, s), "rl_token_logprobs_backward")
 
 
 def _policy(dev, n: int, old_logp, advantages, token_advantages, seq_offsets, ref_logp, mask, clip_low, clip_high,
@@ -649,7 +643,7 @@ def policy_loss_logits(logits: torch.Tensor, targets: torch.Tensor, old_logp: to
     L = lib()
     _run_on(dev, stream, L.rl_policy_logits_workspace_bytes(n, b.n_seqs, V) if workspace is None else 0, workspace,
             lambda ws, nb, s: L.rl_policy_loss_logits(C.byref(b), C.byref(q), V, _dtype_code(logits), z, ld, y,
-                                                      _temperature(temperature), out, lp, ent, dz, ldd, ws, nb, s),
+                                                      temperature, out, lp, ent, dz, ldd, ws, nb, s),
             "rl_policy_loss_logits")
 
 

@@ -176,8 +176,8 @@ def test_binding_refuses_host_tensors():
         R.preference_loss(f, torch.zeros(3, dtype=torch.int32), torch.zeros(8), f)
 
 
-@pytest.mark.parametrize("T", [1e-31, 1e-45, -0.0])
-def test_temperatures_whose_reciprocal_is_no_float(T):
+@pytest.mark.parametrize("T", [1e-31, 1e-300, 2e30, 1e300, -0.0])
+def test_temperatures_out_of_range(T):
     # -0.0 is 0: taken as 1 (no rows, so nothing runs)
     want = R.RL_OK if T == 0 else R.RL_ERR_INVALID_ARG
     assert logprobs(n=0, T=T) == want and backward(n=0, T=T) == want

@@ -789,17 +789,17 @@ def test_workspace_of_a_call_on_another_stream():
         assert torch.equal(g, w)
 
 
-def test_temperatures_that_fp32_takes_for_0():
+def test_temperatures_out_of_range():
     z, y = make(2, 9, F32, 1)
-    for T in (1e-50, -1e-50, 1e-31, NAN):
+    for T in (1e-50, -1e-50, 1e-31, 2e30, INF, NAN):
         with pytest.raises(R.RLError):
             R.token_logprobs(z, y, torch.empty(2, device=DEV), temperature=T)
     lp = torch.empty(2, device=DEV)
     R.token_logprobs(z, y, lp, temperature=0)
     near(lp, formula(z, y, 1.0)[1], 4 * rel(9), 2 * U)
-    # the smallest that is taken, a float: |z| < 16, so log-probabilities are within 32e30, which fp32 holds
-    R.token_logprobs(z, y, lp, temperature=1e-30)
-    near(lp, formula(z, y, float(torch.tensor(1e-30)))[1], 4 * rel(9), 2 * U)
+    for T in (1e-30, 1e30):       # |z| < 16, so log-probabilities are within 32e30, which fp32 holds
+        R.token_logprobs(z, y, lp, temperature=T)
+        near(lp, formula(z, y, T)[1], 4 * rel(9), 2 * U)
 
 
 def test_binding_refusals():
