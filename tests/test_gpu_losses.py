@@ -941,3 +941,106 @@ def test_rollout_to_gradient():
         near(dz, gradient(q, H, y, d, None, T), 1e-5, 1e-5)
     finally:
         eng.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_most_rows_and_sequences(dtype):
+    """2^20 rows, every one a sequence of its own, through every call that takes rows."""
+    n, V = 1 << 20, 5
+    z, y = make(n, V, dtype, 1)
+    q, want, H = formula(z, y, 1.0)
+    lp, ent, st = forward(z, y, 1.0)
+    near(lp, want, 4 * rel(V), 2 * U)
+    near(ent, H, 6 * rel(V) * (1 + math.log(V)), 2 * U)
+    g = torch.randn(n, generator=gen(2), device=DEV)
+    dz = torch.full_like(z, 9.0)
+    R.token_logprobs_backward(z, y, st, g, dz)
+    err, step = gradient_tol(q, H, g, None, 1.0, dtype, V)
+    near(dz, gradient(q, H, y, g, None, 1.0), err + (g.double().abs() * 2 * U)[:, None], step)
+    offs = torch.arange(n + 1, device=DEV, dtype=torch.int32)
+    mask = torch.ones(n, device=DEV, dtype=torch.bool)
+    mask[-1] = False
+    for m in (None, mask):
+        out = torch.empty(8, device=DEV)
+        R.policy_loss_logits(z, y, lp, g, out, lp.clone(), dz, seq_offsets=offs, aggregate="sequence_mean", mask=m)
+        live = n if m is None else n - 1
+        assert float(out[7]) == live
+        # ratios are within U |lp| of 1
+        w = -g.double()[:live]
+        near(out[0], w.mean(), w.abs().mean() * U * float(lp.abs().max()) + 1e-9 * w.abs().mean(), 2 * U)
+        err, step = gradient_tol(q[:live], H[:live], w / live, None, 1.0, dtype, V)
+        near(dz[:live], gradient(q[:live], H[:live], y[:live], w / live, None, 1.0),
+             err + ((w / live).abs() * (4 + lp[:live].abs()) * U)[:, None], step + 4 * U)
+        assert m is None or not dz[-1].any()
+
+
+def test_calls_without_rows():
+    f = lambda *k: torch.full(k, 3.0, device=DEV)
+    z, y = torch.empty(0, 7, device=DEV), torch.empty(0, device=DEV, dtype=torch.int32)
+    R.token_logprobs(z, y, f(0), out_entropy=f(0), out_stats=f(0, 2))
+    R.token_logprobs_backward(z, y, f(0, 2), f(0), torch.empty_like(z))
+    for so in (None, torch.zeros(4, device=DEV, dtype=torch.int32)):
+        out = f(8)
+        R.policy_loss_logits(z, y, f(0), f(1 if so is None else 3), out, f(0), torch.empty_like(z), seq_offsets=so)
+        assert not out.any()
+
+
+def test_captured_call_makes_its_own_workspace():
+    n, V = 300, 3000
+    inputs = [make(n, V, BF, i) for i in range(3)]
+    b = batch([100, 0, 200], 4, masked=0.2)
+    f = lambda *k: torch.empty(*k, device=DEV)
+    z, y = inputs[0][0].clone(), inputs[0][1].clone()
+
+    def call(z, y, out, lp, dz):
+        R.policy_loss_logits(z, y, b["old"], b["adv"], out, lp, dz, seq_offsets=b["offs"], mask=b["mask"],
+                             aggregate="sequence_mean")
+    want = []
+    for zi, yi in inputs:
+        o = (f(8), f(n), torch.empty_like(zi))
+        call(zi, yi, *o)
+        want.append(o)
+    got = (f(8), f(n), torch.empty_like(z))
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        call(z, y, *got)
+    for i in (1, 2, 0, 1):
+        z.copy_(inputs[i][0])
+        y.copy_(inputs[i][1])
+        scratch = torch.full((1 << 20,), NAN, device=DEV)      # eager work between replays
+        graph.replay()
+        o = (f(8), f(n), torch.empty_like(z))
+        call(*inputs[i], *o)
+        torch.cuda.synchronize()
+        for a, e, w in zip(got, o, want[i]):
+            assert torch.equal(a, w) and torch.equal(e, w)
+        del scratch
+
+
+def test_most_tokens_and_pairs():
+    n, pairs = 1 << 24, 1 << 19
+    g = gen(7)
+    lp = -4 * torch.rand(n, generator=g, device=DEV)
+    old = lp + 0.05 * torch.randn(n, generator=g, device=DEV)
+    mask = torch.rand(n, generator=g, device=DEV) < 0.7
+    out, d = torch.empty(8, device=DEV), torch.empty(n, device=DEV)
+    live = mask.double()
+    for aggregate in ("token_mean", "sequence_mean"):       # one sequence: the same
+        R.policy_loss(lp, old, torch.full((1,), -0.5, device=DEV), out, d, mask=mask, clip_low=0.9, clip_high=9.0,
+                      aggregate=aggregate)
+        pg = 0.5 * (lp.double() - old.double()).exp() * live / live.sum()
+        near(out[0], pg.sum(), 1e-11, 2 * U)
+        near(d, pg, 1e-18, 2 * U)
+        assert float(out[7]) == float(live.sum())
+    # pairs of 16 and 16 tokens
+    offs = torch.arange(0, n + 1, 16, device=DEV, dtype=torch.int32)
+    r = torch.empty(2 * pairs, device=DEV)
+    R.preference_loss(lp, offs, out, d, ref_logp=old, mask=mask, out_rewards=r, beta=0.3)
+    s = ((lp.double() - old.double()) * live).view(pairs, 2, 16).sum(2)
+    near(r.view(pairs, 2), 0.3 * s, 1e-12, 2 * U)
+    h = 0.3 * (s[:, 0] - s[:, 1])
+    near(out[0], torch.nn.functional.softplus(-h).mean(), 1e-11, 2 * U)
+    w = -0.3 * torch.sigmoid(-h) / pairs
+    want = (torch.stack([w, -w], 1)[:, :, None] * live.view(pairs, 2, 16)).view(n)
+    near(d, want, 1e-18, 2 * U)
