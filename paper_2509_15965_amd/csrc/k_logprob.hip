@@ -7,9 +7,9 @@
 //   d z_v   = (g (1[v = y] - p_v) - ge p_v (ln p_v + H)) / T
 // Exponents are one fma, z c - R: R stands for m c, and what rounding it costs
 // cancels (sums carry the R they are relative to; a gradient's factor takes
-// 2^(R rounded - R)).  Rows whose entries lie beyond 1e30 leave no such sum
-// (logits of the type's lowest value and nothing else, or of its largest);
-// those are taken again with the difference before the product.
+// 2^(R rounded - R)).  A row with m c past 2^28, where that rounding is more
+// than 8, or without a sum (logits of the type's lowest value and nothing
+// else) is summed again with the difference before the product.
 #include "rl_device.h"
 #include "rl_internal.h"
 #include "train.h"
@@ -186,8 +186,13 @@ template <int WAVES> __device__ __forceinline__ RowPart merge_workgroup(RowPart 
     return merge_of<16>(a, c);
 }
 
-// Whether the sums stand: at least the largest entry's 1, and no NaN.
-__device__ __forceinline__ bool stands(const RowPart& a) { return a.s > 0.5f && a.s < FLT_MAX; }
+// Whether the sums stand: at least the largest entry's 1, no NaN, and an R whose rounding (half a step of fp32 at m c: 8 at
+// 2^28) stays far from kAhead and from what an exponential can hold.  One rounded by more than kAhead would move again at
+// every entry, by what its rounding was, and take the sums before it away.
+constexpr float kFarSum = 268435456.0f;
+__device__ __forceinline__ bool stands(const RowPart& a, float c) {
+    return a.s > 0.5f && a.s < FLT_MAX && fabsf(a.m * c) < kFarSum;
+}
 
 // Entries [0, n) again, with the difference to m before the product.
 template <typename T, int WAVES> __device__ __forceinline__ RowPart sums_again(const T* z, int n, float m, float c, RowPart* sp) {
@@ -285,7 +290,7 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const T* __rest
     }
     add_entries<1, ENT>(acc, &last, c);
     RowPart a = merge_workgroup<WAVES>(close_sum<ENT>(acc, c), sp, c);
-    if (!stands(a)) a = sums_again<T, WAVES>(z, end - beg, a.m, c, sp);
+    if (!stands(a, c)) a = sums_again<T, WAVES>(z, end - beg, a.m, c, sp);
     if (tid != 0) return;
     if (nchunks > 1)
         parts[static_cast<size_t>(row) * nchunks + blockIdx.y] = a;
@@ -471,7 +476,7 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
             }
             add_entries<1, ENT>(acc, &last, c);
             RowPart a = merge_workgroup<WAVES>(close_sum<ENT>(acc, c), sp[turn], c);
-            if (!stands(a)) a = sums_again<T, WAVES>(logits + row * ld, V, a.m, c, sp[turn]);
+            if (!stands(a, c)) a = sums_again<T, WAVES>(logits + row * ld, V, a.m, c, sp[turn]);
             turn ^= 1;
             const double ln_c = ln_sum(a.s), ln_s = straight(ln_c, a, bend);
             double lp = (static_cast<double>(zy) - a.m) * inv_T - ln_s;

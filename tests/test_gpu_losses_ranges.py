@@ -1,0 +1,64 @@
+"""Log-probabilities of logits far from ordinary ranges: small temperatures
+and large logits (needs an MI355X).
+
+Tolerances as in test_gpu_losses.py.  The forms here take the difference to
+the row's largest logit before dividing by the temperature: ln n is lost next
+to 1e10.
+"""
+import math
+
+import pytest
+import torch
+
+from test_gpu_losses import BF, DEV, F32, U, forward, gen, near, rel
+
+pytestmark = pytest.mark.gpu
+
+
+def formula(z, y, T):
+    """log p, log-probabilities of y and entropies in 64 bits."""
+    z = z.double()
+    t = (z - z.max(1, keepdim=True).values) / T
+    q = t - t.exp().sum(1, keepdim=True).log()
+    return q, q.gather(1, y.long()[:, None])[:, 0], torch.special.entr(q.exp()).sum(1)
+
+
+FAR = [1e6, 3e7, 1e8, 1e9, 4e9, 1e10, 1e12, 1e20, 1e30, 1e35, 1e37, 1e38]
+
+
+def far_rows(V, dtype, seed):
+    """Rows of +-v alone, of v and values a few of the type's steps below, and of ordinary values with v at two places."""
+    g = gen(seed)
+    randn = lambda: torch.randn(V, generator=g, device=DEV)
+    step = torch.finfo(dtype).eps
+    rows = []
+    for v in FAR:
+        rows += [torch.full((V,), v, device=DEV), torch.full((V,), -v, device=DEV)]
+        rows.append(-v * (1 + step * torch.randint(0, 4, (V,), generator=g, device=DEV).float()))
+        r = 3 * randn()
+        r[torch.randint(0, V, (2,), generator=g, device=DEV)] = v
+        rows.append(r)
+    return torch.stack(rows).to(dtype).clamp(torch.finfo(dtype).min, torch.finfo(dtype).max)
+
+
+CASES = [("rows", T) for T in (1.0, 0.7)] + [("ordinary", T) for T in (1e-6, 1e-7, 1e-8, 3e-9, 1e-9, 1e-12, 1e-30, 1e30)]
+
+
+def inputs(kind, V, dtype, seed):
+    z = far_rows(V, dtype, seed) if kind == "rows" else (3 * torch.randn(40, V, generator=gen(seed), device=DEV)).to(dtype)
+    y = torch.randint(0, V, (z.shape[0],), generator=gen(seed + 1), device=DEV, dtype=torch.int32)
+    y[::2] = z[::2].float().argmax(1).int()
+    return z, y
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("V", [9, 5000, 70001])
+@pytest.mark.parametrize("kind,T", CASES)
+def test_logprobs(kind, T, V, dtype):
+    z, y = inputs(kind, V, dtype, V)
+    q, want, H = formula(z, y, T)
+    lp, ent, st = forward(z, y, T)
+    near(lp, want, 4 * rel(V), 2 * U)
+    near(ent, H, 6 * rel(V) * (1 + math.log(V)), 2 * U)
+    only, _, _ = forward(z, y, T, entropy=False)
+    near(only, want, 4 * rel(V), 2 * U)
