@@ -188,10 +188,11 @@ template <int WAVES> __device__ __forceinline__ RowPart merge_workgroup(RowPart 
 
 // Whether the sums stand: at least the largest entry's 1, no NaN, and an R whose rounding (half a step of fp32 at m c: 8 at
 // 2^28) stays far from kAhead and from what an exponential can hold.  One rounded by more than kAhead would move again at
-// every entry, by what its rounding was, and take the sums before it away.
+// every entry, by what its rounding was, and take the sums before it away.  (Entries that far below m end as 0, but for a u
+// that they made infinite.)
 constexpr float kFarSum = 268435456.0f;
 __device__ __forceinline__ bool stands(const RowPart& a, float c) {
-    return a.s > 0.5f && a.s < FLT_MAX && fabsf(a.m * c) < kFarSum;
+    return a.s > 0.5f && a.s < FLT_MAX && fabsf(a.u) < FLT_MAX && fabsf(a.m * c) < kFarSum;
 }
 
 // Entries [0, n) again, with the difference to m before the product.

@@ -62,3 +62,22 @@ def test_logprobs(kind, T, V, dtype):
     near(ent, H, 6 * rel(V) * (1 + math.log(V)), 2 * U)
     only, _, _ = forward(z, y, T, entropy=False)
     near(only, want, 4 * rel(V), 2 * U)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("V", [9, 5000, 70001])
+def test_entries_far_below_a_row(V, dtype):
+    """Ordinary rows some of whose entries are masked by a large negative number, 10^9 to 10^11."""
+    n = 100
+    z, y = inputs("ordinary", V, dtype, 5)
+    z = z.repeat(3, 1)[:n]
+    mask = torch.rand(n, V, generator=gen(6), device=DEV) < 0.4
+    mask[:, V // 2] = False
+    z = torch.where(mask, -torch.logspace(9, 11, n, device=DEV)[:, None].to(dtype), z)
+    y = torch.full((n,), V // 2, device=DEV, dtype=torch.int32)
+    q, want, H = formula(z, y, 1.0)
+    for entropy in (True, False):
+        lp, ent, st = forward(z, y, 1.0, entropy)
+        near(lp, want, 4 * rel(V), 2 * U)
+        if entropy:
+            near(ent, H, 6 * rel(V) * (1 + math.log(V)), 2 * U)
