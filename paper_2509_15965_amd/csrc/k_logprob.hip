@@ -9,7 +9,8 @@
 // cancels (sums carry the R they are relative to; a gradient's factor takes
 // 2^(R rounded - R)).  A row with m c past 2^28, where that rounding is more
 // than 8, or without a sum (logits of the type's lowest value and nothing
-// else) is summed again with the difference before the product.
+// else) is summed again with the difference before the product; a gradient
+// takes it first from 2^24 on.
 #include "rl_device.h"
 #include "rl_internal.h"
 #include "train.h"
@@ -321,8 +322,10 @@ __global__ void __launch_bounds__(64) token_logprobs_join_kernel(const RowPart* 
 struct RowGrad {
     float K, A, B, top;
     float m, l2;
-    bool zero, far;   // far: K is beyond fp32, q = (z - m) c - l2
+    bool zero, far;   // far: K is past kFar, q = (z - m) c - l2
 };
+// Rounding K to fp32 moves it by half a step, 1/2 up to here; past 2^32 the factor that makes up for it would not be finite.
+constexpr double kFar = 16777216.0;
 // ln_s: ln s; lp: log p_y; i: 1 / T
 __device__ __forceinline__ RowGrad row_grad(float g, float ge, float H, float i, float m, double ln_s, double lp, float c) {
     RowGrad k;
@@ -330,7 +333,7 @@ __device__ __forceinline__ RowGrad row_grad(float g, float ge, float H, float i,
     k.K = static_cast<float>(K);
     k.m = m;
     k.l2 = static_cast<float>(l2);
-    k.far = __builtin_amdgcn_readfirstlane(!(fabs(K) < 1e37));
+    k.far = __builtin_amdgcn_readfirstlane(!(fabs(K) < kFar));
     const float off = k.far ? 0.0f : static_cast<float>(static_cast<double>(k.K) - K), f = exp2_hw(off);
     k.B = -ge * 0.69314718f * i;
     k.A = f * (-(g + ge * H) * i + k.B * off);

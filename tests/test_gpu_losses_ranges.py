@@ -1,5 +1,5 @@
-"""Log-probabilities of logits far from ordinary ranges: small temperatures
-and large logits (needs an MI355X).
+"""Log-probabilities, their gradient and the policy loss from logits far from
+ordinary ranges: small temperatures and large logits (needs an MI355X).
 
 Tolerances as in test_gpu_losses.py.  The forms here take the difference to
 the row's largest logit before dividing by the temperature: ln n is lost next
@@ -10,7 +10,8 @@ import math
 import pytest
 import torch
 
-from test_gpu_losses import BF, DEV, F32, U, forward, gen, near, rel
+from paper_2509_15965_amd import rl_decode as R
+from test_gpu_losses import BF, DEV, F32, U, forward, gen, gradient, gradient_tol, near, rel
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +82,49 @@ def test_entries_far_below_a_row(V, dtype):
         near(lp, want, 4 * rel(V), 2 * U)
         if entropy:
             near(ent, H, 6 * rel(V) * (1 + math.log(V)), 2 * U)
+
+
+def check_gradient(dz, q, H, y, g, ge, T, dtype, V, more=0.0):
+    """`more`: what the caller allows g to be off, relative."""
+    err, step = gradient_tol(q, H, g, ge, T, dtype, V)
+    if ge is not None:      # the entropy's own error is in the formula
+        err = err + q.exp() * (ge.double().abs() / T * 6 * rel(V) * (1 + math.log(V)))[:, None]
+    near(dz, gradient(q, H, y, g, ge, T), err + (g.double().abs() / T * 2 * U)[:, None], step + 4 * U + more)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("V", [9, 5000, 70001])
+@pytest.mark.parametrize("kind,T", CASES)
+def test_gradient(kind, T, V, dtype):
+    z, y = inputs(kind, V, dtype, V)
+    n = z.shape[0]
+    q, _, H = formula(z, y, T)
+    _, ent, st = forward(z, y, T)
+    g, ge = torch.randn(n, generator=gen(1), device=DEV), torch.randn(n, generator=gen(2), device=DEV)
+    for e in (ge, None):
+        dz = torch.full_like(z, 9.0)
+        R.token_logprobs_backward(z, y, st, g, dz, entropy=None if e is None else ent, d_entropy=e, temperature=T)
+        assert dz.isfinite().all()
+        check_gradient(dz, q, H, y, g, e, T, dtype, V)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("V", [9, 5000, 70001])      # rows in registers, and (70001) cut over the chip
+@pytest.mark.parametrize("kind,T", CASES)
+def test_policy_loss_from_logits(kind, T, V, dtype):
+    z, _ = inputs(kind, V, dtype, V)
+    n = z.shape[0]
+    y = z.float().argmax(1).int()
+    q, lp, H = formula(z, y, T)
+    old = (lp + 0.3 * torch.randn(n, generator=gen(3), device=DEV)).float()
+    adv = torch.randn(n, generator=gen(4), device=DEV)
+    for coef in (0.0, 0.02):
+        out, olp, ent = torch.empty(8, device=DEV), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+        dz = torch.full_like(z, 9.0)
+        R.policy_loss_logits(z, y, old, adv, out, olp, dz, out_entropy=ent, token_advantages=True, aggregate="sum",
+                             clip_low=0.9, clip_high=20.0, entropy_coef=coef, temperature=T)
+        assert out.isfinite().all() and dz.isfinite().all()
+        near(olp, lp, 4 * rel(V), 2 * U)
+        g = -adv.double() * (lp - old.double()).exp()
+        # the log-probability in the ratio is within 4 rel(V)
+        check_gradient(dz, q, H, y, g, torch.full_like(g, -coef) if coef else None, T, dtype, V, 4 * rel(V))
