@@ -357,7 +357,7 @@ __device__ __forceinline__ PairLoss pair_loss(const PrefArgs& p, const SeqSums* 
         // e = exp(-|h|): ln sigmoid(x) = min(x, 0) - ln(1 + e), and sigmoid(-|h|) = e / (1 + e)
         const double e = exp_below(h < 0.0 ? h : -h), tail = log1p_unit(e), q = 1.0 / (1.0 + e);
         const double lp = (h < 0.0 ? h : 0.0) - tail, ln = (h > 0.0 ? -h : 0.0) - tail;
-        r.loss = -(1.0 - p.smooth) * lp - p.smooth * ln;
+        r.loss = -(1.0 - p.smooth) * lp - (p.smooth != 0.0 ? p.smooth * ln : 0.0);   // ln is -inf at h = inf
         dh = p.smooth - (h < 0.0 ? q : e * q);   // s sigmoid(h) - (1 - s) sigmoid(-h)
     } else if (p.form == 1) {
         r.loss = h >= 1.0 ? 0.0 : 1.0 - h;
