@@ -597,6 +597,7 @@ constexpr int kRowVecs = 20;
 
 template <typename T, int THREADS, int NV>
 int rows(const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz, int64_t ldd, hipStream_t s) {
+    static_assert(kCUs * (1024 / THREADS) <= kPolicyMaxRowParts, "a workgroup's sums need a place in the workspace");
     const auto kernel = a.ent ? policy_rows_kernel<T, THREADS, NV, true> : policy_rows_kernel<T, THREADS, NV, false>;
     const int fit = kCUs * (1024 / THREADS), grid = a.n < fit ? a.n : fit;
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(THREADS), 0, s, p, w.counts, w.cparts, w.n_cparts,

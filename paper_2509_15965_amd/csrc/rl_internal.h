@@ -366,7 +366,7 @@ struct PolicyWs {
     int n_cparts;
     double* parts;
 };
-constexpr int kPolicyMaxRowParts = 1024;   // workgroups of a policy_rows launch
+constexpr int kPolicyMaxRowParts = 1024;   // workgroups of a policy_rows launch at most: their sums' room in the workspace
 PolicyWs policy_ws(const PolicyArgs& p, void* ws);
 size_t policy_ws_bytes(int n, int n_seqs);
 size_t policy_loss_ws_bytes(int n, int n_seqs);   // what launch_policy_loss alone needs
