@@ -67,11 +67,12 @@ __device__ __forceinline__ double expm1_20(double x) {
     return e;
 }
 
-// exp(x) for any x <= 0: x = k ln 2 + r.
+// exp(x) for any x <= 0: x = k ln 2 + r.  ln 2 in two parts: rounded to 40 bits behind the point, so that k times it is
+// exact (k has 11 bits here), and what is left.
 __device__ __forceinline__ double exp_below(double x) {
     const double lim = x < -1100.0 ? -1100.0 : x;
     const double k = rint(lim * 1.4426950408889634);
-    const double r = (lim - k * 0.693147180369123816490) - k * 1.90821492927058770002e-10;   // ln 2 in two parts
+    const double r = (lim - k * (762123384786.0 / 1099511627776.0)) + k * 1.7239444525614835e-13;
     return ldexp(1.0 + expm1_20(r), static_cast<int>(k));
 }
 
