@@ -147,7 +147,7 @@ __device__ __forceinline__ void one_token(const PolicyArgs& p, const TokenIn& in
         g = p.scale * w * t.g;
         ge = -p.scale * w * p.ent_coef;
     }
-    if (d_logp) *nth(d_logp, i) = static_cast<float>(g);
+    *nth(d_logp, i) = static_cast<float>(g);
     if (d_ent) *nth(d_ent, i) = static_cast<float>(ge);
 }
 

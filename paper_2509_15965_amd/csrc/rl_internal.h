@@ -378,7 +378,7 @@ hipError_t launch_policy_final(const PolicyArgs& p, const PolicyWs& w, int n_par
 bool policy_rows_fit(int dt, int n, int V);
 hipError_t launch_policy_rows(int dt, const PolicyArgs& p, const PolicyWs& w, const LogprobArgs& a, void* dz, int64_t ldd,
                               int* n_parts, hipStream_t s);
-// ent, d_logp and d_ent may be null (d_logp: the loss alone)
+// ent and d_ent may be null
 hipError_t launch_policy_loss(const PolicyArgs& p, const float* logp, const float* ent, float* out, float* d_logp,
                               float* d_ent, void* ws, hipStream_t s);
 

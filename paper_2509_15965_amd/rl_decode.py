@@ -170,7 +170,7 @@ def lib():
     L.rl_sample_logits_noalloc.argtypes = [i32, i32, vp, i32, vp, vp, vp, C.POINTER(SampleParams), vp, vp, vp]
     L.rl_probe_gumbel_bound.restype = C.c_int
     L.rl_probe_gumbel_bound.argtypes = [C.c_uint32, C.c_uint64, i32, vp, vp, vp]
-    i64, f32 = C.c_int64, C.c_float
+    i64 = C.c_int64
     L.rl_logprob_workspace_bytes.restype = sz
     L.rl_logprob_workspace_bytes.argtypes = [i32, i32]
     L.rl_token_logprobs.restype = C.c_int
