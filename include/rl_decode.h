@@ -390,7 +390,9 @@ rl_status rl_token_logprobs(int32_t n, int32_t vocab, int32_t dtype, const void*
  *  stats    out_stats of the forward call on the same logits and temperature.
  *  entropy  its out_entropy; needed with d_entropy, else NULL.
  * A row with g = e = 0 is written as zeros, whatever its logits are.  Where
- * the target is outside [0, vocab), g is taken as 0. */
+ * the target is outside [0, vocab), g is taken as 0.  Factors are float: a row
+ * whose (|g| + |e| (1 + H)) / T passes the largest float (g past 1e8 at
+ * T = 1e-30) holds infinities and NaN. */
 rl_status rl_token_logprobs_backward(int32_t n, int32_t vocab, int32_t dtype, const void* logits, int64_t ld,
                                      const int32_t* targets, double temperature, const float* stats,
                                      const float* entropy, const float* d_logp, const float* d_entropy,

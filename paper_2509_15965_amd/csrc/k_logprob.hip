@@ -245,8 +245,8 @@ constexpr int kRowThreads = 256;
 // One workgroup per (row, vocabulary chunk), four vectors a lane in flight;
 // chunks of a row are merged in order by token_logprobs_join_kernel.  One
 // read of the logits and one exponential an entry: bound by memory (8192 x
-// 152064 bf16, 2.5 GB, 366 us, 6.8 TB/s; 1792 x 32000 23 us, 4.9 TB/s), few
-// rows by a row's own latency.
+// 152064 bf16, 2.5 GB, 366 us, 6.8 TB/s; 1792 x 32000 21 us, 24 with nothing
+// of them in the caches, 4.8 TB/s), few rows by a row's own latency.
 template <typename T, int THREADS, bool ENT, bool KEEP>
 __global__ void __launch_bounds__(THREADS) token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int V,
         const int32_t* __restrict__ targets, double inv_T, float c, float bend, int chunk, bool check, PolicyArgs live,
@@ -317,8 +317,8 @@ __global__ void __launch_bounds__(64) token_logprobs_join_kernel(const RowPart* 
 }
 
 // Gradients of a row's entries (the same row in every lane): with q = z c - K, 2^q (A + B q); K = m c + log2 s
-// rounded to fp32, and A and B make up for that.  `top` is the target's own, with 1 - p_y as -(exp(log p_y) - 1):
-// a token that is certain has none.
+// rounded to fp32, and A and B make up for that.  `top` is the target's own, with 1 - p_y as -(exp(log p_y) - 1): a token
+// that is certain has none where its lane's sum is relative to it, else a few 2^-23 of g (its term is 2^t 2^-t then).
 struct RowGrad {
     float K, A, B, top;
     float m, l2;
@@ -418,7 +418,10 @@ __global__ void __launch_bounds__(kRowThreads) token_logprobs_backward_kernel(co
 // this row's gradients leave the registers.  Bound by memory: 8192 x 152064
 // bf16 with a tenth of the tokens masked, 2.24 GB in and 2.49 GB out, 990 us
 // (4.8 TB/s, where a copy of 2 GiB reaches 4.95); 1792 x 32000, 229 MB, 49 us
-// (4.7).  Loads pause while a row is summed.
+// (4.7).  Loads pause while a row is summed.  Of 128 registers a lane, 20
+// vectors leave too few for the rest: by the compiler's report those forms keep
+// 10 (bf16) or 27-28 (fp32) registers in scratch, 28 and 96-100 bytes a lane,
+// those of 16 vectors 2 (bf16, 12 bytes) or 9-10 (fp32, 24-28), others none.
 template <typename T, int THREADS, int NV, bool ENT>
 __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, const int32_t* __restrict__ counts,
         const CountPart* __restrict__ cparts, int n_cparts, const T* logits, int64_t ld, int V,
@@ -523,8 +526,9 @@ __global__ void __launch_bounds__(THREADS, 4) policy_rows_kernel(PolicyArgs p, c
                 store_row(vec_at(d, i * THREADS, at), pack<T>(x));
             }
             __builtin_amdgcn_sched_barrier(0);
-            // Four stores, then four loads: 8192 rows of 152064 bf16 logits in 1006 us, one by one 1019, in twos 1023, in
-            // eights 1013; a whole row of stores first 992, and then 59 us for 1792 rows of 32000 where fours take 56.
+            // Four stores, then four loads.  Compared in one sitting (the merge of a row's parts took 15 us more then: now
+            // 990): 8192 rows of 152064 bf16 logits 1006 us, one by one 1019, in twos 1023, in eights 1013; a whole row of
+            // stores first 992, and then 59 us for 1792 rows of 32000 where fours took 56 (now 50).
             if (next_seq >= 0 && (i % 4 == 3 || i == NV - 1)) {
 #pragma unroll
                 for (int j = i / 4 * 4; j <= i; ++j)
