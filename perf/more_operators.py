@@ -1,0 +1,445 @@
+"""The operators of a rollout in 8 bits: e4m3 codes with one power-of-two scale for each block.
+
+Kinds of case:
+  norm       residual addition and RMS norm of rows, the normed rows in 8 bits
+  quantise   rows (as they are, or SwiGLU's product of a gate and an up half) or a weight matrix in 8 bits
+  gemm       rows in 8 bits times a weight in 8 bits
+  cache      keys and values of new tokens written to a paged 8-bit cache, and read back
+  attention  one query row a sequence over its positions in a paged 8-bit cache
+
+The format.  A code c (e4m3) and its block's scale byte b stand for c 2^(b - 127).  With a the largest finite magnitude of
+the block, 2^(b - 127) is the smallest power of two with a / 2^(b - 127) <= 448, and b at least 1; b is 127 where a is 0.
+Codes are rounded to the nearest, ties to even; what is not finite is NaN.
+Blocks: 128 entries of a row (the last one padded with codes of 0), tiles of 128 x 128 of a weight, one head's entries of one
+position in the cache.
+The cache: a pool of pages; page p, head h is B = 2 P (d + 1) bytes rounded up to a multiple of 256, at (p H + h) B: keys
+[P][d], values [P / 8][d][8], key scales [P], value scales [P].  A table names the pages of each sequence.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+DEV = "cuda"
+DTYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+E4M3, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+EPS = 1e-6
+
+
+def listed():
+    return [
+        # the reference decoder: eight responses, fp32 stream
+        dict(name="norm_tiny", kind="norm", n=8, hidden=256, dtype="fp32", add="fp32", pad=0),
+        # 7B-shaped policy, a micro-batch of prompts: fp32 stream, bf16 branch
+        dict(name="norm_prompts", kind="norm", n=8192, hidden=3584, dtype="fp32", add="bf16", pad=0),
+        # 7B-shaped rollout, the whole batch before the down projection
+        dict(name="swiglu_decode", kind="quantise", form="swiglu", n=512, k=18944, dtype="bf16", pad=0),
+        # 7B-shaped policy after an update: the gate and up projections of a layer
+        dict(name="weights_update", kind="quantise", form="tiles", n=37888, k=3584, dtype="bf16", pad=0),
+        # the last response of a rollout: q, k and v of a 1.5B-shaped policy
+        dict(name="gemm_one", kind="gemm", m=1, n=2048, k=1536, out="bf16"),
+        # the long tail of a 7B-shaped rollout: logits of the responses that are left
+        dict(name="gemm_tail", kind="gemm", m=24, n=152064, k=3584, out="fp32"),
+        # the whole batch of a 7B-shaped rollout: gate and up
+        dict(name="gemm_decode", kind="gemm", m=512, n=37888, k=3584, out="bf16"),
+        # a micro-batch of prompts of a 7B-shaped policy: down
+        dict(name="gemm_prompts", kind="gemm", m=8192, n=3584, k=18944, out="bf16"),
+        # one decode step of a 7B-shaped rollout: a token a sequence
+        dict(name="cache_decode", kind="cache", seqs=512, lo=1, hi=1, start=4096, heads=4, dim=128, page=64, dtype="bf16"),
+        # its prompts
+        dict(name="cache_prompts", kind="cache", seqs=32, lo=256, hi=1024, start=0, heads=4, dim=128, page=64, dtype="bf16"),
+        # the long tail of a 32B-shaped rollout: a few long responses
+        dict(name="attention_tail", kind="attention", seqs=3, median=8000, sigma=0.1, cap=8704, q=40, heads=8, dim=128, page=64, dtype="bf16"),
+        # the middle of a 7B-shaped rollout: the whole batch, prompts and responses of uneven lengths
+        dict(name="attention_decode", kind="attention", seqs=512, median=2000, sigma=0.5, cap=5120, q=28, heads=4, dim=128, page=64, dtype="bf16"),
+    ]
+
+
+def _spread(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["norm", "quantise", "gemm", "gemm", "cache", "attention", "attention"])
+    c = dict(kind=kind)
+    if kind == "norm":
+        h = _spread(rng, 64, 8192)
+        c.update(n=_spread(rng, 1, (8192 * 3584) // h), hidden=h, dtype=rng.choice(["fp32", "bf16"]),
+                 add=rng.choice(["fp32", "bf16", ""]), pad=rng.choice([0, 0, rng.randrange(1, 8)]))
+    elif kind == "quantise":
+        k = _spread(rng, 64, 27648)
+        c.update(form=rng.choice(["rows", "swiglu", "tiles"]), n=_spread(rng, 1, (32768 * 1536) // k), k=k,
+                 dtype=rng.choice(["bf16", "bf16", "fp32"]), pad=rng.choice([0, 0, rng.randrange(1, 8)]))
+    elif kind == "gemm":
+        m, k = _spread(rng, 1, 8192), _spread(rng, 128, 18944)
+        n = _spread(rng, 64, max(64, min(65536, (8192 * 3584 * 18944) // (m * k))))
+        c.update(m=m, n=n, k=k, out=rng.choice(["bf16", "bf16", "fp32"]))
+    else:
+        heads = rng.choice([1, 2, 4, 8, 32])
+        c.update(heads=heads, dim=rng.choice([128, 128, 64]), page=rng.choice([32, 64, 128, 256]),
+                 dtype=rng.choice(["bf16", "bf16", "fp32"]))
+        if kind == "cache":
+            seqs = _spread(rng, 1, 512)
+            hi = _spread(rng, 1, max(1, min(2048, 20000 * 4 // (seqs * heads))))
+            c.update(seqs=seqs, lo=(hi + 3) // 4, hi=hi, start=rng.choice([0, _spread(rng, 1, 4096)]))
+        else:
+            seqs, group = _spread(rng, 1, 512), rng.choice([1, 4, 5, 6, 7, 8, 16])
+            median = _spread(rng, 4, max(4, min(16000, 512 * 2000 * 4 // (seqs * heads * 2))))
+            c.update(seqs=seqs, median=median, sigma=rng.choice([0.0, 0.5]), cap=2 * median, q=heads * group)
+    return c
+
+
+# ---------------------------------------------------------------------------------------------- sizes
+
+
+def _up(a, b):
+    return (a + b - 1) // b * b
+
+
+def _blocks(k):
+    return (k + 127) // 128
+
+
+def _lengths(c):
+    """Tokens of each sequence, from the case alone."""
+    rng = np.random.default_rng([c["seqs"], c.get("hi", c.get("median"))])
+    if c["kind"] == "cache":
+        return rng.integers(c["lo"], c["hi"] + 1, c["seqs"])
+    lens = np.round(np.exp(np.log(c["median"]) + c["sigma"] * rng.standard_normal(c["seqs"])))
+    return np.clip(lens, 1, c["cap"]).astype(np.int64)
+
+
+def _block_bytes(c):
+    return _up(2 * c["page"] * (c["dim"] + 1), 256)
+
+
+# ------------------------------------------------------------------------------------ the plain format
+
+
+def _power(e, dtype=torch.float32):
+    """2^e from its bits (e a whole number within the type's normal range)."""
+    if dtype == torch.float64:
+        return ((e.long() + 1023) << 52).view(torch.float64)
+    return ((e.int() + 127) << 23).view(torch.float32)
+
+
+def _exponent(a):
+    """e of the scale 2^e of blocks with largest finite magnitude a (fp32), elementwise."""
+    m, e = torch.frexp(a)                   # a = m 2^e, m in [1/2, 1)
+    e = e - 9 + (m > 0.875).int()           # 448 = 0.875 2^9
+    return torch.where(a > 0, e.clamp(min=-126), torch.zeros_like(e))
+
+
+def _encode(v, dims):
+    """(codes, exponents) of v in fp32, a block being what lies along `dims`."""
+    fine = torch.isfinite(v)
+    e = _exponent(torch.where(fine, v, 0).abs().amax(dims, keepdim=True))
+    return torch.where(fine, v * _power(-e), math.nan).to(E4M3), e
+
+
+def _scale_bytes(e):
+    return (e + 127).to(torch.uint8)
+
+
+def _rows_blocked(v):
+    """[n][k] as [n][blocks][128], padded with 0."""
+    n, k = v.shape
+    return torch.nn.functional.pad(v, (0, 128 * _blocks(k) - k)).view(n, _blocks(k), 128)
+
+
+def _rows_encode(v):
+    codes, e = _encode(_rows_blocked(v), (2,))
+    return codes.flatten(1), _scale_bytes(e.flatten(1)).view(E8M0)
+
+
+def _tiles_encode(w):
+    n, k = w.shape
+    nb, kb = _blocks(n), _blocks(k)
+    t = torch.nn.functional.pad(w, (0, 128 * kb - k, 0, 128 * nb - n)).view(nb, 128, kb, 128)
+    codes, e = _encode(t, (1, 3))
+    return codes.view(128 * nb, 128 * kb)[:n], _scale_bytes(e.view(nb, kb)).view(E8M0)
+
+
+def _factor(scales, dtype):
+    return _power(scales.view(torch.uint8).to(torch.int32) - 127, dtype)
+
+
+def _places(c, table, seqs, pos):
+    """Byte offsets in the pool of K codes, V codes [n][H][d] and of the scales [n][H]."""
+    P, H, d, B = c["page"], c["heads"], c["dim"], _block_bytes(c)
+    page = table.long()[seqs.long(), pos.long() // P]
+    t = (pos.long() % P)[:, None]
+    at = (page[:, None] * H + torch.arange(H, device=page.device)) * B
+    i = torch.arange(d, device=page.device)
+    k = (at + t * d)[..., None] + i
+    v = (at + P * d + t // 8 * (8 * d) + t % 8)[..., None] + 8 * i
+    return k, v, at + 2 * P * d + t, at + 2 * P * d + P + t
+
+
+# ---------------------------------------------------------------------------------------------- inputs
+
+
+def prepare(case, seed):
+    c = case
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(int(seed))
+    randn = lambda *shape: torch.randn(shape, generator=gen, device=DEV)
+    s = dict(case=c)
+
+    def rows(n, k, dtype, pad, by=1.0):
+        """Activations: some channels far above the others, rows of different sizes; rows `pad` entries apart."""
+        x = torch.empty(n, k + pad, dtype=DTYPES[dtype], device=DEV)
+        ch = torch.exp(0.7 * randn(k)) * by
+        step = max(1, (1 << 27) // max(1, k))
+        for a in range(0, n, step):
+            b = min(n, a + step)
+            x[a:b, :k] = randn(b - a, k) * ch * torch.exp(0.5 * randn(b - a, 1))
+        return x[:, :k]
+
+    if c["kind"] == "norm":
+        n, h = c["n"], c["hidden"]
+        s["x"] = rows(n, h, c["dtype"], c["pad"])
+        s["add"] = rows(n, h, c["add"], c["pad"], 0.3) if c["add"] else None
+        s["weight"] = (1 + 0.2 * randn(h)).to(DTYPES[c["add"] or c["dtype"]])
+        s["sum"] = torch.empty(n, h, dtype=s["x"].dtype, device=DEV) if c["add"] else None
+        s["codes"], s["scales"] = _room(n, h)
+    elif c["kind"] == "quantise":
+        wide = 2 * c["k"] if c["form"] == "swiglu" else c["k"]
+        s["x"] = rows(c["n"], wide, c["dtype"], c["pad"], 0.02 if c["form"] == "tiles" else 1.0)
+        s["codes"], s["scales"] = _room(c["n"], c["k"], 128 if c["form"] == "tiles" else 1)
+    elif c["kind"] == "gemm":
+        a, w = _room(c["m"], c["k"]), _room(c["n"], c["k"], 128)
+        for to, made in ((a, _rows_encode(rows(c["m"], c["k"], "fp32", 0))),
+                         (w, _tiles_encode(randn(c["n"], c["k"]) / math.sqrt(c["k"])))):
+            to[0].view(torch.uint8).copy_(made[0].view(torch.uint8))
+            to[1].view(torch.uint8)[:, : made[1].shape[1]] = made[1].view(torch.uint8)
+        s.update(a=a[0], a_scales=a[1], w=w[0], w_scales=w[1],
+                 out=torch.empty(c["m"], c["n"], dtype=DTYPES[c["out"]], device=DEV))
+    else:
+        lens = _lengths(c)
+        P, H, d = c["page"], c["heads"], c["dim"]
+        need = (lens + c.get("start", 0) + P - 1) // P
+        n_pages = int(need.sum()) + 3
+        perm = torch.randperm(n_pages, generator=gen, device=DEV).int().cpu().numpy()
+        table = np.zeros((c["seqs"], int(need.max())), np.int32)
+        at = 0
+        for i, k in enumerate(need):
+            table[i, :k] = perm[at: at + k]
+            at += int(k)
+        s["table"] = torch.from_numpy(table).to(DEV)
+        s["pool"] = torch.zeros(n_pages * H * _block_bytes(c), dtype=torch.uint8, device=DEV)
+        if c["kind"] == "cache":
+            n = int(lens.sum())
+            s["seqs"] = torch.from_numpy(np.repeat(np.arange(c["seqs"]), lens).astype(np.int32)).to(DEV)
+            s["pos"] = torch.from_numpy(np.concatenate([np.arange(k) + c["start"] for k in lens]).astype(np.int32)).to(DEV)
+            qkv = rows(n, 3 * H * d, c["dtype"], 0)      # K and V as they lie in the projection's output
+            s["k"], s["v"] = qkv[:, H * d: 2 * H * d].unflatten(1, (H, d)), qkv[:, 2 * H * d:].unflatten(1, (H, d))
+            s["out_k"], s["out_v"] = (torch.empty(n, H, d, dtype=qkv.dtype, device=DEV) for _ in range(2))
+        else:
+            # codes of normal entries under scales that differ from position to position
+            blocks = s["pool"].view(-1, _block_bytes(c))
+            for a in range(0, blocks.shape[0], 4096):
+                b = blocks[a: a + 4096]
+                codes = (100 * randn(b.shape[0], 2 * P * d)).clamp_(-448, 448)
+                b[:, : 2 * P * d] = codes.to(E4M3).view(torch.uint8)
+                b[:, 2 * P * d: 2 * P * (d + 1)] = (120 + randn(b.shape[0], 2 * P)).round().to(torch.uint8)
+            s["q"] = randn(c["seqs"], c["q"], d).to(DTYPES[c["dtype"]])
+            s["lengths"] = torch.from_numpy(lens.astype(np.int32)).to(DEV)
+            s["longest"] = int(lens.max())
+            s["out"] = torch.empty_like(s["q"])
+    return s
+
+
+def _room(n, k, block_rows=1):
+    """Room for [n][k] in 8 bits: whole blocks of codes, rows of scale bytes a multiple of four apart."""
+    nb = -(-n // block_rows)
+    codes = torch.zeros(n, 128 * _blocks(k), dtype=torch.uint8, device=DEV).view(E4M3)
+    return codes, torch.zeros(nb, _up(_blocks(k), 4), dtype=torch.uint8, device=DEV).view(E8M0)
+
+
+# ----------------------------------------------------------------------------------------------- a pass
+
+
+def run(state):
+    return _own(state) if own else _plain(state)
+
+
+def _own(s):
+    from paper_2509_15965_amd import rl_decode as rl
+    c = s["case"]
+    if c["kind"] == "norm":
+        rl.rmsnorm_fp8(s["x"], s["weight"], s["codes"], s["scales"], add=s["add"], out_sum=s["sum"], eps=EPS)
+        out = [s["codes"], s["scales"][:, : _blocks(c["hidden"])]]
+        return out + [s["sum"]] if c["add"] else out
+    if c["kind"] == "quantise":
+        rl.quantise_fp8(s["x"], s["codes"], s["scales"], form=c["form"])
+        return [s["codes"], s["scales"][:, : _blocks(c["k"])]]
+    if c["kind"] == "gemm":
+        rl.gemm_fp8(s["a"], s["a_scales"], s["w"], s["w_scales"], s["out"])
+        return s["out"]
+    if c["kind"] == "cache":
+        rl.kv_fp8_append(s["pool"], s["table"], s["seqs"], s["pos"], s["k"], s["v"], page_size=c["page"])
+        rl.kv_fp8_read(s["pool"], s["table"], s["seqs"], s["pos"], s["out_k"], s["out_v"], page_size=c["page"])
+        return [s["out_k"], s["out_v"]]
+    rl.attention_fp8(s["pool"], s["table"], s["q"], s["lengths"], s["out"], page_size=c["page"], n_kv_heads=c["heads"],
+                     max_length=s["longest"], scale=c["dim"] ** -0.5)
+    return s["out"]
+
+
+def _plain(s):
+    c = s["case"]
+    if c["kind"] == "norm":
+        x, out = s["x"].float(), []
+        if c["add"]:
+            total = (x + s["add"].float()).to(s["x"].dtype)
+            x, out = total.float(), [total]
+        y = x * torch.rsqrt((x * x).mean(1, keepdim=True) + EPS) * s["weight"].float()
+        return list(_rows_encode(y)) + out
+    if c["kind"] == "quantise":
+        x = s["x"].float()
+        if c["form"] == "tiles":
+            return list(_tiles_encode(x))
+        if c["form"] == "swiglu":
+            g, u = x[:, : c["k"]], x[:, c["k"]:]
+            x = g / (1 + torch.exp(-g)) * u
+        return list(_rows_encode(x))
+    if c["kind"] == "gemm":
+        a, w = _matrices(s, torch.float32)
+        return (a @ w.t()).to(s["out"].dtype)
+    if c["kind"] == "cache":
+        k, v, ks, vs = _places(c, s["table"], s["seqs"], s["pos"])
+        pool, out = s["pool"], []
+        for x, at, sat in ((s["k"], k, ks), (s["v"], v, vs)):
+            codes, e = _encode(x.float(), (2,))
+            pool[at] = codes.view(torch.uint8)
+            pool[sat] = _scale_bytes(e[..., 0])
+        for x, at, sat in ((s["k"], k, ks), (s["v"], v, vs)):
+            out.append((pool[at].view(E4M3).float() * _factor(pool[sat], torch.float32)[..., None]).to(x.dtype))
+        return out
+    return _attend(s, torch.float32).to(s["q"].dtype)
+
+
+def _matrices(s, dtype):
+    """A and W as the numbers that they stand for."""
+    c = s["case"]
+    kb = _blocks(c["k"])
+    a = s["a"].to(dtype).view(c["m"], kb, 128) * _factor(s["a_scales"][:, :kb], dtype)[:, :, None]
+    f = _factor(s["w_scales"][:, :kb], dtype).repeat_interleave(128, 0)[: c["n"]]
+    w = s["w"].to(dtype).view(c["n"], kb, 128) * f[:, :, None]
+    return a.flatten(1), w.flatten(1)
+
+
+def _attend(s, dtype):
+    """Softmax attention of every row over its sequence's positions, padded to the longest."""
+    c = s["case"]
+    P, H, d, B, n = c["page"], c["heads"], c["dim"], _block_bytes(c), c["seqs"]
+    T = s["table"].shape[1] * P
+    blocks = s["pool"].view(-1, H, B)[s["table"].long()]            # [n][pages][H][B]
+    by_head = lambda t: t.transpose(1, 2).reshape(n, H, T, -1)      # [n][pages][H][P][.] -> [n][H][T][.]
+    k = by_head(blocks[..., : P * d].view(E4M3).to(dtype).unflatten(3, (P, d)))
+    k = k * by_head(_factor(blocks[..., 2 * P * d: 2 * P * d + P], dtype)[..., None])
+    q = s["q"].to(dtype).view(n, H, -1, d)
+    x = torch.matmul(q, k.transpose(2, 3).contiguous()) * d ** -0.5
+    del k
+    far = torch.arange(T, device=x.device) >= s["lengths"].long()[:, None, None, None]
+    x = x.masked_fill(far, -math.inf)
+    p = torch.exp(x - x.amax(3, keepdim=True))
+    v = blocks[..., P * d: 2 * P * d].view(E4M3).to(dtype).unflatten(3, (P // 8, d, 8)).transpose(4, 5).flatten(3, 4)
+    v = by_head(v) * by_head(_factor(blocks[..., 2 * P * d + P: 2 * P * (d + 1)], dtype)[..., None])
+    return (torch.matmul(p, v) / p.sum(3, keepdim=True)).reshape(n, c["q"], d)
+
+
+# ------------------------------------------------------------------------------------------------- work
+
+
+def work(case):
+    c = case
+    size = lambda t: 4 if t == "fp32" else 2
+    if c["kind"] == "norm":
+        n, h = c["n"], c["hidden"]
+        moved = n * h * (size(c["dtype"]) * (2 if c["add"] else 1) + (size(c["add"]) if c["add"] else 0) + 1)
+        return {"bytes": moved + n * _blocks(h) + h * size(c["add"] or c["dtype"]), "flops": 6 * n * h}
+    if c["kind"] == "quantise":
+        n, k = c["n"], c["k"]
+        rows = _blocks(n) if c["form"] == "tiles" else n
+        wide = 2 if c["form"] == "swiglu" else 1
+        return {"bytes": n * k * (wide * size(c["dtype"]) + 1) + rows * _blocks(k), "flops": 4 * wide * n * k}
+    if c["kind"] == "gemm":
+        m, n, k = c["m"], c["n"], c["k"]
+        return {"bytes": (m + n) * k + (m + _blocks(n)) * _blocks(k) + m * n * size(c["out"]), "flops": 2 * m * n * k}
+    tokens = int(_lengths(c).sum())
+    if c["kind"] == "cache":   # written from given numbers, read back to numbers
+        return {"bytes": tokens * c["heads"] * (2 * c["dim"] * (2 * size(c["dtype"]) + 2) + 4), "flops": 8 * tokens * c["heads"] * c["dim"]}
+    moved = tokens * c["heads"] * 2 * (c["dim"] + 1) + 2 * c["seqs"] * c["q"] * c["dim"] * size(c["dtype"])
+    return {"bytes": moved, "flops": 4 * tokens * c["q"] * c["dim"]}
+
+
+# ------------------------------------------------------------------------------------------ in 64 bits
+
+
+def _e4m3_64(x):
+    """Nearest e4m3 numbers (ties to even) of |x| <= 448 in fp64: three bits behind the leading one, steps of 2^-9 below 2^-6."""
+    _, e = torch.frexp(x)
+    step = _power((e - 1).clamp(min=-6) - 3, torch.float64)
+    return torch.round(x / step) * step
+
+
+def _encode_64(v, dims):
+    """(codes, scales) in fp64: the scale by comparison with 448 times the powers of two around it."""
+    a = v.abs().amax(dims, keepdim=True)
+    e = torch.ceil(torch.log2(torch.where(a > 0, a, 448.0) / 448)).int()
+    for _ in range(2):   # log2 may be off next to a power
+        e = torch.where(448 * _power(e, torch.float64) < a, e + 1, e)
+        e = torch.where(448 * _power(e - 1, torch.float64) >= a, e - 1, e)
+    e = torch.where(a > 0, e.clamp(min=-126), torch.zeros_like(e))
+    return _e4m3_64(v * _power(-e, torch.float64)), _power(e, torch.float64)
+
+
+def exact(case, seed):
+    c = case
+    s = prepare(case, seed)
+    if c["kind"] in ("norm", "quantise"):
+        x, out = s["x"].double(), []
+        if c["kind"] == "norm":
+            if c["add"]:
+                out = [x + s["add"].double()]
+                x = (s["x"].float() + s["add"].float()).to(s["x"].dtype).double()   # the norm is of the sum as it is stored
+            y = x / torch.sqrt(x.square().mean(1, keepdim=True) + EPS) * s["weight"].double()
+        elif c["form"] == "swiglu":
+            y = x[:, : c["k"]] * torch.sigmoid(x[:, : c["k"]]) * x[:, c["k"]:]
+        else:
+            y = x
+        n, k = y.shape
+        if c.get("form") == "tiles":
+            nb, kb = _blocks(n), _blocks(k)
+            t = torch.nn.functional.pad(y, (0, 128 * kb - k, 0, 128 * nb - n)).view(nb, 128, kb, 128)
+            codes, scales = _encode_64(t, (1, 3))
+            return [codes.view(128 * nb, 128 * kb)[:n], scales.view(nb, kb)]
+        codes, scales = _encode_64(_rows_blocked(y), (2,))
+        return [codes.flatten(1), scales.flatten(1)] + out
+    if c["kind"] == "gemm":
+        a, w = _matrices(s, torch.float64)
+        return a @ w.t()
+    if c["kind"] == "cache":
+        out = []
+        for x in (s["k"], s["v"]):
+            codes, scales = _encode_64(x.double(), (2,))
+            out.append(codes * scales)
+        return out
+    return _exact_attention(s)
+
+
+def _exact_attention(s):
+    """Position by position of the definition, a sequence at a time."""
+    c = s["case"]
+    P, H, d = c["page"], c["heads"], c["dim"]
+    out = torch.empty(c["seqs"], c["q"], d, dtype=torch.float64, device=DEV)
+    for i, n in enumerate(s["lengths"].tolist()):
+        pos = torch.arange(n, device=DEV)
+        k, v, ks, vs = _places(c, s["table"], torch.full_like(pos, i), pos)
+        number = lambda at, sat: (s["pool"][at].view(E4M3).double() * _factor(s["pool"][sat], torch.float64)[..., None])
+        kk, vv = number(k, ks).transpose(0, 1), number(v, vs).transpose(0, 1)     # [H][n][d]
+        x = torch.matmul(s["q"][i].double().view(H, -1, d), kk.transpose(1, 2).contiguous()) / math.sqrt(d)
+        out[i] = torch.matmul(torch.softmax(x, 2), vv.contiguous()).reshape(c["q"], d)
+    return out
