@@ -269,20 +269,20 @@ def _own(s):
     from paper_2509_15965_amd import rl_decode as rl
     c = s["case"]
     if c["kind"] == "norm":
-        rl.rmsnorm_fp8(s["x"], s["weight"], s["codes"], s["scales"], add=s["add"], out_sum=s["sum"], eps=EPS)
+        rl.rmsnorm_quant(s["x"], s["weight"], s["codes"], s["scales"], add=s["add"], out_sum=s["sum"], eps=EPS)
         out = [s["codes"], s["scales"][:, : _blocks(c["hidden"])]]
         return out + [s["sum"]] if c["add"] else out
     if c["kind"] == "quantise":
-        rl.quantise_fp8(s["x"], s["codes"], s["scales"], form=c["form"])
+        rl.quantise(s["x"], s["codes"], s["scales"], form=c["form"])
         return [s["codes"], s["scales"][:, : _blocks(c["k"])]]
     if c["kind"] == "gemm":
-        rl.gemm_fp8(s["a"], s["a_scales"], s["w"], s["w_scales"], s["out"])
+        rl.gemm_quant(s["a"], s["a_scales"], s["w"], s["w_scales"], s["out"])
         return s["out"]
     if c["kind"] == "cache":
-        rl.kv_fp8_append(s["pool"], s["table"], s["seqs"], s["pos"], s["k"], s["v"], page_size=c["page"])
-        rl.kv_fp8_read(s["pool"], s["table"], s["seqs"], s["pos"], s["out_k"], s["out_v"], page_size=c["page"])
+        rl.kv_quant_append(s["pool"], s["table"], s["seqs"], s["pos"], s["k"], s["v"], page_size=c["page"])
+        rl.kv_quant_read(s["pool"], s["table"], s["seqs"], s["pos"], s["out_k"], s["out_v"], page_size=c["page"])
         return [s["out_k"], s["out_v"]]
-    rl.attention_fp8(s["pool"], s["table"], s["q"], s["lengths"], s["out"], page_size=c["page"], n_kv_heads=c["heads"],
+    rl.attention_quant(s["pool"], s["table"], s["q"], s["lengths"], s["out"], page_size=c["page"], n_kv_heads=c["heads"],
                      max_length=s["longest"], scale=c["dim"] ** -0.5)
     return s["out"]
 
