@@ -517,6 +517,140 @@ rl_status rl_preference_loss(int32_t n, int32_t n_pairs, const int32_t* seq_offs
                              void* stream);
 
 /* ---------------------------------------------------------------------
+ * Rollout in 8 bits.  Generation is bound by bytes (Sec. 2.1: by bandwidth; Sec. 5.1.1: by how much K/V fits), so
+ * these calls keep weights, the rows that meet them and the K/V cache in one
+ * byte an entry: e4m3 codes (OCP: largest 448, no infinity) under
+ * power-of-two scales, one for each block of entries.  A policy's weights
+ * change with every iteration and are quantised here, from the trained ones.
+ *
+ * Format.  Code c under scale byte b (1 .. 254) stands for c 2^(b - 127).  The
+ * calls that write codes choose, for a block whose largest finite magnitude
+ * is a, the smallest b >= 1 with a <= 448 * 2^(b - 127), and b = 127 for a = 0;
+ * codes are rounded to nearest, ties to even; NaN and infinities become NaN.
+ *
+ * They need no context: they run on `stream` of the current device, allocate
+ * nothing, keep nothing from one call for the next and can be captured into
+ * a HIP graph.  Scratch memory is the caller's workspace (device, 256-byte
+ * aligned, contents arbitrary, at least the bytes that the matching function
+ * returns; NULL is accepted where that is 0); calls that may overlap in time
+ * need workspaces of their own.  Outputs may not overlap inputs or each
+ * other, but where said.  Results do not depend on timing.  Rows of numbers
+ * ([n][ld] of an rl_dtype) need the element's alignment only; rows that start
+ * on 16 bytes are the fastest.
+ * ------------------------------------------------------------------- */
+
+/* A matrix [rows][k] in 8 bits.  A row has ceil(k / 128) blocks of 128 codes;
+ * entries past k are codes of 0 (the calls that write a matrix write them,
+ * a product reads them).  One scale for each block of a row, or for each tile
+ * of 128 rows x 128 entries (a weight).
+ *  codes      [rows][ld], 16-byte aligned; ld a multiple of 16, at least
+ *             128 * ceil(k / 128), at most 2^20.
+ *  scales     [rows, or ceil(rows / 128) of a weight][ld_scales], 4-byte
+ *             aligned; ld_scales a multiple of 4, at least ceil(k / 128).  A
+ *             product reads whole words: bytes past the last block of a row
+ *             have to be there and may hold anything. */
+typedef struct rl_fp8_matrix {
+    uint8_t* codes;
+    int64_t  ld;
+    uint8_t* scales;
+    int64_t  ld_scales;
+} rl_fp8_matrix;
+
+/* Residual addition and RMS norm of rows, the result in 8 bits:
+ *   s = x + add (rounded to dtype; x where add is NULL), out_sum = s
+ *   out = s w / sqrt(mean_i s_i^2 + eps), a scale for each block of a row
+ *  n <= 2^20 rows of hidden <= 32768 entries; x [n][ldx] of dtype; add
+ *  [n][ld_add] of add_dtype, or NULL; weight [hidden] of w_dtype; out_sum
+ *  [n][ld_sum] of dtype, or NULL; it may be x (same ld), or add (same ld and
+ *  dtype).  eps in (0, 1].  The norm is of s as it is stored. */
+rl_status rl_rmsnorm_quant(int32_t n, int32_t hidden, int32_t dtype, const void* x, int64_t ldx, int32_t add_dtype, const void* add,
+                         int64_t ld_add, int32_t w_dtype, const void* weight, double eps, void* out_sum, int64_t ld_sum,
+                         const rl_fp8_matrix* out, void* stream);
+
+typedef enum rl_fp8_form {
+    RL_FP8_ROWS = 0,             /* rows of k entries, a scale for each block of a row            */
+    RL_FP8_SWIGLU = 1,           /* silu(g) u of rows of 2 k entries, g the first half, u the second */
+    RL_FP8_TILES = 2             /* a weight: a scale for each tile of 128 rows x 128 entries      */
+} rl_fp8_form;
+
+/* [n][ldx] numbers of dtype in 8 bits.  n <= 2^20, k <= 131072. */
+rl_status rl_quantise(int32_t form, int32_t n, int32_t k, int32_t dtype, const void* x, int64_t ldx, const rl_fp8_matrix* out,
+                          void* stream);
+
+/* Bytes of workspace for rl_gemm_quant (0 for invalid sizes, and where none is
+ * needed: most sizes). */
+size_t rl_gemm_quant_workspace_bytes(int32_t m, int32_t n, int32_t k);
+
+/* out = a w^T: [m][ldo] of out_dtype, rounded once from fp32 sums.
+ *  a  [m][k] with a scale for each block of a row (rl_rmsnorm_quant, RL_FP8_ROWS, RL_FP8_SWIGLU).
+ *  w  [n][k] with a scale for each tile (RL_FP8_TILES).
+ *  m, n <= 2^20, k <= 131072. */
+rl_status rl_gemm_quant(int32_t m, int32_t n, int32_t k, const rl_fp8_matrix* a, const rl_fp8_matrix* w, int32_t out_dtype, void* out,
+                      int64_t ldo, void* workspace, size_t ws_bytes, void* stream);
+
+/* A paged K/V cache of one layer in 8 bits, one scale for a head's entries of
+ * one position.  Page p, kv-head h (P = page_size, d = head_dim) is the
+ * B = 2 P (d + 1) bytes, rounded up to a multiple of 256, at (p * n_kv_heads + h) * B:
+ *   K codes   [P][d]                      V codes   [P / 8][d][8] at P d
+ *   K scales  [P] at 2 P d                V scales  [P] at 2 P d + P
+ * Position t of sequence s is position t % P of page
+ * page_table[s * max_pages + t / P].  An id outside [0, n_pages) is no page.
+ *  pool        device, 256-byte aligned, rl_kv_quant_bytes bytes.
+ *  page_table  device int32 [n_seqs][max_pages]; read by the calls' kernels.
+ *  page_size a multiple of 32 in [32, 65536], head_dim 64 or 128,
+ *  n_kv_heads <= 1024, n_seqs <= 2^20, max_pages * page_size < 2^31. */
+typedef struct rl_kv_fp8 {
+    void* pool;
+    const int32_t* page_table;
+    int32_t n_seqs;
+    int32_t max_pages;
+    int32_t n_pages;
+    int32_t page_size;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+} rl_kv_fp8;
+
+/* Bytes of a pool (0 for sizes that are not supported). */
+size_t rl_kv_quant_bytes(int32_t n_pages, int32_t page_size, int32_t n_kv_heads, int32_t head_dim);
+
+/* Write n tokens' keys and values (after RoPE) in 8 bits.  n <= 2^24.
+ *  seqs, positions  device int32 [n]: token i is position positions[i] of
+ *                   sequence seqs[i]; one that has no place (sequence or
+ *                   position out of range, no page) is left out.  No two
+ *                   tokens of a call may have the same place.
+ *  k, v             [n][ld] of dtype, a token's heads one after the other. */
+rl_status rl_kv_quant_append(const rl_kv_fp8* cache, int32_t n, const int32_t* seqs, const int32_t* positions, int32_t dtype,
+                           const void* k, int64_t ldk, const void* v, int64_t ldv, void* stream);
+
+/* Read n tokens' keys and values back as numbers (exact in either dtype);
+ * zeros for a token that has no place.  The same place may be read twice. */
+rl_status rl_kv_quant_read(const rl_kv_fp8* cache, int32_t n, const int32_t* seqs, const int32_t* positions, int32_t dtype,
+                         void* out_k, int64_t ldk, void* out_v, int64_t ldv, void* stream);
+
+/* Bytes of workspace for rl_attention_quant (0 for invalid sizes, and where
+ * none is needed). */
+size_t rl_attention_quant_workspace_bytes(int32_t n, int32_t n_kv_heads, int32_t n_q_heads, int32_t head_dim, int32_t max_length);
+
+/* Attention of n query tokens over the cache: row i's heads attend over
+ * positions 0 .. lengths[i] - 1 of its sequence,
+ *   out = softmax(scale q K^T) V
+ * q-head j uses kv-head j / (n_q_heads / n_kv_heads); at most 16 q-heads a kv-head.
+ *  seqs        device int32 [n], or NULL: row i is sequence i.  Several rows
+ *              may be of one sequence (drafted or prompt tokens, each with
+ *              the length it sees).
+ *  lengths     device int32 [n]; positions of pages that are not there are
+ *              left out.  A row that attends to nothing (length 0 or less, a
+ *              sequence out of range) is zeros.  What the cache holds behind
+ *              a row's length does not matter.
+ *  max_length  no row is longer: a longer one is taken as this long.  The
+ *              work is laid out by it, so a near bound is the fastest.
+ *  q, out      [n][ld] of dtype, a token's heads one after the other.  The
+ *              weights of the values keep 16 bits for bf16 and 24 for fp32. */
+rl_status rl_attention_quant(const rl_kv_fp8* cache, int32_t n, const int32_t* seqs, const int32_t* lengths, int32_t max_length,
+                           int32_t dtype, const void* q, int64_t ldq, int32_t n_q_heads, double scale, void* out, int64_t ldo,
+                           void* workspace, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------
  * Slot bookkeeping (host only; nothing is enqueued).
  * ------------------------------------------------------------------- */
 

@@ -18,7 +18,8 @@ OUT = os.path.join(PKG, "librl_decode.so")
 OBJ_DIR = os.path.join(PKG, "_build")
 
 SOURCES = ["engine.cpp", "k_elementwise.hip", "k_gemm.hip", "k_gemm_lds.hip", "k_attention.hip", "k_sample.hip",
-           "k_moe.hip", "train.cpp", "k_logprob.hip", "k_loss.hip"]
+           "k_moe.hip", "train.cpp", "k_logprob.hip", "k_loss.hip",
+           "fp8.cpp", "k_fp8.hip", "k_fp8_gemm.hip", "k_fp8_attention.hip"]
 ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-I", INCLUDE, "-I", CSRC,
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

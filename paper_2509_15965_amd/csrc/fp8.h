@@ -1,0 +1,173 @@
+// fp8.h -- what the 8-bit operators share: e4m3 codes under power-of-two block
+// scales, wide loads of either element type, the arguments of their launches.
+#pragma once
+
+#include "rl_device.h"
+
+namespace rl {
+
+constexpr int kFp8Block = 128;   // entries of a row under one scale
+__host__ __device__ constexpr int fp8_blocks(int k) { return (k + kFp8Block - 1) / kFp8Block; }
+
+// [rows][ld] codes and [rows or rows / 128][lds] scale bytes
+struct Fp8Out { uint8_t* codes; int64_t ld; uint8_t* scales; int64_t lds; };
+struct Fp8In { const uint8_t* codes; int64_t ld; const uint8_t* scales; int64_t lds; };
+
+struct NormArgs {
+    int n, hidden;
+    const void* x; int64_t ldx; int x_dt;
+    const void* add; int64_t ld_add; int add_dt;   // or null
+    const void* w; int w_dt;
+    float eps;
+    void* sum; int64_t ld_sum;                     // x_dt; or null
+    Fp8Out out;
+};
+hipError_t launch_rmsnorm_fp8(const NormArgs& a, hipStream_t s);
+
+// form: 0 rows, 1 SwiGLU of the row's two halves of k entries, 2 tiles of 128 x 128
+hipError_t launch_quantise_fp8(int form, int n, int k, int dt, const void* x, int64_t ldx, const Fp8Out& out, hipStream_t s);
+
+struct Fp8Gemm {
+    int m, n, kb;                  // kb blocks of 128 codes
+    Fp8In a, w;
+    void* out; int64_t ldo; int out_dt;
+    float* part;                   // fp32 sums of the K slices, [slice][m][n]
+};
+size_t gemm_fp8_ws_bytes(int m, int n, int kb);
+hipError_t launch_gemm_fp8(const Fp8Gemm& g, hipStream_t s);
+
+// The cache: page p, kv-head h is `block` bytes at (p * heads + h) * block.
+struct KvFp8 {
+    uint8_t* pool;
+    const int32_t* table;          // [n_seqs][max_pages]
+    int n_seqs, max_pages, n_pages, page, heads, dim;
+    int64_t block;
+};
+struct KvTokens {
+    int n;
+    const int32_t *seqs, *pos;
+    const void *k, *v; int64_t ldk, ldv;       // append
+    void *out_k, *out_v; int64_t ld_ok, ld_ov; // read
+    int dt;
+};
+hipError_t launch_kv_fp8_append(const KvFp8& c, const KvTokens& t, hipStream_t s);
+hipError_t launch_kv_fp8_read(const KvFp8& c, const KvTokens& t, hipStream_t s);
+
+struct AttnFp8 {
+    KvFp8 c;
+    int n, max_length;
+    const int32_t *seqs, *lengths;             // seqs null: row i is sequence i
+    const void* q; int64_t ldq;
+    void* out; int64_t ldo;
+    int dt, heads;                             // query heads
+    float scale;
+    float* part;
+};
+bool attention_fp8_fits(int n, int kv_heads, int max_length);   // its workgroups can be counted in 31 bits
+size_t attention_fp8_ws_bytes(int n, int kv_heads, int dim, int max_length);
+hipError_t launch_attention_fp8(const AttnFp8& a, hipStream_t s);
+
+inline __host__ bool rows_on_16(const void* p, int64_t ld, size_t es) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * es) % 16 == 0;
+}
+
+
+// Scale byte b of a block whose largest finite magnitude is a: 2^(b - 127) is the
+// smallest power of two with a / 2^(b - 127) <= 448 = 1.75 x 2^8, and b >= 1 so
+// that it and its reciprocal are normal fp32 numbers; 127 for a = 0.  From the
+// bits of a: exponent - 8, one more where the significand is above 1.75.
+__device__ __forceinline__ int fp8_scale_byte(float a) {
+    const uint32_t u = __float_as_uint(a);
+    const int b = static_cast<int>(u >> 23) - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return u == 0u ? 127 : b < 1 ? 1 : b;
+}
+__device__ __forceinline__ float fp8_scale(int b) { return __uint_as_float(static_cast<uint32_t>(b) << 23); }
+__device__ __forceinline__ float fp8_inverse(int b) { return __uint_as_float(static_cast<uint32_t>(254 - b) << 23); }
+
+// |v|, or 0 where v is not finite: what a block's scale goes by
+__device__ __forceinline__ float finite_abs(float v) {
+    const float a = fabsf(v);
+    return a <= 3.402823466e38f ? a : 0.0f;
+}
+// v to be rounded to a code: infinities are NaN in this format
+__device__ __forceinline__ float fp8_arg(float v, float inv) {
+    const float t = v * inv;
+    return fabsf(t) <= 448.0f ? t : __uint_as_float(0x7FC00000u);
+}
+// four codes of four numbers, the first in the lowest byte (round to nearest even)
+__device__ __forceinline__ uint32_t fp8_pack4(const float* v, float inv) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(fp8_arg(v[0], inv), fp8_arg(v[1], inv), 0, false);
+    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(fp8_arg(v[2], inv), fp8_arg(v[3], inv), w, true));
+}
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+// eight codes as bf16 numbers, times the scale
+__device__ __forceinline__ bf16x8 codes_bf16(uint32_t lo, uint32_t hi, float scale) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Eight entries of a row, of which `left` are there (the others are 0); vec:
+// the row starts on 16 bytes.
+template <typename T> __device__ __forceinline__ void load8(const T* p, bool vec, int left, float* v) {
+    if (vec && left >= 8) {
+        if constexpr (sizeof(T) == 4) {
+            const u32x4 a = ld16(p), b = ld16(p + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = __uint_as_float(a[e]);
+                v[4 + e] = __uint_as_float(b[e]);
+            }
+        } else {
+            const u32x4 a = ld16(p);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[2 * e] = __uint_as_float(a[e] << 16);
+                v[2 * e + 1] = __uint_as_float(a[e] & 0xFFFF0000u);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < left ? Elem<T>::load(p, e) : 0.0f;
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, bool vec, int left, const float* v) {
+    if (vec && left >= 8) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        } else {
+            u32x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                w[e] = f32_to_bf16(v[2 * e]) | static_cast<uint32_t>(f32_to_bf16(v[2 * e + 1])) << 16;
+            *reinterpret_cast<u32x4*>(p) = w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < left) Elem<T>::store(p, e, v[e]);
+}
+
+template <int LANES> __device__ __forceinline__ float lanes_max(float v) {
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
+}
+
+// The eight numbers of a lane, LANES lanes a block, as codes; the block's scale byte.
+template <int LANES> __device__ __forceinline__ int fp8_encode8(const float* v, uint2* codes) {
+    float a = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a = fmaxf(a, finite_abs(v[e]));
+    const int b = fp8_scale_byte(lanes_max<LANES>(a));
+    const float inv = fp8_inverse(b);
+    *codes = make_uint2(fp8_pack4(v, inv), fp8_pack4(v + 4, inv));
+    return b;
+}
+
+}  // namespace rl

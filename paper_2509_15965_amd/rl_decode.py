@@ -40,6 +40,8 @@ EXPORTS = ("rl_decode_kv_bytes", "rl_decode_workspace_bytes", "rl_decode_create"
            "rl_sample_logits_noalloc", "rl_logprob_workspace_bytes", "rl_token_logprobs",
            "rl_token_logprobs_backward", "rl_policy_workspace_bytes", "rl_policy_logits_workspace_bytes",
            "rl_policy_loss", "rl_policy_loss_logits", "rl_preference_workspace_bytes", "rl_preference_loss",
+           "rl_rmsnorm_quant", "rl_quantise", "rl_gemm_quant_workspace_bytes", "rl_gemm_quant", "rl_kv_quant_bytes",
+           "rl_kv_quant_append", "rl_kv_quant_read", "rl_attention_quant_workspace_bytes", "rl_attention_quant",
            "rl_decode_tune_gemms", "rl_decode_gemm_plan", "rl_status_string",
            "rl_decode_last_error")
 
@@ -99,6 +101,16 @@ class PreferenceParams(C.Structure):
                 ("form", C.c_int32), ("average", C.c_int32)]
 
 
+class Fp8Matrix(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("ld", C.c_int64), ("scales", C.c_void_p), ("ld_scales", C.c_int64)]
+
+
+class KvFp8(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("page_table", C.c_void_p), ("n_seqs", C.c_int32), ("max_pages", C.c_int32),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+FP8_FORMS = {"rows": 0, "swiglu": 1, "tiles": 2}
 KL_KINDS = {"k1": 1, "k2": 2, "k3": 3}
 AGGREGATES = {"token_mean": 0, "sequence_mean": 1, "sum": 2}
 PREFERENCE_FORMS = {"sigmoid": 0, "hinge": 1, "squared": 2}
@@ -190,6 +202,24 @@ def lib():
     L.rl_preference_workspace_bytes.argtypes = [i32, i32]
     L.rl_preference_loss.restype = C.c_int
     L.rl_preference_loss.argtypes = [i32, i32, vp, vp, vp, vp, C.POINTER(PreferenceParams), vp, vp, vp, vp, sz, vp]
+    mp, kp, f64 = C.POINTER(Fp8Matrix), C.POINTER(KvFp8), C.c_double
+    L.rl_rmsnorm_quant.restype = C.c_int
+    L.rl_rmsnorm_quant.argtypes = [i32, i32, i32, vp, i64, i32, vp, i64, i32, vp, f64, vp, i64, mp, vp]
+    L.rl_quantise.restype = C.c_int
+    L.rl_quantise.argtypes = [i32, i32, i32, i32, vp, i64, mp, vp]
+    L.rl_gemm_quant_workspace_bytes.restype = sz
+    L.rl_gemm_quant_workspace_bytes.argtypes = [i32, i32, i32]
+    L.rl_gemm_quant.restype = C.c_int
+    L.rl_gemm_quant.argtypes = [i32, i32, i32, mp, mp, i32, vp, i64, vp, sz, vp]
+    L.rl_kv_quant_bytes.restype = sz
+    L.rl_kv_quant_bytes.argtypes = [i32, i32, i32, i32]
+    for f in (L.rl_kv_quant_append, L.rl_kv_quant_read):
+        f.restype = C.c_int
+        f.argtypes = [kp, i32, vp, vp, i32, vp, i64, vp, i64, vp]
+    L.rl_attention_quant_workspace_bytes.restype = sz
+    L.rl_attention_quant_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+    L.rl_attention_quant.restype = C.c_int
+    L.rl_attention_quant.argtypes = [kp, i32, vp, vp, i32, i32, vp, i64, i32, f64, vp, i64, vp, sz, vp]
     L.rl_status_string.restype = C.c_char_p
     L.rl_status_string.argtypes = [C.c_int]
     L.rl_decode_last_error.restype = C.c_char_p
@@ -671,3 +701,182 @@ def preference_loss(logp: torch.Tensor, seq_offsets: torch.Tensor, out_loss: tor
     _run_on(dev, stream, L.rl_preference_workspace_bytes(n, P) if workspace is None else 0, workspace,
             lambda ws, nb, s: L.rl_preference_loss(n, P, offs, lp, ref, m, C.byref(q), out, rew, g, ws, nb, s),
             "rl_preference_loss")
+
+
+# -- rollout in 8 bits: norm, quantiser, product, cache and attention ----------
+# Codes: float8_e4m3fn (or uint8) [rows][whole blocks of 128]; scale bytes:
+# float8_e8m0fnu (or uint8) [rows, or tiles of 128 rows][blocks or more].  Rows
+# may be apart (stride(0)).  As above: ValueError for a tensor of the wrong
+# type, size or device, RLError for what the library refuses.
+
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+_SCALES = (torch.float8_e8m0fnu, torch.uint8)
+
+
+def fp8_blocks(k: int) -> int:
+    """Blocks of 128 codes of a row of k entries."""
+    return (int(k) + 127) // 128
+
+
+def empty_fp8(rows: int, k: int, *, weight: bool = False, device="cuda"):
+    """(codes, scales) with room for [rows][k] in 8 bits: a scale for each block of a row, or for each tile of a weight."""
+    kb = fp8_blocks(k)
+    codes = torch.empty(rows, 128 * kb, dtype=torch.float8_e4m3fn, device=device)
+    scales = torch.empty(fp8_blocks(rows) if weight else rows, (kb + 3) // 4 * 4, dtype=torch.uint8, device=device)
+    return codes, scales.view(torch.float8_e8m0fnu)
+
+
+def _bytes_on(dev: int, name: str, t: torch.Tensor, dtypes, rows: int, width: int):
+    """(pointer, row stride) of a matrix of bytes with this many rows of at least `width`."""
+    if t.dim() != 2 or t.dtype not in dtypes or t.get_device() != dev or t.shape[0] != rows or t.shape[1] < width:
+        raise ValueError(f"{name} must be {rows} rows of {width} or more {' or '.join(map(str, dtypes))} on cuda:{dev}, "
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+    ld = t.stride(0) if rows > 1 else max(t.shape[1], t.stride(0))
+    if (t.shape[1] > 1 and t.stride(1) != 1) or ld < t.shape[1]:
+        raise ValueError(f"{name}: entries of a row must be contiguous and rows apart: strides {t.stride()}")
+    return t.data_ptr(), ld
+
+
+def _fp8_on(dev: int, name: str, codes: torch.Tensor, scales: torch.Tensor, rows: int, k: int, weight: bool = False) -> Fp8Matrix:
+    kb = fp8_blocks(k)
+    c, ld = _bytes_on(dev, name, codes, _CODES, rows, 128 * kb)
+    b, lds = _bytes_on(dev, name + " scales", scales, _SCALES, fp8_blocks(rows) if weight else rows, kb)
+    return Fp8Matrix(c, ld, b, lds)
+
+
+def _numbers_on(dev: int, name: str, t: torch.Tensor, rows: int, width: int):
+    """(pointer, row stride) of float32 or bfloat16 rows."""
+    p, ld = _rows_on(dev, name, t)
+    if t.shape != (rows, width):
+        raise ValueError(f"{name} must be {rows} rows of {width} entries, not {tuple(t.shape)}")
+    return p, ld
+
+
+def rmsnorm_quant(x: torch.Tensor, weight: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, *,
+                add: Optional[torch.Tensor] = None, out_sum: Optional[torch.Tensor] = None, eps: float = 1e-6, stream=None):
+    """rl_rmsnorm_quant: rows of x (+ add, the sum to out_sum, which may be x)
+    normed, times weight, in 8 bits."""
+    dev = _gpu_of(x, "x")
+    xp, ldx = _rows_on(dev, "x", x)
+    n, H = x.shape
+    if weight.dim() != 1 or weight.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"weight must be a vector of float32 or bfloat16, not {weight.dtype} {tuple(weight.shape)}")
+    w = _on(dev, "weight", weight, weight.dtype, H)
+    ap, lda = _numbers_on(dev, "add", add, n, H) if add is not None else (None, 0)
+    sp, lds = _numbers_on(dev, "out_sum", out_sum, n, H) if out_sum is not None else (None, 0)
+    if out_sum is not None and out_sum.dtype is not x.dtype:
+        raise ValueError(f"out_sum must be {x.dtype} as x is, not {out_sum.dtype}")
+    out = _fp8_on(dev, "codes", codes, scales, n, H)
+    L = lib()
+    _run_on(dev, stream, 0, None,
+            lambda ws, nb, s: L.rl_rmsnorm_quant(n, H, _dtype_code(x), xp, ldx, _dtype_code(x if add is None else add), ap, lda,
+                                               _dtype_code(weight), w, eps, sp, lds, C.byref(out), s), "rl_rmsnorm_quant")
+
+
+def quantise(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, *, form: str = "rows", stream=None):
+    """rl_quantise: rows of x, silu(first half) * second half of its rows
+    ("swiglu"), or a weight in tiles of 128 x 128 ("tiles"), in 8 bits."""
+    if form not in FP8_FORMS:
+        raise ValueError(f"form is one of {tuple(FP8_FORMS)}")
+    dev = _gpu_of(x, "x")
+    xp, ldx = _rows_on(dev, "x", x)
+    n, k = x.shape
+    if form == "swiglu":
+        if k % 2:
+            raise ValueError("the two halves of a row are of one size")
+        k //= 2
+    out = _fp8_on(dev, "codes", codes, scales, n, k, form == "tiles")
+    L = lib()
+    _run_on(dev, stream, 0, None,
+            lambda ws, nb, s: L.rl_quantise(FP8_FORMS[form], n, k, _dtype_code(x), xp, ldx, C.byref(out), s), "rl_quantise")
+
+
+def gemm_quant(a: torch.Tensor, a_scales: torch.Tensor, w: torch.Tensor, w_scales: torch.Tensor, out: torch.Tensor, *,
+             workspace: Optional[torch.Tensor] = None, stream=None):
+    """rl_gemm_quant: out [m][n] = a [m][k] times the weight w [n][k] (tiles),
+    both in whole blocks of 128 codes."""
+    dev = _gpu_of(out, "out")
+    o, ldo = _rows_on(dev, "out", out)
+    m, n = out.shape
+    k = a.shape[1] if a.dim() == 2 else 0
+    if k < 1 or k % 128:
+        raise ValueError(f"a must hold rows of whole blocks of 128 codes, not {tuple(a.shape)}")
+    A, W = _fp8_on(dev, "a", a, a_scales, m, k), _fp8_on(dev, "w", w, w_scales, n, k, True)
+    if w.shape[1] != k:
+        raise ValueError(f"a has rows of {k} codes, w of {w.shape[1]}")
+    L = lib()
+    _run_on(dev, stream, L.rl_gemm_quant_workspace_bytes(m, n, k) if workspace is None else 0, workspace,
+            lambda ws, nb, s: L.rl_gemm_quant(m, n, k, C.byref(A), C.byref(W), _dtype_code(out), o, ldo, ws, nb, s), "rl_gemm_quant")
+
+
+def kv_quant_bytes(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(lib().rl_kv_quant_bytes(n_pages, page_size, n_kv_heads, head_dim))
+
+
+def _heads_on(dev: int, name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None):
+    """(pointer, row stride) of [n][heads][d] whose heads lie one after the other."""
+    if t.dim() != 3 or t.dtype not in (torch.float32, torch.bfloat16) or t.get_device() != dev or (
+            like is not None and (t.dtype is not like.dtype or t.shape != like.shape)):
+        raise ValueError(f"{name} must be [n][heads][d] of float32 or bfloat16 on cuda:{dev}"
+                         + (f" like the other ({tuple(like.shape)} {like.dtype})" if like is not None else "")
+                         + f", not {t.dtype} {tuple(t.shape)} on {t.device}")
+    n, h, d = t.shape
+    ld = t.stride(0) if n > 1 else h * d
+    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d) or ld < h * d:
+        raise ValueError(f"{name}: a token's heads must be contiguous and tokens apart: strides {t.stride()}")
+    return t.data_ptr(), ld
+
+
+def _cache_on(dev: int, pool: torch.Tensor, page_table: torch.Tensor, page_size: int, heads: int, d: int) -> KvFp8:
+    one = kv_quant_bytes(1, page_size, heads, d)
+    if not one:
+        raise ValueError(f"no cache of pages of {page_size} positions with {heads} heads of {d}")
+    if page_table.dim() != 2:
+        raise ValueError(f"page_table must be [sequences][pages], not {tuple(page_table.shape)}")
+    n_pages = pool.numel() // one
+    if pool.dtype is not torch.uint8 or pool.get_device() != dev or not pool.is_contiguous() or not 0 < n_pages < 1 << 31:
+        raise ValueError(f"pool must be a contiguous uint8 tensor of whole pages ({one} bytes) on cuda:{dev}, not {pool.dtype} "
+                         f"{tuple(pool.shape)} on {pool.device}")
+    return KvFp8(pool.data_ptr(),
+                 _on(dev, "page_table", page_table, torch.int32, page_table.numel()), page_table.shape[0], page_table.shape[1],
+                 n_pages, page_size, heads, d)
+
+
+def _kv_call(name: str, dev: int, pool, page_table, seqs, positions, k, v, page_size, stream):
+    kp, ldk = _heads_on(dev, "k", k)
+    vp, ldv = _heads_on(dev, "v", v, k)
+    n, h, d = k.shape
+    cache = _cache_on(dev, pool, page_table, page_size, h, d)
+    sq, ps = _on(dev, "seqs", seqs, torch.int32, n), _on(dev, "positions", positions, torch.int32, n)
+    f = getattr(lib(), name)
+    _run_on(dev, stream, 0, None, lambda ws, nb, s: f(C.byref(cache), n, sq, ps, _dtype_code(k), kp, ldk, vp, ldv, s), name)
+
+
+def kv_quant_append(pool: torch.Tensor, page_table: torch.Tensor, seqs: torch.Tensor, positions: torch.Tensor, k: torch.Tensor,
+                  v: torch.Tensor, *, page_size: int, stream=None):
+    """rl_kv_quant_append: keys and values [n][kv-heads][d] of tokens (seqs[i],
+    positions[i]) into the pool (uint8, kv_quant_bytes of it)."""
+    _kv_call("rl_kv_quant_append", _gpu_of(pool, "pool"), pool, page_table, seqs, positions, k, v, page_size, stream)
+
+
+def kv_quant_read(pool: torch.Tensor, page_table: torch.Tensor, seqs: torch.Tensor, positions: torch.Tensor, out_k: torch.Tensor,
+                out_v: torch.Tensor, *, page_size: int, stream=None):
+    """rl_kv_quant_read: those tokens' keys and values as numbers."""
+    _kv_call("rl_kv_quant_read", _gpu_of(pool, "pool"), pool, page_table, seqs, positions, out_k, out_v, page_size, stream)
+
+
+def attention_quant(pool: torch.Tensor, page_table: torch.Tensor, q: torch.Tensor, lengths: torch.Tensor, out: torch.Tensor, *,
+                  page_size: int, n_kv_heads: int, max_length: int, scale: float, seqs: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, stream=None):
+    """rl_attention_quant: q and out [n][q-heads][d]; row i attends over the first
+    lengths[i] <= max_length positions of sequence seqs[i] (of i without seqs)."""
+    dev = _gpu_of(q, "q")
+    qp, ldq = _heads_on(dev, "q", q)
+    op, ldo = _heads_on(dev, "out", out, q)
+    n, h, d = q.shape
+    cache = _cache_on(dev, pool, page_table, page_size, n_kv_heads, d)
+    ln, sq = _on(dev, "lengths", lengths, torch.int32, n), _on(dev, "seqs", seqs, torch.int32, n, True)
+    L = lib()
+    _run_on(dev, stream, L.rl_attention_quant_workspace_bytes(n, n_kv_heads, h, d, max_length) if workspace is None else 0, workspace,
+            lambda ws, nb, s: L.rl_attention_quant(C.byref(cache), n, sq, ln, max_length, _dtype_code(q), qp, ldq, h, scale, op, ldo,
+                                                 ws, nb, s), "rl_attention_quant")

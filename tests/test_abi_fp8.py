@@ -1,0 +1,161 @@
+"""The 8-bit entry points on the CPU: struct layouts, enums, sizes and refusals.  No call here reaches the GPU."""
+import ctypes as C
+import re
+
+import pytest
+import torch
+
+from paper_2509_15965_amd import rl_decode as R
+from test_abi_host import HEADER, _compile_and_run
+
+P = 4096           # a pointer that no refused call follows
+BAD, CAP = R.RL_ERR_INVALID_ARG, R.RL_ERR_CAPACITY
+
+
+def test_structs_and_enums_match_the_header(tmp_path):
+    structs = {"rl_fp8_matrix": R.Fp8Matrix, "rl_kv_fp8": R.KvFp8}
+    body = ""
+    for name, py in structs.items():
+        body += f'printf("{name}=%zu\\n", sizeof({name}));\n'
+        for f, _ in py._fields_:
+            body += f'printf("{name}.{f}=%zu\\n", offsetof({name}, {f}));\n'
+    enums = {"RL_FP8_" + k.upper(): v for k, v in R.FP8_FORMS.items()}
+    assert sorted(enums) == sorted(re.findall(r"\b(RL_FP8_[A-Z0-9_]+)\s*=", open(HEADER).read()))
+    body += "".join(f'printf("{k}=%d\\n", (int){k});\n' for k in enums)
+    got = _compile_and_run(tmp_path, body)
+    for name, py in structs.items():
+        assert int(got[name]) == C.sizeof(py)
+        for f, _ in py._fields_:
+            assert int(got[f"{name}.{f}"]) == getattr(py, f).offset, (name, f)
+    for k, v in enums.items():
+        assert int(got[k]) == v, k
+
+
+def matrix(k, codes=P, ld=None, scales=P, lds=None):
+    kb = R.fp8_blocks(k)
+    return R.Fp8Matrix(codes, 128 * kb if ld is None else ld, scales, (kb + 3) // 4 * 4 if lds is None else lds)
+
+
+MATRICES = [dict(codes=None), dict(codes=P + 8), dict(scales=None), dict(scales=P + 2), dict(ld=256), dict(ld=392), dict(ld=1 << 21),
+            dict(lds=0), dict(lds=6), dict(lds=1 << 21)]
+
+
+def norm(n=2, hidden=300, dtype=0, x=P, ldx=300, add_dtype=1, add=P, ld_add=300, w_dtype=1, w=P, eps=1e-6, total=P, ld_sum=300, out=None):
+    m = matrix(hidden, **(out or {}))
+    return R.lib().rl_rmsnorm_quant(n, hidden, dtype, x, ldx, add_dtype, add, ld_add, w_dtype, w, eps, total, ld_sum, C.byref(m), None)
+
+
+@pytest.mark.parametrize("bad", [dict(n=-1), dict(n=(1 << 20) + 1), dict(hidden=0), dict(hidden=32769, ldx=1 << 16), dict(dtype=2),
+                                 dict(dtype=-1), dict(add_dtype=7), dict(w_dtype=2), dict(x=None), dict(x=P + 2), dict(ldx=299),
+                                 dict(ldx=1 << 40), dict(add=P + 1), dict(ld_add=299), dict(w=None), dict(w=P + 1), dict(eps=0.0),
+                                 dict(eps=-1.0), dict(eps=2.0), dict(eps=1e-60), dict(eps=float("nan")), dict(total=P + 2),
+                                 dict(ld_sum=299)] + [dict(out=m) for m in MATRICES])
+def test_rmsnorm_quant_refuses(bad):
+    assert norm(**bad) == BAD
+
+
+def test_no_rows_need_nothing():
+    L = R.lib()
+    assert norm(n=0, x=None, add=None, w=None, total=None, out=dict(codes=None)) == R.RL_OK
+    assert L.rl_quantise(0, 0, 10, 1, None, 10, None, None) == R.RL_OK
+    assert L.rl_gemm_quant(0, 10, 10, None, None, 1, None, 10, None, 0, None) == R.RL_OK
+
+
+def quantise(form=0, n=2, k=300, dtype=1, x=P, ldx=None, out=None):
+    m = matrix(k, **(out or {}))
+    return R.lib().rl_quantise(form, n, k, dtype, x, (2 * k if form == 1 else k) if ldx is None else ldx, C.byref(m), None)
+
+
+@pytest.mark.parametrize("bad", [dict(form=-1), dict(form=3), dict(n=-1), dict(n=(1 << 20) + 1), dict(k=0), dict(k=131073), dict(dtype=2),
+                                 dict(x=None), dict(x=P + 1), dict(dtype=0, x=P + 2), dict(ldx=299), dict(form=1, ldx=599)]
+                         + [dict(out=m) for m in MATRICES])
+def test_quantise_refuses(bad):
+    assert quantise(**bad) == BAD
+
+
+def gemm(m=2, n=300, k=300, a=None, w=None, dt=1, out=P, ldo=300, ws=P, nb=1 << 40):
+    A, W = matrix(k, **(a or {})), matrix(k, **(w or {}))
+    return R.lib().rl_gemm_quant(m, n, k, C.byref(A), C.byref(W), dt, out, ldo, ws, nb, None)
+
+
+@pytest.mark.parametrize("bad", [dict(m=-1), dict(m=(1 << 20) + 1), dict(n=0), dict(n=(1 << 20) + 1), dict(k=0), dict(k=131073),
+                                 dict(dt=2), dict(out=None), dict(out=P + 1), dict(dt=0, out=P + 2), dict(ldo=299)]
+                         + [dict(a=m) for m in MATRICES] + [dict(w=m) for m in MATRICES])
+def test_gemm_quant_refuses(bad):
+    assert gemm(**bad) == BAD
+
+
+def test_gemm_workspace():
+    L = R.lib()
+    for m, n, k in ((0, 8, 8), (8, 0, 8), (8, 8, 0), (-1, 8, 8), ((1 << 20) + 1, 8, 8), (8, (1 << 20) + 1, 8), (8, 8, 131073)):
+        assert L.rl_gemm_quant_workspace_bytes(m, n, k) == 0
+    for m, n, k in ((1, 2048, 1536), (24, 152064, 3584), (512, 3584, 18944), (200, 600, 8192)):
+        need = L.rl_gemm_quant_workspace_bytes(m, n, k)
+        if need:
+            assert gemm(m=m, n=n, k=k, ldo=n, nb=need - 1) == CAP
+            assert gemm(m=m, n=n, k=k, ldo=n, ws=None) == BAD
+            assert gemm(m=m, n=n, k=k, ldo=n, ws=P + 64) == BAD
+
+
+def cache(**more):
+    return R.KvFp8(**dict(dict(pool=P, page_table=P, n_seqs=3, max_pages=4, n_pages=10, page_size=64, n_kv_heads=2, head_dim=128), **more))
+
+
+CACHES = [dict(pool=None), dict(pool=P + 16), dict(page_table=None), dict(page_table=P + 2), dict(n_seqs=0), dict(max_pages=0), dict(n_pages=0),
+          dict(page_size=0), dict(page_size=16), dict(page_size=48), dict(page_size=65568), dict(n_kv_heads=0), dict(n_kv_heads=1025),
+          dict(head_dim=96), dict(head_dim=256), dict(max_pages=1 << 25)]
+
+
+def tokens(f, c=None, n=2, seqs=P, pos=P, dt=1, k=P, ldk=256, v=P, ldv=256):
+    return getattr(R.lib(), f)(C.byref(cache(**(c or {}))), n, seqs, pos, dt, k, ldk, v, ldv, None)
+
+
+@pytest.mark.parametrize("f", ["rl_kv_quant_append", "rl_kv_quant_read"])
+@pytest.mark.parametrize("bad", [dict(c=c) for c in CACHES] + [dict(n=-1), dict(n=(1 << 24) + 1), dict(seqs=None), dict(pos=None), dict(dt=2),
+                                                              dict(k=None), dict(v=None), dict(k=P + 1), dict(ldk=255), dict(ldv=255)])
+def test_cache_calls_refuse(f, bad):
+    assert tokens(f, **bad) == BAD
+    assert tokens(f, n=0, seqs=None, pos=None, k=None, v=None) == R.RL_OK
+
+
+def test_cache_bytes_follow_the_layout():
+    b = R.lib().rl_kv_quant_bytes
+    assert b(1, 32, 1, 128) == 8448 and b(3, 64, 4, 64) == 12 * 8448 and b(1, 64, 1, 128) == 16640
+    for bad in ((0, 32, 1, 128), (1, 31, 1, 128), (1, 32, 0, 128), (1, 32, 1, 80), (1, 131072, 1, 64)):
+        assert b(*bad) == 0
+
+
+def attend(c=None, n=2, seqs=P, lengths=P, longest=200, dt=1, q=P, ldq=1024, heads=8, scale=0.1, out=P, ldo=1024, ws=P, nb=1 << 40):
+    return R.lib().rl_attention_quant(C.byref(cache(**(c or {}))), n, seqs, lengths, longest, dt, q, ldq, heads, scale, out, ldo, ws, nb, None)
+
+
+@pytest.mark.parametrize("bad", [dict(c=c) for c in CACHES]
+                         + [dict(n=-1), dict(n=(1 << 20) + 1), dict(n=4, seqs=None), dict(lengths=None), dict(longest=-1), dict(longest=257),
+                            dict(dt=2), dict(q=None), dict(q=P + 1), dict(ldq=1023), dict(heads=1), dict(heads=7), dict(heads=34, ldq=1 << 20),
+                            dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=1e300), dict(out=None), dict(ldo=1023)])
+def test_attention_quant_refuses(bad):
+    assert attend(**bad) == BAD
+
+
+def test_attention_workspace():
+    f = R.lib().rl_attention_quant_workspace_bytes
+    for bad in ((0, 2, 8, 128, 100), (2, 0, 8, 128, 100), (2, 2, 7, 128, 100), (2, 2, 34, 128, 100), (2, 2, 8, 96, 100), (2, 2, 8, 128, -1)):
+        assert f(*bad) == 0
+    need = f(3, 2, 8, 128, 100000)
+    assert need > 0
+    big = dict(c=dict(max_pages=2000), n=3, longest=100000)
+    assert attend(**big, nb=need - 1) == CAP
+    assert attend(**big, ws=None) == BAD
+    assert attend(**big, ws=P + 16) == BAD
+    assert attend(c=dict(max_pages=1 << 20, page_size=1024, n_kv_heads=1024, n_seqs=1 << 20), n=1 << 20, heads=1024, ldq=1 << 17, ldo=1 << 17,
+                  longest=1 << 30) == R.RL_ERR_UNSUPPORTED
+
+
+def test_binding_checks_its_tensors():
+    x = torch.zeros(2, 256)
+    c, s = R.empty_fp8(2, 256, device="cpu")
+    assert c.shape == (2, 256) and s.shape == (2, 4) and R.empty_fp8(300, 300, weight=True, device="cpu")[1].shape == (3, 4)
+    for f in (lambda: R.rmsnorm_quant(x, torch.ones(256), c, s), lambda: R.quantise(x, c, s), lambda: R.quantise(x, c, s, form="columns"),
+              lambda: R.gemm_quant(c, s, c, s, x), lambda: R.kv_quant_append(c, s, s, s, x, x, page_size=64)):
+        with pytest.raises(ValueError):
+            f()
