@@ -16,6 +16,9 @@
 #include "fp8.h"
 #include "rl_decode.h"
 
+#include <algorithm>
+#include <type_traits>
+
 namespace rl {
 
 namespace {
@@ -41,82 +44,483 @@ template <typename TO> __device__ __forceinline__ void store4(TO* row, int at, i
         if (at + e < n) Elem<TO>::store(row, at + e, v[e]);
 }
 
-// 128 x 128 tiles, 4 waves of 64 x 64, one block of K at a time through LDS.
-// Weights are the rows of the instruction's tile and tokens its columns: a
-// lane then holds four consecutive outputs of one token.
-template <typename TO, bool EXACT>
-__global__ void __launch_bounds__(256) gemm_fp8_kernel(Fp8Gemm p, bool vec) {
-    constexpr int LDK = 144;   // bytes a row: 16 rows' 16-byte reads hit different banks
-    __shared__ __attribute__((aligned(16))) uint8_t As[128 * LDK], Ws[128 * LDK];
-    const int m0 = blockIdx.y * 128, n0 = blockIdx.x * 128;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int wm = wave >> 1, wn = wave & 1, r16 = lane & 15, g = lane >> 4;
-    const int lr = tid >> 3, lc = (tid & 7) * 16;
-    f32x4 acc[4][4];   // [weights][tokens]
+typedef __attribute__((address_space(3))) void lds_void_t;
+
+// BYTES a lane from a uniform base and a lane's offset straight to LDS: lane i to BYTES i past lds.
+template <int BYTES> __device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t off, uint8_t* lds) {
+    if constexpr (BYTES == 16) __builtin_amdgcn_global_load_lds(static_cast<const void*>(base + off), (lds_void_t*)(lds), 16, 0, 0);
+    else __builtin_amdgcn_global_load_lds(static_cast<const void*>(base + off), (lds_void_t*)(lds), 4, 0, 0);
+}
+
+// s_waitcnt vmcnt(N), the other counters left alone
+template <int N> __device__ __forceinline__ void wait_vm() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+}
+
+// Barrier of the workgroup behind which the wave's loads to LDS but the last N, and its reads of LDS, are done.
+template <int N> __device__ __forceinline__ void barrier_vm() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// ---------------------------------------------------------------------------
+// Few tokens: a workgroup takes 16 RW weights, its WV waves every WV-th block of its
+// K slice, straight from memory to registers (U blocks in flight a wave), and
+// the waves' sums meet in LDS in wave order.  MT x 16 tokens.  Bound by the
+// weights' bytes: the exact instructions cost nothing here.  RW = 4 reads the
+// tokens once for 64 weights.
+// ---------------------------------------------------------------------------
+template <typename TO, int RW, int MT, int WV, bool SPLIT>
+__global__ void __launch_bounds__(64 * WV) gemv_fp8_kernel(Fp8Gemm p, int per, bool vec) {
+    constexpr int U = RW * MT >= 8 ? 1 : 2;
+    __shared__ f32x4 red[WV][RW * MT][64];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r16 = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * 16 * RW;
+    const int k0 = blockIdx.y * per, k1 = min(p.kb, k0 + per);
+    const uint8_t* wp[RW];
+    const uint8_t* ap[MT];
+    const uint8_t* sp[MT];
+    const uint8_t* swp[RW];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < RW; ++i) {
+        const int n = min(n0 + 16 * i + r16, p.n - 1);
+        wp[i] = p.w.codes + n * p.w.ld + 16 * g;
+        swp[i] = p.w.scales + static_cast<int64_t>(min(n0 + 16 * i, p.n - 1) / 128) * p.w.lds;
+    }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) acc[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int kb = 0; kb < p.kb; ++kb) {
-        __syncthreads();
+    for (int j = 0; j < MT; ++j) {
+        const int m = min(16 * j + r16, p.m - 1);
+        ap[j] = p.a.codes + m * p.a.ld + 16 * g;
+        sp[j] = p.a.scales + m * p.a.lds;
+    }
+    f32x4 acc[RW][MT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int m = min(m0 + lr + 32 * i, p.m - 1), n = min(n0 + lr + 32 * i, p.n - 1);
-            *reinterpret_cast<u32x4*>(As + (lr + 32 * i) * LDK + lc) = ld16(p.a.codes + m * p.a.ld + kb * 128 + lc);
-            *reinterpret_cast<u32x4*>(Ws + (lr + 32 * i) * LDK + lc) = ld16(p.w.codes + n * p.w.ld + kb * 128 + lc);
+    for (int i = 0; i < RW; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int kb = k0 + wave; kb < k1; kb += U * WV) {
+        u32x4 w[U][RW][2], a[U][MT][2];
+        float sw[U][RW], sa[U][MT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = min(kb + u * WV, k1 - 1);   // past the slice: the last block again, not added
+#pragma unroll
+            for (int i = 0; i < RW; ++i) {
+                w[u][i][0] = ld16(wp[i] + k * 128);
+                w[u][i][1] = ld16(wp[i] + k * 128 + 64);
+                sw[u][i] = fp8_scale(swp[i][k]);
+            }
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+                a[u][j][0] = ld16(ap[j] + k * 128);
+                a[u][j][1] = ld16(ap[j] + k * 128 + 64);
+                sa[u][j] = fp8_scale(sp[j][k]);
+            }
         }
-        __syncthreads();
-        const int sw = p.w.scales[static_cast<int64_t>(n0 / 128) * p.w.lds + kb];
-        u32x4 wf[4][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint8_t* w = Ws + (wn * 64 + 16 * i + r16) * LDK + 16 * g;
-            wf[i][0] = *reinterpret_cast<const u32x4*>(w);
-            wf[i][1] = *reinterpret_cast<const u32x4*>(w + 64);
-        }
+        for (int u = 0; u < U; ++u) {
+            if (u > 0 && kb + u * WV >= k1) break;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int r = wm * 64 + 16 * t + r16;
-            const int sa = p.a.scales[min(m0 + r, p.m - 1) * p.a.lds + kb];
-            const uint8_t* a = As + r * LDK + 16 * g;
-            const u32x4 a0 = *reinterpret_cast<const u32x4*>(a), a1 = *reinterpret_cast<const u32x4*>(a + 64);
+            for (int h = 0; h < 4; ++h) {
+                bf16x8 wf[RW];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (EXACT) {
-                    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+                for (int i = 0; i < RW; ++i) wf[i] = codes_bf16(w[u][i][h / 2][2 * (h & 1)], w[u][i][h / 2][2 * (h & 1) + 1], sw[u][i]);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        s = mfma16x16x32(codes_bf16(wf[i][0][2 * h], wf[i][0][2 * h + 1], 1.0f), codes_bf16(a0[2 * h], a0[2 * h + 1], 1.0f), s);
-                        s = mfma16x16x32(codes_bf16(wf[i][1][2 * h], wf[i][1][2 * h + 1], 1.0f), codes_bf16(a1[2 * h], a1[2 * h + 1], 1.0f), s);
-                    }
+                for (int j = 0; j < MT; ++j) {
+                    const bf16x8 af = codes_bf16(a[u][j][h / 2][2 * (h & 1)], a[u][j][h / 2][2 * (h & 1) + 1], sa[u][j]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][t][e] += ldexpf(s[e], sa + sw - 254);
-                } else {
-                    acc[i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(join(wf[i][0], wf[i][1]), join(a0, a1), acc[i][t], 0, 0, 0,
-                                                                                 sw, 0, sa);
+                    for (int i = 0; i < RW; ++i) acc[i][j] = mfma16x16x32(wf[i], af, acc[i][j]);
                 }
             }
         }
     }
+#pragma unroll
+    for (int i = 0; i < RW; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) red[wave][i * MT + j][lane] = acc[i][j];
+    __syncthreads();
+#pragma unroll
+    for (int x0 = 0; x0 < RW * MT; x0 += WV) {
+        const int x = x0 + wave;
+        if (x >= RW * MT) break;
+        f32x4 v = red[0][x][lane];
+#pragma unroll
+        for (int q = 1; q < WV; ++q) v += red[q][x][lane];
+        const int m = 16 * (x % MT) + r16, n = n0 + 16 * (x / MT) + 4 * g;
+        if (m >= p.m) continue;
+        if constexpr (SPLIT) store4(p.part + (static_cast<int64_t>(blockIdx.y) * p.m + m) * p.n, n, p.n, p.n % 4 == 0, v);
+        else store4(static_cast<TO*>(p.out) + m * p.ldo, n, p.n, vec, v);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Tiles of BM tokens x BN weights, 2 x 2 waves, 32x32x64 instructions (EXACT: four
+// 32x32x16 ones, see above), over the blocks of a K slice.
+//
+// A block of K of either operand is a slot of 128-byte rows in LDS, moved
+// there from memory without passing through registers, eight whole lines an
+// instruction; two slots.  Chunk c (16 bytes) of row r sits at c ^ (r / 2 % 8), which
+// frees the fragment reads of bank conflicts.  A wave holds a block's weights in
+// registers and multiplies them with the first half of its tokens, then with the
+// second; the fragments of the half that follows are read under each half's
+// instructions.  So a block's weights and first tokens have left their slot when its first
+// half begins and the second tokens when that ends: behind a barrier there, the slot
+// takes what the block after the next needs, and all of it has a block and a half's
+// time to arrive (one block's was not enough: memory answers in about 1.1 us, a block is 0.9).
+//
+// LDS row 32 t + 8 q + 4 h + e of a wave's weights (t tile, 4 q + e register and h lane half
+// of the instruction's output) holds weight h TN / 2 + q TN / 8 + 4 t + e: a lane's outputs
+// of one token are runs of TN / 8 weights, stored 16 bytes at a time.
+// Rows past the last token or weight are the last one again, and are not stored.
+// ---------------------------------------------------------------------------
+struct TileMap { int m_tiles, n_tiles, gm; };
+
+template <int BM, int BN, typename TO, bool EXACT>
+__device__ __forceinline__ void tile_fp8(const Fp8Gemm& p, int m0, int n0, int k0, int nk, uint8_t* smem, bool vec, float* part) {
+    constexpr int TM = BM / 2, TN = BN / 2, MT = TM / 32, NT = TN / 32;
+    constexpr int AQ = BM / 64, WQ = BN / 32;                // line instructions a wave issues for half of the tokens, for the weights
+    constexpr int Q1 = WQ + AQ + 2, Q2 = AQ;                 // a block's first refill, with the scale words, and its second
+    constexpr int ASLOT = BM * 128 + 2048, WSLOT = BN * 128; // the scale words ride with the tokens
+    static_assert(BM % 64 == 0 && BM <= 256 && (TN == 64 || TN == 128), "one word instruction, one weight scale a wave");
+    uint8_t* const aslots = smem;
+    uint8_t* const wslots = smem + 2 * ASLOT;
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave >> 1, wn = wave & 1, r32 = lane & 31, kh = lane >> 5;
+
+    const uint8_t* abase = p.a.codes + m0 * p.a.ld + k0 * 128;
+    const uint8_t* wbase = p.w.codes + n0 * p.w.ld + k0 * 128;
+    uint32_t aoff[2][AQ], woff[WQ];
+    auto arow = [&](int half, int q) {   // first LDS row of the eight that an instruction moves: halves of each wave row's tokens
+        const int r = 8 * (wave * AQ + q);
+        return r / (TM / 2) * TM + half * (TM / 2) + r % (TM / 2);
+    };
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int q = 0; q < AQ; ++q) {
+            const int r = arow(f, q) + (lane >> 3);
+            aoff[f][q] = min(r, p.m - 1 - m0) * static_cast<uint32_t>(p.a.ld) + 16u * ((lane & 7) ^ ((r >> 1) & 7));
+        }
+#pragma unroll
+    for (int q = 0; q < WQ; ++q) {
+        const int r = 8 * (wave * WQ + q) + (lane >> 3), b = r % TN;   // b = 32 t + 8 q + 4 h + e
+        const int n = r - b + ((b >> 2) & 1) * (TN / 2) + ((b >> 3) & 3) * (TN / 8) + 4 * (b >> 5) + (b & 3);
+        woff[q] = min(n, p.n - 1 - n0) * static_cast<uint32_t>(p.w.ld) + 16u * ((lane & 7) ^ ((r >> 1) & 7));
+    }
+    const uint32_t soff = min((64 * wave + lane) % BM, p.m - 1 - m0) * static_cast<uint32_t>(p.a.lds);
+    const uint8_t* sabase = p.a.scales + m0 * p.a.lds;
+    const uint8_t* swbase = p.w.scales + static_cast<int64_t>(min((n0 + wn * TN) / 128, (p.n - 1) / 128)) * p.w.lds;
+
+    auto issue = [&](int kt, int slot, int part, int q) {   // instruction q of block kt's first or second refill
+        uint8_t* as = aslots + slot * ASLOT;
+        if (part == 1) to_lds<16>(abase + kt * 128, aoff[1][q < AQ ? q : 0], as + arow(1, q) * 128);
+        else if (q < WQ) to_lds<16>(wbase + kt * 128, woff[q < WQ ? q : 0], wslots + slot * WSLOT + (wave * WQ + q) * 1024);
+        else if (q < WQ + AQ) to_lds<16>(abase + kt * 128, aoff[0][q < WQ + AQ && q >= WQ ? q - WQ : 0], as + arow(0, q - WQ) * 128);
+        else if (q == WQ + AQ) to_lds<4>(sabase + ((k0 + kt) & ~3), soff, as + BM * 128 + wave * 256);
+        else to_lds<4>(swbase + ((k0 + kt) & ~3), 0u, as + BM * 128 + 1024 + wave * 256);
+    };
+
+    f32x16 acc[NT][MT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[t][i][e] = 0.f;
+
+    // the swizzle of a fragment's row goes by r32 alone: rows of tiles are multiples of 32 apart
+    const int swz = (r32 >> 1) & 7;
+    const uint32_t la = (wm * TM + r32) * 128, lw = (wn * TN + r32) * 128;
+    const uint32_t lsa = BM * 128 + (wm * TM + r32) * 4, lsw = BM * 128 + 1024 + wave * 256;
+    uint32_t ch[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) ch[c] = ((2 * c + kh) ^ swz) << 4;
+    struct Weights { i32x8 w[NT][2]; };        // [tile][half of the block]
+    struct Tokens { i32x8 a[2]; };
+    auto frag = [&](const uint8_t* row, int k) {
+        return join(*reinterpret_cast<const u32x4*>(row + ch[2 * k]), *reinterpret_cast<const u32x4*>(row + ch[2 * k + 1]));
+    };
+    auto read_w = [&](int slot, Weights& f, int t, int k) { f.w[t][k] = frag(wslots + slot * WSLOT + lw + 4096 * t, k); };
+    auto read_a = [&](int slot, Tokens& f, int i, int k) { f.a[k] = frag(aslots + slot * ASLOT + la + 4096 * i, k); };
+    struct Scales { uint32_t w, a[MT]; };
+    auto read_scales = [&](int slot, Scales& f) {
+        f.w = *reinterpret_cast<const uint32_t*>(aslots + slot * ASLOT + lsw);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) f.a[i] = *reinterpret_cast<const uint32_t*>(aslots + slot * ASLOT + lsa + 128 * i);
+    };
+    // a block's products in two groups: every weight tile with half of the token tiles
+    constexpr int GA = MT / 2, G = NT * 2 * GA;
+    Weights w;
+    Tokens at[2][GA];
+    Scales sc, sc_next{};
+    // Barriers stand B products into the halves, where the reads of the half before have long arrived.
+    constexpr int B = 2 * GA, B0 = B, B1 = G + B;
+    auto block = [&](int kt, auto slot, auto steady) {   // block kt, in slots SLOT
+        constexpr int SLOT = decltype(slot)::value;
+        constexpr bool ALL = decltype(steady)::value;
+        const bool more = ALL || kt + 1 < nk, refill = ALL || kt + 2 < nk;
+        const int sh = 8 * ((k0 + kt) & 3);
+        const int sw = static_cast<int>(sc.w >> sh);
+        int sa[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) sa[i] = static_cast<int>(sc.a[i] >> sh);
+#pragma unroll
+        for (int y = 0; y < 2 * G; ++y) {
+            // at B0: this block's second tokens are there, and every wave has read its weights and first tokens;
+            // at B1: the next block's weights and first tokens are there, and the second tokens are read
+            if (y == B0 || y == B1) barrier_vm<ALL ? Q1 + Q2 : 0>();
+            const int h = y / G, x = y % G, t = x / (2 * GA), k = x / GA % 2, u = x % GA;
+            f32x16& c = acc[t][h * GA + u];
+            if constexpr (EXACT) {
+                const float fw = fp8_scale(sw & 255), fa = fp8_scale(sa[h * GA + u] & 255);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    c = mfma32x32x16(codes_bf16(w.w[t][k][2 * j], w.w[t][k][2 * j + 1], fw),
+                                     codes_bf16(at[h][u].a[k][2 * j], at[h][u].a[k][2 * j + 1], fa), c);
+            } else {
+                c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w.w[t][k], at[h][u].a[k], c, 0, 0, 0, sw, 0, sa[h * GA + u]);
+            }
+            if (y >= B0 && y < B0 + 2 * GA) read_a(SLOT, at[1][(y - B0) / 2], GA + (y - B0) / 2, (y - B0) % 2);
+            if (more && y >= B1 && y < B1 + 2 * GA) read_a(SLOT ^ 1, at[0][(y - B1) / 2], (y - B1) / 2, (y - B1) % 2);
+            if (more && y == B1 + 1) read_scales(SLOT ^ 1, sc_next);
+#pragma unroll
+            for (int j = 0; j < 2 * NT; ++j) {   // the next block's weights, GA products behind the last of those that they replace
+                const int at_y = B1 + j * GA + GA - 1;
+                if (at_y == y && more) read_w(SLOT ^ 1, w, j / 2, j % 2);
+                if (at_y == y + 2 * G) read_w(SLOT, w, j / 2, j % 2);
+            }
+            constexpr int EACH = Q1 > G ? 2 : 1;   // instructions a product
+            if (refill) {
+                const int from = y >= B1 ? B1 : B0, n = y >= B1 ? Q2 : Q1;   // the first has ended when the second begins
+#pragma unroll
+                for (int q = EACH * (y - from); q < EACH * (y - from + 1); ++q)
+                    if (q >= 0 && q < n) issue(kt + 2, SLOT, y >= B1, q);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        sc = sc_next;
+    };
+    static_assert(2 * G >= Q1 && G >= Q2, "a refill within half a block");
+
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+        if (b < nk) {
+#pragma unroll
+            for (int q = 0; q < Q1; ++q) issue(b, b, 0, q);
+#pragma unroll
+            for (int q = 0; q < Q2; ++q) issue(b, b, 1, q);
+        }
+    if (nk > 1) wait_vm<Q1 + 2 * Q2>();
+    else wait_vm<0>();
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) read_w(0, w, t, k);
+#pragma unroll
+        for (int u = 0; u < GA; ++u) read_a(0, at[0][u], u, k);
+    }
+    read_scales(0, sc);
+    constexpr std::integral_constant<int, 0> even{};
+    constexpr std::integral_constant<int, 1> odd{};
+    int kt = 0;
+    for (; kt + 3 < nk; kt += 2) {
+        block(kt, even, std::true_type{});
+        block(kt + 1, odd, std::true_type{});
+    }
+    for (; kt < nk; kt += 2) {
+        block(kt, even, std::false_type{});
+        if (kt + 1 < nk) block(kt + 1, odd, std::false_type{});
+    }
+
     TO* out = static_cast<TO*>(p.out);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        const int m = m0 + wm * 64 + 16 * t + r16;
+    for (int i = 0; i < MT; ++i) {
+        const int m = m0 + wm * TM + 32 * i + r32;
         if (m >= p.m) continue;
+        TO* row = out + m * p.ldo;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) store4(out + m * p.ldo, n0 + wn * 64 + 16 * i + 4 * g, p.n, vec, acc[i][t]);
+        for (int q = 0; q < 4; ++q) {
+            const int n = n0 + wn * TN + kh * (TN / 2) + q * (TN / 8);
+#pragma unroll
+            for (int t = 0; t < NT; t += 2) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = acc[t][i][4 * q + e];
+                    v[4 + e] = acc[t + 1][i][4 * q + e];
+                }
+                if (part) store8(part + static_cast<int64_t>(m) * p.n + n + 4 * t, p.n % 4 == 0, p.n - n - 4 * t, v);
+                else store8(row + n + 4 * t, vec, p.n - n - 4 * t, v);
+            }
+        }
     }
+}
+
+template <int BM, int BN> constexpr int kTileLds = 2 * (BM * 128 + 2048) + 2 * BN * 128;
+
+// Tile number `tile` of tm: tokens fastest inside groups of gm.
+__device__ __forceinline__ void tile_of(const TileMap& tm, int tile, int* m_tile, int* n_tile) {
+    const int grp = tile / (tm.gm * tm.n_tiles);
+    const int rem = tile - grp * tm.gm * tm.n_tiles;
+    const int gsz = min(tm.gm, tm.m_tiles - grp * tm.gm);
+    *m_tile = grp * tm.gm + rem % gsz;
+    *n_tile = rem / gsz;
+}
+
+// Workgroup 8 j + x runs on XCD x, which takes an eighth of the tiles: those that it runs together share operands in its L2.
+// -1: none.
+__device__ __forceinline__ int tile_of_workgroup(int w, int tiles) {
+    const int per = (tiles + 7) >> 3, j = w >> 3, tile = (w & 7) * per + j;
+    return j < per && tile < tiles ? tile : -1;
+}
+
+// 128 x 128 tiles, two workgroups a CU; blockIdx.y: the K slice of `per` blocks.
+template <typename TO, bool EXACT>
+__global__ void __launch_bounds__(256, 2) gemm_fp8_small_kernel(Fp8Gemm p, TileMap tm, int per, bool vec) {
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[kTileLds<128, 128>];
+    const int tile = tile_of_workgroup(blockIdx.x, tm.m_tiles * tm.n_tiles);
+    if (tile < 0) return;
+    int mt, nt;
+    tile_of(tm, tile, &mt, &nt);
+    const int k0 = blockIdx.y * per;
+    float* part = p.part ? p.part + static_cast<int64_t>(blockIdx.y) * p.m * p.n : nullptr;
+    tile_fp8<128, 128, TO, EXACT>(p, mt * 128, nt * 128, k0, min(per, p.kb - k0), smem, vec, part);
+}
+
+// 256 x 256 tiles, one workgroup a CU.  The last `quartered` tiles are cut into four of 128 x 128.
+template <typename TO>
+__global__ void __launch_bounds__(256, 1) gemm_fp8_large_kernel(Fp8Gemm p, TileMap tm, int quartered, bool vec) {
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[kTileLds<256, 256>];
+    const int whole = tm.m_tiles * tm.n_tiles - quartered, first = (whole + 7) / 8 * 8;
+    int mt, nt;
+    if (static_cast<int>(blockIdx.x) < first) {
+        const int tile = tile_of_workgroup(blockIdx.x, whole);
+        if (tile < 0) return;
+        tile_of(tm, tile, &mt, &nt);
+        tile_fp8<256, 256, TO, false>(p, mt * 256, nt * 256, 0, p.kb, smem, vec, nullptr);
+        return;
+    }
+    const int q = blockIdx.x - first;
+    tile_of(tm, whole + q / 4, &mt, &nt);
+    const int m0 = mt * 256 + (q & 1) * 128, n0 = nt * 256 + (q >> 1 & 1) * 128;
+    if (m0 >= p.m || n0 >= p.n) return;
+    tile_fp8<128, 128, TO, false>(p, m0, n0, 0, p.kb, smem, vec, nullptr);
+}
+
+// Sum of the K slices, in their order.
+template <typename TO>
+__global__ void __launch_bounds__(256) gemm_fp8_join_kernel(Fp8Gemm p, int slices, bool vec) {
+    const int per_row = (p.n + 3) / 4;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int m = static_cast<int>(at / per_row), n = 4 * static_cast<int>(at - static_cast<int64_t>(m) * per_row);
+    if (m >= p.m) return;
+    const float* src = p.part + static_cast<int64_t>(m) * p.n + n;
+    const int64_t step = static_cast<int64_t>(p.m) * p.n;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (p.n % 4 == 0) {
+        for (int s = 0; s < slices; ++s) v += *reinterpret_cast<const f32x4*>(src + s * step);
+    } else {
+        for (int s = 0; s < slices; ++s)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < p.n) v[e] += src[s * step + e];
+    }
+    store4(static_cast<TO*>(p.out) + m * p.ldo, n, p.n, vec, v);
+}
+
+// ---------------------------------------------------------------------------
+// Which kernel, and how many K slices.
+// ---------------------------------------------------------------------------
+struct Plan { int kind; int slices, per; int quartered; };   // kind: 0 16 weights, 1 64 weights a workgroup, 2 small tiles, 3 large tiles
+
+constexpr int kCus = 256;
+
+int up(int a, int b) { return (a + b - 1) / b; }
+
+Plan plan_of(int m, int n, int kb, bool fp32) {
+    Plan q{2, 1, kb, 0};
+    if (m <= 32) {
+        q.kind = up(n, 64) >= 2 * kCus ? 1 : 0;
+        const int wg = up(n, q.kind ? 64 : 16), waves = q.kind ? 4 : 8;
+        if (wg < kCus / 2) q.slices = std::min(kCus / wg, kb / (2 * waves));
+    } else {
+        const int large = up(m, 256) * up(n, 256), small = up(m, 128) * up(n, 128);
+        if (!fp32 && small > 2 * kCus) {
+            q.kind = 3;
+            const int rest = large % kCus;
+            q.quartered = rest <= kCus / 4 ? rest : 0;
+            return q;
+        }
+        if (small <= kCus) {
+            // times in us: a block of K alone on a CU and beside another workgroup; the slices' sums written and read at 5 TB/s
+            double best = 0.73 * kb;
+            for (int s = 2; s <= 16 && s <= kb; ++s) {
+                const int wg = small * s;
+                const double t = up(kb, s) * (wg <= kCus ? 0.73 : 1.18 * up(wg, 2 * kCus)) + 4.0 + 8e-6 * s * m * n / 5.0;
+                if (t < best) {
+                    best = t;
+                    q.slices = s;
+                }
+            }
+        }
+    }
+    if (q.slices < 2) q.slices = 1;
+    q.per = up(kb, q.slices);
+    q.slices = up(kb, q.per);
+    return q;
+}
+
+template <typename TO, int RW, int MT, int WV> void gemv(const Fp8Gemm& g, const Plan& q, bool vec, hipStream_t s) {
+    const dim3 grid(up(g.n, 16 * RW), q.slices);
+    if (q.slices > 1) gemv_fp8_kernel<TO, RW, MT, WV, true><<<grid, 64 * WV, 0, s>>>(g, q.per, vec);
+    else gemv_fp8_kernel<TO, RW, MT, WV, false><<<grid, 64 * WV, 0, s>>>(g, q.per, vec);
+}
+
+template <typename TO> void run_plan(const Fp8Gemm& a, const Plan& q, hipStream_t s) {
+    constexpr bool EXACT = sizeof(TO) == 4;
+    Fp8Gemm g = a;
+    if (q.slices == 1) g.part = nullptr;
+    const bool vec = rows_on_16(g.out, g.ldo, sizeof(TO));
+    if (q.kind == 0) {
+        if (g.m <= 16) gemv<TO, 1, 1, 8>(g, q, vec, s);
+        else gemv<TO, 1, 2, 8>(g, q, vec, s);
+    } else if (q.kind == 1) {
+        if (g.m <= 16) gemv<TO, 4, 1, 4>(g, q, vec, s);
+        else gemv<TO, 4, 2, 4>(g, q, vec, s);
+    } else {
+        const int b = q.kind == 3 ? 256 : 128;
+        TileMap tm{up(g.m, b), up(g.n, b), 0};
+        tm.gm = std::min(tm.m_tiles, 8);
+        const int tiles = tm.m_tiles * tm.n_tiles - q.quartered;
+        if constexpr (!EXACT)
+            if (q.kind == 3) {
+                gemm_fp8_large_kernel<TO><<<up(tiles, 8) * 8 + 4 * q.quartered, 256, 0, s>>>(g, tm, q.quartered, vec);
+                return;
+            }
+        gemm_fp8_small_kernel<TO, EXACT><<<dim3(up(tiles, 8) * 8, q.slices), 256, 0, s>>>(g, tm, q.per, vec);
+    }
+    if (q.slices > 1)
+        gemm_fp8_join_kernel<TO><<<static_cast<int>((static_cast<int64_t>(g.m) * up(g.n, 4) + 255) / 256), 256, 0, s>>>(g, q.slices, vec);
 }
 
 }  // namespace
 
-size_t gemm_fp8_ws_bytes(int, int, int) { return 0; }
+size_t gemm_fp8_ws_bytes(int m, int n, int kb) {
+    // of either output type
+    const int s = std::max(plan_of(m, n, kb, false).slices, plan_of(m, n, kb, true).slices);
+    return s > 1 ? sizeof(float) * static_cast<size_t>(s) * m * n : 0;
+}
 
 hipError_t launch_gemm_fp8(const Fp8Gemm& g, hipStream_t s) {
-    const dim3 grid((g.n + 127) / 128, (g.m + 127) / 128);
-    const bool vec = rows_on_16(g.out, g.ldo, g.out_dt == RL_DTYPE_FP32 ? 4 : 2);
-    if (g.out_dt == RL_DTYPE_FP32) gemm_fp8_kernel<float, true><<<grid, 256, 0, s>>>(g, vec);
-    else gemm_fp8_kernel<uint16_t, false><<<grid, 256, 0, s>>>(g, vec);
+    const Plan q = plan_of(g.m, g.n, g.kb, g.out_dt == RL_DTYPE_FP32);
+    if (g.out_dt == RL_DTYPE_FP32) run_plan<float>(g, q, s);
+    else run_plan<uint16_t>(g, q, s);
     return hipGetLastError();
 }
 
