@@ -123,7 +123,7 @@ size_t rl_attention_quant_workspace_bytes(int32_t n, int32_t n_kv_heads, int32_t
         n_q_heads / n_kv_heads > 16 || (head_dim != 64 && head_dim != 128) || max_length < 0 ||
         !attention_fp8_fits(n, n_kv_heads, max_length))
         return 0;
-    return attention_fp8_ws_bytes(n, n_kv_heads, head_dim, max_length);
+    return attention_fp8_ws_bytes(n, n_kv_heads, n_q_heads, head_dim, max_length);
 }
 
 rl_status rl_attention_quant(const rl_kv_fp8* cache, int32_t n, const int32_t* seqs, const int32_t* lengths, int32_t max_length,
@@ -137,7 +137,7 @@ rl_status rl_attention_quant(const rl_kv_fp8* cache, int32_t n, const int32_t* s
     if (!attention_fp8_fits(n, c.heads, max_length)) return RL_ERR_UNSUPPORTED;
     const int64_t width = static_cast<int64_t>(n_q_heads) * c.dim;
     if (!lengths || !rows_ok(dtype, q, n, width, ldq) || !rows_ok(dtype, out, n, width, ldo)) return RL_ERR_INVALID_ARG;
-    if (const rl_status st = workspace_ok(workspace, ws_bytes, attention_fp8_ws_bytes(n, c.heads, c.dim, max_length)); st != RL_OK)
+    if (const rl_status st = workspace_ok(workspace, ws_bytes, attention_fp8_ws_bytes(n, c.heads, n_q_heads, c.dim, max_length)); st != RL_OK)
         return st;
     const AttnFp8 a{c, n, max_length, seqs, lengths, q, ldq, out, ldo, dtype, n_q_heads, static_cast<float>(scale),
                     static_cast<float*>(workspace)};

@@ -64,10 +64,10 @@ struct AttnFp8 {
     float* part;
 };
 bool attention_fp8_fits(int n, int kv_heads, int max_length);   // its workgroups can be counted in 31 bits
-size_t attention_fp8_ws_bytes(int n, int kv_heads, int dim, int max_length);
+size_t attention_fp8_ws_bytes(int n, int kv_heads, int heads, int dim, int max_length);
 hipError_t launch_attention_fp8(const AttnFp8& a, hipStream_t s);
 
-inline __host__ bool rows_on_16(const void* p, int64_t ld, size_t es) {
+inline __host__ __device__ bool rows_on_16(const void* p, int64_t ld, size_t es) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * es) % 16 == 0;
 }
 

@@ -32,37 +32,73 @@ template <int N> __device__ __forceinline__ void split_bf16(const float* v, bf16
         }
 }
 
-// Partial results of one (row, kv-head, chunk): sums [16][D], then maxima [16] and totals [16].
-template <int D> constexpr int kPartFloats = 16 * D + 32;
+// Four entries of a row; nothing to attend to: zeros.
+template <typename T> __device__ __forceinline__ void write_out(T* out, int at, f32x4 o, float L) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) Elem<T>::store(out, at + e, L == 0.0f ? 0.0f : o[e] / L);
+}
 
+// Partial results of one (row, kv-head, chunk): sums [G][D], then maxima [G] and totals [G].
+__host__ __device__ constexpr int part_floats(int G, int D) { return G * (D + 2); }
+
+// A workgroup takes one chunk of one row's positions for one kv-head, its waves every
+// fourth step of 32, the next step's loads under this one's arithmetic.
 template <typename T, int D, int QT, int PT>
 __global__ void __launch_bounds__(64 * kWaves) attention_fp8_kernel(AttnFp8 p, int chunk, int n_chunks) {
     constexpr int NQ = D / 64;          // 16-byte K loads a row, of 4 lane groups
     constexpr int NV = D / 32;          // 16-byte V loads a lane: two entries each
     const int c = blockIdx.x % n_chunks, pair = blockIdx.x / n_chunks;
     const int row = pair / p.c.heads, kvh = pair - row * p.c.heads;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
     const int G = p.heads / p.c.heads;
     const int seq = p.seqs ? p.seqs[row] : row;
     int len = p.lengths[row];
     len = len < 0 || seq < 0 || seq >= p.c.n_seqs ? 0 : len > p.max_length ? p.max_length : len;
     const int lo = c * chunk, hi = len - lo < chunk ? len : lo + chunk;
+    float* part = n_chunks > 1 ? p.part + (static_cast<int64_t>(pair) * n_chunks + c) * part_floats(G, D) : nullptr;
+    if (part && lo >= hi) return;       // the join goes by the length
 
-    __shared__ __attribute__((aligned(16))) float sums[kWaves][16 * D];
-    __shared__ float maxs[kWaves][16], tots[kWaves][16];
+    const int first = lo + kStep * wave;
+    const int steps = first < hi ? (hi - first + kStep * kWaves - 1) / (kStep * kWaves) : 0;
+    // page of step i in lane i (at most 64 steps: kMaxChunk)
+    int pages = -1;
+    if (lane < steps) pages = p.c.table[static_cast<int64_t>(seq) * p.c.max_pages + (first + kStep * kWaves * lane) / p.c.page];
+
+    // K row r of tile t is position 8 (r / 4) + r % 4 + 4 t of the step
+    struct Step { u32x4 k[2][NQ], v[NV]; uint2 ks, vs; bool there; };
+    auto load = [&](int i, Step& s) {
+        const int pg = __builtin_amdgcn_readlane(pages, i);
+        s.there = pg >= 0 && pg < p.c.n_pages;
+        if (!s.there) return;           // no such page: nothing there to attend to
+        const int local = (first + kStep * kWaves * i) % p.c.page;
+        const uint8_t* blk = p.c.pool + (static_cast<int64_t>(pg) * p.c.heads + kvh) * p.c.block;
+        const uint8_t* vb = blk + p.c.page * D;
+        const uint8_t* sb = vb + p.c.page * D;
+        const int pos = local + 8 * (r >> 2) + (r & 3);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int u = 0; u < NQ; ++u) s.k[t][u] = ld16(blk + (pos + 4 * t) * D + 64 * u + 16 * g);
+        s.ks = *reinterpret_cast<const uint2*>(sb + local + 8 * (r >> 2));
+        s.vs = *reinterpret_cast<const uint2*>(sb + p.c.page + local + 8 * g);
+#pragma unroll
+        for (int i2 = 0; i2 < NV; ++i2) s.v[i2] = ld16(vb + ((local / 8 + g) * D + 32 * i2 + 2 * r) * 8);
+    };
+    Step s0, s1;
+    if (steps > 0) load(0, s0);
 
     // the queries: lane (r, g) holds head r, entries 64 u + 16 g + 8 v .. + 7 for (u, v)
     bf16x8 q[NQ][2][QT];
     {
-        const T* src = static_cast<const T*>(p.q) + row * p.ldq + (kvh * G + r) * D;
+        const T* src = static_cast<const T*>(p.q) + row * p.ldq + (kvh * G + (r < G ? r : 0)) * D + 16 * g;
+        const bool vec = rows_on_16(p.q, p.ldq, sizeof(T));
 #pragma unroll
         for (int u = 0; u < NQ; ++u)
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
                 float x[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = r < G ? Elem<T>::load(src, 64 * u + 16 * g + 8 * v + j) : 0.0f;
+                load8(src + 64 * u + 8 * v, vec, r < G ? 8 : 0, x);
                 split_bf16<QT>(x, q[u][v]);
             }
     }
@@ -74,25 +110,10 @@ __global__ void __launch_bounds__(64 * kWaves) attention_fp8_kernel(AttnFp8 p, i
         for (int v = 0; v < 2; ++v) acc[i][v] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.0f;
 
-    const int32_t* table = p.c.table + static_cast<int64_t>(seq) * p.c.max_pages;
-    for (int at = lo + kStep * wave; at < hi; at += kStep * kWaves) {
-        const int j = at / p.c.page, local = at - j * p.c.page;
-        const int pg = table[j];
-        if (pg < 0 || pg >= p.c.n_pages) continue;   // no such page: nothing there to attend to
-        const uint8_t* blk = p.c.pool + (static_cast<int64_t>(pg) * p.c.heads + kvh) * p.c.block;
-        const uint8_t* vb = blk + p.c.page * D;
-        const uint8_t* sb = vb + p.c.page * D;
-        // K row r of tile t is position 8 (r / 4) + r % 4 + 4 t of the step
-        const int pos = local + 8 * (r >> 2) + (r & 3);
-        u32x4 kw[2][NQ], vw[NV];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int u = 0; u < NQ; ++u) kw[t][u] = ld16(blk + (pos + 4 * t) * D + 64 * u + 16 * g);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) vw[i] = ld16(vb + ((local / 8 + g) * D + 32 * i + 2 * r) * 8);
-        const float ks0 = fp8_scale(sb[pos]), ks1 = fp8_scale(sb[pos + 4]);
-        const uint2 vsb = *reinterpret_cast<const uint2*>(sb + p.c.page + local + 8 * g);
+    auto take = [&](int i, Step& st) {
+        if (!st.there) return;
+        const uint32_t kw = (r & 3) * 8;
+        const float ks0 = fp8_scale((st.ks.x >> kw) & 255u), ks1 = fp8_scale((st.ks.y >> kw) & 255u);
         f32x4 s[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -101,16 +122,28 @@ __global__ void __launch_bounds__(64 * kWaves) attention_fp8_kernel(AttnFp8 p, i
             for (int u = 0; u < NQ; ++u)
 #pragma unroll
                 for (int v = 0; v < 2; ++v) {
-                    const bf16x8 k = codes_bf16(kw[t][u][2 * v], kw[t][u][2 * v + 1], t ? ks1 : ks0);
+                    const bf16x8 k = codes_bf16(st.k[t][u][2 * v], st.k[t][u][2 * v + 1], t ? ks1 : ks0);
 #pragma unroll
                     for (int w = 0; w < QT; ++w) s[t] = mfma16x16x32(k, q[u][v][w], s[t]);
                 }
         }
         // this lane's positions are 8 g .. 8 g + 7 of the step: tile 0 has the first four
         float x[8];
+        const int at = first + kStep * kWaves * i;
         const int left = hi - at - 8 * g;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = e < left ? s[e >> 2][e & 3] * to_log2 : -INFINITY;
+        for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * to_log2;
+        if (hi - at < kStep) {
+            // nothing of what stands behind the last position may enter the sums or the products
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e >= left) x[e] = -INFINITY;
+            const int n = left < 0 ? 0 : left > 8 ? 8 : left;   // bytes kept of each entry's eight
+            const uint32_t lom = n >= 4 ? ~0u : (1u << (8 * n)) - 1u, him = n >= 8 ? ~0u : n <= 4 ? 0u : (1u << (8 * (n - 4))) - 1u;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) st.v[j] = u32x4{st.v[j][0] & lom, st.v[j][1] & him, st.v[j][2] & lom, st.v[j][3] & him};
+            st.vs = make_uint2(st.vs.x & lom, st.vs.y & him);
+        }
         float mx = x[0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
@@ -124,48 +157,53 @@ __global__ void __launch_bounds__(64 * kWaves) attention_fp8_kernel(AttnFp8 p, i
         for (int e = 0; e < 8; ++e) {
             const float w = __builtin_amdgcn_exp2f(x[e] - base);
             sum += w;
-            // nothing of what stands behind the last position may enter the products
-            pv[e] = e < left ? w * fp8_scale(((e < 4 ? vsb.x : vsb.y) >> (8 * (e & 3))) & 255u) : 0.0f;
-        }
-        if (left < 8) {
-            const int n = left < 0 ? 0 : left;   // bytes kept of each entry's eight
-            const uint32_t lom = n >= 4 ? ~0u : (1u << (8 * n)) - 1u, him = n <= 4 ? 0u : (1u << (8 * (n - 4))) - 1u;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) vw[i] = u32x4{vw[i][0] & lom, vw[i][1] & him, vw[i][2] & lom, vw[i][3] & him};
+            pv[e] = w * fp8_scale(((e < 4 ? st.vs.x : st.vs.y) >> (8 * (e & 3))) & 255u);
         }
         l = l * keep + sum;
         m = m_new;
         bf16x8 pt[PT];
         split_bf16<PT>(pv, pt);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
-                acc[i][v] *= keep;
-                const bf16x8 w = codes_bf16(vw[i][2 * v], vw[i][2 * v + 1], 1.0f);
+                acc[j][v] *= keep;
+                const bf16x8 w = codes_bf16(st.v[j][2 * v], st.v[j][2 * v + 1], 1.0f);
 #pragma unroll
-                for (int t = 0; t < PT; ++t) acc[i][v] = mfma16x16x32(w, pt[t], acc[i][v]);
+                for (int t = 0; t < PT; ++t) acc[j][v] = mfma16x16x32(w, pt[t], acc[j][v]);
             }
+    };
+    for (int i = 0; i < steps; i += 2) {
+        if (i + 1 < steps) load(i + 1, s1);
+        take(i, s0);
+        if (i + 1 >= steps) break;
+        if (i + 2 < steps) load(i + 2, s0);
+        take(i + 1, s1);
     }
+
+    extern __shared__ __attribute__((aligned(16))) float sums[];   // [kWaves][G * D]
+    __shared__ float maxs[kWaves][16], tots[kWaves][16];
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     if (g == 0) {
         maxs[wave][r] = m;
         tots[wave][r] = l;
     }
-    // acc[i][v][e] is entry 32 i + 8 g + 2 e + v of head r
+    // acc[j][v][e] is entry 32 j + 8 g + 2 e + v of head r
+    if (r < G) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int v = 0; v < 2; ++v) sums[wave][r * D + 32 * i + 8 * g + 2 * e + v] = acc[i][v][e];
+        for (int j = 0; j < NV; ++j) {
+            float* to = sums + (wave * G + r) * D + 32 * j + 8 * g;
+            *reinterpret_cast<f32x4*>(to) = f32x4{acc[j][0][0], acc[j][1][0], acc[j][0][1], acc[j][1][1]};
+            *reinterpret_cast<f32x4*>(to + 4) = f32x4{acc[j][0][2], acc[j][1][2], acc[j][0][3], acc[j][1][3]};
+        }
+    }
     __syncthreads();
-    float* part = n_chunks > 1 ? p.part + (static_cast<int64_t>(pair) * n_chunks + c) * kPartFloats<D> : nullptr;
     T* out = static_cast<T*>(p.out) + row * p.ldo + kvh * G * D;
-    for (int at = tid; at < G * D; at += 64 * kWaves) {
+    for (int at = 4 * tid; at < G * D; at += 4 * 64 * kWaves) {
         const int h = at / D;
-        float M = -INFINITY, L = 0.0f, o = 0.0f;
+        float M = -INFINITY, L = 0.0f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) M = fmaxf(M, maxs[w][h]);
         const float base = M == -INFINITY ? 0.0f : M;
@@ -173,49 +211,77 @@ __global__ void __launch_bounds__(64 * kWaves) attention_fp8_kernel(AttnFp8 p, i
         for (int w = 0; w < kWaves; ++w) {
             const float f = __builtin_amdgcn_exp2f(maxs[w][h] - base);
             L += f * tots[w][h];
-            o += f * sums[w][at];
+            o += f * *reinterpret_cast<const f32x4*>(sums + w * G * D + at);
         }
         if (part) {
-            part[at] = o;
+            *reinterpret_cast<float2*>(part + at) = make_float2(o[0], o[1]);
+            *reinterpret_cast<float2*>(part + at + 2) = make_float2(o[2], o[3]);
             if (at - h * D == 0) {
-                part[16 * D + h] = M;
-                part[16 * D + 16 + h] = L;
+                part[G * D + h] = M;
+                part[G * D + G + h] = L;
             }
         } else {
-            Elem<T>::store(out, at, L == 0.0f ? 0.0f : o / L);   // nothing to attend to: zeros
+            write_out(out, at, o, L);
         }
     }
 }
 
-// The chunks of one (row, kv-head), joined in their order.
+// The chunks of one (row, kv-head), joined in their order; four entries a thread.
 template <typename T, int D>
-__global__ void __launch_bounds__(256) attention_fp8_join_kernel(AttnFp8 p, int n_chunks) {
+__global__ void __launch_bounds__(256) attention_fp8_join_kernel(AttnFp8 p, int chunk, int n_chunks) {
+    constexpr int U = 8;   // chunks whose loads are in flight together
     const int row = blockIdx.x / p.c.heads, kvh = blockIdx.x - row * p.c.heads;
-    const int G = p.heads / p.c.heads;
-    const float* part = p.part + static_cast<int64_t>(blockIdx.x) * n_chunks * kPartFloats<D>;
+    const int G = p.heads / p.c.heads, step = part_floats(G, D);
+    const int seq = p.seqs ? p.seqs[row] : row;
+    int len = p.lengths[row];
+    len = len < 0 || seq < 0 || seq >= p.c.n_seqs ? 0 : len > p.max_length ? p.max_length : len;
+    const int n = (len + chunk - 1) / chunk;   // chunks with a position
+    const float* part = p.part + static_cast<int64_t>(blockIdx.x) * n_chunks * step;
     T* out = static_cast<T*>(p.out) + row * p.ldo + kvh * G * D;
-    for (int at = threadIdx.x; at < G * D; at += 256) {
+    for (int at = 4 * threadIdx.x; at < G * D; at += 4 * 256) {
         const int h = at / D;
-        float M = -INFINITY;
-        for (int c = 0; c < n_chunks; ++c) M = fmaxf(M, part[c * kPartFloats<D> + 16 * D + h]);
-        const float base = M == -INFINITY ? 0.0f : M;
-        float L = 0.0f, o = 0.0f;
-        for (int c = 0; c < n_chunks; ++c) {
-            const float* q = part + c * kPartFloats<D>;
-            const float f = __builtin_amdgcn_exp2f(q[16 * D + h] - base);
-            L += f * q[16 * D + 16 + h];
-            o += f * q[at];
+        float M = -INFINITY, L = 0.0f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        for (int c0 = 0; c0 < n; c0 += U) {
+            float cm[U], cl[U];
+            float2 a[U], b[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float* q = part + static_cast<int64_t>(c0 + u < n ? c0 + u : c0) * step;
+                cm[u] = q[G * D + h];
+                cl[u] = q[G * D + G + h];
+                a[u] = *reinterpret_cast<const float2*>(q + at);
+                b[u] = *reinterpret_cast<const float2*>(q + at + 2);
+            }
+            float m_new = M;
+#pragma unroll
+            for (int u = 0; u < U; ++u) m_new = fmaxf(m_new, cm[u]);
+            const float base = m_new == -INFINITY ? 0.0f : m_new;
+            const float keep = __builtin_amdgcn_exp2f(M - base);
+            L *= keep;
+            o *= keep;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float f = c0 + u < n ? __builtin_amdgcn_exp2f(cm[u] - base) : 0.0f;
+                if (c0 + u < n) {
+                    L += f * cl[u];
+                    o += f * f32x4{a[u].x, a[u].y, b[u].x, b[u].y};
+                }
+            }
+            M = m_new;
         }
-        Elem<T>::store(out, at, L == 0.0f ? 0.0f : o / L);
+        write_out(out, at, o, L);
     }
 }
 
 // Positions a workgroup takes, a multiple of 128.
+constexpr int kMaxChunk = 64 * kStep * kWaves;
 int chunk_of(int n, int kv_heads, int max_length) {
     int chunk = 1024;
     while (chunk > 256 && static_cast<int64_t>(n) * kv_heads * ((max_length + chunk - 1) / chunk) < 1024) chunk /= 2;
     return chunk;
 }
+static_assert(1024 <= kMaxChunk, "a step's page in a lane");
 int chunks_of(int n, int kv_heads, int max_length) {
     const int c = chunk_of(n, kv_heads, max_length);
     const int k = (max_length + c - 1) / c;
@@ -224,8 +290,9 @@ int chunks_of(int n, int kv_heads, int max_length) {
 
 template <typename T, int D, int QT, int PT> hipError_t attend(const AttnFp8& a, hipStream_t s) {
     const int chunk = chunk_of(a.n, a.c.heads, a.max_length), n_chunks = chunks_of(a.n, a.c.heads, a.max_length);
-    attention_fp8_kernel<T, D, QT, PT><<<a.n * a.c.heads * n_chunks, 64 * kWaves, 0, s>>>(a, chunk, n_chunks);
-    if (n_chunks > 1) attention_fp8_join_kernel<T, D><<<a.n * a.c.heads, 256, 0, s>>>(a, n_chunks);
+    const int lds = kWaves * (a.heads / a.c.heads) * D * sizeof(float);
+    attention_fp8_kernel<T, D, QT, PT><<<a.n * a.c.heads * n_chunks, 64 * kWaves, lds, s>>>(a, chunk, n_chunks);
+    if (n_chunks > 1) attention_fp8_join_kernel<T, D><<<a.n * a.c.heads, 256, 0, s>>>(a, chunk, n_chunks);
     return hipGetLastError();
 }
 
@@ -234,9 +301,9 @@ template <typename T, int D, int QT, int PT> hipError_t attend(const AttnFp8& a,
 bool attention_fp8_fits(int n, int kv_heads, int max_length) {
     return static_cast<int64_t>(n) * kv_heads * chunks_of(n, kv_heads, max_length) < (int64_t(1) << 31);
 }
-size_t attention_fp8_ws_bytes(int n, int kv_heads, int dim, int max_length) {
+size_t attention_fp8_ws_bytes(int n, int kv_heads, int heads, int dim, int max_length) {
     const int c = chunks_of(n, kv_heads, max_length);
-    return c > 1 ? sizeof(float) * static_cast<size_t>(n) * kv_heads * c * (16 * dim + 32) : 0;
+    return c > 1 ? sizeof(float) * static_cast<size_t>(n) * kv_heads * c * part_floats(heads / kv_heads, dim) : 0;
 }
 
 hipError_t launch_attention_fp8(const AttnFp8& a, hipStream_t s) {
