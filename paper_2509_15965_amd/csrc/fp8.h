@@ -84,20 +84,10 @@ __device__ __forceinline__ int fp8_scale_byte(float a) {
 __device__ __forceinline__ float fp8_scale(int b) { return __uint_as_float(static_cast<uint32_t>(b) << 23); }
 __device__ __forceinline__ float fp8_inverse(int b) { return __uint_as_float(static_cast<uint32_t>(254 - b) << 23); }
 
-// |v|, or 0 where v is not finite: what a block's scale goes by
-__device__ __forceinline__ float finite_abs(float v) {
-    const float a = fabsf(v);
-    return a <= 3.402823466e38f ? a : 0.0f;
-}
-// v to be rounded to a code: infinities are NaN in this format
-__device__ __forceinline__ float fp8_arg(float v, float inv) {
-    const float t = v * inv;
-    return fabsf(t) <= 448.0f ? t : __uint_as_float(0x7FC00000u);
-}
-// four codes of four numbers, the first in the lowest byte (round to nearest even)
+// four codes of four numbers, the first in the lowest byte (round to nearest even; NaN stays)
 __device__ __forceinline__ uint32_t fp8_pack4(const float* v, float inv) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(fp8_arg(v[0], inv), fp8_arg(v[1], inv), 0, false);
-    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(fp8_arg(v[2], inv), fp8_arg(v[3], inv), w, true));
+    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inv, v[1] * inv, 0, false);
+    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inv, v[3] * inv, w, true));
 }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -110,63 +100,119 @@ __device__ __forceinline__ bf16x8 codes_bf16(uint32_t lo, uint32_t hi, float sca
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// Eight entries of a row, of which `left` are there (the others are 0); vec:
-// the row starts on 16 bytes.
-template <typename T> __device__ __forceinline__ void load8(const T* p, bool vec, int left, float* v) {
-    if (vec && left >= 8) {
+// Entries of a row that a lane moves at once: 16 bytes of its type.
+template <typename T> constexpr int kEntries = 16 / sizeof(T);
+
+// E entries of a row, of which `left` are there (the others are 0); vec: the row starts on 16 bytes.
+template <int E, typename T> __device__ __forceinline__ void load_row(const T* p, bool vec, int left, float* v) {
+    if (vec && left >= E) {
         if constexpr (sizeof(T) == 4) {
-            const u32x4 a = ld16(p), b = ld16(p + 4);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[e] = __uint_as_float(a[e]);
-                v[4 + e] = __uint_as_float(b[e]);
+            for (int q = 0; q < E; q += 4) {
+                const u32x4 a = ld16(p + q);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[q + e] = __uint_as_float(a[e]);
             }
-        } else {
+        } else if constexpr (E == 8) {
             const u32x4 a = ld16(p);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 v[2 * e] = __uint_as_float(a[e] << 16);
                 v[2 * e + 1] = __uint_as_float(a[e] & 0xFFFF0000u);
             }
-        }
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < left ? Elem<T>::load(p, e) : 0.0f;
-}
-template <typename T> __device__ __forceinline__ void store8(T* p, bool vec, int left, const float* v) {
-    if (vec && left >= 8) {
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-            *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
         } else {
-            u32x4 w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                w[e] = f32_to_bf16(v[2 * e]) | static_cast<uint32_t>(f32_to_bf16(v[2 * e + 1])) << 16;
-            *reinterpret_cast<u32x4*>(p) = w;
+            const uint2 a = *reinterpret_cast<const uint2*>(p);
+            v[0] = __uint_as_float(a.x << 16);
+            v[1] = __uint_as_float(a.x & 0xFFFF0000u);
+            v[2] = __uint_as_float(a.y << 16);
+            v[3] = __uint_as_float(a.y & 0xFFFF0000u);
         }
         return;
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < E; ++e) v[e] = e < left ? Elem<T>::load(p, e) : 0.0f;
+}
+template <int E, typename T> __device__ __forceinline__ void store_row(T* p, bool vec, int left, const float* v) {
+    if (vec && left >= E) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int q = 0; q < E; q += 4) *reinterpret_cast<f32x4*>(p + q) = f32x4{v[q], v[q + 1], v[q + 2], v[q + 3]};
+        } else {
+            uint32_t w[E / 2];
+#pragma unroll
+            for (int e = 0; e < E / 2; ++e) w[e] = f32_to_bf16(v[2 * e]) | static_cast<uint32_t>(f32_to_bf16(v[2 * e + 1])) << 16;
+            if constexpr (E == 8) *reinterpret_cast<u32x4*>(p) = u32x4{w[0], w[1], w[2], w[3]};
+            else *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
         if (e < left) Elem<T>::store(p, e, v[e]);
 }
 
+// v of the lane N places on in its row of 16 (cyclic)
+template <int N> __device__ __forceinline__ float row_rotated(float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x120 + N, 0xF, 0xF, true));
+}
+// largest of LANES neighbouring lanes (8 .. 64); NaN counts only where there is nothing else
 template <int LANES> __device__ __forceinline__ float lanes_max(float v) {
+    if constexpr (LANES == 8) {
 #pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+        for (int o = 4; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+        return v;
+    }
+    v = fmaxf(v, row_rotated<8>(v));
+    v = fmaxf(v, row_rotated<4>(v));
+    v = fmaxf(v, row_rotated<2>(v));
+    v = fmaxf(v, row_rotated<1>(v));
+#pragma unroll
+    for (int o = 16; o < LANES; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
     return v;
 }
+__device__ __forceinline__ float lanes_sum64(float v) {
+    v += row_rotated<8>(v);
+    v += row_rotated<4>(v);
+    v += row_rotated<2>(v);
+    v += row_rotated<1>(v);
+    v += __shfl_xor(v, 16, 64);
+    return v + __shfl_xor(v, 32, 64);
+}
 
-// The eight numbers of a lane, LANES lanes a block, as codes; the block's scale byte.
-template <int LANES> __device__ __forceinline__ int fp8_encode8(const float* v, uint2* codes) {
+constexpr float kLargestFloat = 3.402823466e38f;
+// Infinities in v become NaN; the largest magnitude of the finite ones.
+template <int E> __device__ __forceinline__ float drop_infinities(float* v) {
     float a = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) a = fmaxf(a, finite_abs(v[e]));
-    const int b = fp8_scale_byte(lanes_max<LANES>(a));
-    const float inv = fp8_inverse(b);
-    *codes = make_uint2(fp8_pack4(v, inv), fp8_pack4(v + 4, inv));
+    for (int e = 0; e < E; ++e) {
+        const bool fine = fabsf(v[e]) <= kLargestFloat;
+        a = fine ? fmaxf(a, fabsf(v[e])) : a;
+        v[e] = fine ? v[e] : __uint_as_float(0x7FC00000u);
+    }
+    return a;
+}
+template <int E> __device__ __forceinline__ float largest(const float* v) {
+    float a = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) a = fmaxf(a, fabsf(v[e]));
+    return a;
+}
+
+template <int E> __device__ __forceinline__ void fp8_pack(const float* v, float inv, uint32_t* codes) {
+#pragma unroll
+    for (int q = 0; q < E / 4; ++q) codes[q] = fp8_pack4(v + 4 * q, inv);
+}
+template <int E> __device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t* codes) {
+    if constexpr (E == 4) *reinterpret_cast<uint32_t*>(p) = codes[0];
+    else *reinterpret_cast<uint2*>(p) = make_uint2(codes[0], codes[1]);
+}
+
+// The E numbers of a lane, LANES lanes a block, as codes; the block's scale byte.
+template <int E, int LANES> __device__ __forceinline__ int fp8_encode(float* v, uint32_t* codes) {
+    float a = lanes_max<LANES>(largest<E>(v));
+    if (a > kLargestFloat) a = lanes_max<LANES>(drop_infinities<E>(v));   // the same in all lanes of the block
+    const int b = fp8_scale_byte(a);
+    fp8_pack<E>(v, fp8_inverse(b), codes);
     return b;
 }
 

@@ -9,33 +9,32 @@ namespace {
 
 // ---------------------------------------------------------------------------
 // RMS norm.  s = x + add (as stored), y = s w / sqrt(mean s^2 + eps), y in blocks of
-// 128.  ROWS rows a workgroup, WAVES waves a row, a row in registers from its one
-// read to its codes: 8 NV entries a lane, 16 lanes a block.
+// 128.  WAVES waves a row, a row in registers from its one read to its codes: NV
+// times 16 bytes of x a lane.
 // ---------------------------------------------------------------------------
 template <typename T, int WAVES, int NV>
 __global__ void __launch_bounds__(256) rmsnorm_fp8_kernel(NormArgs p, bool xvec, bool avec, bool svec, bool wvec) {
-    constexpr int ROWS = 4 / WAVES, LANES = 64 * WAVES;
+    constexpr int E = kEntries<T>, ROWS = 4 / WAVES, LANES = 64 * WAVES;
     const int row = blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / LANES : 0);
     const int lane = threadIdx.x % LANES;
     if (row >= p.n) return;   // whole waves; with several waves a row every workgroup has its row
     const int H = p.hidden, kb = fp8_blocks(H);
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
-    float v[NV][8];
-    float ss = 0.0f;
+    float v[NV][E];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int at = 8 * (lane + LANES * i);
-        load8(x + at, xvec, H - at, v[i]);
+        const int at = E * (lane + LANES * i);
+        load_row<E>(x + at, xvec, H - at, v[i]);
     }
     if (p.add) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int at = 8 * (lane + LANES * i);
-            float b[8];
-            if (p.add_dt == RL_DTYPE_FP32) load8(static_cast<const float*>(p.add) + row * p.ld_add + at, avec, H - at, b);
-            else load8(static_cast<const uint16_t*>(p.add) + row * p.ld_add + at, avec, H - at, b);
+            const int at = E * (lane + LANES * i);
+            float b[E];
+            if (p.add_dt == RL_DTYPE_FP32) load_row<E>(static_cast<const float*>(p.add) + row * p.ld_add + at, avec, H - at, b);
+            else load_row<E>(static_cast<const uint16_t*>(p.add) + row * p.ld_add + at, avec, H - at, b);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < E; ++e) {
                 v[i][e] += b[e];
                 if (sizeof(T) == 2) v[i][e] = bf16_to_f32(f32_to_bf16(v[i][e]));   // the norm is of what is stored
             }
@@ -44,15 +43,16 @@ __global__ void __launch_bounds__(256) rmsnorm_fp8_kernel(NormArgs p, bool xvec,
     if (p.sum) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int at = 8 * (lane + LANES * i);
-            store8(static_cast<T*>(p.sum) + row * p.ld_sum + at, svec, H - at, v[i]);
+            const int at = E * (lane + LANES * i);
+            store_row<E>(static_cast<T*>(p.sum) + row * p.ld_sum + at, svec, H - at, v[i]);
         }
     }
+    float ss = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss += v[i][e] * v[i][e];
-    ss = wave_sum(ss);
+        for (int e = 0; e < E; ++e) ss += v[i][e] * v[i][e];
+    ss = lanes_sum64(ss);
     if constexpr (WAVES > 1) {
         __shared__ float part[WAVES];
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = ss;
@@ -64,85 +64,106 @@ __global__ void __launch_bounds__(256) rmsnorm_fp8_kernel(NormArgs p, bool xvec,
     const float r = 1.0f / sqrtf(ss / static_cast<float>(H) + p.eps);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int at = 8 * (lane + LANES * i);
-        float g[8];
-        if (p.w_dt == RL_DTYPE_FP32) load8(static_cast<const float*>(p.w) + at, wvec, H - at, g);
-        else load8(static_cast<const uint16_t*>(p.w) + at, wvec, H - at, g);
+        const int at = E * (lane + LANES * i);
+        float g[E];
+        if (p.w_dt == RL_DTYPE_FP32) load_row<E>(static_cast<const float*>(p.w) + at, wvec, H - at, g);
+        else load_row<E>(static_cast<const uint16_t*>(p.w) + at, wvec, H - at, g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * r * g[e];
-        if (at + 8 > H) {   // nothing behind the row, whatever r is
+        for (int e = 0; e < E; ++e) v[i][e] = v[i][e] * r * g[e];
+        if (at + E > H) {   // nothing behind the row, whatever r is
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
+            for (int e = 0; e < E; ++e)
                 if (at + e >= H) v[i][e] = 0.0f;
         }
-        uint2 c;
-        const int b = fp8_encode8<16>(v[i], &c);
+        uint32_t c[E / 4];
+        const int b = fp8_encode<E, kFp8Block / E>(v[i], c);
         if (at < kb * kFp8Block) {
-            *reinterpret_cast<uint2*>(p.out.codes + row * p.out.ld + at) = c;
-            if ((lane & 15) == 0) p.out.scales[row * p.out.lds + at / kFp8Block] = static_cast<uint8_t>(b);
+            store_codes<E>(p.out.codes + row * p.out.ld + at, c);
+            if (at % kFp8Block == 0) p.out.scales[row * p.out.lds + at / kFp8Block] = static_cast<uint8_t>(b);
         }
     }
 }
 
 // ---------------------------------------------------------------------------
-// Rows: 16 lanes a block of 128 entries, 8 a lane.
+// Rows: 128 / E lanes a block, U blocks a lane group, 256 / (128 / E) apart.
 // ---------------------------------------------------------------------------
-template <typename T, bool SWIGLU>
+template <typename T, bool SWIGLU, int U>
 __global__ void __launch_bounds__(256) quantise_rows_kernel(int n, int k, const T* __restrict__ x, int64_t ldx, bool vec,
                                                             bool uvec, Fp8Out out) {
+    constexpr int E = kEntries<T>, LANES = kFp8Block / E, GROUPS = 256 / LANES;
     const int kb = fp8_blocks(k);
-    const int unit = blockIdx.x * 16 + (threadIdx.x >> 4);
-    if (unit >= n * kb) return;   // whole groups of 16 lanes
-    const int row = unit / kb, blk = unit - row * kb;
-    const int at = blk * kFp8Block + 8 * (threadIdx.x & 15);
-    const T* xr = x + row * ldx;
-    float v[8];
-    load8(xr + at, vec, k - at, v);
-    if (SWIGLU) {
-        float u[8];
-        load8(xr + k + at, uvec, k - at, u);
+    const int lane = threadIdx.x % LANES;
+    float v[U][E], u[U][SWIGLU ? E : 1];
+    int row[U], blk[U];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = v[e] / (1.0f + expf(-v[e])) * u[e];
+    for (int i = 0; i < U; ++i) {
+        const int unit = (blockIdx.x * U + i) * GROUPS + threadIdx.x / LANES;
+        row[i] = unit / kb;
+        blk[i] = unit - row[i] * kb;
+        const int at = blk[i] * kFp8Block + E * lane;
+        const T* xr = x + static_cast<int64_t>(row[i]) * ldx + at;
+        const int left = row[i] < n ? k - at : 0;
+        load_row<E>(xr, vec, left, v[i]);
+        if constexpr (SWIGLU) load_row<E>(xr + k, uvec, left, u[i]);
     }
-    uint2 c;
-    const int b = fp8_encode8<16>(v, &c);
-    *reinterpret_cast<uint2*>(out.codes + row * out.ld + at) = c;
-    if ((threadIdx.x & 15) == 0) out.scales[row * out.lds + blk] = static_cast<uint8_t>(b);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        if constexpr (SWIGLU) {
+            // the hardware's exponential and reciprocal, for either type: within (2 |g| + 10) 2^-24, where e4m3 rounds at 2^-4
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[i][e] = swiglu_bf16(v[i][e], u[i][e]);
+        }
+        uint32_t c[E / 4];
+        const int b = fp8_encode<E, LANES>(v[i], c);
+        if (row[i] >= n) continue;   // whole groups
+        store_codes<E>(out.codes + row[i] * out.ld + blk[i] * kFp8Block + E * lane, c);
+        if (lane == 0) out.scales[row[i] * out.lds + blk[i]] = static_cast<uint8_t>(b);
+    }
 }
 
 // ---------------------------------------------------------------------------
 // Weight tiles of 128 x 128 under one scale: a workgroup a tile, the tile in
-// registers (16 lanes a row, 8 rows a lane).
+// registers.
 // ---------------------------------------------------------------------------
 template <typename T>
 __global__ void __launch_bounds__(256) quantise_tiles_kernel(int n, int k, const T* __restrict__ x, int64_t ldx, bool vec,
                                                              Fp8Out out) {
+    constexpr int E = kEntries<T>, LANES = kFp8Block / E, ROWS = 256 / LANES, U = kFp8Block / ROWS;
     __shared__ float part[4];
     const int kb = fp8_blocks(k);
     const int tr = blockIdx.x / kb, tc = blockIdx.x - tr * kb;
-    const int at = tc * kFp8Block + 8 * (threadIdx.x & 15);
-    float v[8][8];
+    const int at = tc * kFp8Block + E * (threadIdx.x % LANES), r0 = tr * kFp8Block + threadIdx.x / LANES;
+    float v[U][E];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int row = r0 + ROWS * i;
+        load_row<E>(x + static_cast<int64_t>(row) * ldx + at, vec, row < n ? k - at : 0, v[i]);
+    }
+    auto of_tile = [&](float a) {
+        a = lanes_max<64>(a);
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = a;
+        __syncthreads();
+        return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+    };
     float a = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int row = tr * kFp8Block + 16 * i + (threadIdx.x >> 4);
-        load8(x + static_cast<int64_t>(row) * ldx + at, vec, row < n ? k - at : 0, v[i]);
+    for (int i = 0; i < U; ++i) a = fmaxf(a, largest<E>(v[i]));
+    a = of_tile(a);
+    if (a > kLargestFloat) {   // the same in the whole workgroup
+        a = 0.0f;
+#pragma unroll
+        for (int i = 0; i < U; ++i) a = fmaxf(a, drop_infinities<E>(v[i]));
+        __syncthreads();
+        a = of_tile(a);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) a = fmaxf(a, finite_abs(v[i][e]));
-    a = wave_max(a);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = a;
-    __syncthreads();
-    const int b = fp8_scale_byte(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])));
+    const int b = fp8_scale_byte(a);
     const float inv = fp8_inverse(b);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int row = tr * kFp8Block + 16 * i + (threadIdx.x >> 4);
-        if (row < n)
-            *reinterpret_cast<uint2*>(out.codes + static_cast<int64_t>(row) * out.ld + at) =
-                make_uint2(fp8_pack4(v[i], inv), fp8_pack4(v[i] + 4, inv));
+    for (int i = 0; i < U; ++i) {
+        const int row = r0 + ROWS * i;
+        uint32_t c[E / 4];
+        fp8_pack<E>(v[i], inv, c);
+        if (row < n) store_codes<E>(out.codes + static_cast<int64_t>(row) * out.ld + at, c);
     }
     if (threadIdx.x == 0) out.scales[tr * out.lds + tc] = static_cast<uint8_t>(b);
 }
@@ -162,6 +183,20 @@ __device__ __forceinline__ uint8_t* kv_place(const KvFp8& c, const KvTokens& t, 
     return c.pool + (static_cast<int64_t>(pg) * c.heads + h) * c.block;
 }
 
+// Whether token i begins eight that fill positions 8 j .. 8 j + 7 of its sequence; token i of such an eight looks from its
+// place on (first: token of position 8 j).
+__device__ __forceinline__ bool kv_eight(const KvTokens& t, int first) {
+    if (first < 0 || first + 8 > t.n) return false;
+    const int s = t.seqs[first], pos = t.pos[first];
+    bool all = (pos & 7) == 0 && pos >= 0;
+#pragma unroll
+    for (int e = 1; e < 8; ++e) all = all && t.seqs[first + e] == s && t.pos[first + e] == pos + e;
+    return all;
+}
+
+// blockIdx.y 0: keys, a lane group a (token, head).  1: values: eight tokens that fill
+// eight neighbouring positions are written by the first of them, eight bytes an
+// entry; others byte by byte (a rollout's single tokens).
 template <typename T, int D>
 __global__ void __launch_bounds__(256) kv_fp8_append_kernel(KvFp8 c, KvTokens t, bool kvec, bool vvec) {
     constexpr int LANES = D / 8;
@@ -174,27 +209,54 @@ __global__ void __launch_bounds__(256) kv_fp8_append_kernel(KvFp8 c, KvTokens t,
     if (!blk) return;
     const int at = h * D + 8 * lane;
     float v[8];
-    uint2 w;
-    load8(static_cast<const T*>(t.k) + i * t.ldk + at, kvec, 8, v);
-    int b = fp8_encode8<LANES>(v, &w);
-    *reinterpret_cast<uint2*>(blk + local * D + 8 * lane) = w;
-    if (lane == 0) blk[2 * c.page * D + local] = static_cast<uint8_t>(b);
-    load8(static_cast<const T*>(t.v) + i * t.ldv + at, vvec, 8, v);
-    b = fp8_encode8<LANES>(v, &w);
-    uint8_t* dst = blk + c.page * D + (local / 8 * D + 8 * lane) * 8 + local % 8;
+    uint32_t w[2];
+    if (blockIdx.y == 0) {
+        load_row<8>(static_cast<const T*>(t.k) + i * t.ldk + at, kvec, 8, v);
+        const int b = fp8_encode<8, LANES>(v, w);
+        store_codes<8>(blk + local * D + 8 * lane, w);
+        if (lane == 0) blk[2 * c.page * D + local] = static_cast<uint8_t>(b);
+        return;
+    }
+    uint8_t* dst = blk + c.page * D + (local / 8 * D + 8 * lane) * 8;
+    uint8_t* sdst = blk + 2 * c.page * D + c.page + local;
+    if (kv_eight(t, i - local % 8)) {
+        if (local % 8 != 0) return;
+        uint32_t all[8][2];
+        uint32_t sb[2] = {0u, 0u};
+        float x[8][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dst[8 * e] = static_cast<uint8_t>((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
-    if (lane == 0) blk[2 * c.page * D + c.page + local] = static_cast<uint8_t>(b);
+        for (int e = 0; e < 8; ++e) load_row<8>(static_cast<const T*>(t.v) + (i + e) * t.ldv + at, vvec, 8, x[e]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sb[e / 4] |= static_cast<uint32_t>(fp8_encode<8, LANES>(x[e], all[e])) << (8 * (e & 3));
+        // byte e of output entry j is byte j of token e
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            uint32_t o[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int jj = j + q / 2, e0 = 4 * (q & 1), sh = 8 * (jj & 3);
+                o[q] = (all[e0][jj / 4] >> sh & 255u) | (all[e0 + 1][jj / 4] >> sh & 255u) << 8 | (all[e0 + 2][jj / 4] >> sh & 255u) << 16 |
+                       (all[e0 + 3][jj / 4] >> sh & 255u) << 24;
+            }
+            *reinterpret_cast<u32x4*>(dst + 8 * j) = u32x4{o[0], o[1], o[2], o[3]};
+        }
+        if (lane == 0) *reinterpret_cast<uint2*>(sdst) = make_uint2(sb[0], sb[1]);
+        return;
+    }
+    load_row<8>(static_cast<const T*>(t.v) + i * t.ldv + at, vvec, 8, v);
+    const int b = fp8_encode<8, LANES>(v, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dst[8 * e + local % 8] = static_cast<uint8_t>(w[e / 4] >> (8 * (e & 3)));
+    if (lane == 0) *sdst = static_cast<uint8_t>(b);
 }
 
 // eight codes as numbers; the hardware's conversion takes the scale's exponent along
-__device__ __forceinline__ void fp8_decode8(uint2 w, float scale, float* v) {
+__device__ __forceinline__ void fp8_decode8(const uint32_t* w, float scale, float* v) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        const uint32_t q = e ? w.y : w.x;
-        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(q, scale, false);
-        const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(q, scale, true);
+        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[e], scale, false);
+        const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[e], scale, true);
         v[4 * e] = a[0];
         v[4 * e + 1] = a[1];
         v[4 * e + 2] = b[0];
@@ -212,19 +274,36 @@ __global__ void __launch_bounds__(256) kv_fp8_read_kernel(KvFp8 c, KvTokens t, b
     int local = 0;
     const uint8_t* blk = kv_place(c, t, i, h, &local);
     const int at = h * D + 8 * lane;
-    float k[8], v[8];
+    float v[8];
+    uint32_t w[2] = {0u, 0u};
+    float scale = 0.0f;
+    if (blockIdx.y == 0) {
+        if (blk) {
+            const uint2 q = *reinterpret_cast<const uint2*>(blk + local * D + 8 * lane);
+            w[0] = q.x;
+            w[1] = q.y;
+            scale = fp8_scale(blk[2 * c.page * D + local]);
+        }
+        fp8_decode8(w, scale, v);
+        if (!blk) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) k[e] = v[e] = 0.0f;
-    if (blk) {
-        fp8_decode8(*reinterpret_cast<const uint2*>(blk + local * D + 8 * lane), fp8_scale(blk[2 * c.page * D + local]), k);
-        const uint8_t* src = blk + c.page * D + (local / 8 * D + 8 * lane) * 8 + local % 8;
-        uint2 w = make_uint2(0u, 0u);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) (e < 4 ? w.x : w.y) |= static_cast<uint32_t>(src[8 * e]) << (8 * (e & 3));
-        fp8_decode8(w, fp8_scale(blk[2 * c.page * D + c.page + local]), v);
+            for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+        }
+        store_row<8>(static_cast<T*>(t.out_k) + i * t.ld_ok + at, kvec, 8, v);
+        return;
     }
-    store8(static_cast<T*>(t.out_k) + i * t.ld_ok + at, kvec, 8, k);
-    store8(static_cast<T*>(t.out_v) + i * t.ld_ov + at, vvec, 8, v);
+    if (blk) {
+        const uint8_t* src = blk + c.page * D + (local / 8 * D + 8 * lane) * 8 + local % 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e / 4] |= static_cast<uint32_t>(src[8 * e]) << (8 * (e & 3));
+        scale = fp8_scale(blk[2 * c.page * D + c.page + local]);
+    }
+    fp8_decode8(w, scale, v);
+    if (!blk) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    }
+    store_row<8>(static_cast<T*>(t.out_v) + i * t.ld_ov + at, vvec, 8, v);
 }
 
 size_t es_of(int dt) { return dt == RL_DTYPE_FP32 ? 4 : 2; }
@@ -237,23 +316,26 @@ template <typename T, int WAVES, int NV> hipError_t norm_launch(const NormArgs& 
     return hipGetLastError();
 }
 template <typename T> hipError_t norm_for(const NormArgs& a, hipStream_t s) {
-    const int vecs = fp8_blocks(a.hidden) * 16;   // lanes' vectors of a row
+    const int vecs = fp8_blocks(a.hidden) * (kFp8Block / kEntries<T>);   // lanes' vectors of a row
     if (vecs <= 64) return norm_launch<T, 1, 1>(a, s);
     if (vecs <= 128) return norm_launch<T, 1, 2>(a, s);
     if (vecs <= 256) return norm_launch<T, 1, 4>(a, s);
     if (vecs <= 512) return norm_launch<T, 1, 8>(a, s);
     if (vecs <= 1024) return norm_launch<T, 4, 4>(a, s);
-    return norm_launch<T, 4, 16>(a, s);
+    if (vecs <= 2048) return norm_launch<T, 4, 8>(a, s);
+    if (vecs <= 4096) return norm_launch<T, 4, 16>(a, s);
+    return norm_launch<T, 4, 32>(a, s);
 }
 
 template <typename T> hipError_t quantise_for(int form, int n, int k, const void* x, int64_t ldx, const Fp8Out& out, hipStream_t s) {
     const T* p = static_cast<const T*>(x);
     const bool vec = rows_on_16(p, ldx, sizeof(T));
     const int kb = fp8_blocks(k);
+    constexpr int U = 2;
+    const int groups = 256 / (kFp8Block / kEntries<T>) * U, grid = (n * kb + groups - 1) / groups;
     if (form == 2) quantise_tiles_kernel<T><<<fp8_blocks(n) * kb, 256, 0, s>>>(n, k, p, ldx, vec, out);
-    else if (form == 1)
-        quantise_rows_kernel<T, true><<<(n * kb + 15) / 16, 256, 0, s>>>(n, k, p, ldx, vec, rows_on_16(p + k, ldx, sizeof(T)), out);
-    else quantise_rows_kernel<T, false><<<(n * kb + 15) / 16, 256, 0, s>>>(n, k, p, ldx, vec, false, out);
+    else if (form == 1) quantise_rows_kernel<T, true, U><<<grid, 256, 0, s>>>(n, k, p, ldx, vec, rows_on_16(p + k, ldx, sizeof(T)), out);
+    else quantise_rows_kernel<T, false, U><<<grid, 256, 0, s>>>(n, k, p, ldx, vec, false, out);
     return hipGetLastError();
 }
 
@@ -271,7 +353,7 @@ hipError_t launch_kv_fp8_append(const KvFp8& c, const KvTokens& t, hipStream_t s
     const size_t es = es_of(t.dt);
     const bool kv = rows_on_16(t.k, t.ldk, es), vv = rows_on_16(t.v, t.ldv, es);
     const int64_t threads = static_cast<int64_t>(t.n) * c.heads * (c.dim / 8);
-    const int grid = static_cast<int>((threads + 255) / 256);
+    const dim3 grid(static_cast<uint32_t>((threads + 255) / 256), 2);
     if (t.dt == RL_DTYPE_FP32) {
         if (c.dim == 128) kv_fp8_append_kernel<float, 128><<<grid, 256, 0, s>>>(c, t, kv, vv);
         else kv_fp8_append_kernel<float, 64><<<grid, 256, 0, s>>>(c, t, kv, vv);
@@ -286,7 +368,7 @@ hipError_t launch_kv_fp8_read(const KvFp8& c, const KvTokens& t, hipStream_t s) 
     const size_t es = es_of(t.dt);
     const bool kv = rows_on_16(t.out_k, t.ld_ok, es), vv = rows_on_16(t.out_v, t.ld_ov, es);
     const int64_t threads = static_cast<int64_t>(t.n) * c.heads * (c.dim / 8);
-    const int grid = static_cast<int>((threads + 255) / 256);
+    const dim3 grid(static_cast<uint32_t>((threads + 255) / 256), 2);
     if (t.dt == RL_DTYPE_FP32) {
         if (c.dim == 128) kv_fp8_read_kernel<float, 128><<<grid, 256, 0, s>>>(c, t, kv, vv);
         else kv_fp8_read_kernel<float, 64><<<grid, 256, 0, s>>>(c, t, kv, vv);

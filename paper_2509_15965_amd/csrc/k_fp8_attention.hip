@@ -15,7 +15,6 @@ namespace rl {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kWaves = 4;
 constexpr int kStep = 32;   // positions a wave takes at a time
 
 // v as a sum of N bf16 numbers: the rest after each is exact
@@ -38,13 +37,22 @@ template <typename T> __device__ __forceinline__ void write_out(T* out, int at, 
     for (int e = 0; e < 4; ++e) Elem<T>::store(out, at + e, L == 0.0f ? 0.0f : o[e] / L);
 }
 
+// Sums o, total L and maximum M of one part of a row's positions, joined with another's.
+__device__ __forceinline__ void add_part(float& M, float& L, f32x4& o, float m, float l, f32x4 v) {
+    const float m_new = fmaxf(M, m), base = m_new == -INFINITY ? 0.0f : m_new;
+    const float f = __builtin_amdgcn_exp2f(M - base), g = __builtin_amdgcn_exp2f(m - base);
+    L = f * L + g * l;
+    o = f * o + g * v;
+    M = m_new;
+}
+
 // Partial results of one (row, kv-head, chunk): sums [G][D], then maxima [G] and totals [G].
 __host__ __device__ constexpr int part_floats(int G, int D) { return G * (D + 2); }
 
 // A workgroup takes one chunk of one row's positions for one kv-head, its waves every
-// fourth step of 32, the next step's loads under this one's arithmetic.
-template <typename T, int D, int QT, int PT>
-__global__ void __launch_bounds__(64 * kWaves) attention_fp8_kernel(AttnFp8 p, int chunk, int n_chunks) {
+// kWaves-th step of 32, the next step's loads under this one's arithmetic.
+template <typename T, int D, int QT, int PT, int kWaves>
+__global__ void __launch_bounds__(64 * kWaves, 2) attention_fp8_kernel(AttnFp8 p, int chunk, int n_chunks) {
     constexpr int NQ = D / 64;          // 16-byte K loads a row, of 4 lane groups
     constexpr int NV = D / 32;          // 16-byte V loads a lane: two entries each
     const int c = blockIdx.x % n_chunks, pair = blockIdx.x / n_chunks;
@@ -98,7 +106,7 @@ __global__ void __launch_bounds__(64 * kWaves) attention_fp8_kernel(AttnFp8 p, i
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
                 float x[8];
-                load8(src + 64 * u + 8 * v, vec, r < G ? 8 : 0, x);
+                load_row<8>(src + 64 * u + 8 * v, vec, r < G ? 8 : 0, x);
                 split_bf16<QT>(x, q[u][v]);
             }
     }
@@ -253,29 +261,61 @@ __global__ void __launch_bounds__(256) attention_fp8_join_kernel(AttnFp8 p, int 
                 a[u] = *reinterpret_cast<const float2*>(q + at);
                 b[u] = *reinterpret_cast<const float2*>(q + at + 2);
             }
-            float m_new = M;
 #pragma unroll
-            for (int u = 0; u < U; ++u) m_new = fmaxf(m_new, cm[u]);
-            const float base = m_new == -INFINITY ? 0.0f : m_new;
-            const float keep = __builtin_amdgcn_exp2f(M - base);
-            L *= keep;
-            o *= keep;
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const float f = c0 + u < n ? __builtin_amdgcn_exp2f(cm[u] - base) : 0.0f;
-                if (c0 + u < n) {
-                    L += f * cl[u];
-                    o += f * f32x4{a[u].x, a[u].y, b[u].x, b[u].y};
-                }
-            }
-            M = m_new;
+            for (int u = 0; u < U; ++u)
+                if (c0 + u < n) add_part(M, L, o, cm[u], cl[u], f32x4{a[u].x, a[u].y, b[u].x, b[u].y});
         }
         write_out(out, at, o, L);
     }
 }
 
+// The same for many chunks: a workgroup a query head, its lane groups every GROUPS-th chunk, joined in LDS in their order.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) attention_fp8_join_head_kernel(AttnFp8 p, int chunk, int n_chunks) {
+    constexpr int LANES = D / 4, GROUPS = 256 / LANES, U = 4;
+    __shared__ f32x4 os[GROUPS][LANES];
+    __shared__ float ms[GROUPS], ls[GROUPS];
+    const int row = blockIdx.x / p.heads, head = blockIdx.x - row * p.heads;
+    const int G = p.heads / p.c.heads, step = part_floats(G, D), kvh = head / G, h = head - kvh * G;
+    const int seq = p.seqs ? p.seqs[row] : row;
+    int len = p.lengths[row];
+    len = len < 0 || seq < 0 || seq >= p.c.n_seqs ? 0 : len > p.max_length ? p.max_length : len;
+    const int n = (len + chunk - 1) / chunk;
+    const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    const float* part = p.part + (static_cast<int64_t>(row) * p.c.heads + kvh) * n_chunks * step;
+    float M = -INFINITY, L = 0.0f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int c0 = group; c0 < n; c0 += GROUPS * U) {
+        float cm[U], cl[U];
+        float2 a[U], b[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = c0 + GROUPS * u;
+            const float* q = part + static_cast<int64_t>(c < n ? c : c0) * step;
+            cm[u] = q[G * D + h];
+            cl[u] = q[G * D + G + h];
+            a[u] = *reinterpret_cast<const float2*>(q + h * D + 4 * lane);
+            b[u] = *reinterpret_cast<const float2*>(q + h * D + 4 * lane + 2);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (c0 + GROUPS * u >= n) break;
+            add_part(M, L, o, cm[u], cl[u], f32x4{a[u].x, a[u].y, b[u].x, b[u].y});
+        }
+    }
+    os[group][lane] = o;
+    if (lane == 0) {
+        ms[group] = M;
+        ls[group] = L;
+    }
+    __syncthreads();
+    if (group > 0) return;
+    for (int q = 1; q < GROUPS; ++q) add_part(M, L, o, ms[q], ls[q], os[q][lane]);
+    write_out(static_cast<T*>(p.out) + row * p.ldo + head * D, 4 * lane, o, L);
+}
+
 // Positions a workgroup takes, a multiple of 128.
-constexpr int kMaxChunk = 64 * kStep * kWaves;
+constexpr int kMaxChunk = 64 * kStep;
 int chunk_of(int n, int kv_heads, int max_length) {
     int chunk = 1024;
     while (chunk > 256 && static_cast<int64_t>(n) * kv_heads * ((max_length + chunk - 1) / chunk) < 1024) chunk /= 2;
@@ -288,11 +328,22 @@ int chunks_of(int n, int kv_heads, int max_length) {
     return k < 1 ? 1 : k;
 }
 
+template <typename T, int D, int QT, int PT, int WAVES> void start(const AttnFp8& a, int chunk, int n_chunks, hipStream_t s) {
+    const int lds = WAVES * (a.heads / a.c.heads) * D * sizeof(float);
+    attention_fp8_kernel<T, D, QT, PT, WAVES><<<a.n * a.c.heads * n_chunks, 64 * WAVES, lds, s>>>(a, chunk, n_chunks);
+}
+
 template <typename T, int D, int QT, int PT> hipError_t attend(const AttnFp8& a, hipStream_t s) {
     const int chunk = chunk_of(a.n, a.c.heads, a.max_length), n_chunks = chunks_of(a.n, a.c.heads, a.max_length);
-    const int lds = kWaves * (a.heads / a.c.heads) * D * sizeof(float);
-    attention_fp8_kernel<T, D, QT, PT><<<a.n * a.c.heads * n_chunks, 64 * kWaves, lds, s>>>(a, chunk, n_chunks);
-    if (n_chunks > 1) attention_fp8_join_kernel<T, D><<<a.n * a.c.heads, 256, 0, s>>>(a, chunk, n_chunks);
+    // Waves a workgroup: one where rows are short and many (11968 pairs of 105 positions: 92 us, with two 96, four 119), four where
+    // workgroups are few (304 of them: 18 us, with two 20, one 23), else two (512 x 4 x 2000: 252, four 249; 24 x 8000: 23 and 25;
+    // 1732 x 820 in fp32: 130 and 135).
+    const int64_t pairs = static_cast<int64_t>(a.n) * a.c.heads;
+    if (pairs * n_chunks < 512) start<T, D, QT, PT, 4>(a, chunk, n_chunks, s);
+    else if (a.max_length <= 128 && pairs >= 2048) start<T, D, QT, PT, 1>(a, chunk, n_chunks, s);
+    else start<T, D, QT, PT, 2>(a, chunk, n_chunks, s);
+    if (n_chunks > 8) attention_fp8_join_head_kernel<T, D><<<a.n * a.heads, 256, 0, s>>>(a, chunk, n_chunks);
+    else if (n_chunks > 1) attention_fp8_join_kernel<T, D><<<a.n * a.c.heads, 256, 0, s>>>(a, chunk, n_chunks);
     return hipGetLastError();
 }
 

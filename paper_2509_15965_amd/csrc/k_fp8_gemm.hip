@@ -355,8 +355,8 @@ __device__ __forceinline__ void tile_fp8(const Fp8Gemm& p, int m0, int n0, int k
                     v[e] = acc[t][i][4 * q + e];
                     v[4 + e] = acc[t + 1][i][4 * q + e];
                 }
-                if (part) store8(part + static_cast<int64_t>(m) * p.n + n + 4 * t, p.n % 4 == 0, p.n - n - 4 * t, v);
-                else store8(row + n + 4 * t, vec, p.n - n - 4 * t, v);
+                if (part) store_row<8>(part + static_cast<int64_t>(m) * p.n + n + 4 * t, p.n % 4 == 0, p.n - n - 4 * t, v);
+                else store_row<8>(row + n + 4 * t, vec, p.n - n - 4 * t, v);
             }
         }
     }
