@@ -613,7 +613,8 @@ typedef struct rl_kv_fp8 {
 /* Bytes of a pool (0 for sizes that are not supported). */
 size_t rl_kv_quant_bytes(int32_t n_pages, int32_t page_size, int32_t n_kv_heads, int32_t head_dim);
 
-/* Write n tokens' keys and values (after RoPE) in 8 bits.  n <= 2^24.
+/* Write n tokens' keys and values (after RoPE) in 8 bits.  n <= 2^24, and
+ * n * n_kv_heads < 2^31.
  *  seqs, positions  device int32 [n]: token i is position positions[i] of
  *                   sequence seqs[i]; one that has no place (sequence or
  *                   position out of range, no page) is left out.  No two

@@ -101,6 +101,7 @@ rl_status rl_kv_quant_append(const rl_kv_fp8* cache, int32_t n, const int32_t* s
     KvFp8 c;
     if (!cache_ok(cache, &c) || n < 0 || n > kMaxTokens || !dtype_ok(dtype)) return RL_ERR_INVALID_ARG;
     if (n == 0) return RL_OK;
+    if (static_cast<int64_t>(n) * c.heads > INT32_MAX) return RL_ERR_UNSUPPORTED;
     const int64_t width = static_cast<int64_t>(c.heads) * c.dim;
     if (!seqs || !positions || !rows_ok(dtype, k, n, width, ldk) || !rows_ok(dtype, v, n, width, ldv)) return RL_ERR_INVALID_ARG;
     const KvTokens t{n, seqs, positions, k, v, ldk, ldv, nullptr, nullptr, 0, 0, dtype};
@@ -112,6 +113,7 @@ rl_status rl_kv_quant_read(const rl_kv_fp8* cache, int32_t n, const int32_t* seq
     KvFp8 c;
     if (!cache_ok(cache, &c) || n < 0 || n > kMaxTokens || !dtype_ok(dtype)) return RL_ERR_INVALID_ARG;
     if (n == 0) return RL_OK;
+    if (static_cast<int64_t>(n) * c.heads > INT32_MAX) return RL_ERR_UNSUPPORTED;
     const int64_t width = static_cast<int64_t>(c.heads) * c.dim;
     if (!seqs || !positions || !rows_ok(dtype, out_k, n, width, ldk) || !rows_ok(dtype, out_v, n, width, ldv)) return RL_ERR_INVALID_ARG;
     const KvTokens t{n, seqs, positions, nullptr, nullptr, 0, 0, out_k, out_v, ldk, ldv, dtype};

@@ -67,11 +67,6 @@ bool attention_fp8_fits(int n, int kv_heads, int max_length);   // its workgroup
 size_t attention_fp8_ws_bytes(int n, int kv_heads, int heads, int dim, int max_length);
 hipError_t launch_attention_fp8(const AttnFp8& a, hipStream_t s);
 
-inline __host__ __device__ bool rows_on_16(const void* p, int64_t ld, size_t es) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * es) % 16 == 0;
-}
-
-
 // Scale byte b of a block whose largest finite magnitude is a: 2^(b - 127) is the
 // smallest power of two with a / 2^(b - 127) <= 448 = 1.75 x 2^8, and b >= 1 so
 // that it and its reciprocal are normal fp32 numbers; 127 for a = 0.  From the
@@ -103,46 +98,56 @@ __device__ __forceinline__ bf16x8 codes_bf16(uint32_t lo, uint32_t hi, float sca
 // Entries of a row that a lane moves at once: 16 bytes of its type.
 template <typename T> constexpr int kEntries = 16 / sizeof(T);
 
-// E entries of a row, of which `left` are there (the others are 0); vec: the row starts on 16 bytes.
-template <int E, typename T> __device__ __forceinline__ void load_row(const T* p, bool vec, int left, float* v) {
-    if (vec && left >= E) {
+// Vectors at any address that their elements' alignment allows: the hardware takes unaligned global accesses.
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+
+// E entries of a row, of which `left` are there (the others are 0).
+template <int E, typename T> __device__ __forceinline__ void load_row(const T* p, int left, float* v) {
+    if (left >= E) {
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int q = 0; q < E; q += 4) {
-                const u32x4 a = ld16(p + q);
+                const u32x4 a = *reinterpret_cast<const u32x4_any*>(p + q);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[q + e] = __uint_as_float(a[e]);
             }
-        } else if constexpr (E == 8) {
-            const u32x4 a = ld16(p);
+        } else {
+            uint32_t a[E / 2];
+            if constexpr (E == 8) {
+                const u32x4 w = *reinterpret_cast<const u32x4_any*>(p);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < 4; ++e) a[e] = w[e];
+            } else {
+                const u32x2 w = *reinterpret_cast<const u32x2_any*>(p);
+                a[0] = w[0];
+                a[1] = w[1];
+            }
+#pragma unroll
+            for (int e = 0; e < E / 2; ++e) {
                 v[2 * e] = __uint_as_float(a[e] << 16);
                 v[2 * e + 1] = __uint_as_float(a[e] & 0xFFFF0000u);
             }
-        } else {
-            const uint2 a = *reinterpret_cast<const uint2*>(p);
-            v[0] = __uint_as_float(a.x << 16);
-            v[1] = __uint_as_float(a.x & 0xFFFF0000u);
-            v[2] = __uint_as_float(a.y << 16);
-            v[3] = __uint_as_float(a.y & 0xFFFF0000u);
         }
         return;
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] = e < left ? Elem<T>::load(p, e) : 0.0f;
 }
-template <int E, typename T> __device__ __forceinline__ void store_row(T* p, bool vec, int left, const float* v) {
-    if (vec && left >= E) {
+template <int E, typename T> __device__ __forceinline__ void store_row(T* p, int left, const float* v) {
+    if (left >= E) {
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int q = 0; q < E; q += 4) *reinterpret_cast<f32x4*>(p + q) = f32x4{v[q], v[q + 1], v[q + 2], v[q + 3]};
+            for (int q = 0; q < E; q += 4)
+                *reinterpret_cast<u32x4_any*>(p + q) = u32x4{__float_as_uint(v[q]), __float_as_uint(v[q + 1]), __float_as_uint(v[q + 2]),
+                                                             __float_as_uint(v[q + 3])};
         } else {
             uint32_t w[E / 2];
 #pragma unroll
             for (int e = 0; e < E / 2; ++e) w[e] = f32_to_bf16(v[2 * e]) | static_cast<uint32_t>(f32_to_bf16(v[2 * e + 1])) << 16;
-            if constexpr (E == 8) *reinterpret_cast<u32x4*>(p) = u32x4{w[0], w[1], w[2], w[3]};
-            else *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+            if constexpr (E == 8) *reinterpret_cast<u32x4_any*>(p) = u32x4{w[0], w[1], w[2], w[3]};
+            else *reinterpret_cast<u32x2_any*>(p) = u32x2{w[0], w[1]};
         }
         return;
     }

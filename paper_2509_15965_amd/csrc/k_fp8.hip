@@ -13,7 +13,7 @@ namespace {
 // times 16 bytes of x a lane.
 // ---------------------------------------------------------------------------
 template <typename T, int WAVES, int NV>
-__global__ void __launch_bounds__(256) rmsnorm_fp8_kernel(NormArgs p, bool xvec, bool avec, bool svec, bool wvec) {
+__global__ void __launch_bounds__(256) rmsnorm_fp8_kernel(NormArgs p) {
     constexpr int E = kEntries<T>, ROWS = 4 / WAVES, LANES = 64 * WAVES;
     const int row = blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / LANES : 0);
     const int lane = threadIdx.x % LANES;
@@ -24,15 +24,15 @@ __global__ void __launch_bounds__(256) rmsnorm_fp8_kernel(NormArgs p, bool xvec,
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int at = E * (lane + LANES * i);
-        load_row<E>(x + at, xvec, H - at, v[i]);
+        load_row<E>(x + at, H - at, v[i]);
     }
     if (p.add) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int at = E * (lane + LANES * i);
             float b[E];
-            if (p.add_dt == RL_DTYPE_FP32) load_row<E>(static_cast<const float*>(p.add) + row * p.ld_add + at, avec, H - at, b);
-            else load_row<E>(static_cast<const uint16_t*>(p.add) + row * p.ld_add + at, avec, H - at, b);
+            if (p.add_dt == RL_DTYPE_FP32) load_row<E>(static_cast<const float*>(p.add) + row * p.ld_add + at, H - at, b);
+            else load_row<E>(static_cast<const uint16_t*>(p.add) + row * p.ld_add + at, H - at, b);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 v[i][e] += b[e];
@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(256) rmsnorm_fp8_kernel(NormArgs p, bool xvec,
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int at = E * (lane + LANES * i);
-            store_row<E>(static_cast<T*>(p.sum) + row * p.ld_sum + at, svec, H - at, v[i]);
+            store_row<E>(static_cast<T*>(p.sum) + row * p.ld_sum + at, H - at, v[i]);
         }
     }
     float ss = 0.0f;
@@ -66,8 +66,8 @@ __global__ void __launch_bounds__(256) rmsnorm_fp8_kernel(NormArgs p, bool xvec,
     for (int i = 0; i < NV; ++i) {
         const int at = E * (lane + LANES * i);
         float g[E];
-        if (p.w_dt == RL_DTYPE_FP32) load_row<E>(static_cast<const float*>(p.w) + at, wvec, H - at, g);
-        else load_row<E>(static_cast<const uint16_t*>(p.w) + at, wvec, H - at, g);
+        if (p.w_dt == RL_DTYPE_FP32) load_row<E>(static_cast<const float*>(p.w) + at, H - at, g);
+        else load_row<E>(static_cast<const uint16_t*>(p.w) + at, H - at, g);
 #pragma unroll
         for (int e = 0; e < E; ++e) v[i][e] = v[i][e] * r * g[e];
         if (at + E > H) {   // nothing behind the row, whatever r is
@@ -88,8 +88,7 @@ __global__ void __launch_bounds__(256) rmsnorm_fp8_kernel(NormArgs p, bool xvec,
 // Rows: 128 / E lanes a block, U blocks a lane group, 256 / (128 / E) apart.
 // ---------------------------------------------------------------------------
 template <typename T, bool SWIGLU, int U>
-__global__ void __launch_bounds__(256) quantise_rows_kernel(int n, int k, const T* __restrict__ x, int64_t ldx, bool vec,
-                                                            bool uvec, Fp8Out out) {
+__global__ void __launch_bounds__(256) quantise_rows_kernel(int n, int k, const T* __restrict__ x, int64_t ldx, Fp8Out out) {
     constexpr int E = kEntries<T>, LANES = kFp8Block / E, GROUPS = 256 / LANES;
     const int kb = fp8_blocks(k);
     const int lane = threadIdx.x % LANES;
@@ -103,8 +102,8 @@ __global__ void __launch_bounds__(256) quantise_rows_kernel(int n, int k, const 
         const int at = blk[i] * kFp8Block + E * lane;
         const T* xr = x + static_cast<int64_t>(row[i]) * ldx + at;
         const int left = row[i] < n ? k - at : 0;
-        load_row<E>(xr, vec, left, v[i]);
-        if constexpr (SWIGLU) load_row<E>(xr + k, uvec, left, u[i]);
+        load_row<E>(xr, left, v[i]);
+        if constexpr (SWIGLU) load_row<E>(xr + k, left, u[i]);
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -126,8 +125,7 @@ __global__ void __launch_bounds__(256) quantise_rows_kernel(int n, int k, const 
 // registers.
 // ---------------------------------------------------------------------------
 template <typename T>
-__global__ void __launch_bounds__(256) quantise_tiles_kernel(int n, int k, const T* __restrict__ x, int64_t ldx, bool vec,
-                                                             Fp8Out out) {
+__global__ void __launch_bounds__(256) quantise_tiles_kernel(int n, int k, const T* __restrict__ x, int64_t ldx, Fp8Out out) {
     constexpr int E = kEntries<T>, LANES = kFp8Block / E, ROWS = 256 / LANES, U = kFp8Block / ROWS;
     __shared__ float part[4];
     const int kb = fp8_blocks(k);
@@ -137,7 +135,7 @@ __global__ void __launch_bounds__(256) quantise_tiles_kernel(int n, int k, const
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int row = r0 + ROWS * i;
-        load_row<E>(x + static_cast<int64_t>(row) * ldx + at, vec, row < n ? k - at : 0, v[i]);
+        load_row<E>(x + static_cast<int64_t>(row) * ldx + at, row < n ? k - at : 0, v[i]);
     }
     auto of_tile = [&](float a) {
         a = lanes_max<64>(a);
@@ -194,56 +192,67 @@ __device__ __forceinline__ bool kv_eight(const KvTokens& t, int first) {
     return all;
 }
 
+// Token and head of this lane group, of LANES lanes.
+template <int LANES> __device__ __forceinline__ int kv_unit(const KvFp8& c, int* h) {
+    const uint32_t unit = static_cast<uint32_t>((static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x) / LANES);
+    const uint32_t i = unit / static_cast<uint32_t>(c.heads);
+    *h = static_cast<int>(unit - i * c.heads);
+    return static_cast<int>(i);
+}
+
+// 8 x 8 bytes turned: byte e of o[j] (as 64 bits) is byte j of a[e].
+__device__ __forceinline__ void turn8(const uint32_t (&a)[8][2], uint32_t (&o)[8][2]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int sh = 8 * (j & 3);
+            o[j][q] = (a[4 * q][j / 4] >> sh & 255u) | (a[4 * q + 1][j / 4] >> sh & 255u) << 8 | (a[4 * q + 2][j / 4] >> sh & 255u) << 16 |
+                      (a[4 * q + 3][j / 4] >> sh & 255u) << 24;
+        }
+}
+
 // blockIdx.y 0: keys, a lane group a (token, head).  1: values: eight tokens that fill
 // eight neighbouring positions are written by the first of them, eight bytes an
 // entry; others byte by byte (a rollout's single tokens).
 template <typename T, int D>
-__global__ void __launch_bounds__(256) kv_fp8_append_kernel(KvFp8 c, KvTokens t, bool kvec, bool vvec) {
+__global__ void __launch_bounds__(256) kv_fp8_append_kernel(KvFp8 c, KvTokens t) {
     constexpr int LANES = D / 8;
-    const int64_t unit = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / LANES;
     const int lane = threadIdx.x % LANES;
-    const int i = static_cast<int>(unit / c.heads), h = static_cast<int>(unit - static_cast<int64_t>(i) * c.heads);
+    int h, local = 0;
+    const int i = kv_unit<LANES>(c, &h);
     if (i >= t.n) return;   // whole groups of LANES lanes
-    int local = 0;
-    uint8_t* blk = kv_place(c, t, i, h, &local);
-    if (!blk) return;
     const int at = h * D + 8 * lane;
     float v[8];
     uint32_t w[2];
     if (blockIdx.y == 0) {
-        load_row<8>(static_cast<const T*>(t.k) + i * t.ldk + at, kvec, 8, v);
+        load_row<8>(static_cast<const T*>(t.k) + i * t.ldk + at, 8, v);   // on its way while the place is looked up
+        uint8_t* blk = kv_place(c, t, i, h, &local);
         const int b = fp8_encode<8, LANES>(v, w);
+        if (!blk) return;
         store_codes<8>(blk + local * D + 8 * lane, w);
         if (lane == 0) blk[2 * c.page * D + local] = static_cast<uint8_t>(b);
         return;
     }
+    load_row<8>(static_cast<const T*>(t.v) + i * t.ldv + at, 8, v);
+    uint8_t* blk = kv_place(c, t, i, h, &local);
+    const bool eight = kv_eight(t, i - t.pos[i] % 8);
+    if (!blk || (eight && local % 8 != 0)) return;
     uint8_t* dst = blk + c.page * D + (local / 8 * D + 8 * lane) * 8;
     uint8_t* sdst = blk + 2 * c.page * D + c.page + local;
-    if (kv_eight(t, i - local % 8)) {
-        if (local % 8 != 0) return;
-        uint32_t all[8][2];
-        uint32_t sb[2] = {0u, 0u};
+    if (eight) {
+        uint32_t all[8][2], o[8][2], sb[2] = {0u, 0u};
         float x[8][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) load_row<8>(static_cast<const T*>(t.v) + (i + e) * t.ldv + at, vvec, 8, x[e]);
+        for (int e = 0; e < 8; ++e) load_row<8>(static_cast<const T*>(t.v) + (i + e) * t.ldv + at, 8, x[e]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) sb[e / 4] |= static_cast<uint32_t>(fp8_encode<8, LANES>(x[e], all[e])) << (8 * (e & 3));
-        // byte e of output entry j is byte j of token e
+        turn8(all, o);
 #pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-            uint32_t o[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int jj = j + q / 2, e0 = 4 * (q & 1), sh = 8 * (jj & 3);
-                o[q] = (all[e0][jj / 4] >> sh & 255u) | (all[e0 + 1][jj / 4] >> sh & 255u) << 8 | (all[e0 + 2][jj / 4] >> sh & 255u) << 16 |
-                       (all[e0 + 3][jj / 4] >> sh & 255u) << 24;
-            }
-            *reinterpret_cast<u32x4*>(dst + 8 * j) = u32x4{o[0], o[1], o[2], o[3]};
-        }
+        for (int j = 0; j < 8; j += 2) *reinterpret_cast<u32x4*>(dst + 8 * j) = u32x4{o[j][0], o[j][1], o[j + 1][0], o[j + 1][1]};
         if (lane == 0) *reinterpret_cast<uint2*>(sdst) = make_uint2(sb[0], sb[1]);
         return;
     }
-    load_row<8>(static_cast<const T*>(t.v) + i * t.ldv + at, vvec, 8, v);
     const int b = fp8_encode<8, LANES>(v, w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) dst[8 * e + local % 8] = static_cast<uint8_t>(w[e / 4] >> (8 * (e & 3)));
@@ -264,55 +273,60 @@ __device__ __forceinline__ void fp8_decode8(const uint32_t* w, float scale, floa
     }
 }
 
+// blockIdx.y 0: keys, 1: values, eight positions at a time as they were written.
 template <typename T, int D>
-__global__ void __launch_bounds__(256) kv_fp8_read_kernel(KvFp8 c, KvTokens t, bool kvec, bool vvec) {
+__global__ void __launch_bounds__(256) kv_fp8_read_kernel(KvFp8 c, KvTokens t) {
     constexpr int LANES = D / 8;
-    const int64_t unit = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / LANES;
     const int lane = threadIdx.x % LANES;
-    const int i = static_cast<int>(unit / c.heads), h = static_cast<int>(unit - static_cast<int64_t>(i) * c.heads);
+    int h, local = 0;
+    const int i = kv_unit<LANES>(c, &h);
     if (i >= t.n) return;
-    int local = 0;
     const uint8_t* blk = kv_place(c, t, i, h, &local);
     const int at = h * D + 8 * lane;
-    float v[8];
+    T* out = (blockIdx.y == 0 ? static_cast<T*>(t.out_k) + i * t.ld_ok : static_cast<T*>(t.out_v) + i * t.ld_ov) + at;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     uint32_t w[2] = {0u, 0u};
-    float scale = 0.0f;
-    if (blockIdx.y == 0) {
-        if (blk) {
-            const uint2 q = *reinterpret_cast<const uint2*>(blk + local * D + 8 * lane);
-            w[0] = q.x;
-            w[1] = q.y;
-            scale = fp8_scale(blk[2 * c.page * D + local]);
-        }
-        fp8_decode8(w, scale, v);
-        if (!blk) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-        }
-        store_row<8>(static_cast<T*>(t.out_k) + i * t.ld_ok + at, kvec, 8, v);
+    if (!blk) {
+        store_row<8>(out, 8, v);
         return;
     }
-    if (blk) {
-        const uint8_t* src = blk + c.page * D + (local / 8 * D + 8 * lane) * 8 + local % 8;
+    const uint8_t* sb = blk + 2 * c.page * D + (blockIdx.y == 0 ? 0 : c.page) + local;
+    if (blockIdx.y == 0) {
+        const uint2 q = *reinterpret_cast<const uint2*>(blk + local * D + 8 * lane);
+        w[0] = q.x;
+        w[1] = q.y;
+    } else {
+        const uint8_t* src = blk + c.page * D + (local / 8 * D + 8 * lane) * 8;
+        if (kv_eight(t, i - local % 8)) {
+            if (local % 8 != 0) return;
+            uint32_t all[8][2], o[8][2];
+            const uint2 s8 = *reinterpret_cast<const uint2*>(sb);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e / 4] |= static_cast<uint32_t>(src[8 * e]) << (8 * (e & 3));
-        scale = fp8_scale(blk[2 * c.page * D + c.page + local]);
-    }
-    fp8_decode8(w, scale, v);
-    if (!blk) {
+            for (int j = 0; j < 8; j += 2) {
+                const u32x4 q = ld16(src + 8 * j);
+                all[j][0] = q[0];
+                all[j][1] = q[1];
+                all[j + 1][0] = q[2];
+                all[j + 1][1] = q[3];
+            }
+            turn8(all, o);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+            for (int e = 0; e < 8; ++e) {
+                fp8_decode8(o[e], fp8_scale((e < 4 ? s8.x : s8.y) >> (8 * (e & 3)) & 255u), v);
+                store_row<8>(out + e * t.ld_ov, 8, v);
+            }
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e / 4] |= static_cast<uint32_t>(src[8 * e + local % 8]) << (8 * (e & 3));
     }
-    store_row<8>(static_cast<T*>(t.out_v) + i * t.ld_ov + at, vvec, 8, v);
+    fp8_decode8(w, fp8_scale(*sb), v);
+    store_row<8>(out, 8, v);
 }
-
-size_t es_of(int dt) { return dt == RL_DTYPE_FP32 ? 4 : 2; }
 
 template <typename T, int WAVES, int NV> hipError_t norm_launch(const NormArgs& a, hipStream_t s) {
     constexpr int ROWS = 4 / WAVES;
-    rmsnorm_fp8_kernel<T, WAVES, NV><<<(a.n + ROWS - 1) / ROWS, 256, 0, s>>>(
-        a, rows_on_16(a.x, a.ldx, sizeof(T)), a.add && rows_on_16(a.add, a.ld_add, es_of(a.add_dt)),
-        a.sum && rows_on_16(a.sum, a.ld_sum, sizeof(T)), rows_on_16(a.w, 0, es_of(a.w_dt)));
+    rmsnorm_fp8_kernel<T, WAVES, NV><<<(a.n + ROWS - 1) / ROWS, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename T> hipError_t norm_for(const NormArgs& a, hipStream_t s) {
@@ -323,19 +337,19 @@ template <typename T> hipError_t norm_for(const NormArgs& a, hipStream_t s) {
     if (vecs <= 512) return norm_launch<T, 1, 8>(a, s);
     if (vecs <= 1024) return norm_launch<T, 4, 4>(a, s);
     if (vecs <= 2048) return norm_launch<T, 4, 8>(a, s);
-    if (vecs <= 4096) return norm_launch<T, 4, 16>(a, s);
-    return norm_launch<T, 4, 32>(a, s);
+    if constexpr (sizeof(T) == 4)
+        if (vecs > 4096) return norm_launch<T, 4, 32>(a, s);
+    return norm_launch<T, 4, 16>(a, s);
 }
 
 template <typename T> hipError_t quantise_for(int form, int n, int k, const void* x, int64_t ldx, const Fp8Out& out, hipStream_t s) {
     const T* p = static_cast<const T*>(x);
-    const bool vec = rows_on_16(p, ldx, sizeof(T));
     const int kb = fp8_blocks(k);
     constexpr int U = 2;
     const int groups = 256 / (kFp8Block / kEntries<T>) * U, grid = (n * kb + groups - 1) / groups;
-    if (form == 2) quantise_tiles_kernel<T><<<fp8_blocks(n) * kb, 256, 0, s>>>(n, k, p, ldx, vec, out);
-    else if (form == 1) quantise_rows_kernel<T, true, U><<<grid, 256, 0, s>>>(n, k, p, ldx, vec, rows_on_16(p + k, ldx, sizeof(T)), out);
-    else quantise_rows_kernel<T, false, U><<<grid, 256, 0, s>>>(n, k, p, ldx, vec, false, out);
+    if (form == 2) quantise_tiles_kernel<T><<<fp8_blocks(n) * kb, 256, 0, s>>>(n, k, p, ldx, out);
+    else if (form == 1) quantise_rows_kernel<T, true, U><<<grid, 256, 0, s>>>(n, k, p, ldx, out);
+    else quantise_rows_kernel<T, false, U><<<grid, 256, 0, s>>>(n, k, p, ldx, out);
     return hipGetLastError();
 }
 
@@ -349,32 +363,30 @@ hipError_t launch_quantise_fp8(int form, int n, int k, int dt, const void* x, in
     return dt == RL_DTYPE_FP32 ? quantise_for<float>(form, n, k, x, ldx, out, s) : quantise_for<uint16_t>(form, n, k, x, ldx, out, s);
 }
 
+namespace {
+dim3 kv_grid(const KvFp8& c, int n) { return dim3(static_cast<uint32_t>((static_cast<int64_t>(n) * c.heads * (c.dim / 8) + 255) / 256), 2); }
+}  // namespace
+
 hipError_t launch_kv_fp8_append(const KvFp8& c, const KvTokens& t, hipStream_t s) {
-    const size_t es = es_of(t.dt);
-    const bool kv = rows_on_16(t.k, t.ldk, es), vv = rows_on_16(t.v, t.ldv, es);
-    const int64_t threads = static_cast<int64_t>(t.n) * c.heads * (c.dim / 8);
-    const dim3 grid(static_cast<uint32_t>((threads + 255) / 256), 2);
+    const dim3 grid = kv_grid(c, t.n);
     if (t.dt == RL_DTYPE_FP32) {
-        if (c.dim == 128) kv_fp8_append_kernel<float, 128><<<grid, 256, 0, s>>>(c, t, kv, vv);
-        else kv_fp8_append_kernel<float, 64><<<grid, 256, 0, s>>>(c, t, kv, vv);
+        if (c.dim == 128) kv_fp8_append_kernel<float, 128><<<grid, 256, 0, s>>>(c, t);
+        else kv_fp8_append_kernel<float, 64><<<grid, 256, 0, s>>>(c, t);
     } else {
-        if (c.dim == 128) kv_fp8_append_kernel<uint16_t, 128><<<grid, 256, 0, s>>>(c, t, kv, vv);
-        else kv_fp8_append_kernel<uint16_t, 64><<<grid, 256, 0, s>>>(c, t, kv, vv);
+        if (c.dim == 128) kv_fp8_append_kernel<uint16_t, 128><<<grid, 256, 0, s>>>(c, t);
+        else kv_fp8_append_kernel<uint16_t, 64><<<grid, 256, 0, s>>>(c, t);
     }
     return hipGetLastError();
 }
 
 hipError_t launch_kv_fp8_read(const KvFp8& c, const KvTokens& t, hipStream_t s) {
-    const size_t es = es_of(t.dt);
-    const bool kv = rows_on_16(t.out_k, t.ld_ok, es), vv = rows_on_16(t.out_v, t.ld_ov, es);
-    const int64_t threads = static_cast<int64_t>(t.n) * c.heads * (c.dim / 8);
-    const dim3 grid(static_cast<uint32_t>((threads + 255) / 256), 2);
+    const dim3 grid = kv_grid(c, t.n);
     if (t.dt == RL_DTYPE_FP32) {
-        if (c.dim == 128) kv_fp8_read_kernel<float, 128><<<grid, 256, 0, s>>>(c, t, kv, vv);
-        else kv_fp8_read_kernel<float, 64><<<grid, 256, 0, s>>>(c, t, kv, vv);
+        if (c.dim == 128) kv_fp8_read_kernel<float, 128><<<grid, 256, 0, s>>>(c, t);
+        else kv_fp8_read_kernel<float, 64><<<grid, 256, 0, s>>>(c, t);
     } else {
-        if (c.dim == 128) kv_fp8_read_kernel<uint16_t, 128><<<grid, 256, 0, s>>>(c, t, kv, vv);
-        else kv_fp8_read_kernel<uint16_t, 64><<<grid, 256, 0, s>>>(c, t, kv, vv);
+        if (c.dim == 128) kv_fp8_read_kernel<uint16_t, 128><<<grid, 256, 0, s>>>(c, t);
+        else kv_fp8_read_kernel<uint16_t, 64><<<grid, 256, 0, s>>>(c, t);
     }
     return hipGetLastError();
 }

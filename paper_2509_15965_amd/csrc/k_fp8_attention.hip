@@ -100,13 +100,12 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attention_fp8_kernel(AttnFp8 p
     bf16x8 q[NQ][2][QT];
     {
         const T* src = static_cast<const T*>(p.q) + row * p.ldq + (kvh * G + (r < G ? r : 0)) * D + 16 * g;
-        const bool vec = rows_on_16(p.q, p.ldq, sizeof(T));
 #pragma unroll
         for (int u = 0; u < NQ; ++u)
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
                 float x[8];
-                load_row<8>(src + 64 * u + 8 * v, vec, r < G ? 8 : 0, x);
+                load_row<8>(src + 64 * u + 8 * v, r < G ? 8 : 0, x);
                 split_bf16<QT>(x, q[u][v]);
             }
     }

@@ -30,20 +30,6 @@ __device__ __forceinline__ i32x8 join(u32x4 a, u32x4 b) {
                  static_cast<int>(b[0]), static_cast<int>(b[1]), static_cast<int>(b[2]), static_cast<int>(b[3])};
 }
 
-// Four consecutive entries of a row of n, from entry at on.
-template <typename TO> __device__ __forceinline__ void store4(TO* row, int at, int n, bool vec, f32x4 v) {
-    if (vec && at + 4 <= n) {
-        if constexpr (sizeof(TO) == 4) *reinterpret_cast<f32x4*>(row + at) = v;
-        else
-            *reinterpret_cast<uint2*>(row + at) = make_uint2(f32_to_bf16(v[0]) | static_cast<uint32_t>(f32_to_bf16(v[1])) << 16,
-                                                             f32_to_bf16(v[2]) | static_cast<uint32_t>(f32_to_bf16(v[3])) << 16);
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (at + e < n) Elem<TO>::store(row, at + e, v[e]);
-}
-
 typedef __attribute__((address_space(3))) void lds_void_t;
 
 // BYTES a lane from a uniform base and a lane's offset straight to LDS: lane i to BYTES i past lds.
@@ -72,7 +58,7 @@ template <int N> __device__ __forceinline__ void barrier_vm() {
 // tokens once for 64 weights.
 // ---------------------------------------------------------------------------
 template <typename TO, int RW, int MT, int WV, bool SPLIT>
-__global__ void __launch_bounds__(64 * WV) gemv_fp8_kernel(Fp8Gemm p, int per, bool vec) {
+__global__ void __launch_bounds__(64 * WV) gemv_fp8_kernel(Fp8Gemm p, int per) {
     constexpr int U = RW * MT >= 8 ? 1 : 2;
     __shared__ f32x4 red[WV][RW * MT][64];
     const int lane = threadIdx.x & 63;
@@ -151,8 +137,9 @@ __global__ void __launch_bounds__(64 * WV) gemv_fp8_kernel(Fp8Gemm p, int per, b
         for (int q = 1; q < WV; ++q) v += red[q][x][lane];
         const int m = 16 * (x % MT) + r16, n = n0 + 16 * (x / MT) + 4 * g;
         if (m >= p.m) continue;
-        if constexpr (SPLIT) store4(p.part + (static_cast<int64_t>(blockIdx.y) * p.m + m) * p.n, n, p.n, p.n % 4 == 0, v);
-        else store4(static_cast<TO*>(p.out) + m * p.ldo, n, p.n, vec, v);
+        const float f[4] = {v[0], v[1], v[2], v[3]};
+        if constexpr (SPLIT) store_row<4>(p.part + (static_cast<int64_t>(blockIdx.y) * p.m + m) * p.n + n, p.n - n, f);
+        else store_row<4>(static_cast<TO*>(p.out) + m * p.ldo + n, p.n - n, f);
     }
 }
 
@@ -179,7 +166,7 @@ __global__ void __launch_bounds__(64 * WV) gemv_fp8_kernel(Fp8Gemm p, int per, b
 struct TileMap { int m_tiles, n_tiles, gm; };
 
 template <int BM, int BN, typename TO, bool EXACT>
-__device__ __forceinline__ void tile_fp8(const Fp8Gemm& p, int m0, int n0, int k0, int nk, uint8_t* smem, bool vec, float* part) {
+__device__ __forceinline__ void tile_fp8(const Fp8Gemm& p, int m0, int n0, int k0, int nk, uint8_t* smem, float* part) {
     constexpr int TM = BM / 2, TN = BN / 2, MT = TM / 32, NT = TN / 32;
     constexpr int AQ = BM / 64, WQ = BN / 32;                // line instructions a wave issues for half of the tokens, for the weights
     constexpr int Q1 = WQ + AQ + 2, Q2 = AQ;                 // a block's first refill, with the scale words, and its second
@@ -355,8 +342,8 @@ __device__ __forceinline__ void tile_fp8(const Fp8Gemm& p, int m0, int n0, int k
                     v[e] = acc[t][i][4 * q + e];
                     v[4 + e] = acc[t + 1][i][4 * q + e];
                 }
-                if (part) store_row<8>(part + static_cast<int64_t>(m) * p.n + n + 4 * t, p.n % 4 == 0, p.n - n - 4 * t, v);
-                else store_row<8>(row + n + 4 * t, vec, p.n - n - 4 * t, v);
+                if (part) store_row<8>(part + static_cast<int64_t>(m) * p.n + n + 4 * t, p.n - n - 4 * t, v);
+                else store_row<8>(row + n + 4 * t, p.n - n - 4 * t, v);
             }
         }
     }
@@ -382,7 +369,7 @@ __device__ __forceinline__ int tile_of_workgroup(int w, int tiles) {
 
 // 128 x 128 tiles, two workgroups a CU; blockIdx.y: the K slice of `per` blocks.
 template <typename TO, bool EXACT>
-__global__ void __launch_bounds__(256, 2) gemm_fp8_small_kernel(Fp8Gemm p, TileMap tm, int per, bool vec) {
+__global__ void __launch_bounds__(256, 2) gemm_fp8_small_kernel(Fp8Gemm p, TileMap tm, int per) {
     __shared__ __attribute__((aligned(1024))) uint8_t smem[kTileLds<128, 128>];
     const int tile = tile_of_workgroup(blockIdx.x, tm.m_tiles * tm.n_tiles);
     if (tile < 0) return;
@@ -390,12 +377,12 @@ __global__ void __launch_bounds__(256, 2) gemm_fp8_small_kernel(Fp8Gemm p, TileM
     tile_of(tm, tile, &mt, &nt);
     const int k0 = blockIdx.y * per;
     float* part = p.part ? p.part + static_cast<int64_t>(blockIdx.y) * p.m * p.n : nullptr;
-    tile_fp8<128, 128, TO, EXACT>(p, mt * 128, nt * 128, k0, min(per, p.kb - k0), smem, vec, part);
+    tile_fp8<128, 128, TO, EXACT>(p, mt * 128, nt * 128, k0, min(per, p.kb - k0), smem, part);
 }
 
 // 256 x 256 tiles, one workgroup a CU.  The last `quartered` tiles are cut into four of 128 x 128.
 template <typename TO>
-__global__ void __launch_bounds__(256, 1) gemm_fp8_large_kernel(Fp8Gemm p, TileMap tm, int quartered, bool vec) {
+__global__ void __launch_bounds__(256, 1) gemm_fp8_large_kernel(Fp8Gemm p, TileMap tm, int quartered) {
     __shared__ __attribute__((aligned(1024))) uint8_t smem[kTileLds<256, 256>];
     const int whole = tm.m_tiles * tm.n_tiles - quartered, first = (whole + 7) / 8 * 8;
     int mt, nt;
@@ -403,35 +390,33 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_large_kernel(Fp8Gemm p, TileM
         const int tile = tile_of_workgroup(blockIdx.x, whole);
         if (tile < 0) return;
         tile_of(tm, tile, &mt, &nt);
-        tile_fp8<256, 256, TO, false>(p, mt * 256, nt * 256, 0, p.kb, smem, vec, nullptr);
+        tile_fp8<256, 256, TO, false>(p, mt * 256, nt * 256, 0, p.kb, smem, nullptr);
         return;
     }
     const int q = blockIdx.x - first;
     tile_of(tm, whole + q / 4, &mt, &nt);
     const int m0 = mt * 256 + (q & 1) * 128, n0 = nt * 256 + (q >> 1 & 1) * 128;
     if (m0 >= p.m || n0 >= p.n) return;
-    tile_fp8<128, 128, TO, false>(p, m0, n0, 0, p.kb, smem, vec, nullptr);
+    tile_fp8<128, 128, TO, false>(p, m0, n0, 0, p.kb, smem, nullptr);
 }
 
 // Sum of the K slices, in their order.
 template <typename TO>
-__global__ void __launch_bounds__(256) gemm_fp8_join_kernel(Fp8Gemm p, int slices, bool vec) {
+__global__ void __launch_bounds__(256) gemm_fp8_join_kernel(Fp8Gemm p, int slices) {
     const int per_row = (p.n + 3) / 4;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     const int m = static_cast<int>(at / per_row), n = 4 * static_cast<int>(at - static_cast<int64_t>(m) * per_row);
     if (m >= p.m) return;
     const float* src = p.part + static_cast<int64_t>(m) * p.n + n;
     const int64_t step = static_cast<int64_t>(p.m) * p.n;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (p.n % 4 == 0) {
-        for (int s = 0; s < slices; ++s) v += *reinterpret_cast<const f32x4*>(src + s * step);
-    } else {
-        for (int s = 0; s < slices; ++s)
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < slices; ++s) {
+        float x[4];
+        load_row<4>(src + s * step, p.n - n, x);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (n + e < p.n) v[e] += src[s * step + e];
+        for (int e = 0; e < 4; ++e) v[e] += x[e];
     }
-    store4(static_cast<TO*>(p.out) + m * p.ldo, n, p.n, vec, v);
+    store_row<4>(static_cast<TO*>(p.out) + m * p.ldo + n, p.n - n, v);
 }
 
 // ---------------------------------------------------------------------------
@@ -476,23 +461,22 @@ Plan plan_of(int m, int n, int kb, bool fp32) {
     return q;
 }
 
-template <typename TO, int RW, int MT, int WV> void gemv(const Fp8Gemm& g, const Plan& q, bool vec, hipStream_t s) {
+template <typename TO, int RW, int MT, int WV> void gemv(const Fp8Gemm& g, const Plan& q, hipStream_t s) {
     const dim3 grid(up(g.n, 16 * RW), q.slices);
-    if (q.slices > 1) gemv_fp8_kernel<TO, RW, MT, WV, true><<<grid, 64 * WV, 0, s>>>(g, q.per, vec);
-    else gemv_fp8_kernel<TO, RW, MT, WV, false><<<grid, 64 * WV, 0, s>>>(g, q.per, vec);
+    if (q.slices > 1) gemv_fp8_kernel<TO, RW, MT, WV, true><<<grid, 64 * WV, 0, s>>>(g, q.per);
+    else gemv_fp8_kernel<TO, RW, MT, WV, false><<<grid, 64 * WV, 0, s>>>(g, q.per);
 }
 
 template <typename TO> void run_plan(const Fp8Gemm& a, const Plan& q, hipStream_t s) {
     constexpr bool EXACT = sizeof(TO) == 4;
     Fp8Gemm g = a;
     if (q.slices == 1) g.part = nullptr;
-    const bool vec = rows_on_16(g.out, g.ldo, sizeof(TO));
     if (q.kind == 0) {
-        if (g.m <= 16) gemv<TO, 1, 1, 8>(g, q, vec, s);
-        else gemv<TO, 1, 2, 8>(g, q, vec, s);
+        if (g.m <= 16) gemv<TO, 1, 1, 8>(g, q, s);
+        else gemv<TO, 1, 2, 8>(g, q, s);
     } else if (q.kind == 1) {
-        if (g.m <= 16) gemv<TO, 4, 1, 4>(g, q, vec, s);
-        else gemv<TO, 4, 2, 4>(g, q, vec, s);
+        if (g.m <= 16) gemv<TO, 4, 1, 4>(g, q, s);
+        else gemv<TO, 4, 2, 4>(g, q, s);
     } else {
         const int b = q.kind == 3 ? 256 : 128;
         TileMap tm{up(g.m, b), up(g.n, b), 0};
@@ -500,13 +484,13 @@ template <typename TO> void run_plan(const Fp8Gemm& a, const Plan& q, hipStream_
         const int tiles = tm.m_tiles * tm.n_tiles - q.quartered;
         if constexpr (!EXACT)
             if (q.kind == 3) {
-                gemm_fp8_large_kernel<TO><<<up(tiles, 8) * 8 + 4 * q.quartered, 256, 0, s>>>(g, tm, q.quartered, vec);
+                gemm_fp8_large_kernel<TO><<<up(tiles, 8) * 8 + 4 * q.quartered, 256, 0, s>>>(g, tm, q.quartered);
                 return;
             }
-        gemm_fp8_small_kernel<TO, EXACT><<<dim3(up(tiles, 8) * 8, q.slices), 256, 0, s>>>(g, tm, q.per, vec);
+        gemm_fp8_small_kernel<TO, EXACT><<<dim3(up(tiles, 8) * 8, q.slices), 256, 0, s>>>(g, tm, q.per);
     }
     if (q.slices > 1)
-        gemm_fp8_join_kernel<TO><<<static_cast<int>((static_cast<int64_t>(g.m) * up(g.n, 4) + 255) / 256), 256, 0, s>>>(g, q.slices, vec);
+        gemm_fp8_join_kernel<TO><<<static_cast<int>((static_cast<int64_t>(g.m) * up(g.n, 4) + 255) / 256), 256, 0, s>>>(g, q.slices);
 }
 
 }  // namespace
