@@ -51,15 +51,17 @@ template <int N> __device__ __forceinline__ void barrier_vm() {
 }
 
 // ---------------------------------------------------------------------------
-// Few tokens: a workgroup takes 16 RW weights, its WV waves every WV-th block of its
-// K slice, straight from memory to registers (U blocks in flight a wave), and
-// the waves' sums meet in LDS in wave order.  MT x 16 tokens.  Bound by the
-// weights' bytes: the exact instructions cost nothing here.  RW = 4 reads the
-// tokens once for 64 weights.
+// Few tokens: a workgroup takes 16 RW weights, its eight waves every eighth block of
+// its K slice, straight from memory to registers, and the waves' sums meet in LDS
+// in wave order.  MT x 16 tokens.  Bound by the weights' bytes, read at 5.6 TB/s
+// (one token, 152064 x 3584): the exact instructions cost nothing here.  Two
+// blocks in flight a wave, or non-temporal loads, are 4 to 14% and 14 to 26% slower:
+// more waves do better than more registers each.
 // ---------------------------------------------------------------------------
-template <typename TO, int RW, int MT, int WV, bool SPLIT>
-__global__ void __launch_bounds__(64 * WV) gemv_fp8_kernel(Fp8Gemm p, int per) {
-    constexpr int U = RW * MT >= 8 ? 1 : 2;
+constexpr int kGemvWaves = 8;
+template <typename TO, int RW, int MT, bool SPLIT>
+__global__ void __launch_bounds__(64 * kGemvWaves, 4) gemv_fp8_kernel(Fp8Gemm p, int per) {
+    constexpr int WV = kGemvWaves;
     __shared__ f32x4 red[WV][RW * MT][64];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -87,39 +89,31 @@ __global__ void __launch_bounds__(64 * WV) gemv_fp8_kernel(Fp8Gemm p, int per) {
     for (int i = 0; i < RW; ++i)
 #pragma unroll
         for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int kb = k0 + wave; kb < k1; kb += U * WV) {
-        u32x4 w[U][RW][2], a[U][MT][2];
-        float sw[U][RW], sa[U][MT];
+    for (int k = k0 + wave; k < k1; k += WV) {
+        u32x4 w[RW][2], a[MT][2];
+        float sw[RW], sa[MT];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int k = min(kb + u * WV, k1 - 1);   // past the slice: the last block again, not added
-#pragma unroll
-            for (int i = 0; i < RW; ++i) {
-                w[u][i][0] = ld16(wp[i] + k * 128);
-                w[u][i][1] = ld16(wp[i] + k * 128 + 64);
-                sw[u][i] = fp8_scale(swp[i][k]);
-            }
-#pragma unroll
-            for (int j = 0; j < MT; ++j) {
-                a[u][j][0] = ld16(ap[j] + k * 128);
-                a[u][j][1] = ld16(ap[j] + k * 128 + 64);
-                sa[u][j] = fp8_scale(sp[j][k]);
-            }
+        for (int i = 0; i < RW; ++i) {
+            w[i][0] = ld16(wp[i] + k * 128);
+            w[i][1] = ld16(wp[i] + k * 128 + 64);
+            sw[i] = fp8_scale(swp[i][k]);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (u > 0 && kb + u * WV >= k1) break;
+        for (int j = 0; j < MT; ++j) {
+            a[j][0] = ld16(ap[j] + k * 128);
+            a[j][1] = ld16(ap[j] + k * 128 + 64);
+            sa[j] = fp8_scale(sp[j][k]);
+        }
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                bf16x8 wf[RW];
+        for (int h = 0; h < 4; ++h) {
+            bf16x8 wf[RW];
 #pragma unroll
-                for (int i = 0; i < RW; ++i) wf[i] = codes_bf16(w[u][i][h / 2][2 * (h & 1)], w[u][i][h / 2][2 * (h & 1) + 1], sw[u][i]);
+            for (int i = 0; i < RW; ++i) wf[i] = codes_bf16(w[i][h / 2][2 * (h & 1)], w[i][h / 2][2 * (h & 1) + 1], sw[i]);
 #pragma unroll
-                for (int j = 0; j < MT; ++j) {
-                    const bf16x8 af = codes_bf16(a[u][j][h / 2][2 * (h & 1)], a[u][j][h / 2][2 * (h & 1) + 1], sa[u][j]);
+            for (int j = 0; j < MT; ++j) {
+                const bf16x8 af = codes_bf16(a[j][h / 2][2 * (h & 1)], a[j][h / 2][2 * (h & 1) + 1], sa[j]);
 #pragma unroll
-                    for (int i = 0; i < RW; ++i) acc[i][j] = mfma16x16x32(wf[i], af, acc[i][j]);
-                }
+                for (int i = 0; i < RW; ++i) acc[i][j] = mfma16x16x32(wf[i], af, acc[i][j]);
             }
         }
     }
@@ -422,28 +416,47 @@ __global__ void __launch_bounds__(256) gemm_fp8_join_kernel(Fp8Gemm p, int slice
 // ---------------------------------------------------------------------------
 // Which kernel, and how many K slices.
 // ---------------------------------------------------------------------------
-struct Plan { int kind; int slices, per; int quartered; };   // kind: 0 16 weights, 1 64 weights a workgroup, 2 small tiles, 3 large tiles
+enum Kind { GEMV, SMALL_TILES, LARGE_TILES };
+struct Plan {
+    Kind kind;
+    int slices, per;   // K slices of `per` blocks
+    int rw;            // GEMV: 16 rw weights a workgroup
+    int quartered;     // LARGE_TILES: tiles cut into four
+};
 
 constexpr int kCus = 256;
 
 int up(int a, int b) { return (a + b - 1) / b; }
 
+// Slices that give every CU a workgroup, with two blocks a wave at least.
+int gemv_slices(int workgroups, int kb) {
+    return workgroups >= kCus / 2 ? 1 : std::max(1, std::min(kCus / workgroups, kb / (2 * kGemvWaves)));
+}
+
 Plan plan_of(int m, int n, int kb, bool fp32) {
-    Plan q{2, 1, kb, 0};
+    Plan q{SMALL_TILES, 1, kb, 1, 0};
     if (m <= 32) {
-        q.kind = up(n, 64) >= 2 * kCus ? 1 : 0;
-        const int wg = up(n, q.kind ? 64 : 16), waves = q.kind ? 4 : 8;
-        if (wg < kCus / 2) q.slices = std::min(kCus / wg, kb / (2 * waves));
+        // From 33 tokens on tiles are faster (64 x 3584 x 18944: 32 us, 58 here).  Past 16 tokens their re-reading shows: 64
+        // weights a workgroup where those fill the chip (32 x 37888 x 3584: 39 us, with 32 weights 41, with 16 54; 24 x
+        // 152064: 127, 138, 174), else 32 (20 x 4608 x 3584: 10.1, with 64 12.7, with 16 11.1).  Up to 16 tokens 16 weights
+        // (1 x 37888 x 3584: 26.3, with 32 26.8, with 64 29.6; 1 x 2048 x 1536: 3.6, 4.4, 6.3).
+        q.kind = GEMV;
+        if (m > 16) q.rw = up(n, 64) * gemv_slices(up(n, 64), kb) >= kCus * 7 / 8 ? 4 : 2;
+        q.slices = gemv_slices(up(n, 16 * q.rw), kb);
     } else {
         const int large = up(m, 256) * up(n, 256), small = up(m, 128) * up(n, 128);
         if (!fp32 && small > 2 * kCus) {
-            q.kind = 3;
+            // A block of K takes a large tile 1.5 us, a small one 0.73 alone on its CU and 1.18 beside another: large tiles win
+            // wherever they fill the chip (8192 x 3584 x 18944: 466 us, small ones 620).  A last round of few is cut into small
+            // tiles, each alone on a CU, half a large one's time (512 x 37888 x 3584: 82 us, uncut 104, small ones 91).
+            q.kind = LARGE_TILES;
             const int rest = large % kCus;
             q.quartered = rest <= kCus / 4 ? rest : 0;
             return q;
         }
         if (small <= kCus) {
-            // times in us: a block of K alone on a CU and beside another workgroup; the slices' sums written and read at 5 TB/s
+            // K slices: their time by those figures, and their sums written and read at 5 TB/s in a launch of 4 us more
+            // (512 x 3584 x 18944 in four: 67 us, whole 108)
             double best = 0.73 * kb;
             for (int s = 2; s <= 16 && s <= kb; ++s) {
                 const int wg = small * s;
@@ -455,35 +468,32 @@ Plan plan_of(int m, int n, int kb, bool fp32) {
             }
         }
     }
-    if (q.slices < 2) q.slices = 1;
     q.per = up(kb, q.slices);
     q.slices = up(kb, q.per);
     return q;
 }
 
-template <typename TO, int RW, int MT, int WV> void gemv(const Fp8Gemm& g, const Plan& q, hipStream_t s) {
+template <typename TO, int RW, int MT> void gemv(const Fp8Gemm& g, const Plan& q, hipStream_t s) {
     const dim3 grid(up(g.n, 16 * RW), q.slices);
-    if (q.slices > 1) gemv_fp8_kernel<TO, RW, MT, WV, true><<<grid, 64 * WV, 0, s>>>(g, q.per);
-    else gemv_fp8_kernel<TO, RW, MT, WV, false><<<grid, 64 * WV, 0, s>>>(g, q.per);
+    if (q.slices > 1) gemv_fp8_kernel<TO, RW, MT, true><<<grid, 64 * kGemvWaves, 0, s>>>(g, q.per);
+    else gemv_fp8_kernel<TO, RW, MT, false><<<grid, 64 * kGemvWaves, 0, s>>>(g, q.per);
 }
 
 template <typename TO> void run_plan(const Fp8Gemm& a, const Plan& q, hipStream_t s) {
     constexpr bool EXACT = sizeof(TO) == 4;
     Fp8Gemm g = a;
     if (q.slices == 1) g.part = nullptr;
-    if (q.kind == 0) {
-        if (g.m <= 16) gemv<TO, 1, 1, 8>(g, q, s);
-        else gemv<TO, 1, 2, 8>(g, q, s);
-    } else if (q.kind == 1) {
-        if (g.m <= 16) gemv<TO, 4, 1, 4>(g, q, s);
-        else gemv<TO, 4, 2, 4>(g, q, s);
+    if (q.kind == GEMV) {
+        if (g.m <= 16) gemv<TO, 1, 1>(g, q, s);
+        else if (q.rw == 2) gemv<TO, 2, 2>(g, q, s);
+        else gemv<TO, 4, 2>(g, q, s);
     } else {
-        const int b = q.kind == 3 ? 256 : 128;
+        const int b = q.kind == LARGE_TILES ? 256 : 128;
         TileMap tm{up(g.m, b), up(g.n, b), 0};
         tm.gm = std::min(tm.m_tiles, 8);
         const int tiles = tm.m_tiles * tm.n_tiles - q.quartered;
         if constexpr (!EXACT)
-            if (q.kind == 3) {
+            if (q.kind == LARGE_TILES) {
                 gemm_fp8_large_kernel<TO><<<up(tiles, 8) * 8 + 4 * q.quartered, 256, 0, s>>>(g, tm, q.quartered);
                 return;
             }
