@@ -32,10 +32,16 @@ __device__ __forceinline__ i32x8 join(u32x4 a, u32x4 b) {
 
 typedef __attribute__((address_space(3))) void lds_void_t;
 
-// BYTES a lane from a uniform base and a lane's offset straight to LDS: lane i to BYTES i past lds.
-template <int BYTES> __device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t off, uint8_t* lds) {
-    if constexpr (BYTES == 16) __builtin_amdgcn_global_load_lds(static_cast<const void*>(base + off), (lds_void_t*)(lds), 16, 0, 0);
-    else __builtin_amdgcn_global_load_lds(static_cast<const void*>(base + off), (lds_void_t*)(lds), 4, 0, 0);
+// Rows of memory that lanes load from to LDS.  `there` 0: nothing is there, and a load reads nothing (the
+// hardware compares each offset with the number of bytes).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const uint8_t* p, bool there) {
+    constexpr int kFormat32 = 4 << 15;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, there ? 0x7FFFFFFF : 0, kFormat32);
+}
+// BYTES a lane, off + more past the first row, straight to LDS: lane i to BYTES i past lds.
+template <int BYTES> __device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t rows, uint32_t off, int more, uint8_t* lds) {
+    if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_void_t*)(lds), 16, off, more, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_void_t*)(lds), 4, off, more, 0, 0);
 }
 
 // s_waitcnt vmcnt(N), the other counters left alone
@@ -139,7 +145,7 @@ __global__ void __launch_bounds__(64 * kGemvWaves, 4) gemv_fp8_kernel(Fp8Gemm p,
 
 // ---------------------------------------------------------------------------
 // Tiles of BM tokens x BN weights, 2 x 2 waves, 32x32x64 instructions (EXACT: four
-// 32x32x16 ones, see above), over the blocks of a K slice.
+// 32x32x16 ones, see above), over the nk blocks of K from k0 on, a multiple of four.
 //
 // A block of K of either operand is a slot of 128-byte rows in LDS, moved
 // there from memory without passing through registers, eight whole lines an
@@ -163,11 +169,12 @@ template <int BM, int BN, typename TO, bool EXACT>
 __device__ __forceinline__ void tile_fp8(const Fp8Gemm& p, int m0, int n0, int k0, int nk, uint8_t* smem, float* part) {
     constexpr int TM = BM / 2, TN = BN / 2, MT = TM / 32, NT = TN / 32;
     constexpr int AQ = BM / 64, WQ = BN / 32;                // line instructions a wave issues for half of the tokens, for the weights
-    constexpr int Q1 = WQ + AQ + 2, Q2 = AQ;                 // a block's first refill, with the scale words, and its second
-    constexpr int ASLOT = BM * 128 + 2048, WSLOT = BN * 128; // the scale words ride with the tokens
+    constexpr int Q1 = WQ + AQ, Q2 = AQ;                     // a block's first refill and its second
+    constexpr int ASLOT = BM * 128, WSLOT = BN * 128, SSLOT = 2048;   // SSLOT: scale words, of four blocks each
     static_assert(BM % 64 == 0 && BM <= 256 && (TN == 64 || TN == 128), "one word instruction, one weight scale a wave");
     uint8_t* const aslots = smem;
     uint8_t* const wslots = smem + 2 * ASLOT;
+    uint8_t* const sslots = smem + 2 * (ASLOT + WSLOT);
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -194,16 +201,23 @@ __device__ __forceinline__ void tile_fp8(const Fp8Gemm& p, int m0, int n0, int k
         woff[q] = min(n, p.n - 1 - n0) * static_cast<uint32_t>(p.w.ld) + 16u * ((lane & 7) ^ ((r >> 1) & 7));
     }
     const uint32_t soff = min((64 * wave + lane) % BM, p.m - 1 - m0) * static_cast<uint32_t>(p.a.lds);
-    const uint8_t* sabase = p.a.scales + m0 * p.a.lds;
-    const uint8_t* swbase = p.w.scales + static_cast<int64_t>(min((n0 + wn * TN) / 128, (p.n - 1) / 128)) * p.w.lds;
+    const uint8_t* sabase = p.a.scales + m0 * p.a.lds + k0;
+    const uint8_t* swbase = p.w.scales + static_cast<int64_t>(min((n0 + wn * TN) / 128, (p.n - 1) / 128)) * p.w.lds + k0;
 
-    auto issue = [&](int kt, int slot, int part, int q) {   // instruction q of block kt's first or second refill
+    struct Source { __amdgpu_buffer_rsrc_t a, w, sa, sw; };
+    auto source = [&](bool there) { return Source{rows_at(abase, there), rows_at(wbase, there), rows_at(sabase, there), rows_at(swbase, there)}; };
+    auto issue = [&](const Source& from, int kt, int slot, int part, int q) {   // instruction q of block kt's first or second refill
         uint8_t* as = aslots + slot * ASLOT;
-        if (part == 1) to_lds<16>(abase + kt * 128, aoff[1][q < AQ ? q : 0], as + arow(1, q) * 128);
-        else if (q < WQ) to_lds<16>(wbase + kt * 128, woff[q < WQ ? q : 0], wslots + slot * WSLOT + (wave * WQ + q) * 1024);
-        else if (q < WQ + AQ) to_lds<16>(abase + kt * 128, aoff[0][q < WQ + AQ && q >= WQ ? q - WQ : 0], as + arow(0, q - WQ) * 128);
-        else if (q == WQ + AQ) to_lds<4>(sabase + ((k0 + kt) & ~3), soff, as + BM * 128 + wave * 256);
-        else to_lds<4>(swbase + ((k0 + kt) & ~3), 0u, as + BM * 128 + 1024 + wave * 256);
+        if (part == 1) to_lds<16>(from.a, aoff[1][q < AQ ? q : 0], kt * 128, as + arow(1, q) * 128);
+        else if (q < WQ) to_lds<16>(from.w, woff[q < WQ ? q : 0], kt * 128, wslots + slot * WSLOT + (wave * WQ + q) * 1024);
+        else to_lds<16>(from.a, aoff[0][q >= WQ ? q - WQ : 0], kt * 128, as + arow(0, q - WQ) * 128);
+    };
+    // The scales of four blocks are one word of each row, 64 lines an instruction: they come with every second block's first
+    // refill and serve both.
+    auto issue_scales = [&](const Source& from, int kt) {
+        uint8_t* to = sslots + (kt >> 1 & 1) * SSLOT + wave * 256;
+        to_lds<4>(from.sa, soff, kt & ~3, to);
+        to_lds<4>(from.sw, 0u, kt & ~3, to + 1024);
     };
 
     f32x16 acc[NT][MT];
@@ -217,7 +231,7 @@ __device__ __forceinline__ void tile_fp8(const Fp8Gemm& p, int m0, int n0, int k
     // the swizzle of a fragment's row goes by r32 alone: rows of tiles are multiples of 32 apart
     const int swz = (r32 >> 1) & 7;
     const uint32_t la = (wm * TM + r32) * 128, lw = (wn * TN + r32) * 128;
-    const uint32_t lsa = BM * 128 + (wm * TM + r32) * 4, lsw = BM * 128 + 1024 + wave * 256;
+    const uint32_t lsa = (wm * TM + r32) * 4, lsw = 1024 + wave * 256;
     uint32_t ch[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c) ch[c] = ((2 * c + kh) ^ swz) << 4;
@@ -229,10 +243,11 @@ __device__ __forceinline__ void tile_fp8(const Fp8Gemm& p, int m0, int n0, int k
     auto read_w = [&](int slot, Weights& f, int t, int k) { f.w[t][k] = frag(wslots + slot * WSLOT + lw + 4096 * t, k); };
     auto read_a = [&](int slot, Tokens& f, int i, int k) { f.a[k] = frag(aslots + slot * ASLOT + la + 4096 * i, k); };
     struct Scales { uint32_t w, a[MT]; };
-    auto read_scales = [&](int slot, Scales& f) {
-        f.w = *reinterpret_cast<const uint32_t*>(aslots + slot * ASLOT + lsw);
+    auto read_scales = [&](int kt, Scales& f) {
+        const uint8_t* from = sslots + (kt >> 1 & 1) * SSLOT;
+        f.w = *reinterpret_cast<const uint32_t*>(from + lsw);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) f.a[i] = *reinterpret_cast<const uint32_t*>(aslots + slot * ASLOT + lsa + 128 * i);
+        for (int i = 0; i < MT; ++i) f.a[i] = *reinterpret_cast<const uint32_t*>(from + lsa + 128 * i);
     };
     // a block's products in two groups: every weight tile with half of the token tiles
     constexpr int GA = MT / 2, G = NT * 2 * GA;
@@ -241,20 +256,25 @@ __device__ __forceinline__ void tile_fp8(const Fp8Gemm& p, int m0, int n0, int k
     Scales sc, sc_next{};
     // Barriers stand B products into the halves, where the reads of the half before have long arrived.
     constexpr int B = 2 * GA, B0 = B, B1 = G + B;
-    auto block = [&](int kt, auto slot, auto steady) {   // block kt, in slots SLOT
+    // Block kt, in slots SLOT = kt % 2.  Past the last block the same instructions run: their loads bring nothing, what they read is
+    // not used, and where the blocks are odd in number the one behind the last multiplies codes that were there, of one
+    // of the blocks, under scales of 2^-127 each, which leaves every sum as it is.  (An end of its own for each number of
+    // blocks costs registers: the accumulators of several ways meet, and are spilled.)
+    auto block = [&](int kt, auto slot) {
         constexpr int SLOT = decltype(slot)::value;
-        constexpr bool ALL = decltype(steady)::value;
-        const bool more = ALL || kt + 1 < nk, refill = ALL || kt + 2 < nk;
-        const int sh = 8 * ((k0 + kt) & 3);
-        const int sw = static_cast<int>(sc.w >> sh);
+        const Source from = source(kt + 2 < nk);
+        const int sh = 8 * (kt & 3);
+        const bool real = SLOT == 0 || kt < nk;
+        const int sw = static_cast<int>(real ? sc.w >> sh : 0u);
         int sa[MT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) sa[i] = static_cast<int>(sc.a[i] >> sh);
+        for (int i = 0; i < MT; ++i) sa[i] = static_cast<int>(real ? sc.a[i] >> sh : 0u);
 #pragma unroll
         for (int y = 0; y < 2 * G; ++y) {
             // at B0: this block's second tokens are there, and every wave has read its weights and first tokens;
             // at B1: the next block's weights and first tokens are there, and the second tokens are read
-            if (y == B0 || y == B1) barrier_vm<ALL ? Q1 + Q2 : 0>();
+            // (where scale words are among those under way, the wait is for two more than it need be)
+            if (y == B0 || y == B1) barrier_vm<Q1 + Q2>();
             const int h = y / G, x = y % G, t = x / (2 * GA), k = x / GA % 2, u = x % GA;
             f32x16& c = acc[t][h * GA + u];
             if constexpr (EXACT) {
@@ -267,38 +287,36 @@ __device__ __forceinline__ void tile_fp8(const Fp8Gemm& p, int m0, int n0, int k
                 c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w.w[t][k], at[h][u].a[k], c, 0, 0, 0, sw, 0, sa[h * GA + u]);
             }
             if (y >= B0 && y < B0 + 2 * GA) read_a(SLOT, at[1][(y - B0) / 2], GA + (y - B0) / 2, (y - B0) % 2);
-            if (more && y >= B1 && y < B1 + 2 * GA) read_a(SLOT ^ 1, at[0][(y - B1) / 2], (y - B1) / 2, (y - B1) % 2);
-            if (more && y == B1 + 1) read_scales(SLOT ^ 1, sc_next);
+            if (y >= B1 && y < B1 + 2 * GA) read_a(SLOT ^ 1, at[0][(y - B1) / 2], (y - B1) / 2, (y - B1) % 2);
+            if (SLOT == 1 && y == B1 + 1) read_scales(kt + 1, sc_next);
 #pragma unroll
             for (int j = 0; j < 2 * NT; ++j) {   // the next block's weights, GA products behind the last of those that they replace
                 const int at_y = B1 + j * GA + GA - 1;
-                if (at_y == y && more) read_w(SLOT ^ 1, w, j / 2, j % 2);
+                if (at_y == y) read_w(SLOT ^ 1, w, j / 2, j % 2);
                 if (at_y == y + 2 * G) read_w(SLOT, w, j / 2, j % 2);
             }
             constexpr int EACH = Q1 > G ? 2 : 1;   // instructions a product
-            if (refill) {
-                const int from = y >= B1 ? B1 : B0, n = y >= B1 ? Q2 : Q1;   // the first has ended when the second begins
+            if (SLOT == 0 && y == B0) issue_scales(from, kt + 2);
+            const int since = y >= B1 ? y - B1 : y - B0, n = y >= B1 ? Q2 : Q1;   // the first refill has ended when the second begins
 #pragma unroll
-                for (int q = EACH * (y - from); q < EACH * (y - from + 1); ++q)
-                    if (q >= 0 && q < n) issue(kt + 2, SLOT, y >= B1, q);
-            }
+            for (int q = EACH * since; q < EACH * (since + 1); ++q)
+                if (q >= 0 && q < n) issue(from, kt + 2, SLOT, y >= B1, q);
             __builtin_amdgcn_sched_barrier(0);
         }
-        sc = sc_next;
+        if (SLOT == 1) sc = sc_next;
     };
     static_assert(2 * G >= Q1 && G >= Q2, "a refill within half a block");
 
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-        if (b < nk) {
+    for (int b = 0; b < 2; ++b) {
+        const Source from = source(true);
+        if (b == 0) issue_scales(from, 0);
 #pragma unroll
-            for (int q = 0; q < Q1; ++q) issue(b, b, 0, q);
+        for (int q = 0; q < Q1; ++q) issue(from, min(b, nk - 1), b, 0, q);
 #pragma unroll
-            for (int q = 0; q < Q2; ++q) issue(b, b, 1, q);
-        }
-    if (nk > 1) wait_vm<Q1 + 2 * Q2>();
-    else wait_vm<0>();
-    __syncthreads();
+        for (int q = 0; q < Q2; ++q) issue(from, min(b, nk - 1), b, 1, q);
+    }
+    barrier_vm<Q1 + 2 * Q2>();
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
 #pragma unroll
@@ -307,17 +325,11 @@ __device__ __forceinline__ void tile_fp8(const Fp8Gemm& p, int m0, int n0, int k
         for (int u = 0; u < GA; ++u) read_a(0, at[0][u], u, k);
     }
     read_scales(0, sc);
-    constexpr std::integral_constant<int, 0> even{};
-    constexpr std::integral_constant<int, 1> odd{};
-    int kt = 0;
-    for (; kt + 3 < nk; kt += 2) {
-        block(kt, even, std::true_type{});
-        block(kt + 1, odd, std::true_type{});
+    for (int kt = 0; kt < nk; kt += 2) {
+        block(kt, std::integral_constant<int, 0>{});
+        block(kt + 1, std::integral_constant<int, 1>{});
     }
-    for (; kt < nk; kt += 2) {
-        block(kt, even, std::false_type{});
-        if (kt + 1 < nk) block(kt + 1, odd, std::false_type{});
-    }
+    wait_vm<0>();   // nothing may come to LDS behind the workgroup's end
 
     TO* out = static_cast<TO*>(p.out);
 #pragma unroll
@@ -343,7 +355,7 @@ __device__ __forceinline__ void tile_fp8(const Fp8Gemm& p, int m0, int n0, int k
     }
 }
 
-template <int BM, int BN> constexpr int kTileLds = 2 * (BM * 128 + 2048) + 2 * BN * 128;
+template <int BM, int BN> constexpr int kTileLds = 2 * (BM * 128 + BN * 128 + 2048);
 
 // Tile number `tile` of tm: tokens fastest inside groups of gm.
 __device__ __forceinline__ void tile_of(const TileMap& tm, int tile, int* m_tile, int* n_tile) {
@@ -446,9 +458,10 @@ Plan plan_of(int m, int n, int kb, bool fp32) {
     } else {
         const int large = up(m, 256) * up(n, 256), small = up(m, 128) * up(n, 128);
         if (!fp32 && small > 2 * kCus) {
-            // A block of K takes a large tile 1.5 us, a small one 0.73 alone on its CU and 1.18 beside another: large tiles win
-            // wherever they fill the chip (8192 x 3584 x 18944: 466 us, small ones 620).  A last round of few is cut into small
-            // tiles, each alone on a CU, half a large one's time (512 x 37888 x 3584: 82 us, uncut 104, small ones 91).
+            // A block of K takes a large tile 1.2 to 1.4 us, a small one 0.65 alone on its CU and 1.1 beside another: large tiles
+            // win wherever they fill the chip (8192 x 3584 x 18944: 406 us, small ones 553; 512 x 18944 x 3584: 47 and 53; but 512
+            // x 14336 x 3584, 448 small tiles: 46 and 39).  A last round of few is cut into small tiles, each alone on a CU, half a
+            // large one's time (512 x 37888 x 3584: 77 us, uncut 97, small ones 90).
             q.kind = LARGE_TILES;
             const int rest = large % kCus;
             q.quartered = rest <= kCus / 4 ? rest : 0;
@@ -456,11 +469,11 @@ Plan plan_of(int m, int n, int kb, bool fp32) {
         }
         if (small <= kCus) {
             // K slices: their time by those figures, and their sums written and read at 5 TB/s in a launch of 4 us more
-            // (512 x 3584 x 18944 in four: 67 us, whole 108)
-            double best = 0.73 * kb;
+            // (512 x 3584 x 18944 in four: 67 us, whole 94)
+            double best = 0.65 * kb;
             for (int s = 2; s <= 16 && s <= kb; ++s) {
                 const int wg = small * s;
-                const double t = up(kb, s) * (wg <= kCus ? 0.73 : 1.18 * up(wg, 2 * kCus)) + 4.0 + 8e-6 * s * m * n / 5.0;
+                const double t = std::min(kb, up(up(kb, s), 4) * 4) * (wg <= kCus ? 0.65 : 1.1 * up(wg, 2 * kCus)) + 4.0 + 8e-6 * s * m * n / 5.0;
                 if (t < best) {
                     best = t;
                     q.slices = s;
@@ -469,6 +482,7 @@ Plan plan_of(int m, int n, int kb, bool fp32) {
         }
     }
     q.per = up(kb, q.slices);
+    if (q.kind == SMALL_TILES) q.per = up(q.per, 4) * 4;   // whole scale words
     q.slices = up(kb, q.per);
     return q;
 }
