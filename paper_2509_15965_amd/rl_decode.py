@@ -728,28 +728,46 @@ def empty_fp8(rows: int, k: int, *, weight: bool = False, device="cuda"):
 
 def _bytes_on(dev: int, name: str, t: torch.Tensor, dtypes, rows: int, width: int):
     """(pointer, row stride) of a matrix of bytes with this many rows of at least `width`."""
-    if t.dim() != 2 or t.dtype not in dtypes or t.get_device() != dev or t.shape[0] != rows or t.shape[1] < width:
-        raise ValueError(f"{name} must be {rows} rows of {width} or more {' or '.join(map(str, dtypes))} on cuda:{dev}, "
-                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
-    ld = t.stride(0) if rows > 1 else max(t.shape[1], t.stride(0))
-    if (t.shape[1] > 1 and t.stride(1) != 1) or ld < t.shape[1]:
-        raise ValueError(f"{name}: entries of a row must be contiguous and rows apart: strides {t.stride()}")
-    return t.data_ptr(), ld
+    shape, st = t.shape, t.stride()
+    if len(shape) == 2 and shape[0] == rows and shape[1] >= width and t.dtype in dtypes and t.get_device() == dev:
+        w = shape[1]
+        ld = st[0] if rows > 1 else max(w, st[0])
+        if ld >= w and (st[1] == 1 or w < 2):
+            return t.data_ptr(), ld
+    raise ValueError(f"{name} must be {rows} rows, apart, of {width} or more contiguous {' or '.join(map(str, dtypes))} on "
+                     f"cuda:{dev}, not {t.dtype} {tuple(shape)} with strides {st} on {t.device}")
 
 
 def _fp8_on(dev: int, name: str, codes: torch.Tensor, scales: torch.Tensor, rows: int, k: int, weight: bool = False) -> Fp8Matrix:
-    kb = fp8_blocks(k)
+    kb = (k + 127) // 128
     c, ld = _bytes_on(dev, name, codes, _CODES, rows, 128 * kb)
-    b, lds = _bytes_on(dev, name + " scales", scales, _SCALES, fp8_blocks(rows) if weight else rows, kb)
+    b, lds = _bytes_on(dev, name, scales, _SCALES, (rows + 127) // 128 if weight else rows, kb)
     return Fp8Matrix(c, ld, b, lds)
 
 
-def _numbers_on(dev: int, name: str, t: torch.Tensor, rows: int, width: int):
-    """(pointer, row stride) of float32 or bfloat16 rows."""
-    p, ld = _rows_on(dev, name, t)
-    if t.shape != (rows, width):
-        raise ValueError(f"{name} must be {rows} rows of {width} entries, not {tuple(t.shape)}")
-    return p, ld
+def _numbers_on(dev: int, name: str, t: torch.Tensor, rows: Optional[int] = None, width: Optional[int] = None):
+    """(pointer, row stride, rows, entries, rl_dtype) of float32 or bfloat16 rows."""
+    shape, st, dt = t.shape, t.stride(), t.dtype
+    if len(shape) == 2 and (dt is torch.bfloat16 or dt is torch.float32) and t.get_device() == dev:
+        n, w = shape
+        ld = st[0] if n > 1 else w
+        if (rows is None or (n == rows and w == width)) and ld >= w and w < 1 << 31 and (st[1] == 1 or w < 2):
+            return t.data_ptr(), ld, n, w, RL_DTYPE_BF16 if dt is torch.bfloat16 else RL_DTYPE_FP32
+    size = "" if rows is None else f"{rows} rows of {width} entries, "
+    raise ValueError(f"{name} must be a matrix of float32 or bfloat16, {size}rows apart and of contiguous entries, on cuda:{dev}, "
+                     f"not {dt} {tuple(shape)} with strides {st} on {t.device}")
+
+
+def _launch_on(dev: int, stream, what: str, call, *args):
+    """call(*args, stream) with GPU `dev` current: a call without a workspace."""
+    if torch.cuda.current_device() != dev:
+        with torch.cuda.device(dev):
+            return _launch_on(dev, stream, what, call, *args)
+    if stream is not None and stream.device.index != dev:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{dev}")
+    st = call(*args, _current_stream(dev) if stream is None else stream.cuda_stream)
+    if st != RL_OK:
+        raise RLError(st, what)
 
 
 def rmsnorm_quant(x: torch.Tensor, weight: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, *,
@@ -757,20 +775,22 @@ def rmsnorm_quant(x: torch.Tensor, weight: torch.Tensor, codes: torch.Tensor, sc
     """rl_rmsnorm_quant: rows of x (+ add, the sum to out_sum, which may be x)
     normed, times weight, in 8 bits."""
     dev = _gpu_of(x, "x")
-    xp, ldx = _rows_on(dev, "x", x)
-    n, H = x.shape
-    if weight.dim() != 1 or weight.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"weight must be a vector of float32 or bfloat16, not {weight.dtype} {tuple(weight.shape)}")
-    w = _on(dev, "weight", weight, weight.dtype, H)
-    ap, lda = _numbers_on(dev, "add", add, n, H) if add is not None else (None, 0)
-    sp, lds = _numbers_on(dev, "out_sum", out_sum, n, H) if out_sum is not None else (None, 0)
-    if out_sum is not None and out_sum.dtype is not x.dtype:
-        raise ValueError(f"out_sum must be {x.dtype} as x is, not {out_sum.dtype}")
+    xp, ldx, n, H, dt = _numbers_on(dev, "x", x)
+    wdt = weight.dtype
+    if weight.dim() != 1 or (wdt is not torch.bfloat16 and wdt is not torch.float32):
+        raise ValueError(f"weight must be a vector of float32 or bfloat16, not {wdt} {tuple(weight.shape)}")
+    w = _on(dev, "weight", weight, wdt, H)
+    ap, lda, adt = None, 0, dt
+    if add is not None:
+        ap, lda, _, _, adt = _numbers_on(dev, "add", add, n, H)
+    sp, lds = None, 0
+    if out_sum is not None:
+        sp, lds, _, _, sdt = _numbers_on(dev, "out_sum", out_sum, n, H)
+        if sdt != dt:
+            raise ValueError(f"out_sum must be {x.dtype} as x is, not {out_sum.dtype}")
     out = _fp8_on(dev, "codes", codes, scales, n, H)
-    L = lib()
-    _run_on(dev, stream, 0, None,
-            lambda ws, nb, s: L.rl_rmsnorm_quant(n, H, _dtype_code(x), xp, ldx, _dtype_code(x if add is None else add), ap, lda,
-                                               _dtype_code(weight), w, eps, sp, lds, C.byref(out), s), "rl_rmsnorm_quant")
+    _launch_on(dev, stream, "rl_rmsnorm_quant", lib().rl_rmsnorm_quant, n, H, dt, xp, ldx, adt, ap, lda,
+               RL_DTYPE_BF16 if wdt is torch.bfloat16 else RL_DTYPE_FP32, w, eps, sp, lds, C.byref(out))
 
 
 def quantise(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, *, form: str = "rows", stream=None):
@@ -779,16 +799,13 @@ def quantise(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, *, form
     if form not in FP8_FORMS:
         raise ValueError(f"form is one of {tuple(FP8_FORMS)}")
     dev = _gpu_of(x, "x")
-    xp, ldx = _rows_on(dev, "x", x)
-    n, k = x.shape
+    xp, ldx, n, k, dt = _numbers_on(dev, "x", x)
     if form == "swiglu":
         if k % 2:
             raise ValueError("the two halves of a row are of one size")
         k //= 2
     out = _fp8_on(dev, "codes", codes, scales, n, k, form == "tiles")
-    L = lib()
-    _run_on(dev, stream, 0, None,
-            lambda ws, nb, s: L.rl_quantise(FP8_FORMS[form], n, k, _dtype_code(x), xp, ldx, C.byref(out), s), "rl_quantise")
+    _launch_on(dev, stream, "rl_quantise", lib().rl_quantise, FP8_FORMS[form], n, k, dt, xp, ldx, C.byref(out))
 
 
 def gemm_quant(a: torch.Tensor, a_scales: torch.Tensor, w: torch.Tensor, w_scales: torch.Tensor, out: torch.Tensor, *,
@@ -796,17 +813,20 @@ def gemm_quant(a: torch.Tensor, a_scales: torch.Tensor, w: torch.Tensor, w_scale
     """rl_gemm_quant: out [m][n] = a [m][k] times the weight w [n][k] (tiles),
     both in whole blocks of 128 codes."""
     dev = _gpu_of(out, "out")
-    o, ldo = _rows_on(dev, "out", out)
-    m, n = out.shape
-    k = a.shape[1] if a.dim() == 2 else 0
+    o, ldo, m, n, dt = _numbers_on(dev, "out", out)
+    k = a.shape[-1] if a.dim() == 2 else 0
     if k < 1 or k % 128:
         raise ValueError(f"a must hold rows of whole blocks of 128 codes, not {tuple(a.shape)}")
     A, W = _fp8_on(dev, "a", a, a_scales, m, k), _fp8_on(dev, "w", w, w_scales, n, k, True)
     if w.shape[1] != k:
         raise ValueError(f"a has rows of {k} codes, w of {w.shape[1]}")
     L = lib()
-    _run_on(dev, stream, L.rl_gemm_quant_workspace_bytes(m, n, k) if workspace is None else 0, workspace,
-            lambda ws, nb, s: L.rl_gemm_quant(m, n, k, C.byref(A), C.byref(W), _dtype_code(out), o, ldo, ws, nb, s), "rl_gemm_quant")
+    need = L.rl_gemm_quant_workspace_bytes(m, n, k) if workspace is None else 0
+    if workspace is None and not need:
+        _launch_on(dev, stream, "rl_gemm_quant", L.rl_gemm_quant, m, n, k, C.byref(A), C.byref(W), dt, o, ldo, None, 0)
+        return
+    _run_on(dev, stream, need, workspace,
+            lambda ws, nb, s: L.rl_gemm_quant(m, n, k, C.byref(A), C.byref(W), dt, o, ldo, ws, nb, s), "rl_gemm_quant")
 
 
 def kv_quant_bytes(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int) -> int:
@@ -815,31 +835,31 @@ def kv_quant_bytes(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int)
 
 def _heads_on(dev: int, name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None):
     """(pointer, row stride) of [n][heads][d] whose heads lie one after the other."""
-    if t.dim() != 3 or t.dtype not in (torch.float32, torch.bfloat16) or t.get_device() != dev or (
-            like is not None and (t.dtype is not like.dtype or t.shape != like.shape)):
-        raise ValueError(f"{name} must be [n][heads][d] of float32 or bfloat16 on cuda:{dev}"
-                         + (f" like the other ({tuple(like.shape)} {like.dtype})" if like is not None else "")
-                         + f", not {t.dtype} {tuple(t.shape)} on {t.device}")
-    n, h, d = t.shape
-    ld = t.stride(0) if n > 1 else h * d
-    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d) or ld < h * d:
-        raise ValueError(f"{name}: a token's heads must be contiguous and tokens apart: strides {t.stride()}")
-    return t.data_ptr(), ld
+    shape, st, dt = t.shape, t.stride(), t.dtype
+    if len(shape) == 3 and (dt is torch.bfloat16 or dt is torch.float32) and t.get_device() == dev and (
+            like is None or (dt is like.dtype and shape == like.shape)):
+        n, h, d = shape
+        ld = st[0] if n > 1 else h * d
+        if (st[2] == 1 or d < 2) and (st[1] == d or h < 2) and ld >= h * d:
+            return t.data_ptr(), ld
+    raise ValueError(f"{name} must be [n][heads][d] of float32 or bfloat16 on cuda:{dev}, a token's heads contiguous and tokens apart"
+                     + (f", like the other ({tuple(like.shape)} {like.dtype})" if like is not None else "")
+                     + f", not {dt} {tuple(shape)} with strides {st} on {t.device}")
 
 
 def _cache_on(dev: int, pool: torch.Tensor, page_table: torch.Tensor, page_size: int, heads: int, d: int) -> KvFp8:
-    one = kv_quant_bytes(1, page_size, heads, d)
+    one = lib().rl_kv_quant_bytes(1, page_size, heads, d)
     if not one:
         raise ValueError(f"no cache of pages of {page_size} positions with {heads} heads of {d}")
-    if page_table.dim() != 2:
-        raise ValueError(f"page_table must be [sequences][pages], not {tuple(page_table.shape)}")
+    shape = page_table.shape
+    if len(shape) != 2:
+        raise ValueError(f"page_table must be [sequences][pages], not {tuple(shape)}")
     n_pages = pool.numel() // one
     if pool.dtype is not torch.uint8 or pool.get_device() != dev or not pool.is_contiguous() or not 0 < n_pages < 1 << 31:
         raise ValueError(f"pool must be a contiguous uint8 tensor of whole pages ({one} bytes) on cuda:{dev}, not {pool.dtype} "
                          f"{tuple(pool.shape)} on {pool.device}")
-    return KvFp8(pool.data_ptr(),
-                 _on(dev, "page_table", page_table, torch.int32, page_table.numel()), page_table.shape[0], page_table.shape[1],
-                 n_pages, page_size, heads, d)
+    table = _on(dev, "page_table", page_table, torch.int32, shape[0] * shape[1])
+    return KvFp8(pool.data_ptr(), table, shape[0], shape[1], n_pages, page_size, heads, d)
 
 
 def _kv_call(name: str, dev: int, pool, page_table, seqs, positions, k, v, page_size, stream):
@@ -848,8 +868,7 @@ def _kv_call(name: str, dev: int, pool, page_table, seqs, positions, k, v, page_
     n, h, d = k.shape
     cache = _cache_on(dev, pool, page_table, page_size, h, d)
     sq, ps = _on(dev, "seqs", seqs, torch.int32, n), _on(dev, "positions", positions, torch.int32, n)
-    f = getattr(lib(), name)
-    _run_on(dev, stream, 0, None, lambda ws, nb, s: f(C.byref(cache), n, sq, ps, _dtype_code(k), kp, ldk, vp, ldv, s), name)
+    _launch_on(dev, stream, name, getattr(lib(), name), C.byref(cache), n, sq, ps, _dtype_code(k), kp, ldk, vp, ldv)
 
 
 def kv_quant_append(pool: torch.Tensor, page_table: torch.Tensor, seqs: torch.Tensor, positions: torch.Tensor, k: torch.Tensor,
