@@ -584,7 +584,12 @@ size_t rl_gemm_quant_workspace_bytes(int32_t m, int32_t n, int32_t k);
 /* out = a w^T: [m][ldo] of out_dtype, rounded once from fp32 sums.
  *  a  [m][k] with a scale for each block of a row (rl_rmsnorm_quant, RL_FP8_ROWS, RL_FP8_SWIGLU).
  *  w  [n][k] with a scale for each tile (RL_FP8_TILES).
- *  m, n <= 2^20, k <= 131072. */
+ *  m, n <= 2^20, k <= 131072.
+ * Sums are fp32.  Up to 32 rows, and with an fp32 out, the products are added
+ * as fp32 numbers (numbers below 2^-126 count as 0, from 2^128 on as infinite);
+ * with a bf16 out of more rows the matrix unit adds eight products at a time
+ * with 14 bits from the leading bit of the largest on (1.3e-5 of the result on
+ * normal numbers, where the rounding to bf16 is 1.7e-3). */
 rl_status rl_gemm_quant(int32_t m, int32_t n, int32_t k, const rl_fp8_matrix* a, const rl_fp8_matrix* w, int32_t out_dtype, void* out,
                       int64_t ldo, void* workspace, size_t ws_bytes, void* stream);
 
@@ -646,7 +651,8 @@ size_t rl_attention_quant_workspace_bytes(int32_t n, int32_t n_kv_heads, int32_t
  *  max_length  no row is longer: a longer one is taken as this long.  The
  *              work is laid out by it, so a near bound is the fastest.
  *  q, out      [n][ld] of dtype, a token's heads one after the other.  The
- *              weights of the values keep 16 bits for bf16 and 24 for fp32. */
+ *              weights of the values keep 16 bits for bf16 and 24 for fp32;
+ *              values below about 1e-33 count as 0. */
 rl_status rl_attention_quant(const rl_kv_fp8* cache, int32_t n, const int32_t* seqs, const int32_t* lengths, int32_t max_length,
                            int32_t dtype, const void* q, int64_t ldq, int32_t n_q_heads, double scale, void* out, int64_t ldo,
                            void* workspace, size_t ws_bytes, void* stream);

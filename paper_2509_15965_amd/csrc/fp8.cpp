@@ -123,7 +123,7 @@ rl_status rl_kv_quant_read(const rl_kv_fp8* cache, int32_t n, const int32_t* seq
 size_t rl_attention_quant_workspace_bytes(int32_t n, int32_t n_kv_heads, int32_t n_q_heads, int32_t head_dim, int32_t max_length) {
     if (n < 1 || n > kMaxSeqs || n_kv_heads < 1 || n_kv_heads > 1024 || n_q_heads < n_kv_heads || n_q_heads % n_kv_heads != 0 ||
         n_q_heads / n_kv_heads > 16 || (head_dim != 64 && head_dim != 128) || max_length < 0 ||
-        !attention_fp8_fits(n, n_kv_heads, max_length))
+        !attention_fp8_fits(n, n_kv_heads, n_q_heads, max_length))
         return 0;
     return attention_fp8_ws_bytes(n, n_kv_heads, n_q_heads, head_dim, max_length);
 }
@@ -136,7 +136,7 @@ rl_status rl_attention_quant(const rl_kv_fp8* cache, int32_t n, const int32_t* s
     if (n_q_heads < c.heads || n_q_heads % c.heads != 0 || n_q_heads / c.heads > 16) return RL_ERR_INVALID_ARG;
     if (max_length < 0 || max_length > static_cast<int64_t>(c.max_pages) * c.page || (!seqs && n > c.n_seqs)) return RL_ERR_INVALID_ARG;
     if (n == 0) return RL_OK;
-    if (!attention_fp8_fits(n, c.heads, max_length)) return RL_ERR_UNSUPPORTED;
+    if (!attention_fp8_fits(n, c.heads, n_q_heads, max_length)) return RL_ERR_UNSUPPORTED;
     const int64_t width = static_cast<int64_t>(n_q_heads) * c.dim;
     if (!lengths || !rows_ok(dtype, q, n, width, ldq) || !rows_ok(dtype, out, n, width, ldo)) return RL_ERR_INVALID_ARG;
     if (const rl_status st = workspace_ok(workspace, ws_bytes, attention_fp8_ws_bytes(n, c.heads, n_q_heads, c.dim, max_length)); st != RL_OK)

@@ -10,6 +10,8 @@
 #include "fp8.h"
 #include "rl_decode.h"
 
+#include <algorithm>
+
 namespace rl {
 
 namespace {
@@ -348,8 +350,9 @@ template <typename T, int D, int QT, int PT> hipError_t attend(const AttnFp8& a,
 
 }  // namespace
 
-bool attention_fp8_fits(int n, int kv_heads, int max_length) {
-    return static_cast<int64_t>(n) * kv_heads * chunks_of(n, kv_heads, max_length) < (int64_t(1) << 31);
+bool attention_fp8_fits(int n, int kv_heads, int heads, int max_length) {
+    const int64_t most = std::max(static_cast<int64_t>(kv_heads) * chunks_of(n, kv_heads, max_length), static_cast<int64_t>(heads));
+    return n * most < (int64_t(1) << 31);
 }
 size_t attention_fp8_ws_bytes(int n, int kv_heads, int heads, int dim, int max_length) {
     const int c = chunks_of(n, kv_heads, max_length);

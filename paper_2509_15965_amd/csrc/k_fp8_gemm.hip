@@ -458,14 +458,17 @@ Plan plan_of(int m, int n, int kb, bool fp32) {
     } else {
         const int large = up(m, 256) * up(n, 256), small = up(m, 128) * up(n, 128);
         if (!fp32 && small > 2 * kCus) {
-            // A block of K takes a large tile 1.2 to 1.4 us, a small one 0.65 alone on its CU and 1.1 beside another: large tiles
-            // win wherever they fill the chip (8192 x 3584 x 18944: 406 us, small ones 553; 512 x 18944 x 3584: 47 and 53; but 512
+            // A block of K takes a large tile 1.2 to 1.4 us, a small one 0.65 alone on its CU and 1.1 beside another, so large tiles
+            // win where they are well filled (8192 x 3584 x 18944: 406 us, small ones 553; 512 x 18944 x 3584: 47 and 53; but 512
             // x 14336 x 3584, 448 small tiles: 46 and 39).  A last round of few is cut into small tiles, each alone on a CU, half a
             // large one's time (512 x 37888 x 3584: 77 us, uncut 97, small ones 90).
-            q.kind = LARGE_TILES;
-            const int rest = large % kCus;
-            q.quartered = rest <= kCus / 4 ? rest : 0;
-            return q;
+            const int rest = large % kCus, quartered = rest <= kCus / 4 ? rest : 0;
+            const double rounds = large / kCus + (rest == 0 ? 0.0 : quartered ? 0.5 : 1.0);
+            if (1.3 * rounds < 1.1 * up(small, 2 * kCus)) {
+                q.kind = LARGE_TILES;
+                q.quartered = quartered;
+                return q;
+            }
         }
         if (small <= kCus) {
             // K slices: their time by those figures, and their sums written and read at 5 TB/s in a launch of 4 us more
