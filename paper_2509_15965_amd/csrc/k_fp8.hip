@@ -181,15 +181,15 @@ __device__ __forceinline__ uint8_t* kv_place(const KvFp8& c, const KvTokens& t, 
     return c.pool + (static_cast<int64_t>(pg) * c.heads + h) * c.block;
 }
 
-// Whether token i begins eight that fill positions 8 j .. 8 j + 7 of its sequence; token i of such an eight looks from its
-// place on (first: token of position 8 j).
-__device__ __forceinline__ bool kv_eight(const KvTokens& t, int first) {
-    if (first < 0 || first + 8 > t.n) return false;
-    const int s = t.seqs[first], pos = t.pos[first];
-    bool all = (pos & 7) == 0 && pos >= 0;
-#pragma unroll
-    for (int e = 1; e < 8; ++e) all = all && t.seqs[first + e] == s && t.pos[first + e] == pos + e;
-    return all;
+// Whether token i is of eight that follow one another in the call and fill positions 8 j .. 8 j + 7 of their sequence: each
+// of the lane group's first eight lanes looks at one of them.
+template <int LANES> __device__ __forceinline__ bool kv_eight(const KvTokens& t, int i) {
+    const int s = t.seqs[i], pos = t.pos[i], first = i - (pos & 7), e = threadIdx.x & 7;
+    const bool in = first >= 0 && first + 8 <= t.n;
+    const int at = in ? first + e : i;
+    const bool same = t.seqs[at] == s, next = t.pos[at] == (pos & ~7) + e;
+    const uint64_t all = __ballot(in && same && next) >> ((threadIdx.x & 63) / LANES * LANES);
+    return (all & 255u) == 255u;
 }
 
 // Token and head of this lane group, of LANES lanes.
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(256) kv_fp8_append_kernel(KvFp8 c, KvTokens t)
     }
     load_row<8>(static_cast<const T*>(t.v) + i * t.ldv + at, 8, v);
     uint8_t* blk = kv_place(c, t, i, h, &local);
-    const bool eight = kv_eight(t, i - t.pos[i] % 8);
+    const bool eight = kv_eight<LANES>(t, i);
     if (!blk || (eight && local % 8 != 0)) return;
     uint8_t* dst = blk + c.page * D + (local / 8 * D + 8 * lane) * 8;
     uint8_t* sdst = blk + 2 * c.page * D + c.page + local;
@@ -282,6 +282,7 @@ __global__ void __launch_bounds__(256) kv_fp8_read_kernel(KvFp8 c, KvTokens t) {
     const int i = kv_unit<LANES>(c, &h);
     if (i >= t.n) return;
     const uint8_t* blk = kv_place(c, t, i, h, &local);
+    const bool eight = blockIdx.y != 0 && kv_eight<LANES>(t, i);
     const int at = h * D + 8 * lane;
     T* out = (blockIdx.y == 0 ? static_cast<T*>(t.out_k) + i * t.ld_ok : static_cast<T*>(t.out_v) + i * t.ld_ov) + at;
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -297,7 +298,7 @@ __global__ void __launch_bounds__(256) kv_fp8_read_kernel(KvFp8 c, KvTokens t) {
         w[1] = q.y;
     } else {
         const uint8_t* src = blk + c.page * D + (local / 8 * D + 8 * lane) * 8;
-        if (kv_eight(t, i - local % 8)) {
+        if (eight) {
             if (local % 8 != 0) return;
             uint32_t all[8][2], o[8][2];
             const uint2 s8 = *reinterpret_cast<const uint2*>(sb);
