@@ -10,7 +10,9 @@ namespace {
 // ---------------------------------------------------------------------------
 // RMS norm.  s = x + add (as stored), y = s w / sqrt(mean s^2 + eps), y in blocks of
 // 128.  WAVES waves a row, a row in registers from its one read to its codes: NV
-// times 16 bytes of x a lane.
+// times 16 bytes of x a lane.  Bound by memory: 8192 x 3584 in fp32 with a bf16
+// branch, 323 MB, 66 us (4.9 TB/s, a copy's rate); 32 bytes of x a lane, so that an
+// instruction takes every other 16: 87.
 // ---------------------------------------------------------------------------
 template <typename T, int WAVES, int NV>
 __global__ void __launch_bounds__(256) rmsnorm_fp8_kernel(NormArgs p) {
@@ -85,7 +87,9 @@ __global__ void __launch_bounds__(256) rmsnorm_fp8_kernel(NormArgs p) {
 }
 
 // ---------------------------------------------------------------------------
-// Rows: 128 / E lanes a block, U blocks a lane group, 256 / (128 / E) apart.
+// Rows: 128 / E lanes a block, U blocks a lane group.  Bound by memory: SwiGLU of 512 x
+// 18944 bf16, 49 MB, 10.5 us (4.6 TB/s); with division and the library's exponential
+// and one block a lane group 15.6, bound by arithmetic.
 // ---------------------------------------------------------------------------
 template <typename T, bool SWIGLU, int U>
 __global__ void __launch_bounds__(256) quantise_rows_kernel(int n, int k, const T* __restrict__ x, int64_t ldx, Fp8Out out) {
@@ -122,7 +126,7 @@ __global__ void __launch_bounds__(256) quantise_rows_kernel(int n, int k, const 
 
 // ---------------------------------------------------------------------------
 // Weight tiles of 128 x 128 under one scale: a workgroup a tile, the tile in
-// registers.
+// registers.  Bound by memory: 37888 x 3584 bf16, 407 MB, 80 us (5.1 TB/s).
 // ---------------------------------------------------------------------------
 template <typename T>
 __global__ void __launch_bounds__(256) quantise_tiles_kernel(int n, int k, const T* __restrict__ x, int64_t ldx, Fp8Out out) {
@@ -168,7 +172,9 @@ __global__ void __launch_bounds__(256) quantise_tiles_kernel(int n, int k, const
 
 // ---------------------------------------------------------------------------
 // The cache.  One scale for a head's entries of one position; D / 8 lanes a
-// head, 8 entries a lane.
+// head, 8 entries a lane.  21162 tokens of 4 heads of 128 in bf16, 65 MB each way: written
+// in 22.4 us, read in 20.7 (keys alone 10; values byte by byte 62 and 27); 512 single
+// tokens 5.0 and 4.2, chains of three loads: place, page, data.
 // ---------------------------------------------------------------------------
 // Page block of (token i, head h) and the position in it; null where the token has no place.
 __device__ __forceinline__ uint8_t* kv_place(const KvFp8& c, const KvTokens& t, int i, int h, int* local) {

@@ -5,8 +5,10 @@
 // Per 32 positions a wave computes S^T = K q^T and adds V^T P^T to its sums with
 // 16x16x32 bf16 matrix instructions: e4m3 codes and their power-of-two scales
 // are bf16 numbers exactly, and the layout of the S tiles is that of the P operand
-// when the rows of K are taken in the order of row_of below, so nothing crosses lanes
-// but two maxima.  P and fp32 queries enter as sums of bf16 numbers (TERMS).
+// when the rows of K are taken in the order that Step says, so nothing crosses lanes but
+// two maxima.  P and fp32 queries enter as sums of bf16 numbers (PT, QT).
+// Bound by the cache's bytes: 512 sequences of 2000 positions, 28 q-heads on 4 kv-heads
+// of 128, 1.2 GB, take 240 us (5.0 TB/s); three of 8000, 40 on 8, 52 MB, 14.
 #include "fp8.h"
 #include "rl_decode.h"
 
@@ -235,7 +237,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) attention_fp8_kernel(AttnFp8 p
     }
 }
 
-// The chunks of one (row, kv-head), joined in their order; four entries a thread.
+// The chunks of one (row, kv-head), joined in their order; four entries a thread, eight chunks' loads at once.  8 us
+// for 512 x 4 of at most five chunks.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) attention_fp8_join_kernel(AttnFp8 p, int chunk, int n_chunks) {
     constexpr int U = 8;   // chunks whose loads are in flight together
@@ -271,6 +274,7 @@ __global__ void __launch_bounds__(256) attention_fp8_join_kernel(AttnFp8 p, int 
 }
 
 // The same for many chunks: a workgroup a query head, its lane groups every GROUPS-th chunk, joined in LDS in their order.
+// 24 x 34 chunks of 5 heads take 4.2 us, 7 the other way, where a thread reads them all.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) attention_fp8_join_head_kernel(AttnFp8 p, int chunk, int n_chunks) {
     constexpr int LANES = D / 4, GROUPS = 256 / LANES, U = 4;
@@ -315,7 +319,8 @@ __global__ void __launch_bounds__(256) attention_fp8_join_head_kernel(AttnFp8 p,
     write_out(static_cast<T*>(p.out) + row * p.ldo + head * D, 4 * lane, o, L);
 }
 
-// Positions a workgroup takes, a multiple of 128.
+// Positions a workgroup takes, a multiple of 128: 1024 (512 x 4 x 2000: 248 us; with 512 278, with 2048 247), fewer where
+// that leaves fewer than 1024 workgroups.
 constexpr int kMaxChunk = 64 * kStep;
 int chunk_of(int n, int kv_heads, int max_length) {
     int chunk = 1024;

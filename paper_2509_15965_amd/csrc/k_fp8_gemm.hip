@@ -1,18 +1,18 @@
 // k_fp8_gemm.hip -- out = A W^T of matrices in 8 bits: e4m3 codes, a power-of-two
 // scale for each row's 128 entries of A and each 128 x 128 tile of W.
 //
-// A product over one block of 128 is one 16x16x128 matrix instruction, which takes the
+// A product over half a block is one 32x32x64 matrix instruction, which takes the
 // scales of its rows and columns as exponent bytes: the fp32 sum over the
-// blocks needs no further arithmetic.  Which 32 entries of the block a lane
-// group holds is free, as long as A and W agree.
+// blocks needs no further arithmetic.  Which entries of the block a lane group
+// holds is free, as long as A and W agree.
 //
 // That instruction adds eight products at a time with 14 bits, counted from the
 // leading bit of the largest (measured: with one product of 2^16 among the
 // eight, 2^3 still counts and 2^2 does not); what it adds across eights and to the sum so
 // far has fp32's 24.  On normal numbers 1.3e-5 of the result, 1/100 of the
 // rounding to bf16 that follows.  Where the output is fp32, or the product is bound
-// by its bytes anyway, the codes go as bf16 numbers, exactly, through 16x16x32
-// bf16 instructions, which add in fp32 throughout (9e-9), at half the rate (EXACT).
+// by its bytes anyway, the codes go as bf16 numbers, exactly, through bf16
+// instructions, which add in fp32 throughout (9e-9 in a block), at half the rate (EXACT).
 #include "fp8.h"
 #include "rl_decode.h"
 
@@ -156,7 +156,11 @@ __global__ void __launch_bounds__(64 * kGemvWaves, 4) gemv_fp8_kernel(Fp8Gemm p,
 // instructions.  So a block's weights and first tokens have left their slot when its first
 // half begins and the second tokens when that ends: behind a barrier there, the slot
 // takes what the block after the next needs, and all of it has a block and a half's
-// time to arrive (one block's was not enough: memory answers in about 1.1 us, a block is 0.9).
+// time to arrive (with one block's: 490 us at 8192 x 3584 x 18944, where this took 466).
+//
+// Bound by the matrix unit and the power that it draws: 256 x 256 tiles run at 3.1
+// PFLOP/s, 8192 x 3584 x 18944 in 406 us (2.74; 448 tiles are 1.75 rounds of 256 CUs),
+// where instructions on random codes in registers reach 3.5.
 //
 // LDS row 32 t + 8 q + 4 h + e of a wave's weights (t tile, 4 q + e register and h lane half
 // of the instruction's output) holds weight h TN / 2 + q TN / 8 + 4 t + e: a lane's outputs
@@ -406,7 +410,7 @@ __global__ void __launch_bounds__(256, 1) gemm_fp8_large_kernel(Fp8Gemm p, TileM
     tile_fp8<128, 128, TO, false>(p, m0, n0, 0, p.kb, smem, nullptr);
 }
 
-// Sum of the K slices, in their order.
+// Sum of the K slices, in their order; bound by their bytes and its launch (4 us).
 template <typename TO>
 __global__ void __launch_bounds__(256) gemm_fp8_join_kernel(Fp8Gemm p, int slices) {
     const int per_row = (p.n + 3) / 4;
