@@ -21,6 +21,9 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kStep = 32;   // positions a wave takes at a time
 
+// Chunks of a row of `len` positions; len + chunk may pass 31 bits.
+__host__ __device__ constexpr int chunks_in(int len, int chunk) { return len / chunk + (len % chunk != 0); }
+
 // v as a sum of N bf16 numbers: the rest after each is exact
 template <int N> __device__ __forceinline__ void split_bf16(const float* v, bf16x8* out) {
     float r[8];
@@ -247,7 +250,7 @@ __global__ void __launch_bounds__(256) attention_fp8_join_kernel(AttnFp8 p, int 
     const int seq = p.seqs ? p.seqs[row] : row;
     int len = p.lengths[row];
     len = len < 0 || seq < 0 || seq >= p.c.n_seqs ? 0 : len > p.max_length ? p.max_length : len;
-    const int n = (len + chunk - 1) / chunk;   // chunks with a position
+    const int n = chunks_in(len, chunk);   // chunks with a position
     const float* part = p.part + static_cast<int64_t>(blockIdx.x) * n_chunks * step;
     T* out = static_cast<T*>(p.out) + row * p.ldo + kvh * G * D;
     for (int at = 4 * threadIdx.x; at < G * D; at += 4 * 256) {
@@ -285,7 +288,7 @@ __global__ void __launch_bounds__(256) attention_fp8_join_head_kernel(AttnFp8 p,
     const int seq = p.seqs ? p.seqs[row] : row;
     int len = p.lengths[row];
     len = len < 0 || seq < 0 || seq >= p.c.n_seqs ? 0 : len > p.max_length ? p.max_length : len;
-    const int n = (len + chunk - 1) / chunk;
+    const int n = chunks_in(len, chunk);
     const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES;
     const float* part = p.part + (static_cast<int64_t>(row) * p.c.heads + kvh) * n_chunks * step;
     float M = -INFINITY, L = 0.0f;
@@ -324,14 +327,12 @@ __global__ void __launch_bounds__(256) attention_fp8_join_head_kernel(AttnFp8 p,
 constexpr int kMaxChunk = 64 * kStep;
 int chunk_of(int n, int kv_heads, int max_length) {
     int chunk = 1024;
-    while (chunk > 256 && static_cast<int64_t>(n) * kv_heads * ((max_length + chunk - 1) / chunk) < 1024) chunk /= 2;
+    while (chunk > 256 && static_cast<int64_t>(n) * kv_heads * chunks_in(max_length, chunk) < 1024) chunk /= 2;
     return chunk;
 }
 static_assert(1024 <= kMaxChunk, "a step's page in a lane");
 int chunks_of(int n, int kv_heads, int max_length) {
-    const int c = chunk_of(n, kv_heads, max_length);
-    const int k = (max_length + c - 1) / c;
-    return k < 1 ? 1 : k;
+    return std::max(1, chunks_in(max_length, chunk_of(n, kv_heads, max_length)));
 }
 
 template <typename T, int D, int QT, int PT, int WAVES> void start(const AttnFp8& a, int chunk, int n_chunks, hipStream_t s) {

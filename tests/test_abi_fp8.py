@@ -151,6 +151,14 @@ def test_attention_workspace():
                   longest=1 << 30) == R.RL_ERR_UNSUPPORTED
 
 
+def test_attention_workspace_of_the_longest_rows():
+    """Lengths next to 2^31: a chunk of 1024 positions still has its 64 + 2 sums."""
+    f = R.lib().rl_attention_quant_workspace_bytes
+    for longest in ((1 << 31) - 32, (1 << 31) - 1):
+        assert f(1, 1, 1, 64, longest) == 4 * 66 * (1 << 21)
+    assert f(1, 1, 1, 64, 1 << 30) == 4 * 66 * (1 << 20) and f(1, 1, 1, 64, 1) == 0
+
+
 def test_binding_checks_its_tensors():
     x = torch.zeros(2, 256)
     c, s = R.empty_fp8(2, 256, device="cpu")

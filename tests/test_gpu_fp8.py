@@ -551,6 +551,23 @@ def test_attention_past_two_gib():
     assert all(torch.equal(o.double(), w) for o, w in zip(out, c.numbers(0, 600)))
 
 
+def test_attention_of_the_longest_row():
+    """A row of nearly 2^31 positions in pages of 32, of which only the last three pages are there."""
+    heads, group, d, page = 1, 2, 64, 32
+    c = Cache([96], page, heads, d, 1)
+    pages = c.table[0].clone()
+    n_pages = (1 << 26) - 1
+    c.table = torch.full((1, n_pages), -1, dtype=torch.int32, device=DEV)
+    c.table[0, -3:] = pages
+    seqs, pos = packed([96], [page * (n_pages - 3)])
+    c.append(seqs, pos, *kv(96, heads, d, BF, 3))
+    a, b, e, f = F.places(page, heads, d, c.table, seqs, pos)
+    k, v = F.cache_numbers(c.pool, a, e), F.cache_numbers(c.pool, b, f)
+    q = rows(1, group * d, BF, 4, 0, 0, 0.3).unflatten(1, (group, d))
+    for gone in (0, 31, 70):
+        check_attention(attend(c, q, [page * n_pages - gone], page * n_pages)[0], q[0], k[:96 - gone], v[:96 - gone], d ** -0.5)
+
+
 # ------------------------------------------------------------------------------------------------ together
 
 
