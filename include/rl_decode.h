@@ -573,7 +573,8 @@ typedef enum rl_fp8_form {
     RL_FP8_TILES = 2             /* a weight: a scale for each tile of 128 rows x 128 entries      */
 } rl_fp8_form;
 
-/* [n][ldx] numbers of dtype in 8 bits.  n <= 2^20, k <= 131072. */
+/* [n][ldx] numbers of dtype in 8 bits.  n <= 2^20, k <= 131072, and
+ * n * ceil(k / 128) < 2^28. */
 rl_status rl_quantise(int32_t form, int32_t n, int32_t k, int32_t dtype, const void* x, int64_t ldx, const rl_fp8_matrix* out,
                           void* stream);
 
@@ -603,7 +604,8 @@ rl_status rl_gemm_quant(int32_t m, int32_t n, int32_t k, const rl_fp8_matrix* a,
  *  pool        device, 256-byte aligned, rl_kv_quant_bytes bytes.
  *  page_table  device int32 [n_seqs][max_pages]; read by the calls' kernels.
  *  page_size a multiple of 32 in [32, 65536], head_dim 64 or 128,
- *  n_kv_heads <= 1024, n_seqs <= 2^20, max_pages * page_size < 2^31. */
+ *  n_kv_heads <= 1024, n_seqs <= 2^20, max_pages * page_size < 2^31; a pool of
+ *  at most 2^48 bytes. */
 typedef struct rl_kv_fp8 {
     void* pool;
     const int32_t* page_table;
@@ -619,7 +621,7 @@ typedef struct rl_kv_fp8 {
 size_t rl_kv_quant_bytes(int32_t n_pages, int32_t page_size, int32_t n_kv_heads, int32_t head_dim);
 
 /* Write n tokens' keys and values (after RoPE) in 8 bits.  n <= 2^24, and
- * n * n_kv_heads < 2^31.
+ * n * n_kv_heads < 2^28.
  *  seqs, positions  device int32 [n]: token i is position positions[i] of
  *                   sequence seqs[i]; one that has no place (sequence or
  *                   position out of range, no page) is left out.  No two
@@ -641,6 +643,8 @@ size_t rl_attention_quant_workspace_bytes(int32_t n, int32_t n_kv_heads, int32_t
  * positions 0 .. lengths[i] - 1 of its sequence,
  *   out = softmax(scale q K^T) V
  * q-head j uses kv-head j / (n_q_heads / n_kv_heads); at most 16 q-heads a kv-head.
+ * n <= 2^20; RL_ERR_UNSUPPORTED from 2^25 (row, kv-head, 1024 positions) on, and
+ * for rows past 8192 positions from 2^24 (row, q-head) on.
  *  seqs        device int32 [n], or NULL: row i is sequence i.  Several rows
  *              may be of one sequence (drafted or prompt tokens, each with
  *              the length it sees).

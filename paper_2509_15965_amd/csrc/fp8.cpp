@@ -40,11 +40,19 @@ int64_t page_bytes(int32_t page_size, int32_t head_dim) {
     return (2 * static_cast<int64_t>(page_size) * (head_dim + 1) + 255) / 256 * 256;
 }
 
+// Pools end below 2^48 bytes: every offset in them, and their size, is a 64-bit number.
+bool pool_ok(int32_t n_pages, int32_t n_kv_heads, int64_t block) {
+    return n_pages > 0 && n_kv_heads > 0 && n_kv_heads <= 1024 && block > 0 && n_pages <= (int64_t(1) << 48) / (block * n_kv_heads);
+}
+
+// The runtime counts a launch's threads in 32 bits: 16 of them take 128 entries of an fp32 matrix, or one token's head.
+constexpr int64_t kMaxBlocks = int64_t(1) << 28;
+
 bool cache_ok(const rl_kv_fp8* c, KvFp8* o) {
     if (!c || !c->pool || !aligned(c->pool, 256) || !c->page_table || !aligned(c->page_table, 4)) return false;
-    if (c->n_seqs < 1 || c->n_seqs > kMaxSeqs || c->max_pages < 1 || c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 1024) return false;
+    if (c->n_seqs < 1 || c->n_seqs > kMaxSeqs || c->max_pages < 1) return false;
     const int64_t block = page_bytes(c->page_size, c->head_dim);
-    if (block == 0 || static_cast<int64_t>(c->max_pages) * c->page_size > INT32_MAX) return false;
+    if (!pool_ok(c->n_pages, c->n_kv_heads, block) || static_cast<int64_t>(c->max_pages) * c->page_size > INT32_MAX) return false;
     *o = KvFp8{static_cast<uint8_t*>(c->pool), c->page_table, c->n_seqs, c->max_pages, c->n_pages, c->page_size, c->n_kv_heads,
                c->head_dim, block};
     return true;
@@ -73,6 +81,7 @@ rl_status rl_quantise(int32_t form, int32_t n, int32_t k, int32_t dtype, const v
     if (form < RL_FP8_ROWS || form > RL_FP8_TILES || n < 0 || n > kMaxRows || k < 1 || k > kMaxWidth) return RL_ERR_INVALID_ARG;
     if (n == 0) return dtype_ok(dtype) ? RL_OK : RL_ERR_INVALID_ARG;
     if (!rows_ok(dtype, x, n, form == RL_FP8_SWIGLU ? 2 * static_cast<int64_t>(k) : k, ldx) || !matrix_ok(out, k)) return RL_ERR_INVALID_ARG;
+    if (static_cast<int64_t>(n) * fp8_blocks(k) >= kMaxBlocks) return RL_ERR_UNSUPPORTED;
     return status_of(launch_quantise_fp8(form, n, k, dtype, x, ldx, out_of(out), static_cast<hipStream_t>(stream)));
 }
 
@@ -92,8 +101,8 @@ rl_status rl_gemm_quant(int32_t m, int32_t n, int32_t k, const rl_fp8_matrix* a,
 }
 
 size_t rl_kv_quant_bytes(int32_t n_pages, int32_t page_size, int32_t n_kv_heads, int32_t head_dim) {
-    if (n_pages < 1 || n_kv_heads < 1 || n_kv_heads > 1024) return 0;
-    return static_cast<size_t>(page_bytes(page_size, head_dim)) * n_pages * n_kv_heads;
+    const int64_t block = page_bytes(page_size, head_dim);
+    return pool_ok(n_pages, n_kv_heads, block) ? static_cast<size_t>(block) * n_pages * n_kv_heads : 0;
 }
 
 rl_status rl_kv_quant_append(const rl_kv_fp8* cache, int32_t n, const int32_t* seqs, const int32_t* positions, int32_t dtype,
@@ -101,7 +110,7 @@ rl_status rl_kv_quant_append(const rl_kv_fp8* cache, int32_t n, const int32_t* s
     KvFp8 c;
     if (!cache_ok(cache, &c) || n < 0 || n > kMaxTokens || !dtype_ok(dtype)) return RL_ERR_INVALID_ARG;
     if (n == 0) return RL_OK;
-    if (static_cast<int64_t>(n) * c.heads > INT32_MAX) return RL_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(n) * c.heads >= kMaxBlocks) return RL_ERR_UNSUPPORTED;
     const int64_t width = static_cast<int64_t>(c.heads) * c.dim;
     if (!seqs || !positions || !rows_ok(dtype, k, n, width, ldk) || !rows_ok(dtype, v, n, width, ldv)) return RL_ERR_INVALID_ARG;
     const KvTokens t{n, seqs, positions, k, v, ldk, ldv, nullptr, nullptr, 0, 0, dtype};
@@ -113,7 +122,7 @@ rl_status rl_kv_quant_read(const rl_kv_fp8* cache, int32_t n, const int32_t* seq
     KvFp8 c;
     if (!cache_ok(cache, &c) || n < 0 || n > kMaxTokens || !dtype_ok(dtype)) return RL_ERR_INVALID_ARG;
     if (n == 0) return RL_OK;
-    if (static_cast<int64_t>(n) * c.heads > INT32_MAX) return RL_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(n) * c.heads >= kMaxBlocks) return RL_ERR_UNSUPPORTED;
     const int64_t width = static_cast<int64_t>(c.heads) * c.dim;
     if (!seqs || !positions || !rows_ok(dtype, out_k, n, width, ldk) || !rows_ok(dtype, out_v, n, width, ldv)) return RL_ERR_INVALID_ARG;
     const KvTokens t{n, seqs, positions, nullptr, nullptr, 0, 0, out_k, out_v, ldk, ldv, dtype};

@@ -63,7 +63,7 @@ struct AttnFp8 {
     float scale;
     float* part;
 };
-bool attention_fp8_fits(int n, int kv_heads, int heads, int max_length);   // its workgroups can be counted in 31 bits
+bool attention_fp8_fits(int n, int kv_heads, int heads, int max_length);   // its launches' threads can be counted in 32 bits
 size_t attention_fp8_ws_bytes(int n, int kv_heads, int heads, int dim, int max_length);
 hipError_t launch_attention_fp8(const AttnFp8& a, hipStream_t s);
 

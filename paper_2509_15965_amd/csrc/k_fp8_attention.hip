@@ -357,8 +357,9 @@ template <typename T, int D, int QT, int PT> hipError_t attend(const AttnFp8& a,
 }  // namespace
 
 bool attention_fp8_fits(int n, int kv_heads, int heads, int max_length) {
-    const int64_t most = std::max(static_cast<int64_t>(kv_heads) * chunks_of(n, kv_heads, max_length), static_cast<int64_t>(heads));
-    return n * most < (int64_t(1) << 31);
+    const int64_t chunks = chunks_of(n, kv_heads, max_length), pairs = static_cast<int64_t>(n) * kv_heads;
+    const int64_t threads = pairs * chunks * 128, join = chunks > 8 ? 256ll * n * heads : chunks > 1 ? 256 * pairs : 0;   // at most
+    return std::max(threads, join) < (int64_t(1) << 32);
 }
 size_t attention_fp8_ws_bytes(int n, int kv_heads, int heads, int dim, int max_length) {
     const int c = chunks_of(n, kv_heads, max_length);

@@ -151,6 +151,23 @@ def test_attention_workspace():
                   longest=1 << 30) == R.RL_ERR_UNSUPPORTED
 
 
+def test_sizes_that_do_not_fit_a_launch_or_64_bits():
+    no = R.RL_ERR_UNSUPPORTED
+    assert quantise(n=1 << 20, k=128 * 256, dtype=0) == no and quantise(n=1 << 18, k=128 * 1024, dtype=1) == no
+    assert quantise(form=1, n=1 << 20, k=128 * 256) == no and quantise(form=2, n=1 << 20, k=128 * 256) == no
+    heads = dict(c=dict(n_kv_heads=16), ldk=2048, ldv=2048, n=1 << 24)
+    assert tokens("rl_kv_quant_append", **heads) == no and tokens("rl_kv_quant_read", **heads) == no
+    f = R.lib().rl_attention_quant_workspace_bytes
+    assert f(1 << 20, 16, 16, 64, 2000) == 0 and f((1 << 20) - 1, 16, 16, 64, 2000) > 0 and f(1 << 19, 16, 16, 64, 2049) > 0
+    assert f(1 << 18, 4, 64, 64, 9000) == 0 and f((1 << 18) - 1, 4, 64, 64, 9000) > 0
+    for c in (dict(n_kv_heads=32), dict(n_kv_heads=16, max_pages=40)):
+        assert attend(c=dict(n_seqs=1 << 20, **c), n=1 << 20, heads=32, ldq=4096, ldo=4096, longest=c.get("max_pages", 4) * 64) == no
+    # pools past 2^48 bytes: their size would pass 64 bits
+    b = R.lib().rl_kv_quant_bytes
+    assert b((1 << 31) - 1, 65536, 1024, 128) == 0 and b((1 << 31) - 1, 32, 31, 64) == 0 and b((1 << 31) - 1, 32, 30, 64) == ((1 << 31) - 1) * 30 * 4352
+    assert tokens("rl_kv_quant_append", c=dict(n_pages=(1 << 31) - 1, page_size=65536, n_kv_heads=1024)) == BAD
+
+
 def test_attention_workspace_of_the_longest_rows():
     """Lengths next to 2^31: a chunk of 1024 positions still has its 64 + 2 sums."""
     f = R.lib().rl_attention_quant_workspace_bytes
