@@ -562,7 +562,9 @@ typedef struct rl_fp8_matrix {
  *  n <= 2^20 rows of hidden <= 32768 entries; x [n][ldx] of dtype; add
  *  [n][ld_add] of add_dtype, or NULL; weight [hidden] of w_dtype; out_sum
  *  [n][ld_sum] of dtype, or NULL; it may be x (same ld), or add (same ld and
- *  dtype).  eps in (0, 1].  The norm is of s as it is stored. */
+ *  dtype).  eps in (0, 1].  The norm is of s as it is stored; the sum
+ *  of squares is fp32, and a row where it is infinite becomes zeros (NaN where
+ *  s is infinite). */
 rl_status rl_rmsnorm_quant(int32_t n, int32_t hidden, int32_t dtype, const void* x, int64_t ldx, int32_t add_dtype, const void* add,
                          int64_t ld_add, int32_t w_dtype, const void* weight, double eps, void* out_sum, int64_t ld_sum,
                          const rl_fp8_matrix* out, void* stream);
@@ -630,8 +632,9 @@ size_t rl_kv_quant_bytes(int32_t n_pages, int32_t page_size, int32_t n_kv_heads,
 rl_status rl_kv_quant_append(const rl_kv_fp8* cache, int32_t n, const int32_t* seqs, const int32_t* positions, int32_t dtype,
                            const void* k, int64_t ldk, const void* v, int64_t ldv, void* stream);
 
-/* Read n tokens' keys and values back as numbers (exact in either dtype);
- * zeros for a token that has no place.  The same place may be read twice. */
+/* Read n tokens' keys and values back as numbers, rounded to dtype (exact
+ * below 2^128 in fp32, from 2^-126 on in bf16 too); zeros for a token that has
+ * no place.  The same place may be read twice. */
 rl_status rl_kv_quant_read(const rl_kv_fp8* cache, int32_t n, const int32_t* seqs, const int32_t* positions, int32_t dtype,
                          void* out_k, int64_t ldk, void* out_v, int64_t ldv, void* stream);
 

@@ -197,6 +197,19 @@ def test_norm_sum_in_place(which):
     assert torch.equal(to, total) and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+def test_norm_of_rows_whose_squares_pass_fp32():
+    """The sum of squares is infinite: zeros, and NaN for an infinite entry."""
+    x = torch.full((3, 300), 1e19, device=DEV)
+    x[0] = 3e38
+    x[1] = 1.0
+    x[1, 7] = -2e19
+    x[2, 299] = INF
+    codes, scales = room(3, 300)
+    R.rmsnorm_quant(x, torch.ones(300, device=DEV), codes, scales)
+    v = F.matrix(codes, scales)
+    assert (v[:2] == 0).all() and (v[2, :299] == 0).all() and torch.isnan(v[2, 299]) and (v[2, 300:] == 0).all()
+
+
 def test_norm_of_rows_that_are_zero_or_not_finite():
     x = rows(5, 300, F32, 4)
     x[1] = 0.0
@@ -378,6 +391,27 @@ def test_cache_is_exact(dtype, lens, starts, page, heads, d, pad, shift):
         b = F.scale_bytes(x.double().abs().amax(2))
         want = F.encode(x.double(), b[..., None]) * F.factor(b.to(torch.uint8))[..., None]
         assert torch.equal(o.double(), want[order])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("order", ["single", "eights"])
+def test_cache_read_of_every_code_under_every_scale(dtype, order):
+    """Numbers that the type does not hold are rounded to it: of bf16 below 2^-133, of either from 2^128 on."""
+    n, page, heads, d = 508, 512, 1, 128
+    c = Cache([n], page, heads, d, 0, 0)
+    block = c.pool.view(1, -1)[0]
+    i = torch.arange(n, device=DEV)
+    seqs, pos = packed([n], [0])
+    a, b, e, f = F.places(page, heads, d, c.table, seqs, pos)
+    code = (128 * (i % 2)[:, None] + torch.arange(d, device=DEV)).to(torch.uint8)[:, None]
+    block[a], block[b] = code, code
+    block[e] = block[f] = (i // 2 + 1).to(torch.uint8)[:, None]
+    if order == "single":
+        pos, seqs = pos.flip(0), seqs
+    out = [torch.empty(n, heads, d, dtype=dtype, device=DEV) for _ in range(2)]
+    R.kv_quant_read(c.pool, c.table, seqs, pos, *out, page_size=page)
+    for o, w in zip(out, c.numbers(0, n)):
+        assert same(o.flip(0) if order == "single" else o, w.to(dtype))
 
 
 def test_cache_tokens_in_any_order_and_one_by_one():
