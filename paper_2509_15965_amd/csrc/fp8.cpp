@@ -16,6 +16,8 @@ bool dtype_ok(int32_t dt) { return dt == RL_DTYPE_FP32 || dt == RL_DTYPE_BF16; }
 size_t elem_bytes(int dt) { return dt == RL_DTYPE_FP32 ? 4 : 2; }
 rl_status status_of(hipError_t e) { return e == hipSuccess ? RL_OK : RL_ERR_HIP; }
 
+bool numbers_ok(const int32_t* p) { return p && aligned(p, 4); }
+
 // rows of `width` entries, ld apart, at p; below 2^40 entries in all
 bool rows_ok(int32_t dt, const void* p, int32_t n, int64_t width, int64_t ld) {
     return dtype_ok(dt) && p && aligned(p, elem_bytes(dt)) && ld >= width && ld <= (int64_t(1) << 40) / (n > 0 ? n : 1);
@@ -112,7 +114,7 @@ rl_status rl_kv_quant_append(const rl_kv_fp8* cache, int32_t n, const int32_t* s
     if (n == 0) return RL_OK;
     if (static_cast<int64_t>(n) * c.heads >= kMaxBlocks) return RL_ERR_UNSUPPORTED;
     const int64_t width = static_cast<int64_t>(c.heads) * c.dim;
-    if (!seqs || !positions || !rows_ok(dtype, k, n, width, ldk) || !rows_ok(dtype, v, n, width, ldv)) return RL_ERR_INVALID_ARG;
+    if (!numbers_ok(seqs) || !numbers_ok(positions) || !rows_ok(dtype, k, n, width, ldk) || !rows_ok(dtype, v, n, width, ldv)) return RL_ERR_INVALID_ARG;
     const KvTokens t{n, seqs, positions, k, v, ldk, ldv, nullptr, nullptr, 0, 0, dtype};
     return status_of(launch_kv_fp8_append(c, t, static_cast<hipStream_t>(stream)));
 }
@@ -124,7 +126,7 @@ rl_status rl_kv_quant_read(const rl_kv_fp8* cache, int32_t n, const int32_t* seq
     if (n == 0) return RL_OK;
     if (static_cast<int64_t>(n) * c.heads >= kMaxBlocks) return RL_ERR_UNSUPPORTED;
     const int64_t width = static_cast<int64_t>(c.heads) * c.dim;
-    if (!seqs || !positions || !rows_ok(dtype, out_k, n, width, ldk) || !rows_ok(dtype, out_v, n, width, ldv)) return RL_ERR_INVALID_ARG;
+    if (!numbers_ok(seqs) || !numbers_ok(positions) || !rows_ok(dtype, out_k, n, width, ldk) || !rows_ok(dtype, out_v, n, width, ldv)) return RL_ERR_INVALID_ARG;
     const KvTokens t{n, seqs, positions, nullptr, nullptr, 0, 0, out_k, out_v, ldk, ldv, dtype};
     return status_of(launch_kv_fp8_read(c, t, static_cast<hipStream_t>(stream)));
 }
@@ -147,7 +149,7 @@ rl_status rl_attention_quant(const rl_kv_fp8* cache, int32_t n, const int32_t* s
     if (n == 0) return RL_OK;
     if (!attention_fp8_fits(n, c.heads, n_q_heads, max_length)) return RL_ERR_UNSUPPORTED;
     const int64_t width = static_cast<int64_t>(n_q_heads) * c.dim;
-    if (!lengths || !rows_ok(dtype, q, n, width, ldq) || !rows_ok(dtype, out, n, width, ldo)) return RL_ERR_INVALID_ARG;
+    if (!numbers_ok(lengths) || !aligned(seqs, 4) || !rows_ok(dtype, q, n, width, ldq) || !rows_ok(dtype, out, n, width, ldo)) return RL_ERR_INVALID_ARG;
     if (const rl_status st = workspace_ok(workspace, ws_bytes, attention_fp8_ws_bytes(n, c.heads, n_q_heads, c.dim, max_length)); st != RL_OK)
         return st;
     const AttnFp8 a{c, n, max_length, seqs, lengths, q, ldq, out, ldo, dtype, n_q_heads, static_cast<float>(scale),

@@ -112,6 +112,7 @@ def tokens(f, c=None, n=2, seqs=P, pos=P, dt=1, k=P, ldk=256, v=P, ldv=256):
 
 @pytest.mark.parametrize("f", ["rl_kv_quant_append", "rl_kv_quant_read"])
 @pytest.mark.parametrize("bad", [dict(c=c) for c in CACHES] + [dict(n=-1), dict(n=(1 << 24) + 1), dict(seqs=None), dict(pos=None), dict(dt=2),
+                                                              dict(seqs=P + 2), dict(pos=P + 1),
                                                               dict(k=None), dict(v=None), dict(k=P + 1), dict(ldk=255), dict(ldv=255)])
 def test_cache_calls_refuse(f, bad):
     assert tokens(f, **bad) == BAD
@@ -130,7 +131,7 @@ def attend(c=None, n=2, seqs=P, lengths=P, longest=200, dt=1, q=P, ldq=1024, hea
 
 
 @pytest.mark.parametrize("bad", [dict(c=c) for c in CACHES]
-                         + [dict(n=-1), dict(n=(1 << 20) + 1), dict(n=4, seqs=None), dict(lengths=None), dict(longest=-1), dict(longest=257),
+                         + [dict(n=-1), dict(n=(1 << 20) + 1), dict(n=4, seqs=None), dict(lengths=None), dict(lengths=P + 2), dict(seqs=P + 2), dict(longest=-1), dict(longest=257),
                             dict(dt=2), dict(q=None), dict(q=P + 1), dict(ldq=1023), dict(heads=1), dict(heads=7), dict(heads=34, ldq=1 << 20),
                             dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=1e300), dict(out=None), dict(ldo=1023)])
 def test_attention_quant_refuses(bad):
