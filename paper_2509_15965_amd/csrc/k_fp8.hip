@@ -187,17 +187,6 @@ __device__ __forceinline__ uint8_t* kv_place(const KvFp8& c, const KvTokens& t, 
     return c.pool + (static_cast<int64_t>(pg) * c.heads + h) * c.block;
 }
 
-// Whether token i is of eight that follow one another in the call and fill positions 8 j .. 8 j + 7 of their sequence: each
-// of the lane group's first eight lanes looks at one of them.
-template <int LANES> __device__ __forceinline__ bool kv_eight(const KvTokens& t, int i) {
-    const int s = t.seqs[i], pos = t.pos[i], first = i - (pos & 7), e = threadIdx.x & 7;
-    const bool in = first >= 0 && first + 8 <= t.n;
-    const int at = in ? first + e : i;
-    const bool same = t.seqs[at] == s, next = t.pos[at] == (pos & ~7) + e;
-    const uint64_t all = __ballot(in && same && next) >> ((threadIdx.x & 63) / LANES * LANES);
-    return (all & 255u) == 255u;
-}
-
 // Token and head of this lane group, of LANES lanes.
 template <int LANES> __device__ __forceinline__ int kv_unit(const KvFp8& c, int* h) {
     const uint32_t unit = static_cast<uint32_t>((static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x) / LANES);
@@ -218,51 +207,20 @@ __device__ __forceinline__ void turn8(const uint32_t (&a)[8][2], uint32_t (&o)[8
         }
 }
 
-// blockIdx.y 0: keys, a lane group a (token, head).  1: values: eight tokens that fill
-// eight neighbouring positions are written by the first of them, eight bytes an
-// entry; others byte by byte (a rollout's single tokens).
-template <typename T, int D>
-__global__ void __launch_bounds__(256) kv_fp8_append_kernel(KvFp8 c, KvTokens t) {
-    constexpr int LANES = D / 8;
-    const int lane = threadIdx.x % LANES;
-    int h, local = 0;
-    const int i = kv_unit<LANES>(c, &h);
-    if (i >= t.n) return;   // whole groups of LANES lanes
-    const int at = h * D + 8 * lane;
-    float v[8];
+// One token and head's entries v of a lane, at its page block.
+template <int LANES> __device__ __forceinline__ void kv_put(const KvFp8& c, uint8_t* blk, int local, bool values, int lane, float* v) {
+    constexpr int D = 8 * LANES;
     uint32_t w[2];
-    if (blockIdx.y == 0) {
-        load_row<8>(static_cast<const T*>(t.k) + i * t.ldk + at, 8, v);   // on its way while the place is looked up
-        uint8_t* blk = kv_place(c, t, i, h, &local);
-        const int b = fp8_encode<8, LANES>(v, w);
-        if (!blk) return;
-        store_codes<8>(blk + local * D + 8 * lane, w);
-        if (lane == 0) blk[2 * c.page * D + local] = static_cast<uint8_t>(b);
-        return;
-    }
-    load_row<8>(static_cast<const T*>(t.v) + i * t.ldv + at, 8, v);
-    uint8_t* blk = kv_place(c, t, i, h, &local);
-    const bool eight = kv_eight<LANES>(t, i);
-    if (!blk || (eight && local % 8 != 0)) return;
-    uint8_t* dst = blk + c.page * D + (local / 8 * D + 8 * lane) * 8;
-    uint8_t* sdst = blk + 2 * c.page * D + c.page + local;
-    if (eight) {
-        uint32_t all[8][2], o[8][2], sb[2] = {0u, 0u};
-        float x[8][8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) load_row<8>(static_cast<const T*>(t.v) + (i + e) * t.ldv + at, 8, x[e]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sb[e / 4] |= static_cast<uint32_t>(fp8_encode<8, LANES>(x[e], all[e])) << (8 * (e & 3));
-        turn8(all, o);
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) *reinterpret_cast<u32x4*>(dst + 8 * j) = u32x4{o[j][0], o[j][1], o[j + 1][0], o[j + 1][1]};
-        if (lane == 0) *reinterpret_cast<uint2*>(sdst) = make_uint2(sb[0], sb[1]);
-        return;
-    }
     const int b = fp8_encode<8, LANES>(v, w);
+    if (!blk) return;
+    if (lane == 0) blk[2 * c.page * D + (values ? c.page : 0) + local] = static_cast<uint8_t>(b);
+    if (!values) {
+        store_codes<8>(blk + local * D + 8 * lane, w);
+        return;
+    }
+    uint8_t* dst = blk + c.page * D + (local / 8 * D + 8 * lane) * 8 + local % 8;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dst[8 * e + local % 8] = static_cast<uint8_t>(w[e / 4] >> (8 * (e & 3)));
-    if (lane == 0) *sdst = static_cast<uint8_t>(b);
+    for (int e = 0; e < 8; ++e) dst[8 * e] = static_cast<uint8_t>(w[e / 4] >> (8 * (e & 3)));
 }
 
 // eight codes as numbers; the hardware's conversion takes the scale's exponent along
@@ -279,35 +237,179 @@ __device__ __forceinline__ void fp8_decode8(const uint32_t* w, float scale, floa
     }
 }
 
-// blockIdx.y 0: keys, 1: values, eight positions at a time as they were written.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) kv_fp8_read_kernel(KvFp8 c, KvTokens t) {
-    constexpr int LANES = D / 8;
-    const int lane = threadIdx.x % LANES;
-    int h, local = 0;
-    const int i = kv_unit<LANES>(c, &h);
-    if (i >= t.n) return;
-    const uint8_t* blk = kv_place(c, t, i, h, &local);
-    const bool eight = blockIdx.y != 0 && kv_eight<LANES>(t, i);
-    const int at = h * D + 8 * lane;
-    T* out = (blockIdx.y == 0 ? static_cast<T*>(t.out_k) + i * t.ld_ok : static_cast<T*>(t.out_v) + i * t.ld_ov) + at;
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    uint32_t w[2] = {0u, 0u};
+// The same read; zeros where there is no block.
+template <int LANES> __device__ __forceinline__ void kv_get(const KvFp8& c, const uint8_t* blk, int local, bool values, int lane, float* v) {
+    constexpr int D = 8 * LANES;
     if (!blk) {
-        store_row<8>(out, 8, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
         return;
     }
-    const uint8_t* sb = blk + 2 * c.page * D + (blockIdx.y == 0 ? 0 : c.page) + local;
-    if (blockIdx.y == 0) {
+    uint32_t w[2] = {0u, 0u};
+    if (!values) {
         const uint2 q = *reinterpret_cast<const uint2*>(blk + local * D + 8 * lane);
         w[0] = q.x;
         w[1] = q.y;
     } else {
-        const uint8_t* src = blk + c.page * D + (local / 8 * D + 8 * lane) * 8;
-        if (eight) {
-            if (local % 8 != 0) return;
-            uint32_t all[8][2], o[8][2];
-            const uint2 s8 = *reinterpret_cast<const uint2*>(sb);
+        const uint8_t* src = blk + c.page * D + (local / 8 * D + 8 * lane) * 8 + local % 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e / 4] |= static_cast<uint32_t>(src[8 * e]) << (8 * (e & 3));
+    }
+    fp8_decode8(w, fp8_scale(blk[2 * c.page * D + (values ? c.page : 0) + local]), v);
+}
+
+// Few tokens: a lane group a (token, head); blockIdx.y 0: keys, 1: values.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) kv_fp8_append_kernel(KvFp8 c, KvTokens t) {
+    constexpr int LANES = D / 8;
+    const int lane = threadIdx.x % LANES;
+    const bool values = blockIdx.y != 0;
+    int h, local = 0;
+    const int i = kv_unit<LANES>(c, &h);
+    if (i >= t.n) return;   // whole groups of LANES lanes
+    float v[8];
+    load_row<8>((values ? static_cast<const T*>(t.v) + i * t.ldv : static_cast<const T*>(t.k) + i * t.ldk) + h * D + 8 * lane, 8, v);
+    uint8_t* blk = kv_place(c, t, i, h, &local);   // under the load
+    kv_put<LANES>(c, blk, local, values, lane, v);
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) kv_fp8_read_kernel(KvFp8 c, KvTokens t) {
+    constexpr int LANES = D / 8;
+    const int lane = threadIdx.x % LANES;
+    const bool values = blockIdx.y != 0;
+    int h, local = 0;
+    const int i = kv_unit<LANES>(c, &h);
+    if (i >= t.n) return;
+    const uint8_t* blk = kv_place(c, t, i, h, &local);
+    float v[8];
+    kv_get<LANES>(c, blk, local, values, lane, v);
+    store_row<8>((values ? static_cast<T*>(t.out_v) + i * t.ld_ov : static_cast<T*>(t.out_k) + i * t.ld_ok) + h * D + 8 * lane, 8, v);
+}
+
+// Many tokens: a lane group a head of the window of tokens i0 .. i0 + 7, whose rows are all under way at once.  Values of eight
+// tokens that follow one another in the call and fill positions 8 j .. 8 j + 7 of their sequence are one 64-bit word an
+// entry: the window in which those start takes them whole, and each takes its tokens that are of no such eight one by one.
+struct KvWindow {
+    int start;        // token at which an eight starts, or -1: at most one in a window
+    uint32_t alone;   // bit e: token i0 + e is there, and of no eight
+};
+template <int LANES> __device__ __forceinline__ KvWindow kv_window(const KvTokens& t, int i0, int lane) {
+    constexpr int LOADS = (24 + LANES - 1) / LANES;   // tokens i0 - 8 .. i0 + 15 at least: bit b is token i0 - 8 + b
+    uint32_t there = 0u, first = 0u, next = 0u;       // a token; at a position of 8 j; the one after the token before
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) {
+        const int j = i0 - 8 + u * LANES + lane;
+        const bool in = j >= 0 && j < t.n;
+        const uint32_t pos = in ? static_cast<uint32_t>(t.pos[j]) : 1u;
+        const bool follows = in && j > 0 && t.seqs[j - 1] == t.seqs[j] && static_cast<uint32_t>(t.pos[j - 1]) == pos - 1u;
+        const int sh = (threadIdx.x & 63) / LANES * LANES;
+        constexpr uint64_t kMine = (uint64_t(1) << LANES) - 1;
+        there |= static_cast<uint32_t>(__ballot(in) >> sh & kMine) << (u * LANES);
+        first |= static_cast<uint32_t>(__ballot(pos % 8 == 0) >> sh & kMine) << (u * LANES);
+        next |= static_cast<uint32_t>(__ballot(follows) >> sh & kMine) << (u * LANES);
+    }
+    uint32_t eights = first, of = 0u;
+#pragma unroll
+    for (int e = 1; e < 8; ++e) eights &= next >> e;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) of |= eights << e;
+    const uint32_t here = eights >> 8 & 255u;
+    return KvWindow{here ? i0 + __ffs(static_cast<int>(here)) - 1 : -1, (there & ~of) >> 8 & 255u};
+}
+
+// A token's place from the lane of its group that looked it up.
+template <int LANES> __device__ __forceinline__ uint8_t* kv_from(uint8_t* blk, int e) {
+    return reinterpret_cast<uint8_t*>(__shfl(reinterpret_cast<unsigned long long>(blk), e, LANES));
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) kv_fp8_append_window_kernel(KvFp8 c, KvTokens t) {
+    constexpr int LANES = D / 8;
+    const int lane = threadIdx.x % LANES;
+    int h, local = 0;
+    const int i0 = 8 * kv_unit<LANES>(c, &h);
+    if (i0 >= t.n) return;   // whole groups of LANES lanes
+    const int at = h * D + 8 * lane;
+    float x[8][8];
+    uint32_t w[8][2];
+    int b[8];
+    if (blockIdx.y == 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) load_row<8>(static_cast<const T*>(t.k) + (i0 + e) * t.ldk + at, i0 + e < t.n ? 8 : 0, x[e]);
+        uint8_t* mine = i0 + (lane & 7) < t.n ? kv_place(c, t, i0 + (lane & 7), h, &local) : nullptr;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] = fp8_encode<8, LANES>(x[e], w[e]);
+        int scale = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            uint8_t* blk = kv_from<LANES>(mine, e);
+            const int l = __shfl(local, e, LANES);
+            if (blk) store_codes<8>(blk + l * D + 8 * lane, w[e]);
+            scale = lane == e ? b[e] : scale;
+        }
+        if (lane < 8 && mine) mine[2 * c.page * D + local] = static_cast<uint8_t>(scale);
+        return;
+    }
+    const KvWindow win = kv_window<LANES>(t, i0, lane);
+    if (win.start >= 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) load_row<8>(static_cast<const T*>(t.v) + (win.start + e) * t.ldv + at, 8, x[e]);
+        uint8_t* blk = kv_place(c, t, win.start, h, &local);
+        uint32_t o[8][2], sb[2] = {0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sb[e / 4] |= static_cast<uint32_t>(fp8_encode<8, LANES>(x[e], w[e])) << (8 * (e & 3));
+        turn8(w, o);
+        if (blk) {
+            uint8_t* dst = blk + c.page * D + (local * D + 64 * lane);
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) *reinterpret_cast<u32x4*>(dst + 8 * j) = u32x4{o[j][0], o[j][1], o[j + 1][0], o[j + 1][1]};
+            if (lane == 0) *reinterpret_cast<uint2*>(blk + 2 * c.page * D + c.page + local) = make_uint2(sb[0], sb[1]);
+        }
+    }
+    for (uint32_t left = win.alone; left; left &= left - 1) {
+        const int i = i0 + __ffs(static_cast<int>(left)) - 1;
+        load_row<8>(static_cast<const T*>(t.v) + i * t.ldv + at, 8, x[0]);
+        uint8_t* blk = kv_place(c, t, i, h, &local);
+        kv_put<LANES>(c, blk, local, true, lane, x[0]);
+    }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) kv_fp8_read_window_kernel(KvFp8 c, KvTokens t) {
+    constexpr int LANES = D / 8;
+    const int lane = threadIdx.x % LANES;
+    int h, local = 0;
+    const int i0 = 8 * kv_unit<LANES>(c, &h);
+    if (i0 >= t.n) return;
+    const int at = h * D + 8 * lane;
+    float v[8];
+    if (blockIdx.y == 0) {
+        uint8_t* mine = i0 + (lane & 7) < t.n ? kv_place(c, t, i0 + (lane & 7), h, &local) : nullptr;
+        const float scale = mine ? fp8_scale(mine[2 * c.page * D + local]) : 0.0f;
+        uint2 q[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint8_t* blk = kv_from<LANES>(mine, e);
+            const int l = __shfl(local, e, LANES);
+            q[e] = blk ? *reinterpret_cast<const uint2*>(blk + l * D + 8 * lane) : make_uint2(0u, 0u);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t w[2] = {q[e].x, q[e].y};
+            fp8_decode8(w, __shfl(scale, e, LANES), v);
+            if (i0 + e < t.n) store_row<8>(static_cast<T*>(t.out_k) + (i0 + e) * t.ld_ok + at, 8, v);
+        }
+        return;
+    }
+    const KvWindow win = kv_window<LANES>(t, i0, lane);
+    if (win.start >= 0) {
+        const uint8_t* blk = kv_place(c, t, win.start, h, &local);
+        uint32_t all[8][2] = {}, o[8][2];
+        uint2 s8 = make_uint2(0u, 0u);
+        if (blk) {
+            const uint8_t* src = blk + c.page * D + (local * D + 64 * lane);
+            s8 = *reinterpret_cast<const uint2*>(blk + 2 * c.page * D + c.page + local);
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
                 const u32x4 q = ld16(src + 8 * j);
@@ -316,19 +418,20 @@ __global__ void __launch_bounds__(256) kv_fp8_read_kernel(KvFp8 c, KvTokens t) {
                 all[j + 1][0] = q[2];
                 all[j + 1][1] = q[3];
             }
-            turn8(all, o);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                fp8_decode8(o[e], fp8_scale((e < 4 ? s8.x : s8.y) >> (8 * (e & 3)) & 255u), v);
-                store_row<8>(out + e * t.ld_ov, 8, v);
-            }
-            return;
         }
+        turn8(all, o);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e / 4] |= static_cast<uint32_t>(src[8 * e + local % 8]) << (8 * (e & 3));
+        for (int e = 0; e < 8; ++e) {
+            fp8_decode8(o[e], fp8_scale((e < 4 ? s8.x : s8.y) >> (8 * (e & 3)) & 255u), v);
+            store_row<8>(static_cast<T*>(t.out_v) + (win.start + e) * t.ld_ov + at, 8, v);
+        }
     }
-    fp8_decode8(w, fp8_scale(*sb), v);
-    store_row<8>(out, 8, v);
+    for (uint32_t left = win.alone; left; left &= left - 1) {
+        const int i = i0 + __ffs(static_cast<int>(left)) - 1;
+        const uint8_t* blk = kv_place(c, t, i, h, &local);
+        kv_get<LANES>(c, blk, local, true, lane, v);
+        store_row<8>(static_cast<T*>(t.out_v) + i * t.ld_ov + at, 8, v);
+    }
 }
 
 template <typename T, int WAVES, int NV> hipError_t norm_launch(const NormArgs& a, hipStream_t s) {
@@ -371,30 +474,34 @@ hipError_t launch_quantise_fp8(int form, int n, int k, int dt, const void* x, in
 }
 
 namespace {
-dim3 kv_grid(const KvFp8& c, int n) { return dim3(static_cast<uint32_t>((static_cast<int64_t>(n) * c.heads * (c.dim / 8) + 255) / 256), 2); }
+
+// Lanes a (token, head) that fill the chip: from here on windows
+constexpr int64_t kManyTokens = 1 << 13;
+
+template <typename T, int D> void kv_append(const KvFp8& c, const KvTokens& t, hipStream_t s) {
+    const int64_t units = static_cast<int64_t>(t.n) * c.heads, windows = (t.n + 7) / 8 * static_cast<int64_t>(c.heads);
+    constexpr int GROUPS = 256 / (D / 8);
+    if (units >= kManyTokens) kv_fp8_append_window_kernel<T, D><<<dim3((windows + GROUPS - 1) / GROUPS, 2), 256, 0, s>>>(c, t);
+    else kv_fp8_append_kernel<T, D><<<dim3((units + GROUPS - 1) / GROUPS, 2), 256, 0, s>>>(c, t);
+}
+template <typename T, int D> void kv_read(const KvFp8& c, const KvTokens& t, hipStream_t s) {
+    const int64_t units = static_cast<int64_t>(t.n) * c.heads, windows = (t.n + 7) / 8 * static_cast<int64_t>(c.heads);
+    constexpr int GROUPS = 256 / (D / 8);
+    if (units >= kManyTokens) kv_fp8_read_window_kernel<T, D><<<dim3((windows + GROUPS - 1) / GROUPS, 2), 256, 0, s>>>(c, t);
+    else kv_fp8_read_kernel<T, D><<<dim3((units + GROUPS - 1) / GROUPS, 2), 256, 0, s>>>(c, t);
+}
+
 }  // namespace
 
 hipError_t launch_kv_fp8_append(const KvFp8& c, const KvTokens& t, hipStream_t s) {
-    const dim3 grid = kv_grid(c, t.n);
-    if (t.dt == RL_DTYPE_FP32) {
-        if (c.dim == 128) kv_fp8_append_kernel<float, 128><<<grid, 256, 0, s>>>(c, t);
-        else kv_fp8_append_kernel<float, 64><<<grid, 256, 0, s>>>(c, t);
-    } else {
-        if (c.dim == 128) kv_fp8_append_kernel<uint16_t, 128><<<grid, 256, 0, s>>>(c, t);
-        else kv_fp8_append_kernel<uint16_t, 64><<<grid, 256, 0, s>>>(c, t);
-    }
+    if (t.dt == RL_DTYPE_FP32) c.dim == 128 ? kv_append<float, 128>(c, t, s) : kv_append<float, 64>(c, t, s);
+    else c.dim == 128 ? kv_append<uint16_t, 128>(c, t, s) : kv_append<uint16_t, 64>(c, t, s);
     return hipGetLastError();
 }
 
 hipError_t launch_kv_fp8_read(const KvFp8& c, const KvTokens& t, hipStream_t s) {
-    const dim3 grid = kv_grid(c, t.n);
-    if (t.dt == RL_DTYPE_FP32) {
-        if (c.dim == 128) kv_fp8_read_kernel<float, 128><<<grid, 256, 0, s>>>(c, t);
-        else kv_fp8_read_kernel<float, 64><<<grid, 256, 0, s>>>(c, t);
-    } else {
-        if (c.dim == 128) kv_fp8_read_kernel<uint16_t, 128><<<grid, 256, 0, s>>>(c, t);
-        else kv_fp8_read_kernel<uint16_t, 64><<<grid, 256, 0, s>>>(c, t);
-    }
+    if (t.dt == RL_DTYPE_FP32) c.dim == 128 ? kv_read<float, 128>(c, t, s) : kv_read<float, 64>(c, t, s);
+    else c.dim == 128 ? kv_read<uint16_t, 128>(c, t, s) : kv_read<uint16_t, 64>(c, t, s);
     return hipGetLastError();
 }
 

@@ -431,6 +431,71 @@ def test_cache_tokens_in_any_order_and_one_by_one():
     assert torch.equal(whole.pool, single.pool)
 
 
+# (lengths, starts, page, heads, d, pad, shift): at least 8192 pairs of a token and a head
+MANY = [([33, 100, 64, 1, 7, 8, 9, 16, 1, 1], [0, 0, 128, 5, 1, 8, 0, 7, 8, 15], 64, 64, 128, 0, 0), ([300, 1, 4], [5, 0, 28], 32, 32, 64, 3, 1),
+        ([1] * 131, list(range(131)), 32, 64, 128, 0, 0), ([2100], [0], 4096, 4, 128, 8, 0), ([2047, 6], [4090, 2], 64, 4, 64, 0, 4),
+        ([9, 15, 17, 23] * 40, [0, 7, 8, 1] * 40, 256, 5, 128, 1, 0)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("lens,starts,page,heads,d,pad,shift", MANY)
+def test_cache_of_many_tokens(dtype, lens, starts, page, heads, d, pad, shift):
+    """In order, shuffled in parts, with tokens in between that have no place."""
+    seqs, pos = packed(lens, starts)
+    n = seqs.numel()
+    assert n * heads >= 8192
+    k, v = kv(n, heads, d, dtype, n, pad, shift)
+    want = []
+    for x in (k, v):
+        b = F.scale_bytes(x.double().abs().amax(2))
+        want.append(F.encode(x.double(), b[..., None]) * F.factor(b.to(torch.uint8))[..., None])
+    some = torch.arange(n, device=DEV)
+    some = torch.cat([some[:n // 3], some[n // 3:n // 2].flip(0), some[n // 2:]])
+    gone = torch.zeros(n, dtype=torch.bool, device=DEV)
+    gone[[n // 5, n - 1]] = True
+    gone[n // 4:n // 4 + 9] = True
+    for order, lost in ((torch.arange(n, device=DEV), None), (some, None), (torch.arange(n, device=DEV), gone)):
+        c = Cache([s + m for s, m in zip(starts, lens)], page, heads, d, n)
+        before = c.pool.clone()
+        sq, ps = seqs[order], pos[order]
+        ok = torch.ones(n, dtype=torch.bool, device=DEV)
+        if lost is not None:
+            sq, ps = torch.where(lost, -1, sq), torch.where(lost & (order % 2 == 0), -ps, ps)
+            ok = ~lost
+        kk, vv = (rows(n, 3 * heads * d, dtype, 0, pad, shift)[:, i * heads * d:(i + 1) * heads * d].unflatten(1, (heads, d)) for i in (1, 2))
+        kk.copy_(k[order]), vv.copy_(v[order])
+        c.append(sq, ps, kk, vv)
+        a, b, e, f = F.places(page, heads, d, c.table, sq[ok], ps[ok])
+        for w, at, sat in zip(want, (a, b), (e, f)):
+            assert torch.equal(F.cache_numbers(c.pool, at, sat), w[order][ok])
+            before[at], before[sat] = c.pool[at], c.pool[sat]
+        assert torch.equal(c.pool, before)
+        out = [torch.full((n, heads, d), NAN, dtype=dtype, device=DEV) for _ in range(2)]
+        R.kv_quant_read(c.pool, c.table, sq, ps, *out, page_size=page)
+        for w, o in zip(want, out):
+            assert torch.equal(o.double(), torch.where(ok[:, None, None], w[order], 0.0))
+
+
+def test_cache_of_many_tokens_past_the_pages():
+    """A prompt of which a page in the middle is not there: nothing is written for it, and zeros are read."""
+    n, page, heads, d = 2048, 64, 4, 128
+    c = Cache([n], page, heads, d, 1, 0)
+    c.table[0, 7], c.table[0, 20] = -1, c.n_pages
+    seqs, pos = packed([n], [0])
+    k, v = kv(n, heads, d, BF, 3)
+    c.append(seqs, pos, k, v)
+    ok = ((pos // page) != 7) & ((pos // page) != 20)
+    a, b, e, f = F.places(page, heads, d, c.table, seqs[ok], pos[ok])
+    written = torch.zeros_like(c.pool, dtype=torch.bool)
+    for at in (a, b, e, f):
+        written[at] = True
+    assert (c.pool[~written] == 0xFF).all()
+    out = [torch.full((n, heads, d), NAN, device=DEV) for _ in range(2)]
+    R.kv_quant_read(c.pool, c.table, seqs, pos, *out, page_size=page)
+    for o, at, sat in zip(out, (a, b), (e, f)):
+        assert torch.equal(o[ok].double(), F.cache_numbers(c.pool, at, sat)) and (o[~ok] == 0).all() and (o[ok] != 0).any()
+
+
 def test_cache_tokens_without_a_place():
     c = Cache([64, 64], 32, 2, 64, 1)
     c.table[1, 1] = c.n_pages            # no such page
