@@ -172,9 +172,10 @@ __global__ void __launch_bounds__(256) quantise_tiles_kernel(int n, int k, const
 
 // ---------------------------------------------------------------------------
 // The cache.  One scale for a head's entries of one position; D / 8 lanes a
-// head, 8 entries a lane.  21162 tokens of 4 heads of 128 in bf16, 65 MB each way: written
-// in 22.4 us, read in 20.7 (keys alone 10; values byte by byte 62 and 27); 512 single
-// tokens 5.0 and 4.2, chains of three loads: place, page, data.
+// head, 8 entries a lane.  Bound by chains of three loads (place, page, data): 512 single tokens of 4 heads of 128 in bf16 take
+// 5.1 us to write and 4.2 to read.  Many tokens go eight a lane group, so that there is one chain for eight rows: 21162 of
+// them, 65 MB each way, 17.3 and 17.4 us (3.8 TB/s; a lane group a token and eights found together 22.4 and 20.7, values
+// byte by byte 62 and 27).
 // ---------------------------------------------------------------------------
 // Page block of (token i, head h) and the position in it; null where the token has no place.
 __device__ __forceinline__ uint8_t* kv_place(const KvFp8& c, const KvTokens& t, int i, int h, int* local) {
@@ -237,25 +238,29 @@ __device__ __forceinline__ void fp8_decode8(const uint32_t* w, float scale, floa
     }
 }
 
-// The same read; zeros where there is no block.
-template <int LANES> __device__ __forceinline__ void kv_get(const KvFp8& c, const uint8_t* blk, int local, bool values, int lane, float* v) {
+// The same read: codes and scale byte, of the pool's first place where there is no block (no branch: the loads of several
+// tokens are under way together).
+struct KvRead { uint32_t w[2]; int scale; };
+template <int LANES> __device__ __forceinline__ KvRead kv_get(const KvFp8& c, const uint8_t* blk, int local, bool values, int lane) {
     constexpr int D = 8 * LANES;
-    if (!blk) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-        return;
-    }
-    uint32_t w[2] = {0u, 0u};
+    const uint8_t* p = blk ? blk : c.pool;
+    KvRead r{{0u, 0u}, 0};
+    r.scale = p[2 * c.page * D + (values ? c.page : 0) + local];
     if (!values) {
-        const uint2 q = *reinterpret_cast<const uint2*>(blk + local * D + 8 * lane);
-        w[0] = q.x;
-        w[1] = q.y;
+        const uint2 q = *reinterpret_cast<const uint2*>(p + local * D + 8 * lane);
+        r.w[0] = q.x;
+        r.w[1] = q.y;
     } else {
-        const uint8_t* src = blk + c.page * D + (local / 8 * D + 8 * lane) * 8 + local % 8;
+        const uint8_t* src = p + c.page * D + (local / 8 * D + 8 * lane) * 8 + local % 8;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e / 4] |= static_cast<uint32_t>(src[8 * e]) << (8 * (e & 3));
+        for (int e = 0; e < 8; ++e) r.w[e / 4] |= static_cast<uint32_t>(src[8 * e]) << (8 * (e & 3));
     }
-    fp8_decode8(w, fp8_scale(blk[2 * c.page * D + (values ? c.page : 0) + local]), v);
+    return r;
+}
+// Its numbers; zeros where there is no block.
+__device__ __forceinline__ void kv_numbers(const uint8_t* blk, const KvRead& r, float* v) {
+    const uint32_t w[2] = {blk ? r.w[0] : 0u, blk ? r.w[1] : 0u};
+    fp8_decode8(w, fp8_scale(blk ? r.scale : 127), v);
 }
 
 // Few tokens: a lane group a (token, head); blockIdx.y 0: keys, 1: values.
@@ -283,7 +288,7 @@ __global__ void __launch_bounds__(256) kv_fp8_read_kernel(KvFp8 c, KvTokens t) {
     if (i >= t.n) return;
     const uint8_t* blk = kv_place(c, t, i, h, &local);
     float v[8];
-    kv_get<LANES>(c, blk, local, values, lane, v);
+    kv_numbers(blk, kv_get<LANES>(c, blk, local, values, lane), v);
     store_row<8>((values ? static_cast<T*>(t.out_v) + i * t.ld_ov : static_cast<T*>(t.out_k) + i * t.ld_ok) + h * D + 8 * lane, 8, v);
 }
 
@@ -336,7 +341,7 @@ __global__ void __launch_bounds__(256) kv_fp8_append_window_kernel(KvFp8 c, KvTo
     int b[8];
     if (blockIdx.y == 0) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) load_row<8>(static_cast<const T*>(t.k) + (i0 + e) * t.ldk + at, i0 + e < t.n ? 8 : 0, x[e]);
+        for (int e = 0; e < 8; ++e) load_row<8>(static_cast<const T*>(t.k) + min(i0 + e, t.n - 1) * t.ldk + at, 8, x[e]);
         uint8_t* mine = i0 + (lane & 7) < t.n ? kv_place(c, t, i0 + (lane & 7), h, &local) : nullptr;
 #pragma unroll
         for (int e = 0; e < 8; ++e) b[e] = fp8_encode<8, LANES>(x[e], w[e]);
@@ -367,12 +372,12 @@ __global__ void __launch_bounds__(256) kv_fp8_append_window_kernel(KvFp8 c, KvTo
             if (lane == 0) *reinterpret_cast<uint2*>(blk + 2 * c.page * D + c.page + local) = make_uint2(sb[0], sb[1]);
         }
     }
-    for (uint32_t left = win.alone; left; left &= left - 1) {
-        const int i = i0 + __ffs(static_cast<int>(left)) - 1;
-        load_row<8>(static_cast<const T*>(t.v) + i * t.ldv + at, 8, x[0]);
-        uint8_t* blk = kv_place(c, t, i, h, &local);
-        kv_put<LANES>(c, blk, local, true, lane, x[0]);
-    }
+    if (!win.alone) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) load_row<8>(static_cast<const T*>(t.v) + min(i0 + e, t.n - 1) * t.ldv + at, 8, x[e]);
+    uint8_t* mine = win.alone >> (lane & 7) & 1u ? kv_place(c, t, i0 + (lane & 7), h, &local) : nullptr;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) kv_put<LANES>(c, kv_from<LANES>(mine, e), __shfl(local, e, LANES), true, lane, x[e]);
 }
 
 template <typename T, int D>
@@ -386,18 +391,12 @@ __global__ void __launch_bounds__(256) kv_fp8_read_window_kernel(KvFp8 c, KvToke
     float v[8];
     if (blockIdx.y == 0) {
         uint8_t* mine = i0 + (lane & 7) < t.n ? kv_place(c, t, i0 + (lane & 7), h, &local) : nullptr;
-        const float scale = mine ? fp8_scale(mine[2 * c.page * D + local]) : 0.0f;
-        uint2 q[8];
+        KvRead r[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = kv_get<LANES>(c, kv_from<LANES>(mine, e), __shfl(local, e, LANES), false, lane);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint8_t* blk = kv_from<LANES>(mine, e);
-            const int l = __shfl(local, e, LANES);
-            q[e] = blk ? *reinterpret_cast<const uint2*>(blk + l * D + 8 * lane) : make_uint2(0u, 0u);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t w[2] = {q[e].x, q[e].y};
-            fp8_decode8(w, __shfl(scale, e, LANES), v);
+            kv_numbers(kv_from<LANES>(mine, e), r[e], v);
             if (i0 + e < t.n) store_row<8>(static_cast<T*>(t.out_k) + (i0 + e) * t.ld_ok + at, 8, v);
         }
         return;
@@ -426,11 +425,15 @@ __global__ void __launch_bounds__(256) kv_fp8_read_window_kernel(KvFp8 c, KvToke
             store_row<8>(static_cast<T*>(t.out_v) + (win.start + e) * t.ld_ov + at, 8, v);
         }
     }
-    for (uint32_t left = win.alone; left; left &= left - 1) {
-        const int i = i0 + __ffs(static_cast<int>(left)) - 1;
-        const uint8_t* blk = kv_place(c, t, i, h, &local);
-        kv_get<LANES>(c, blk, local, true, lane, v);
-        store_row<8>(static_cast<T*>(t.out_v) + i * t.ld_ov + at, 8, v);
+    if (!win.alone) return;
+    uint8_t* mine = win.alone >> (lane & 7) & 1u ? kv_place(c, t, i0 + (lane & 7), h, &local) : nullptr;
+    KvRead r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = kv_get<LANES>(c, kv_from<LANES>(mine, e), __shfl(local, e, LANES), true, lane);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        kv_numbers(kv_from<LANES>(mine, e), r[e], v);
+        if (win.alone >> e & 1u) store_row<8>(static_cast<T*>(t.out_v) + (i0 + e) * t.ld_ov + at, 8, v);
     }
 }
 
@@ -475,8 +478,10 @@ hipError_t launch_quantise_fp8(int form, int n, int k, int dt, const void* x, in
 
 namespace {
 
-// Lanes a (token, head) that fill the chip: from here on windows
-constexpr int64_t kManyTokens = 1 << 13;
+// Pairs of a token and a head from which on windows are taken, whose one round costs 4 to 12 us whatever the tokens.  4096
+// tokens of 4 heads of 128, written and read: of prompts 5.7 + 5.4 us (a lane group a token 15.0 + 8.1), single ones 19.3
+// + 13.4 (16.4 + 8.2); half as many: 5.2 + 4.7 (8.5 + 5.2) and 14.4 + 12.5 (9.8 + 5.1); 32768 single ones: 104 + 54 (98 + 49).
+constexpr int64_t kManyTokens = 1 << 14;
 
 template <typename T, int D> void kv_append(const KvFp8& c, const KvTokens& t, hipStream_t s) {
     const int64_t units = static_cast<int64_t>(t.n) * c.heads, windows = (t.n + 7) / 8 * static_cast<int64_t>(c.heads);

@@ -394,10 +394,10 @@ def test_cache_is_exact(dtype, lens, starts, page, heads, d, pad, shift):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF])
-@pytest.mark.parametrize("order", ["single", "eights"])
+@pytest.mark.parametrize("order", ["single", "eights", "many"])
 def test_cache_read_of_every_code_under_every_scale(dtype, order):
     """Numbers that the type does not hold are rounded to it: of bf16 below 2^-133, of either from 2^128 on."""
-    n, page, heads, d = 508, 512, 1, 128
+    n, page, heads, d = 508, 512, 33 if order == "many" else 1, 128
     c = Cache([n], page, heads, d, 0, 0)
     block = c.pool.view(1, -1)[0]
     i = torch.arange(n, device=DEV)
@@ -431,10 +431,10 @@ def test_cache_tokens_in_any_order_and_one_by_one():
     assert torch.equal(whole.pool, single.pool)
 
 
-# (lengths, starts, page, heads, d, pad, shift): at least 8192 pairs of a token and a head
-MANY = [([33, 100, 64, 1, 7, 8, 9, 16, 1, 1], [0, 0, 128, 5, 1, 8, 0, 7, 8, 15], 64, 64, 128, 0, 0), ([300, 1, 4], [5, 0, 28], 32, 32, 64, 3, 1),
-        ([1] * 131, list(range(131)), 32, 64, 128, 0, 0), ([2100], [0], 4096, 4, 128, 8, 0), ([2047, 6], [4090, 2], 64, 4, 64, 0, 4),
-        ([9, 15, 17, 23] * 40, [0, 7, 8, 1] * 40, 256, 5, 128, 1, 0)]
+# (lengths, starts, page, heads, d, pad, shift): at least 16384 pairs of a token and a head
+MANY = [([33, 100, 64, 1, 7, 8, 9, 16, 1, 1], [0, 0, 128, 5, 1, 8, 0, 7, 8, 15], 64, 96, 128, 0, 0), ([300, 1, 4], [5, 0, 28], 32, 64, 64, 3, 1),
+        ([1] * 131, list(range(131)), 32, 128, 128, 0, 0), ([2100], [0], 4096, 8, 128, 8, 0), ([2047, 6], [4090, 2], 64, 8, 64, 0, 4),
+        ([9, 15, 17, 23] * 40, [0, 7, 8, 1] * 40, 256, 7, 128, 1, 0)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF])
@@ -443,7 +443,7 @@ def test_cache_of_many_tokens(dtype, lens, starts, page, heads, d, pad, shift):
     """In order, shuffled in parts, with tokens in between that have no place."""
     seqs, pos = packed(lens, starts)
     n = seqs.numel()
-    assert n * heads >= 8192
+    assert n * heads >= 16384
     k, v = kv(n, heads, d, dtype, n, pad, shift)
     want = []
     for x in (k, v):
@@ -478,7 +478,7 @@ def test_cache_of_many_tokens(dtype, lens, starts, page, heads, d, pad, shift):
 
 def test_cache_of_many_tokens_past_the_pages():
     """A prompt of which a page in the middle is not there: nothing is written for it, and zeros are read."""
-    n, page, heads, d = 2048, 64, 4, 128
+    n, page, heads, d = 2048, 64, 8, 128
     c = Cache([n], page, heads, d, 1, 0)
     c.table[0, 7], c.table[0, 20] = -1, c.n_pages
     seqs, pos = packed([n], [0])
