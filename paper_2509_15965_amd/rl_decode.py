@@ -6,6 +6,7 @@ kernels.  There is no fallback: if librl_decode.so is missing or a call
 fails, an exception is raised.
 """
 import ctypes as C
+import functools
 import os
 from typing import Dict, Optional, Sequence
 
@@ -539,11 +540,12 @@ def _gpu_of(t: torch.Tensor, name: str) -> int:
 # the stream's handle without a Stream object around it (a sixth of a short call's time), where torch has it
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device   # the same without its check of the start-up
 
 
 def _run_on(dev: int, stream, nbytes: int, workspace: Optional[torch.Tensor], call, what: str):
     """call(workspace pointer, its bytes, stream) with GPU `dev` current."""
-    if torch.cuda.current_device() != dev:
+    if _current_device() != dev:
         with torch.cuda.device(dev):
             return _run_on(dev, stream, nbytes, workspace, call, what)
     if stream is not None and stream.device.index != dev:
@@ -760,7 +762,7 @@ def _numbers_on(dev: int, name: str, t: torch.Tensor, rows: Optional[int] = None
 
 def _launch_on(dev: int, stream, what: str, call, *args):
     """call(*args, stream) with GPU `dev` current: a call without a workspace."""
-    if torch.cuda.current_device() != dev:
+    if _current_device() != dev:
         with torch.cuda.device(dev):
             return _launch_on(dev, stream, what, call, *args)
     if stream is not None and stream.device.index != dev:
@@ -847,8 +849,13 @@ def _heads_on(dev: int, name: str, t: torch.Tensor, like: Optional[torch.Tensor]
                      + f", not {dt} {tuple(shape)} with strides {st} on {t.device}")
 
 
+@functools.lru_cache(maxsize=64)
+def _kv_page_bytes(page_size: int, heads: int, d: int) -> int:
+    return lib().rl_kv_quant_bytes(1, page_size, heads, d)
+
+
 def _cache_on(dev: int, pool: torch.Tensor, page_table: torch.Tensor, page_size: int, heads: int, d: int) -> KvFp8:
-    one = lib().rl_kv_quant_bytes(1, page_size, heads, d)
+    one = _kv_page_bytes(page_size, heads, d)
     if not one:
         raise ValueError(f"no cache of pages of {page_size} positions with {heads} heads of {d}")
     shape = page_table.shape
