@@ -455,9 +455,12 @@ Plan plan_of(int m, int n, int kb, bool fp32) {
         // From 33 tokens on tiles are faster (64 x 3584 x 18944: 32 us, 58 here).  Past 16 tokens their re-reading shows: 64
         // weights a workgroup where those fill the chip (32 x 37888 x 3584: 39 us, with 32 weights 41, with 16 54; 24 x
         // 152064: 127, 138, 174), else 32 (20 x 4608 x 3584: 10.1, with 64 12.7, with 16 11.1).  Up to 16 tokens 16 weights
-        // (1 x 37888 x 3584: 26.3, with 32 26.8, with 64 29.6; 1 x 2048 x 1536: 3.6, 4.4, 6.3).
+        // (8 x 2048 x 1536: 3.9, with 32 4.7, with 64 6.4; 4096 x 4096: 6.5 and 8.1; 8960 x 1536: 6.4 and 6.7), or 32 where their
+        // workgroups are half the rounds (8 x 4608 x 3584: 7.2, with 16 8.2, with 64 11.2; 16 x 37888 x 3584: 33, 38, 35; one
+        // token: 26.9 and 26.3).
         q.kind = GEMV;
-        if (m > 16) q.rw = up(n, 64) * gemv_slices(up(n, 64), kb) >= kCus * 7 / 8 ? 4 : 2;
+        if (m <= 16) q.rw = 2 * up(up(n, 32), kCus) <= up(up(n, 16), kCus) ? 2 : 1;
+        else q.rw = up(n, 64) * gemv_slices(up(n, 64), kb) >= kCus * 7 / 8 ? 4 : 2;
         q.slices = gemv_slices(up(n, 16 * q.rw), kb);
     } else {
         const int large = up(m, 256) * up(n, 256), small = up(m, 128) * up(n, 128);
@@ -496,8 +499,13 @@ Plan plan_of(int m, int n, int kb, bool fp32) {
 
 template <typename TO, int RW, int MT> void gemv(const Fp8Gemm& g, const Plan& q, hipStream_t s) {
     const dim3 grid(up(g.n, 16 * RW), q.slices);
-    if (q.slices > 1) gemv_fp8_kernel<TO, RW, MT, true><<<grid, 64 * kGemvWaves, 0, s>>>(g, q.per);
-    else gemv_fp8_kernel<TO, RW, MT, false><<<grid, 64 * kGemvWaves, 0, s>>>(g, q.per);
+    constexpr bool MANY = RW == 2 && MT == 1;   // taken from 129 workgroups on, so never in K slices
+    if constexpr (!MANY)
+        if (q.slices > 1) {
+            gemv_fp8_kernel<TO, RW, MT, true><<<grid, 64 * kGemvWaves, 0, s>>>(g, q.per);
+            return;
+        }
+    gemv_fp8_kernel<TO, RW, MT, false><<<grid, 64 * kGemvWaves, 0, s>>>(g, q.per);
 }
 
 template <typename TO> void run_plan(const Fp8Gemm& a, const Plan& q, hipStream_t s) {
@@ -505,7 +513,8 @@ template <typename TO> void run_plan(const Fp8Gemm& a, const Plan& q, hipStream_
     Fp8Gemm g = a;
     if (q.slices == 1) g.part = nullptr;
     if (q.kind == GEMV) {
-        if (g.m <= 16) gemv<TO, 1, 1>(g, q, s);
+        if (g.m <= 16 && q.rw == 1) gemv<TO, 1, 1>(g, q, s);
+        else if (g.m <= 16) gemv<TO, 2, 1>(g, q, s);
         else if (q.rw == 2) gemv<TO, 2, 2>(g, q, s);
         else gemv<TO, 4, 2>(g, q, s);
     } else {

@@ -248,7 +248,9 @@ GEMMS = [(1, 1, 1), (1, 16, 128), (1, 2048, 1536), (1, 4097, 300), (2, 130, 1894
          (65, 129, 512), (100, 1000, 1536), (128, 256, 18944), (129, 385, 640), (200, 600, 8192), (255, 256, 384), (256, 512, 128), (257, 257, 257),
          (300, 4096, 1536), (512, 3584, 2048), (1000, 700, 1000), (1024, 1024, 3584), (2049, 1027, 896), (5, 40000, 256), (4100, 70, 3000),
          # more than 512 tiles of 128 x 128: large tiles, whole and with a last round cut into four, and small ones for few rows
-         (1000, 9300, 300), (2100, 4301, 896), (512, 33001, 640), (770, 24600, 128), (40, 66000, 384)]
+         (1000, 9300, 300), (2100, 4301, 896), (512, 33001, 640), (770, 24600, 128), (40, 66000, 384),
+         # up to 16 tokens, 16 and 32 weights a workgroup
+         (12, 5003, 1000), (16, 8192, 384), (9, 8193, 384), (16, 12289, 200), (1, 65537, 130)]
 
 
 @pytest.mark.parametrize("m,n,k", GEMMS)
