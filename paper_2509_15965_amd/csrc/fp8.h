@@ -175,13 +175,15 @@ template <int LANES> __device__ __forceinline__ float lanes_max(float v) {
     for (int o = 16; o < LANES; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
     return v;
 }
-__device__ __forceinline__ float lanes_sum64(float v) {
+// sum of LANES neighbouring lanes (16 .. 64)
+template <int LANES> __device__ __forceinline__ float lanes_sum(float v) {
     v += row_rotated<8>(v);
     v += row_rotated<4>(v);
     v += row_rotated<2>(v);
     v += row_rotated<1>(v);
-    v += __shfl_xor(v, 16, 64);
-    return v + __shfl_xor(v, 32, 64);
+#pragma unroll
+    for (int o = 16; o < LANES; o <<= 1) v += __shfl_xor(v, o, 64);
+    return v;
 }
 
 constexpr float kLargestFloat = 3.402823466e38f;

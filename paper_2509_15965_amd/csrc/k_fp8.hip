@@ -14,12 +14,13 @@ namespace {
 // branch, 323 MB, 66 us (4.9 TB/s, a copy's rate); 32 bytes of x a lane, so that an
 // instruction takes every other 16: 87.
 // ---------------------------------------------------------------------------
-template <typename T, int WAVES, int NV>
-__global__ void __launch_bounds__(256) rmsnorm_fp8_kernel(NormArgs p) {
-    constexpr int E = kEntries<T>, ROWS = 4 / WAVES, LANES = 64 * WAVES;
+template <typename T, int LANES, int NV>
+__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) rmsnorm_fp8_kernel(NormArgs p) {
+    constexpr int E = kEntries<T>, ROWS = LANES < 256 ? 256 / LANES : 1, WAVES = LANES / 64;
+    static_assert(LANES >= kFp8Block / E && (LANES <= 64 || LANES >= 256), "a block within a row's lanes; rows of whole workgroups or waves");
     const int row = blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / LANES : 0);
     const int lane = threadIdx.x % LANES;
-    if (row >= p.n) return;   // whole waves; with several waves a row every workgroup has its row
+    if (row >= p.n) return;   // all lanes of a row; with several waves a row every workgroup has its row
     const int H = p.hidden, kb = fp8_blocks(H);
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
     float v[NV][E];
@@ -54,7 +55,7 @@ __global__ void __launch_bounds__(256) rmsnorm_fp8_kernel(NormArgs p) {
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int e = 0; e < E; ++e) ss += v[i][e] * v[i][e];
-    ss = lanes_sum64(ss);
+    ss = lanes_sum<LANES < 64 ? LANES : 64>(ss);
     if constexpr (WAVES > 1) {
         __shared__ float part[WAVES];
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = ss;
@@ -437,22 +438,25 @@ __global__ void __launch_bounds__(256) kv_fp8_read_window_kernel(KvFp8 c, KvToke
     }
 }
 
-template <typename T, int WAVES, int NV> hipError_t norm_launch(const NormArgs& a, hipStream_t s) {
-    constexpr int ROWS = 4 / WAVES;
-    rmsnorm_fp8_kernel<T, WAVES, NV><<<(a.n + ROWS - 1) / ROWS, 256, 0, s>>>(a);
+template <typename T, int LANES, int NV> hipError_t norm_launch(const NormArgs& a, hipStream_t s) {
+    constexpr int ROWS = LANES < 256 ? 256 / LANES : 1;
+    rmsnorm_fp8_kernel<T, LANES, NV><<<(a.n + ROWS - 1) / ROWS, LANES < 256 ? 256 : LANES, 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename T> hipError_t norm_for(const NormArgs& a, hipStream_t s) {
     const int vecs = fp8_blocks(a.hidden) * (kFp8Block / kEntries<T>);   // lanes' vectors of a row
-    if (vecs <= 64) return norm_launch<T, 1, 1>(a, s);
-    if (vecs <= 128) return norm_launch<T, 1, 2>(a, s);
-    if (vecs <= 256) return norm_launch<T, 1, 4>(a, s);
-    if (vecs <= 512) return norm_launch<T, 1, 8>(a, s);
-    if (vecs <= 1024) return norm_launch<T, 4, 4>(a, s);
-    if (vecs <= 2048) return norm_launch<T, 4, 8>(a, s);
+    if constexpr (sizeof(T) == 2)
+        if (vecs <= 16) return norm_launch<T, 16, 1>(a, s);
+    if (vecs <= 32) return norm_launch<T, 32, 1>(a, s);
+    if (vecs <= 64) return norm_launch<T, 64, 1>(a, s);
+    if (vecs <= 128) return norm_launch<T, 64, 2>(a, s);
+    if (vecs <= 256) return norm_launch<T, 64, 4>(a, s);
+    if (vecs <= 512) return norm_launch<T, 256, 2>(a, s);
+    if (vecs <= 1024) return norm_launch<T, 256, 4>(a, s);
+    if (vecs <= 2048) return norm_launch<T, 512, 4>(a, s);
     if constexpr (sizeof(T) == 4)
-        if (vecs > 4096) return norm_launch<T, 4, 32>(a, s);
-    return norm_launch<T, 4, 16>(a, s);
+        if (vecs > 4096) return norm_launch<T, 1024, 8>(a, s);
+    return norm_launch<T, 1024, 4>(a, s);
 }
 
 template <typename T> hipError_t quantise_for(int form, int n, int k, const void* x, int64_t ldx, const Fp8Out& out, hipStream_t s) {

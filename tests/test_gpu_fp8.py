@@ -162,7 +162,8 @@ def test_swiglu_of_far_numbers():
 
 
 NORMS = [(1, 1, 0, 0), (3, 100, 0, 0), (8, 256, 0, 0), (5, 512, 1, 0), (7, 1000, 0, 3), (65, 1536, 0, 0), (4, 2048, 8, 0), (513, 3584, 0, 0),
-         (3, 4096, 0, 8), (2, 4097, 0, 0), (9, 5120, 0, 0), (2, 8192, 0, 0), (3, 8193, 7, 0), (2, 32768, 0, 0)]
+         (3, 4096, 0, 8), (2, 4097, 0, 0), (9, 5120, 0, 0), (2, 8192, 0, 0), (3, 8193, 7, 0), (2, 32768, 0, 0),
+         (37, 64, 0, 0), (33, 128, 3, 1), (70, 127, 0, 0), (6, 200, 0, 2), (3, 12288, 0, 0), (2, 16385, 0, 0), (2, 20000, 5, 0)]
 
 
 @pytest.mark.parametrize("n,h,pad,shift", NORMS)
