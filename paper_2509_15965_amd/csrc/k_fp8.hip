@@ -9,10 +9,10 @@ namespace {
 
 // ---------------------------------------------------------------------------
 // RMS norm.  s = x + add (as stored), y = s w / sqrt(mean s^2 + eps), y in blocks of
-// 128.  WAVES waves a row, a row in registers from its one read to its codes: NV
+// 128.  LANES lanes a row, a row in registers from its one read to its codes: NV
 // times 16 bytes of x a lane.  Bound by memory: 8192 x 3584 in fp32 with a bf16
-// branch, 323 MB, 66 us (4.9 TB/s, a copy's rate); 32 bytes of x a lane, so that an
-// instruction takes every other 16: 87.
+// branch, 323 MB, 63 us (5.1 TB/s, a copy's rate); 32 bytes of x a lane at a time, so that
+// an instruction takes every other 16: a third more.
 // ---------------------------------------------------------------------------
 template <typename T, int LANES, int NV>
 __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) rmsnorm_fp8_kernel(NormArgs p) {
@@ -444,7 +444,11 @@ template <typename T, int LANES, int NV> hipError_t norm_launch(const NormArgs& 
     return hipGetLastError();
 }
 template <typename T> hipError_t norm_for(const NormArgs& a, hipStream_t s) {
-    const int vecs = fp8_blocks(a.hidden) * (kFp8Block / kEntries<T>);   // lanes' vectors of a row
+    // 16-byte vectors of a row.  Two to a lane, so that many waves fit a SIMD; a wave takes a short row alone, up to four to a
+    // lane, and no barrier.  67 M entries, a bf16 branch, the sum stored; us, other lanes in brackets: fp32 rows of 128 145 (64
+    // lanes: 258), of 640 148 (256: 216), of 3584 137 (256: 146), of 8192 137 (512: 142, 256: 159), of 16384 144 (256: 220); bf16
+    // rows of 128 87 (64: 284), of 4096 86 (64: 128), of 5120 96 (256: 101), of 12288 92 (512: 98, 256: 138).
+    const int vecs = fp8_blocks(a.hidden) * (kFp8Block / kEntries<T>);
     if constexpr (sizeof(T) == 2)
         if (vecs <= 16) return norm_launch<T, 16, 1>(a, s);
     if (vecs <= 32) return norm_launch<T, 32, 1>(a, s);
@@ -452,8 +456,8 @@ template <typename T> hipError_t norm_for(const NormArgs& a, hipStream_t s) {
     if (vecs <= 128) return norm_launch<T, 64, 2>(a, s);
     if (vecs <= 256) return norm_launch<T, 64, 4>(a, s);
     if (vecs <= 512) return norm_launch<T, 256, 2>(a, s);
-    if (vecs <= 1024) return norm_launch<T, 256, 4>(a, s);
-    if (vecs <= 2048) return norm_launch<T, 512, 4>(a, s);
+    if (vecs <= 1024) return norm_launch<T, 512, 2>(a, s);
+    if (vecs <= 2048) return norm_launch<T, 1024, 2>(a, s);
     if constexpr (sizeof(T) == 4)
         if (vecs > 4096) return norm_launch<T, 1024, 8>(a, s);
     return norm_launch<T, 1024, 4>(a, s);
