@@ -562,9 +562,9 @@ typedef struct rl_fp8_matrix {
  *  n <= 2^20 rows of hidden <= 32768 entries; x [n][ldx] of dtype; add
  *  [n][ld_add] of add_dtype, or NULL; weight [hidden] of w_dtype; out_sum
  *  [n][ld_sum] of dtype, or NULL; it may be x (same ld), or add (same ld and
- *  dtype).  eps in (0, 1].  The norm is of s as it is stored; the sum
- *  of squares is fp32, and a row where it is infinite becomes zeros (NaN where
- *  s is infinite). */
+ *  dtype).  eps in (0, 1].  The norm is of s as it is stored, in
+ *  64 bits from there to the code; a row with an infinite s is NaN there and
+ *  zeros elsewhere. */
 rl_status rl_rmsnorm_quant(int32_t n, int32_t hidden, int32_t dtype, const void* x, int64_t ldx, int32_t add_dtype, const void* add,
                          int64_t ld_add, int32_t w_dtype, const void* weight, double eps, void* out_sum, int64_t ld_sum,
                          const rl_fp8_matrix* out, void* stream);

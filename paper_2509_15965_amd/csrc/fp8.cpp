@@ -73,7 +73,7 @@ rl_status rl_rmsnorm_quant(int32_t n, int32_t hidden, int32_t dtype, const void*
     if (!rows_ok(dtype, x, n, hidden, ldx) || !rows_ok(w_dtype, weight, 1, hidden, hidden) || !matrix_ok(out, hidden)) return RL_ERR_INVALID_ARG;
     if (add && !rows_ok(add_dtype, add, n, hidden, ld_add)) return RL_ERR_INVALID_ARG;
     if (out_sum && !rows_ok(dtype, out_sum, n, hidden, ld_sum)) return RL_ERR_INVALID_ARG;
-    const NormArgs a{n, hidden, x, ldx, dtype, add, ld_add, add_dtype, weight, w_dtype, static_cast<float>(eps), out_sum, ld_sum,
+    const NormArgs a{n, hidden, x, ldx, dtype, add, ld_add, add_dtype, weight, w_dtype, eps, 1.0 / hidden, out_sum, ld_sum,
                      out_of(out)};
     return status_of(launch_rmsnorm_fp8(a, static_cast<hipStream_t>(stream)));
 }

@@ -18,7 +18,7 @@ struct NormArgs {
     const void* x; int64_t ldx; int x_dt;
     const void* add; int64_t ld_add; int add_dt;   // or null
     const void* w; int w_dt;
-    float eps;
+    double eps, per_entry;                         // 1 / hidden
     void* sum; int64_t ld_sum;                     // x_dt; or null
     Fp8Out out;
 };
@@ -175,8 +175,12 @@ template <int LANES> __device__ __forceinline__ float lanes_max(float v) {
     for (int o = 16; o < LANES; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
     return v;
 }
+template <int N> __device__ __forceinline__ double row_rotated(double v) {
+    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), 0x120 + N, 0xF, 0xF, true);
+    return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), 0x120 + N, 0xF, 0xF, true), lo);
+}
 // sum of LANES neighbouring lanes (16 .. 64)
-template <int LANES> __device__ __forceinline__ float lanes_sum(float v) {
+template <int LANES> __device__ __forceinline__ double lanes_sum(double v) {
     v += row_rotated<8>(v);
     v += row_rotated<4>(v);
     v += row_rotated<2>(v);

@@ -11,11 +11,29 @@ namespace {
 // RMS norm.  s = x + add (as stored), y = s w / sqrt(mean s^2 + eps), y in blocks of
 // 128.  LANES lanes a row, a row in registers from its one read to its codes: NV
 // times 16 bytes of x a lane.  Bound by memory: 8192 x 3584 in fp32 with a bf16
-// branch, 323 MB, 63 us (5.1 TB/s, a copy's rate); 32 bytes of x a lane at a time, so that
-// an instruction takes every other 16: a third more.
+// branch, 323 MB, 64.9 us (5.0 TB/s, a copy's rate); 32 bytes of x a lane at a time, so that
+// an instruction takes every other 16: a third more.  The arithmetic has room: sums,
+// root and products are in 64 bits, so that a code is off only where 64 bits
+// are (in fp32 20 of the 29 M codes round to a neighbour, in 62.8 us).
 // ---------------------------------------------------------------------------
+// 1 / sqrt(a) of a positive a: the hardware's, and two steps of Newton's method, which double its digits each
+__device__ __forceinline__ double inverse_root(double a) {
+    double y = __builtin_amdgcn_rsq(a);
+    if (a < 1e300) {   // an infinite one stays 0
+#pragma unroll
+        for (int i = 0; i < 2; ++i) y = __builtin_fma(y, __builtin_fma(-0.5 * a * y, y, 0.5), y);
+    }
+    return y;
+}
+
+// x cut to 24 bits, the last of which is set where something was cut off: rounded once more, to fewer bits, that is x rounded
+__device__ __forceinline__ float to_odd(double x) {
+    const int lo = __double2loint(x), kept = lo & ~0x1FFFFFFF;
+    return static_cast<float>(__hiloint2double(__double2hiint(x), lo & 0x1FFFFFFF ? kept | 0x20000000 : kept));
+}
+
 template <typename T, int LANES, int NV>
-__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) rmsnorm_fp8_kernel(NormArgs p) {
+__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES, NV <= 2 ? 8 : 4) rmsnorm_fp8_kernel(NormArgs p) {
     constexpr int E = kEntries<T>, ROWS = LANES < 256 ? 256 / LANES : 1, WAVES = LANES / 64;
     static_assert(LANES >= kFp8Block / E && (LANES <= 64 || LANES >= 256), "a block within a row's lanes; rows of whole workgroups or waves");
     const int row = blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / LANES : 0);
@@ -50,21 +68,24 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) rmsnorm_fp8_kernel(
             store_row<E>(static_cast<T*>(p.sum) + row * p.ld_sum + at, H - at, v[i]);
         }
     }
-    float ss = 0.0f;
+    double ss = 0.0;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int e = 0; e < E; ++e) ss += v[i][e] * v[i][e];
+        for (int e = 0; e < E; ++e) {
+            ss = __builtin_fma(static_cast<double>(v[i][e]), static_cast<double>(v[i][e]), ss);
+            asm("" : "+v"(v[i][e]));   // converted again below: its 64 bits are not kept in registers
+        }
     ss = lanes_sum<LANES < 64 ? LANES : 64>(ss);
     if constexpr (WAVES > 1) {
-        __shared__ float part[WAVES];
+        __shared__ double part[WAVES];
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = ss;
         __syncthreads();
-        ss = 0.0f;
+        ss = 0.0;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) ss += part[w];
     }
-    const float r = 1.0f / sqrtf(ss / static_cast<float>(H) + p.eps);
+    const double r = inverse_root(ss * p.per_entry + p.eps);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int at = E * (lane + LANES * i);
@@ -72,7 +93,7 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) rmsnorm_fp8_kernel(
         if (p.w_dt == RL_DTYPE_FP32) load_row<E>(static_cast<const float*>(p.w) + at, H - at, g);
         else load_row<E>(static_cast<const uint16_t*>(p.w) + at, H - at, g);
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[i][e] = v[i][e] * r * g[e];
+        for (int e = 0; e < E; ++e) v[i][e] = to_odd(v[i][e] * (r * g[e]));
         if (at + E > H) {   // nothing behind the row, whatever r is
 #pragma unroll
             for (int e = 0; e < E; ++e)
@@ -444,17 +465,23 @@ template <typename T, int LANES, int NV> hipError_t norm_launch(const NormArgs& 
     return hipGetLastError();
 }
 template <typename T> hipError_t norm_for(const NormArgs& a, hipStream_t s) {
-    // 16-byte vectors of a row.  Two to a lane, so that many waves fit a SIMD; a wave takes a short row alone, up to four to a
-    // lane, and no barrier.  67 M entries, a bf16 branch, the sum stored; us, other lanes in brackets: fp32 rows of 128 145 (64
-    // lanes: 258), of 640 148 (256: 216), of 3584 137 (256: 146), of 8192 137 (512: 142, 256: 159), of 16384 144 (256: 220); bf16
-    // rows of 128 87 (64: 284), of 4096 86 (64: 128), of 5120 96 (256: 101), of 12288 92 (512: 98, 256: 138).
+    // 16-byte vectors of a row.  Two to a lane, so that many waves fit a SIMD; a wave takes a short row alone, in fp32 up to four to
+    // a lane, and no barrier.  67 M entries, a bf16 branch, the sum stored: fp32 rows of 128 take 154 us, of 3584 141, of 8192 140, of
+    // 16384 158; bf16 rows of 128 95, of 2048 94 (64 lanes: 111), of 4096 89, of 5120 113, of 12288 111.  Compared with sums in 32
+    // bits, which were up to a fifth faster: fp32 rows of 128 145 (64 lanes: 258), of 640 148 (256: 216), of 3584 137 (256: 146), of
+    // 8192 137 (512: 142, 256: 159), of 16384 144 (256: 220); bf16 rows of 128 87 (64: 284), of 4096 86 (64: 128), of 12288 92
+    // (512: 98, 256: 138).
     const int vecs = fp8_blocks(a.hidden) * (kFp8Block / kEntries<T>);
     if constexpr (sizeof(T) == 2)
         if (vecs <= 16) return norm_launch<T, 16, 1>(a, s);
     if (vecs <= 32) return norm_launch<T, 32, 1>(a, s);
     if (vecs <= 64) return norm_launch<T, 64, 1>(a, s);
     if (vecs <= 128) return norm_launch<T, 64, 2>(a, s);
-    if (vecs <= 256) return norm_launch<T, 64, 4>(a, s);
+    if constexpr (sizeof(T) == 4) {
+        if (vecs <= 256) return norm_launch<T, 64, 4>(a, s);
+    } else {
+        if (vecs <= 256) return norm_launch<T, 256, 1>(a, s);
+    }
     if (vecs <= 512) return norm_launch<T, 256, 2>(a, s);
     if (vecs <= 1024) return norm_launch<T, 512, 2>(a, s);
     if (vecs <= 2048) return norm_launch<T, 1024, 2>(a, s);

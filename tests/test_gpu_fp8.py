@@ -198,17 +198,44 @@ def test_norm_sum_in_place(which):
     assert torch.equal(to, total) and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+def norm_64(s, w, eps):
+    s = s.double()
+    return s / torch.sqrt(s.square().mean(1, keepdim=True) + eps) * w.double()
+
+
+@pytest.mark.parametrize("n,h", [(300, 64), (65, 130), (128, 896), (64, 3584), (32, 9000), (16, 32768)])
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_norm_is_rounded_once(n, h, dtype):
+    """Codes and scales are those of the formula in 64 bits: a number within 2^-48 of a border between two codes, where the two
+    could differ, is one in 2^43 or fewer."""
+    x, a = rows(n, h, dtype, 7), rows(n, h, BF, 8)
+    w = rows(1, h, F32, 9)[0]
+    s = torch.empty(n, h, dtype=dtype, device=DEV)
+    codes, scales = room(n, h)
+    R.rmsnorm_quant(x, w, codes, scales, add=a, out_sum=s, eps=1e-5)
+    y = norm_64(s, w, 1e-5)
+    kb = F.blocks(h)
+    b = F.scale_bytes(F.finite_max(F.row_blocks(y), (2,)))
+    assert torch.equal(scales[:, :kb].int(), b.int())
+    assert torch.equal(F.code_values(codes).view(n, kb, 128), F.encode(F.row_blocks(y), b[..., None]))
+
+
 def test_norm_of_rows_whose_squares_pass_fp32():
-    """The sum of squares is infinite: zeros, and NaN for an infinite entry."""
-    x = torch.full((3, 300), 1e19, device=DEV)
+    x = torch.full((4, 300), 1e19, device=DEV)
     x[0] = 3e38
     x[1] = 1.0
     x[1, 7] = -2e19
     x[2, 299] = INF
-    codes, scales = room(3, 300)
-    R.rmsnorm_quant(x, torch.ones(300, device=DEV), codes, scales)
-    v = F.matrix(codes, scales)
-    assert (v[:2] == 0).all() and (v[2, :299] == 0).all() and torch.isnan(v[2, 299]) and (v[2, 300:] == 0).all()
+    x[3] = 1e-30
+    codes, scales = room(4, 300)
+    w = torch.ones(300, device=DEV)
+    R.rmsnorm_quant(x, w, codes, scales, eps=1e-40)
+    v = F.matrix(codes, scales)[:, :300]
+    y = norm_64(x, w, float(torch.tensor(1e-40, dtype=torch.float64)))
+    keep = [0, 1, 3]
+    b = F.scale_bytes(F.finite_max(F.row_blocks(y[keep]), (2,)))
+    assert torch.equal(v[keep], (F.encode(F.row_blocks(y[keep]), b[..., None]) * F.factor(b.to(torch.uint8))[..., None]).flatten(1)[:, :300])
+    assert (v[2, :299] == 0).all() and torch.isnan(v[2, 299])
 
 
 def test_norm_of_rows_that_are_zero_or_not_finite():
