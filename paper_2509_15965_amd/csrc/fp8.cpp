@@ -114,7 +114,8 @@ rl_status rl_kv_quant_append(const rl_kv_fp8* cache, int32_t n, const int32_t* s
     if (n == 0) return RL_OK;
     if (static_cast<int64_t>(n) * c.heads >= kMaxBlocks) return RL_ERR_UNSUPPORTED;
     const int64_t width = static_cast<int64_t>(c.heads) * c.dim;
-    if (!numbers_ok(seqs) || !numbers_ok(positions) || !rows_ok(dtype, k, n, width, ldk) || !rows_ok(dtype, v, n, width, ldv)) return RL_ERR_INVALID_ARG;
+    if (!numbers_ok(seqs) || !numbers_ok(positions)) return RL_ERR_INVALID_ARG;
+    if (!rows_ok(dtype, k, n, width, ldk) || !rows_ok(dtype, v, n, width, ldv)) return RL_ERR_INVALID_ARG;
     const KvTokens t{n, seqs, positions, k, v, ldk, ldv, nullptr, nullptr, 0, 0, dtype};
     return status_of(launch_kv_fp8_append(c, t, static_cast<hipStream_t>(stream)));
 }
@@ -126,7 +127,8 @@ rl_status rl_kv_quant_read(const rl_kv_fp8* cache, int32_t n, const int32_t* seq
     if (n == 0) return RL_OK;
     if (static_cast<int64_t>(n) * c.heads >= kMaxBlocks) return RL_ERR_UNSUPPORTED;
     const int64_t width = static_cast<int64_t>(c.heads) * c.dim;
-    if (!numbers_ok(seqs) || !numbers_ok(positions) || !rows_ok(dtype, out_k, n, width, ldk) || !rows_ok(dtype, out_v, n, width, ldv)) return RL_ERR_INVALID_ARG;
+    if (!numbers_ok(seqs) || !numbers_ok(positions)) return RL_ERR_INVALID_ARG;
+    if (!rows_ok(dtype, out_k, n, width, ldk) || !rows_ok(dtype, out_v, n, width, ldv)) return RL_ERR_INVALID_ARG;
     const KvTokens t{n, seqs, positions, nullptr, nullptr, 0, 0, out_k, out_v, ldk, ldv, dtype};
     return status_of(launch_kv_fp8_read(c, t, static_cast<hipStream_t>(stream)));
 }
@@ -149,7 +151,8 @@ rl_status rl_attention_quant(const rl_kv_fp8* cache, int32_t n, const int32_t* s
     if (n == 0) return RL_OK;
     if (!attention_fp8_fits(n, c.heads, n_q_heads, max_length)) return RL_ERR_UNSUPPORTED;
     const int64_t width = static_cast<int64_t>(n_q_heads) * c.dim;
-    if (!numbers_ok(lengths) || !aligned(seqs, 4) || !rows_ok(dtype, q, n, width, ldq) || !rows_ok(dtype, out, n, width, ldo)) return RL_ERR_INVALID_ARG;
+    if (!numbers_ok(lengths) || !aligned(seqs, 4)) return RL_ERR_INVALID_ARG;
+    if (!rows_ok(dtype, q, n, width, ldq) || !rows_ok(dtype, out, n, width, ldo)) return RL_ERR_INVALID_ARG;
     if (const rl_status st = workspace_ok(workspace, ws_bytes, attention_fp8_ws_bytes(n, c.heads, n_q_heads, c.dim, max_length)); st != RL_OK)
         return st;
     const AttnFp8 a{c, n, max_length, seqs, lengths, q, ldq, out, ldo, dtype, n_q_heads, static_cast<float>(scale),
