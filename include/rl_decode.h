@@ -655,8 +655,8 @@ size_t rl_attention_quant_workspace_bytes(int32_t n, int32_t n_kv_heads, int32_t
  *  max_length  no row is longer: a longer one is taken as this long.  The
  *              work is laid out by it, so a near bound is the fastest.
  *  q, out      [n][ld] of dtype, a token's heads one after the other.  The
- *              weights of the values keep 16 bits for bf16 and 24 for fp32;
- *              values below about 1e-33 count as 0. */
+ *              weights of the values keep 24 bits; values below about 1e-33
+ *              count as 0. */
 rl_status rl_attention_quant(const rl_kv_fp8* cache, int32_t n, const int32_t* seqs, const int32_t* lengths, int32_t max_length,
                            int32_t dtype, const void* q, int64_t ldq, int32_t n_q_heads, double scale, void* out, int64_t ldo,
                            void* workspace, size_t ws_bytes, void* stream);

@@ -6,7 +6,7 @@
 // 16x16x32 bf16 matrix instructions: e4m3 codes and their power-of-two scales
 // are bf16 numbers exactly, and the layout of the S tiles is that of the P operand
 // when the rows of K are taken in the order that Step says, so nothing crosses lanes but
-// two maxima.  P and fp32 queries enter as sums of bf16 numbers (PT, QT).
+// two maxima.  P and fp32 queries enter as sums of three bf16 numbers, 24 bits (PT, QT).
 // Bound by the cache's bytes: 512 sequences of 2000 positions, 28 q-heads on 4 kv-heads
 // of 128, 1.2 GB, take 240 us (5.0 TB/s); three of 8000, 40 on 8, 52 MB, 14.
 #include "fp8.h"
@@ -20,6 +20,9 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kStep = 32;   // positions a wave takes at a time
+// bf16 numbers whose sum is a weight.  With two, 16 bits, weights that cancel lose what is left of them; the third costs at most
+// 5% (512 x 4 x 2000: 216 us and 215; 8 x 32 x 4000: 50 and 48).
+constexpr int PT = 3;
 
 // Chunks of a row of `len` positions; len + chunk may pass 31 bits.
 __host__ __device__ constexpr int chunks_in(int len, int chunk) { return len / chunk + (len % chunk != 0); }
@@ -58,7 +61,7 @@ __host__ __device__ constexpr int part_floats(int G, int D) { return G * (D + 2)
 
 // A workgroup takes one chunk of one row's positions for one kv-head, its waves every
 // kWaves-th step of 32, the next step's loads under this one's arithmetic.
-template <typename T, int D, int QT, int PT, int kWaves>
+template <typename T, int D, int QT, int kWaves>
 __global__ void __launch_bounds__(64 * kWaves, 2) attention_fp8_kernel(AttnFp8 p, int chunk, int n_chunks) {
     constexpr int NQ = D / 64;          // 16-byte K loads a row, of 4 lane groups
     constexpr int NV = D / 32;          // 16-byte V loads a lane: two entries each
@@ -335,20 +338,20 @@ int chunks_of(int n, int kv_heads, int max_length) {
     return std::max(1, chunks_in(max_length, chunk_of(n, kv_heads, max_length)));
 }
 
-template <typename T, int D, int QT, int PT, int WAVES> void start(const AttnFp8& a, int chunk, int n_chunks, hipStream_t s) {
+template <typename T, int D, int QT, int WAVES> void start(const AttnFp8& a, int chunk, int n_chunks, hipStream_t s) {
     const int lds = WAVES * (a.heads / a.c.heads) * D * sizeof(float);
-    attention_fp8_kernel<T, D, QT, PT, WAVES><<<a.n * a.c.heads * n_chunks, 64 * WAVES, lds, s>>>(a, chunk, n_chunks);
+    attention_fp8_kernel<T, D, QT, WAVES><<<a.n * a.c.heads * n_chunks, 64 * WAVES, lds, s>>>(a, chunk, n_chunks);
 }
 
-template <typename T, int D, int QT, int PT> hipError_t attend(const AttnFp8& a, hipStream_t s) {
+template <typename T, int D, int QT> hipError_t attend(const AttnFp8& a, hipStream_t s) {
     const int chunk = chunk_of(a.n, a.c.heads, a.max_length), n_chunks = chunks_of(a.n, a.c.heads, a.max_length);
     // Waves a workgroup: one where rows are short and many (11968 pairs of 105 positions: 92 us, with two 96, four 119), four where
     // workgroups are few (304 of them: 18 us, with two 20, one 23), else two (512 x 4 x 2000: 252, four 249; 24 x 8000: 23 and 25;
     // 1732 x 820 in fp32: 130 and 135).
     const int64_t pairs = static_cast<int64_t>(a.n) * a.c.heads;
-    if (pairs * n_chunks < 512) start<T, D, QT, PT, 4>(a, chunk, n_chunks, s);
-    else if (a.max_length <= 128 && pairs >= 2048) start<T, D, QT, PT, 1>(a, chunk, n_chunks, s);
-    else start<T, D, QT, PT, 2>(a, chunk, n_chunks, s);
+    if (pairs * n_chunks < 512) start<T, D, QT, 4>(a, chunk, n_chunks, s);
+    else if (a.max_length <= 128 && pairs >= 2048) start<T, D, QT, 1>(a, chunk, n_chunks, s);
+    else start<T, D, QT, 2>(a, chunk, n_chunks, s);
     if (n_chunks > 8) attention_fp8_join_head_kernel<T, D><<<a.n * a.heads, 256, 0, s>>>(a, chunk, n_chunks);
     else if (n_chunks > 1) attention_fp8_join_kernel<T, D><<<a.n * a.c.heads, 256, 0, s>>>(a, chunk, n_chunks);
     return hipGetLastError();
@@ -367,9 +370,9 @@ size_t attention_fp8_ws_bytes(int n, int kv_heads, int heads, int dim, int max_l
 }
 
 hipError_t launch_attention_fp8(const AttnFp8& a, hipStream_t s) {
-    // bf16 queries are one bf16 number; the weights keep 16 bits for bf16 outputs, 24 for fp32
-    if (a.dt == RL_DTYPE_FP32) return a.c.dim == 128 ? attend<float, 128, 3, 3>(a, s) : attend<float, 64, 3, 3>(a, s);
-    return a.c.dim == 128 ? attend<uint16_t, 128, 1, 2>(a, s) : attend<uint16_t, 64, 1, 2>(a, s);
+    // a bf16 query is one bf16 number, an fp32 one the sum of three
+    if (a.dt == RL_DTYPE_FP32) return a.c.dim == 128 ? attend<float, 128, 3>(a, s) : attend<float, 64, 3>(a, s);
+    return a.c.dim == 128 ? attend<uint16_t, 128, 1>(a, s) : attend<uint16_t, 64, 1>(a, s);
 }
 
 }  // namespace rl
