@@ -109,10 +109,31 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES, NV <= 2 ? 8 : 4) rm
 }
 
 // ---------------------------------------------------------------------------
-// Rows: 128 / E lanes a block, U blocks a lane group.  Bound by memory: SwiGLU of 512 x
-// 18944 bf16, 49 MB, 10.5 us (4.6 TB/s); with division and the library's exponential
-// and one block a lane group 15.6, bound by arithmetic.
+// Rows: 128 / E lanes a block, U blocks a lane group.  Bound by memory: SwiGLU of 8192 x
+// 18944 bf16, 0.78 GB, 152 us (5.1 TB/s; with an exponential of the rounded argument, 16 times the error,
+// 149); of 512 x 18944 from memory 15 us.  With division and the library's exponential
+// and one block a lane group the latter is bound by arithmetic (15.6 from the caches, where this takes 11).
 // ---------------------------------------------------------------------------
+// log2(e) as the nearest fp32 number and what it leaves
+constexpr float kLog2eHi = 1.44269502e+0f, kLog2eLo = 1.92596303e-8f, kLn2 = 0.693147182f;
+
+constexpr float kFarGate = 80.0f;
+// silu(g) u = g u / (1 + e^-g) for |g| <= 80, within 8 2^-24: the exponential is the hardware's of g log2(e) rounded, times
+// 1 + ln(2) of what the rounding left, the reciprocal the hardware's.
+__device__ __forceinline__ float swiglu_near(float g, float u) {
+    const float h = g * kLog2eHi, left = __builtin_fmaf(g, kLog2eLo, __builtin_fmaf(g, kLog2eHi, -h));
+    const float e = __builtin_amdgcn_exp2f(-h);
+    return g * __builtin_amdgcn_rcpf(1.0f + __builtin_fmaf(e, -kLn2 * left, e)) * u;
+}
+// The same beyond, where 1 + e^-|g| is 1.  For a negative gate e^g = f 2^i may pass fp32 where g e^g u does not: 2^i is shared by
+// the gate, which takes up to 2^-120 of it and stays a normal number, and u.
+__device__ __forceinline__ float swiglu_far(float g, float u) {
+    const float c = fminf(fmaxf(g, -700.0f), 0.0f), i = __builtin_rintf(c * kLog2eHi);
+    const float f = __builtin_amdgcn_exp2f(__builtin_fmaf(c, kLog2eLo, __builtin_fmaf(c, kLog2eHi, -i)));
+    const int n = static_cast<int>(i), gate = max(n, -120);
+    return __builtin_ldexpf(g * f, gate) * __builtin_ldexpf(u, n - gate);
+}
+
 template <typename T, bool SWIGLU, int U>
 __global__ void __launch_bounds__(256) quantise_rows_kernel(int n, int k, const T* __restrict__ x, int64_t ldx, Fp8Out out) {
     constexpr int E = kEntries<T>, LANES = kFp8Block / E, GROUPS = 256 / LANES;
@@ -134,9 +155,20 @@ __global__ void __launch_bounds__(256) quantise_rows_kernel(int n, int k, const 
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         if constexpr (SWIGLU) {
-            // the hardware's exponential and reciprocal, for either type: within (2 |g| + 10) 2^-24, where e4m3 rounds at 2^-4
+            bool far = false;
+            float y[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[i][e] = swiglu_bf16(v[i][e], u[i][e]);
+            for (int e = 0; e < E; ++e) {
+                far |= !(fabsf(v[i][e]) <= kFarGate);
+                y[e] = swiglu_near(v[i][e], u[i][e]);
+            }
+            if (far) {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (!(fabsf(v[i][e]) <= kFarGate)) y[e] = swiglu_far(v[i][e], u[i][e]);
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[i][e] = y[e];
         }
         uint32_t c[E / 4];
         const int b = fp8_encode<E, LANES>(v[i], c);
