@@ -576,7 +576,7 @@ typedef enum rl_fp8_form {
 } rl_fp8_form;
 
 /* [n][ldx] numbers of dtype in 8 bits.  n <= 2^20, k <= 131072, and
- * n * ceil(k / 128) < 2^28. */
+ * n * ceil(k / 128) <= 2^28 - 16. */
 rl_status rl_quantise(int32_t form, int32_t n, int32_t k, int32_t dtype, const void* x, int64_t ldx, const rl_fp8_matrix* out,
                           void* stream);
 

@@ -47,8 +47,9 @@ bool pool_ok(int32_t n_pages, int32_t n_kv_heads, int64_t block) {
     return n_pages > 0 && n_kv_heads > 0 && n_kv_heads <= 1024 && block > 0 && n_pages <= (int64_t(1) << 48) / (block * n_kv_heads);
 }
 
-// The runtime counts a launch's threads in 32 bits: 16 of them take 128 entries of an fp32 matrix, or one token's head.
-constexpr int64_t kMaxBlocks = int64_t(1) << 28;
+// The runtime counts a launch's threads in 32 bits.  A workgroup of 256 takes 16 blocks of an fp32 matrix, so that the last 16
+// below 2^28 would need 2^32; 16 threads take one token's head.
+constexpr int64_t kMaxBlocks = (int64_t(1) << 28) - 16, kMaxHeads = (int64_t(1) << 28) - 1;
 
 bool cache_ok(const rl_kv_fp8* c, KvFp8* o) {
     if (!c || !c->pool || !aligned(c->pool, 256) || !c->page_table || !aligned(c->page_table, 4)) return false;
@@ -83,7 +84,7 @@ rl_status rl_quantise(int32_t form, int32_t n, int32_t k, int32_t dtype, const v
     if (form < RL_FP8_ROWS || form > RL_FP8_TILES || n < 0 || n > kMaxRows || k < 1 || k > kMaxWidth) return RL_ERR_INVALID_ARG;
     if (n == 0) return dtype_ok(dtype) ? RL_OK : RL_ERR_INVALID_ARG;
     if (!rows_ok(dtype, x, n, form == RL_FP8_SWIGLU ? 2 * static_cast<int64_t>(k) : k, ldx) || !matrix_ok(out, k)) return RL_ERR_INVALID_ARG;
-    if (static_cast<int64_t>(n) * fp8_blocks(k) >= kMaxBlocks) return RL_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(n) * fp8_blocks(k) > kMaxBlocks) return RL_ERR_UNSUPPORTED;
     return status_of(launch_quantise_fp8(form, n, k, dtype, x, ldx, out_of(out), static_cast<hipStream_t>(stream)));
 }
 
@@ -112,7 +113,7 @@ rl_status rl_kv_quant_append(const rl_kv_fp8* cache, int32_t n, const int32_t* s
     KvFp8 c;
     if (!cache_ok(cache, &c) || n < 0 || n > kMaxTokens || !dtype_ok(dtype)) return RL_ERR_INVALID_ARG;
     if (n == 0) return RL_OK;
-    if (static_cast<int64_t>(n) * c.heads >= kMaxBlocks) return RL_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(n) * c.heads > kMaxHeads) return RL_ERR_UNSUPPORTED;
     const int64_t width = static_cast<int64_t>(c.heads) * c.dim;
     if (!numbers_ok(seqs) || !numbers_ok(positions)) return RL_ERR_INVALID_ARG;
     if (!rows_ok(dtype, k, n, width, ldk) || !rows_ok(dtype, v, n, width, ldv)) return RL_ERR_INVALID_ARG;
@@ -125,7 +126,7 @@ rl_status rl_kv_quant_read(const rl_kv_fp8* cache, int32_t n, const int32_t* seq
     KvFp8 c;
     if (!cache_ok(cache, &c) || n < 0 || n > kMaxTokens || !dtype_ok(dtype)) return RL_ERR_INVALID_ARG;
     if (n == 0) return RL_OK;
-    if (static_cast<int64_t>(n) * c.heads >= kMaxBlocks) return RL_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(n) * c.heads > kMaxHeads) return RL_ERR_UNSUPPORTED;
     const int64_t width = static_cast<int64_t>(c.heads) * c.dim;
     if (!numbers_ok(seqs) || !numbers_ok(positions)) return RL_ERR_INVALID_ARG;
     if (!rows_ok(dtype, out_k, n, width, ldk) || !rows_ok(dtype, out_v, n, width, ldv)) return RL_ERR_INVALID_ARG;

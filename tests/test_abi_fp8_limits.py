@@ -1,0 +1,12 @@
+"""Sizes at the limits of the 8-bit entry points, on the CPU.  No call here reaches the GPU."""
+import pytest
+
+from paper_2509_15965_amd import rl_decode as R
+from test_abi_fp8 import quantise
+
+
+@pytest.mark.parametrize("form", [0, 1, 2])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_quantise_refuses_blocks_whose_launch_cannot_be_counted(form, dtype):
+    """617093 rows of 435 blocks are 2^28 - 1: 2^24 workgroups of 256 threads in fp32, one more than 32 bits count."""
+    assert quantise(form=form, n=617093, k=435 * 128, dtype=dtype) == R.RL_ERR_UNSUPPORTED
