@@ -587,7 +587,7 @@ size_t rl_gemm_quant_workspace_bytes(int32_t m, int32_t n, int32_t k);
 /* out = a w^T: [m][ldo] of out_dtype, rounded once from fp32 sums.
  *  a  [m][k] with a scale for each block of a row (rl_rmsnorm_quant, RL_FP8_ROWS, RL_FP8_SWIGLU).
  *  w  [n][k] with a scale for each tile (RL_FP8_TILES).
- *  m, n <= 2^20, k <= 131072.
+ *  m, n <= 2^20, k <= 131072, and ceil(m / 128) * ceil(n / 128) <= 2^24 - 8.
  * Sums are fp32: the products, exact, are added as fp32 numbers (numbers below
  * 2^-126 count as 0, from 2^128 on as infinite). */
 rl_status rl_gemm_quant(int32_t m, int32_t n, int32_t k, const rl_fp8_matrix* a, const rl_fp8_matrix* w, int32_t out_dtype, void* out,

@@ -50,6 +50,7 @@ bool pool_ok(int32_t n_pages, int32_t n_kv_heads, int64_t block) {
 // The runtime counts a launch's threads in 32 bits.  A workgroup of 256 takes 16 blocks of an fp32 matrix, so that the last 16
 // below 2^28 would need 2^32; 16 threads take one token's head.
 constexpr int64_t kMaxBlocks = (int64_t(1) << 28) - 16, kMaxHeads = (int64_t(1) << 28) - 1;
+constexpr int64_t kMaxTiles = (int64_t(1) << 24) - 8;   // of 128 x 128, a workgroup each, rounded up to eights
 
 bool cache_ok(const rl_kv_fp8* c, KvFp8* o) {
     if (!c || !c->pool || !aligned(c->pool, 256) || !c->page_table || !aligned(c->page_table, 4)) return false;
@@ -98,6 +99,7 @@ rl_status rl_gemm_quant(int32_t m, int32_t n, int32_t k, const rl_fp8_matrix* a,
     if (m == 0) return RL_OK;
     if (!matrix_ok(a, k) || !matrix_ok(w, k) || !rows_ok(out_dtype, out, m, n, ldo)) return RL_ERR_INVALID_ARG;
     const int kb = fp8_blocks(k);
+    if (static_cast<int64_t>(fp8_blocks(m)) * fp8_blocks(n) > kMaxTiles) return RL_ERR_UNSUPPORTED;
     if (const rl_status st = workspace_ok(workspace, ws_bytes, gemm_fp8_ws_bytes(m, n, kb)); st != RL_OK) return st;
     const Fp8Gemm g{m, n, kb, in_of(a), in_of(w), out, ldo, out_dtype, static_cast<float*>(workspace)};
     return status_of(launch_gemm_fp8(g, static_cast<hipStream_t>(stream)));

@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2509_15965_amd import rl_decode as R
-from test_abi_fp8 import quantise
+from test_abi_fp8 import gemm, quantise
 
 
 @pytest.mark.parametrize("form", [0, 1, 2])
@@ -10,3 +10,10 @@ from test_abi_fp8 import quantise
 def test_quantise_refuses_blocks_whose_launch_cannot_be_counted(form, dtype):
     """617093 rows of 435 blocks are 2^28 - 1: 2^24 workgroups of 256 threads in fp32, one more than 32 bits count."""
     assert quantise(form=form, n=617093, k=435 * 128, dtype=dtype) == R.RL_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("dt", [0, 1])
+def test_product_refuses_tiles_whose_launch_cannot_be_counted(dt):
+    """4096 x 4096 tiles and more, of 256 threads each."""
+    for m, n in ((1 << 20, 1 << 20), (1 << 19, 1 << 19)):
+        assert gemm(m=m, n=n, k=128, ldo=n, dt=dt) == R.RL_ERR_UNSUPPORTED
