@@ -831,7 +831,14 @@ def gemm_quant(a: torch.Tensor, a_scales: torch.Tensor, w: torch.Tensor, w_scale
             lambda ws, nb, s: L.rl_gemm_quant(m, n, k, C.byref(A), C.byref(W), dt, o, ldo, ws, nb, s), "rl_gemm_quant")
 
 
+def _counts(*numbers: int) -> bool:
+    """Whether C takes them all as they are: ctypes cuts a number to its 32 bits without a word."""
+    return all(-1 << 31 <= i < 1 << 31 for i in numbers)
+
+
 def kv_quant_bytes(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int) -> int:
+    if not _counts(n_pages, page_size, n_kv_heads, head_dim):
+        return 0
     return int(lib().rl_kv_quant_bytes(n_pages, page_size, n_kv_heads, head_dim))
 
 
@@ -851,7 +858,7 @@ def _heads_on(dev: int, name: str, t: torch.Tensor, like: Optional[torch.Tensor]
 
 @functools.lru_cache(maxsize=64)
 def _kv_page_bytes(page_size: int, heads: int, d: int) -> int:
-    return lib().rl_kv_quant_bytes(1, page_size, heads, d)
+    return kv_quant_bytes(1, page_size, heads, d)
 
 
 def _cache_on(dev: int, pool: torch.Tensor, page_table: torch.Tensor, page_size: int, heads: int, d: int) -> KvFp8:
@@ -900,6 +907,8 @@ def attention_quant(pool: torch.Tensor, page_table: torch.Tensor, q: torch.Tenso
     qp, ldq = _heads_on(dev, "q", q)
     op, ldo = _heads_on(dev, "out", out, q)
     n, h, d = q.shape
+    if not _counts(max_length):
+        raise ValueError(f"max_length must be a count of 32 bits, not {max_length}")
     cache = _cache_on(dev, pool, page_table, page_size, n_kv_heads, d)
     ln, sq = _on(dev, "lengths", lengths, torch.int32, n), _on(dev, "seqs", seqs, torch.int32, n, True)
     L = lib()

@@ -17,3 +17,9 @@ def test_product_refuses_tiles_whose_launch_cannot_be_counted(dt):
     """4096 x 4096 tiles and more, of 256 threads each."""
     for m, n in ((1 << 20, 1 << 20), (1 << 19, 1 << 19)):
         assert gemm(m=m, n=n, k=128, ldo=n, dt=dt) == R.RL_ERR_UNSUPPORTED
+
+
+def test_cache_bytes_of_counts_past_32_bits():
+    for bad in (((1 << 32) + 1, 32, 1, 64), (1, (1 << 32) + 32, 1, 64), (1, 32, (1 << 32) + 1, 64), (1, 32, 1, (1 << 32) + 64)):
+        assert R.kv_quant_bytes(*bad) == 0, bad
+    assert R.kv_quant_bytes(1, 32, 1, 64) == 4352

@@ -54,3 +54,17 @@ def test_swiglu_of_gates_without_a_finite_exponential():
     R.quantise(torch.stack([g, u], 1), codes, scales, form="swiglu")
     v = F.matrix(codes, scales)[:, 0]
     assert (v[:4] == 0).all() and (scales[:4, 0] == 127).all() and torch.isnan(v[4:]).all()
+
+
+def test_binding_refuses_counts_past_32_bits():
+    """Counts that C takes in 32 bits: none may come out as another."""
+    pool = torch.zeros(R.kv_quant_bytes(2, 32, 2, 64), dtype=torch.uint8, device=DEV)
+    table, ln = torch.zeros(1, 2, dtype=torch.int32, device=DEV), torch.ones(1, dtype=torch.int32, device=DEV)
+    q = torch.zeros(1, 2, 64, device=DEV)
+    call = lambda **kw: R.attention_quant(pool, table, q, ln, torch.empty_like(q), scale=1.0, **dict(dict(page_size=32, n_kv_heads=2, max_length=4), **kw))
+    call()
+    for more in (dict(max_length=(1 << 32) + 4), dict(max_length=-(1 << 32)), dict(page_size=(1 << 32) + 32), dict(n_kv_heads=(1 << 32) + 2)):
+        with pytest.raises(ValueError):
+            call(**more)
+    with pytest.raises(ValueError):
+        R.kv_quant_append(pool, table, ln, ln, q, q, page_size=(1 << 32) + 32)
