@@ -557,7 +557,7 @@ typedef struct rl_fp8_matrix {
 } rl_fp8_matrix;
 
 /* Residual addition and RMS norm of rows, the result in 8 bits:
- *   s = x + add (rounded to dtype; x where add is NULL), out_sum = s
+ *   s = x + add (in fp32, rounded to dtype; x where add is NULL), out_sum = s
  *   out = s w / sqrt(mean_i s_i^2 + eps), a scale for each block of a row
  *  n <= 2^20 rows of hidden <= 32768 entries; x [n][ldx] of dtype; add
  *  [n][ld_add] of add_dtype, or NULL; weight [hidden] of w_dtype; out_sum

@@ -110,9 +110,9 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES, NV <= 2 ? 8 : 4) rm
 
 // ---------------------------------------------------------------------------
 // Rows: 128 / E lanes a block, U blocks a lane group.  Bound by memory: SwiGLU of 8192 x
-// 18944 bf16, 0.78 GB, 152 us (5.1 TB/s; with an exponential of the rounded argument, 16 times the error,
-// 149); of 512 x 18944 from memory 15 us.  With division and the library's exponential
-// and one block a lane group the latter is bound by arithmetic (15.6 from the caches, where this takes 11).
+// 18944 bf16, 0.78 GB, 152 us (5.1 TB/s; 149 with the exponential of the rounded argument, whose error
+// grows with the gate, (2 |g| + 10) 2^-24); of 512 x 18944, 49 MB, 12.6 (15 where nothing is in the caches).  With division and
+// the library's exponential and one block a lane group the latter took 15.6, bound by arithmetic.
 // ---------------------------------------------------------------------------
 // log2(e) as the nearest fp32 number and what it leaves
 constexpr float kLog2eHi = 1.44269502e+0f, kLog2eLo = 1.92596303e-8f, kLn2 = 0.693147182f;

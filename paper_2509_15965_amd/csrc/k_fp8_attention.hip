@@ -8,7 +8,7 @@
 // when the rows of K are taken in the order that Step says, so nothing crosses lanes but
 // two maxima.  P and fp32 queries enter as sums of three bf16 numbers, 24 bits (PT, QT).
 // Bound by the cache's bytes: 512 sequences of 2000 positions, 28 q-heads on 4 kv-heads
-// of 128, 1.2 GB, take 240 us (5.0 TB/s); three of 8000, 40 on 8, 52 MB, 14.
+// of 128, 1.2 GB, take 247 us (4.9 TB/s); three of 8000, 40 on 8, 52 MB, 15.
 #include "fp8.h"
 #include "rl_decode.h"
 

@@ -151,9 +151,9 @@ __global__ void __launch_bounds__(64 * kGemvWaves, 4) gemv_fp8_kernel(Fp8Gemm p,
 // takes what the block after the next needs, and all of it has a block and a half's
 // time to arrive.
 //
-// Bound by the matrix unit beside the conversions in front of it, four an instruction:
-// 8192 x 3584 x 18944 takes 836 us, 1.33 PFLOP/s, where such instructions alone, on
-// codes in registers, reach 1.8 to 2.0.
+// Bound by the matrix unit and the power that it draws: 8192 x 3584 x 18944 takes 836 to
+// 868 us, 1.3 PFLOP/s, with the unit busy 73% of the cycles at 1.7 GHz, beside four conversions an
+// instruction; such instructions alone, on codes in registers, reach 1.8 to 2.0.
 //
 // LDS row 32 t + 8 q + 4 h + e of a wave's weights (t tile, 4 q + e register and h lane half
 // of the instruction's output) holds weight h TN / 2 + q TN / 8 + 4 t + e: a lane's outputs
